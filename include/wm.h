@@ -165,6 +165,16 @@ wm_status wm_kv_mix(const wm_config* cfg, const wm_cache* cache, const wm_mix_we
                     int32_t max_pages, void* workspace, size_t ws_bytes, int32_t* dev_status,
                     void* stream);
 
+/*
+ * wm_kv_mix with the tokens' positions given: pos, device int32 [B], is the
+ * position that token b's keys are rotated at (wm_kv_mix uses slot[b] - 1).
+ * For caches whose slots no longer count positions, after wm_cache_evict.
+ */
+wm_status wm_kv_mix_at(const wm_config* cfg, const wm_cache* cache, const wm_mix_weights* w,
+                       const void* h, const int32_t* page_table, const int32_t* slot,
+                       const int32_t* pos, int32_t B, int32_t max_pages, void* workspace,
+                       size_t ws_bytes, int32_t* dev_status, void* stream);
+
 /* Kernels one wm_kv_mix call of B tokens enqueues (0 for B = 0), -1 for an
  * invalid config or B < 0; no GPU work: prenorm, router, mix and the
  * projection with its fused epilogue (4 for bf16), or a separate epilogue
@@ -285,6 +295,118 @@ wm_status wm_prefill_attn(const wm_config* cfg, const wm_cache* cache, int32_t l
                           const void* q, const int32_t* pos, const int32_t* page_table,
                           int32_t B, int32_t Tq, int32_t max_pages, void* out,
                           int32_t* dev_status, void* stream);
+
+/*
+ * Attention over part of the cache, for long contexts (no counterpart in the
+ * paper).  All of it reads channel c(layer) as wm_decode_attn does, for both
+ * dtypes, every page size and group size, with fp32 softmax and accumulation;
+ * bf16 probabilities enter the P V product as bf16.  A sequence may hold no
+ * slot at all (length 0): its rows are zeros, and so is any row whose mask
+ * leaves nothing.  A negative length, or one past the page table, zero-fills
+ * the row and sets WM_ERR_BOUNDS.  Page-table entries of pages without a
+ * visible slot are not read into anything: the pages may be gone.  Slots that
+ * are not visible may hold anything, NaN included.
+ */
+
+/*
+ * Decode attention over a sliding window and the first slots (sinks): with
+ * n = seq_lens[b], the query heads of sequence b see the slots t < n with
+ * t < sinks or t >= n - window.  sinks, window >= 0, of any size; with
+ * sinks + window >= n the result is wm_decode_attn's.
+ *   q, out      device [B][Hq][d], 16-byte aligned
+ *   seq_lens    device int32 [B], 0 <= seq_lens[b] <= max_pages*page_size
+ * No workspace.  B = 0 is a no-op; B above 4096 returns WM_ERR_UNSUPPORTED.
+ */
+wm_status wm_window_attn(const wm_config* cfg, const wm_cache* cache, int32_t layer, const void* q,
+                         const int32_t* page_table, const int32_t* seq_lens, int32_t sinks,
+                         int32_t window, int32_t B, int32_t max_pages, void* out,
+                         int32_t* dev_status, void* stream);
+
+/*
+ * The same mask for many query positions at once, as wm_prefill_attn: the
+ * query at position i = pos[b][r] sees the slots t <= i with t < sinks or
+ * t > i - window.
+ *   q, out  device [B][Tq][Hq][d], 16-byte aligned
+ *   pos     device int32 [B][Tq], 0 <= pos < max_pages*page_size, any order
+ * No workspace.  A bad position zero-fills that row and sets WM_ERR_BOUNDS.
+ */
+wm_status wm_window_prefill_attn(const wm_config* cfg, const wm_cache* cache, int32_t layer,
+                                 const void* q, const int32_t* pos, const int32_t* page_table,
+                                 int32_t sinks, int32_t window, int32_t B, int32_t Tq,
+                                 int32_t max_pages, void* out, int32_t* dev_status, void* stream);
+
+/* Workspace bytes of wm_prefix_attn (0 for bad arguments). */
+size_t wm_prefix_attn_workspace(const wm_config* cfg, int32_t B, int32_t max_pages,
+                                int32_t shared_pages);
+
+/*
+ * Decode attention of a batch whose sequences share a prefix: the first
+ * shared_pages entries of every page-table row name the same pages (only row
+ * 0's are read), so their slots are read once for the whole batch instead of
+ * once per sequence.  The result is wm_decode_attn's.  A sequence may end
+ * inside the prefix.  0 <= shared_pages <= max_pages.
+ *   q, out      device [B][Hq][d], 16-byte aligned
+ *   seq_lens    device int32 [B], slots of each sequence, prefix included
+ *   workspace   device, >= wm_prefix_attn_workspace(cfg, B, max_pages,
+ *               shared_pages) bytes, 256-byte aligned, no contents required;
+ *               calls that share one must not overlap on the GPU
+ * B = 0 is a no-op; B above 4096 returns WM_ERR_UNSUPPORTED.
+ */
+wm_status wm_prefix_attn(const wm_config* cfg, const wm_cache* cache, int32_t layer, const void* q,
+                         const int32_t* page_table, const int32_t* seq_lens, int32_t shared_pages,
+                         int32_t B, int32_t max_pages, void* out, void* workspace, size_t ws_bytes,
+                         int32_t* dev_status, void* stream);
+
+/* Workspace bytes of wm_decode_attn_mass (0 for bad arguments): partial
+ * results and one fp32 score per query head and slot. */
+size_t wm_decode_attn_mass_workspace(const wm_config* cfg, int32_t B, int32_t max_pages);
+
+/*
+ * Decode attention of one layer (as wm_decode_attn) that also adds up what
+ * each slot was given: for kv head h of sequence b and every slot
+ * t < seq_lens[b],
+ *   mass[c(layer)][b][h][t] += sum over the G query heads of h of the
+ *                              softmax weight of t.
+ *   mass        device fp32 [k][B][Hkv][max_pages*page_size]; only the
+ *               layer's channel is touched.  Each element is added to once,
+ *               so the sums are reproducible.
+ *   workspace   device, >= wm_decode_attn_mass_workspace(cfg, B, max_pages)
+ *               bytes, 256-byte aligned, no contents required; calls that
+ *               share one must not overlap on the GPU
+ * B = 0 is a no-op; B above 4096 returns WM_ERR_UNSUPPORTED.
+ */
+wm_status wm_decode_attn_mass(const wm_config* cfg, const wm_cache* cache, int32_t layer,
+                              const void* q, const int32_t* page_table, const int32_t* seq_lens,
+                              float* mass, int32_t B, int32_t max_pages, void* out,
+                              void* workspace, size_t ws_bytes, int32_t* dev_status, void* stream);
+
+/*
+ * Cut every (channel, sequence, kv head) of the cache to at most `budget`
+ * slots by the sums that wm_decode_attn_mass keeps.  With n = seq_lens[b]:
+ * if n <= budget nothing moves; else the slots t < sinks, the slots
+ * t >= n - recent and, of the slots between, the budget - sinks - recent with
+ * the largest mass stay (among equal sums the lowest slots; NaN counts as
+ * the smallest).  Kept K and V rows move, in order, to slots 0, 1, ...,
+ * budget - 1 of the same pages.  Keys keep the rotation that they have: later
+ * tokens take wm_kv_mix_at, whose position is not slot - 1 any more.
+ *   mass        device fp32 [k][B][Hkv][max_pages*page_size]
+ *   mass_out    device, same shape: the kept slots' sums in their new places,
+ *               zero behind them (up to max_pages*page_size).  May be mass.
+ *   seq_lens    device int32 [B], 0 <= seq_lens[b] <= max_pages*page_size
+ *   kept        device int32 [k][B][Hkv][budget]: the slot each kept row came
+ *               from, ascending; -1 from min(n, budget) on
+ *   new_lens    device int32 [B]: min(n, budget); not seq_lens itself
+ * budget >= 1, budget <= max_pages*page_size, sinks, recent >= 0, sinks +
+ * recent <= budget.  The pages of a sequence must be its own: rows of a
+ * prefix that other sequences share would move under them.  A bad page id
+ * leaves the rows that it holds out and sets WM_ERR_BOUNDS; a bad length
+ * counts as 0 and sets it too.  B = 0 is a no-op.
+ */
+wm_status wm_cache_evict(const wm_config* cfg, const wm_cache* cache, const float* mass,
+                         float* mass_out, const int32_t* page_table, const int32_t* seq_lens,
+                         int32_t budget, int32_t sinks, int32_t recent, int32_t B,
+                         int32_t max_pages, int32_t* kept, int32_t* new_lens,
+                         int32_t* dev_status, void* stream);
 
 /*
  * Self-test of the kernels' failure detection (no counterpart in the paper).

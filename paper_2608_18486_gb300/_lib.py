@@ -19,7 +19,9 @@ WM_DT_F32, WM_DT_BF16 = 0, 1
 EXPORTED = ["wm_status_string", "wm_config_check", "wm_cache_bytes", "wm_cache_alloc",
             "wm_kv_mix_workspace", "wm_kv_mix", "wm_decode_attn_workspace", "wm_decode_attn",
             "wm_decode_attn_flags", "wm_decode_attn_plan", "wm_prefill_attn",
-            "wm_kv_mix_launches"]
+            "wm_kv_mix_launches", "wm_kv_mix_at", "wm_window_attn", "wm_window_prefill_attn",
+            "wm_prefix_attn_workspace", "wm_prefix_attn", "wm_decode_attn_mass_workspace",
+            "wm_decode_attn_mass", "wm_cache_evict"]
 WM_ATTN_INPUTS_READY = 1
 WM_ATTN_DYNAMIC_SPLIT = 2
 WM_ATTN_UNIT_SPLIT = 4
@@ -92,6 +94,25 @@ def lib():
         L.wm_prefill_attn.restype = ctypes.c_int
         L.wm_prefill_attn.argtypes = [cp, ctypes.POINTER(wm_cache), i32, vp, vp, vp, i32, i32, i32,
                                       vp, vp, vp]
+        ccp = ctypes.POINTER(wm_cache)
+        L.wm_kv_mix_at.restype = ctypes.c_int
+        L.wm_kv_mix_at.argtypes = [cp, ccp, ctypes.POINTER(wm_mix_weights), vp, vp, vp, vp, i32, i32,
+                                   vp, sz, vp, vp]
+        L.wm_window_attn.restype = ctypes.c_int
+        L.wm_window_attn.argtypes = [cp, ccp, i32, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
+        L.wm_window_prefill_attn.restype = ctypes.c_int
+        L.wm_window_prefill_attn.argtypes = [cp, ccp, i32, vp, vp, vp, i32, i32, i32, i32, i32, vp,
+                                             vp, vp]
+        L.wm_prefix_attn_workspace.restype = sz
+        L.wm_prefix_attn_workspace.argtypes = [cp, i32, i32, i32]
+        L.wm_prefix_attn.restype = ctypes.c_int
+        L.wm_prefix_attn.argtypes = [cp, ccp, i32, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp, vp]
+        L.wm_decode_attn_mass_workspace.restype = sz
+        L.wm_decode_attn_mass_workspace.argtypes = [cp, i32, i32]
+        L.wm_decode_attn_mass.restype = ctypes.c_int
+        L.wm_decode_attn_mass.argtypes = [cp, ccp, i32, vp, vp, vp, vp, i32, i32, vp, vp, sz, vp, vp]
+        L.wm_cache_evict.restype = ctypes.c_int
+        L.wm_cache_evict.argtypes = [cp, ccp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -200,6 +221,57 @@ def wm_prefill_attn(cfg, cache, layer, q, pos, page_table, B, Tq, max_pages, out
     return lib().wm_prefill_attn(ctypes.byref(cfg), ctypes.byref(cache), int(layer), _p(q), _p(pos),
                                  _p(page_table), int(B), int(Tq), int(max_pages), _p(out),
                                  _p(dev_status), stream)
+
+
+def wm_kv_mix_at(cfg, cache, weights, h, page_table, slot, pos, B, max_pages, workspace, ws_bytes,
+                 dev_status, stream) -> int:
+    return lib().wm_kv_mix_at(ctypes.byref(cfg), ctypes.byref(cache), ctypes.byref(weights), _p(h),
+                              _p(page_table), _p(slot), _p(pos), int(B), int(max_pages),
+                              _p(workspace), int(ws_bytes), _p(dev_status), stream)
+
+
+def wm_window_attn(cfg, cache, layer, q, page_table, seq_lens, sinks, window, B, max_pages, out,
+                   dev_status, stream) -> int:
+    return lib().wm_window_attn(ctypes.byref(cfg), ctypes.byref(cache), layer, _p(q), _p(page_table),
+                                _p(seq_lens), sinks, window, B, max_pages, _p(out), _p(dev_status),
+                                stream)
+
+
+def wm_window_prefill_attn(cfg, cache, layer, q, pos, page_table, sinks, window, B, Tq, max_pages,
+                           out, dev_status, stream) -> int:
+    return lib().wm_window_prefill_attn(ctypes.byref(cfg), ctypes.byref(cache), layer, _p(q), _p(pos),
+                                        _p(page_table), sinks, window, B, Tq, max_pages, _p(out),
+                                        _p(dev_status), stream)
+
+
+def wm_prefix_attn_workspace(cfg, B, max_pages, shared_pages) -> int:
+    return int(lib().wm_prefix_attn_workspace(ctypes.byref(cfg), int(B), int(max_pages),
+                                              int(shared_pages)))
+
+
+def wm_prefix_attn(cfg, cache, layer, q, page_table, seq_lens, shared_pages, B, max_pages, out,
+                   workspace, ws_bytes, dev_status, stream) -> int:
+    return lib().wm_prefix_attn(ctypes.byref(cfg), ctypes.byref(cache), layer, _p(q), _p(page_table),
+                                _p(seq_lens), shared_pages, B, max_pages, _p(out), _p(workspace),
+                                ws_bytes, _p(dev_status), stream)
+
+
+def wm_decode_attn_mass_workspace(cfg, B, max_pages) -> int:
+    return int(lib().wm_decode_attn_mass_workspace(ctypes.byref(cfg), int(B), int(max_pages)))
+
+
+def wm_decode_attn_mass(cfg, cache, layer, q, page_table, seq_lens, mass, B, max_pages, out,
+                        workspace, ws_bytes, dev_status, stream) -> int:
+    return lib().wm_decode_attn_mass(ctypes.byref(cfg), ctypes.byref(cache), layer, _p(q),
+                                     _p(page_table), _p(seq_lens), _p(mass), B, max_pages, _p(out),
+                                     _p(workspace), ws_bytes, _p(dev_status), stream)
+
+
+def wm_cache_evict(cfg, cache, mass, mass_out, page_table, seq_lens, budget, sinks, recent, B,
+                   max_pages, kept, new_lens, dev_status, stream) -> int:
+    return lib().wm_cache_evict(ctypes.byref(cfg), ctypes.byref(cache), _p(mass), _p(mass_out),
+                                _p(page_table), _p(seq_lens), budget, sinks, recent, B, max_pages,
+                                _p(kept), _p(new_lens), _p(dev_status), stream)
 
 
 def wm_decode_attn_noalloc(cfg, cache, layer, q, page_table, seq_lens, B, max_pages, out,

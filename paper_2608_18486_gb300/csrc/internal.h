@@ -113,6 +113,7 @@ struct MixParams {
   const void* qk_g;
   const int32_t* page_table;
   const int32_t* slot;
+  const int32_t* pos;             // [B] positions, or NULL: slot - 1
   // cache
   void* k_pool;
   void* v_pool;

@@ -1,0 +1,292 @@
+// C ABI of the long-context operators (declared in include/wm.h): attention
+// over a sliding window with sinks, over a shared prefix, decode attention
+// that sums each slot's weight, and eviction by those sums.  Argument checks,
+// work splits and kernel dispatch; all device memory belongs to the caller.
+#include <math.h>
+
+#include "api_util.h"
+#include "common.cuh"
+#include "internal.h"
+#include "range_attn.h"
+#include "wm.h"
+
+namespace {
+
+using namespace wm;
+
+constexpr int kMaxBatch = 4096;
+
+// Work a warp of a split launch is left with at least, in stages.
+constexpr int kMinStagesPerWarp = 4;
+
+int clamp_int(int64_t x, int64_t lo, int64_t hi) { return (int)(x < lo ? lo : x > hi ? hi : x); }
+
+// CTAs per unit of a launch whose partial records a later kernel joins: enough
+// for about `waves` waves of resident CTAs, so that sequences of unequal length
+// still fill the SMs, while each warp keeps kMinStagesPerWarp stages.
+int split_pieces(int64_t units, int64_t stages, int waves) {
+  const int64_t by_work = stages / (kRangeWarps * kMinStagesPerWarp);
+  const int64_t by_sms = ((int64_t)sm_count() * kRangeCtasPerSm * waves + units - 1) / units;
+  return clamp_int(by_work < by_sms ? by_work : by_sms, 1, 64);
+}
+
+int64_t stages_of(const wm_config& c, int64_t slots) {
+  const int ss = range_stage_slots(c.dtype, c.d);
+  return (slots + ss - 1) / ss;
+}
+
+// CTAs per unit (one cluster, joined on chip) of a window launch: as many as
+// keep every CTA resident and leave each warp a stage.
+int window_cluster(const wm_config& c, int64_t units, int64_t visible) {
+  const int64_t stages = stages_of(c, visible) + 1;
+  int C = 1;
+  while (C < kRangeMaxCluster && units * C * 2 <= (int64_t)sm_count() * kRangeCtasPerSm &&
+         (int64_t)C * kRangeWarps < stages)
+    C *= 2;
+  return C;
+}
+
+// Checks every attention call of this file makes.
+wm_status check_attn(const wm_config* c, const wm_cache* cache, int32_t layer, int32_t B, int32_t max_pages) {
+  wm_status st = wm_config_check(c);
+  if (st != WM_OK) return st;
+  if ((st = check_cache(*c, cache)) != WM_OK) return st;
+  if (layer < 0 || layer >= c->L || B < 0 || max_pages < 1) return WM_ERR_INVALID_ARG;
+  if ((int64_t)max_pages * c->page_size > INT32_MAX / 2) return WM_ERR_INVALID_ARG;
+  // 32-bit cache rows per channel
+  if ((int64_t)cache->num_pages * c->Hkv * c->page_size > INT32_MAX) return WM_ERR_UNSUPPORTED;
+  return WM_OK;
+}
+
+RangeParams range_params(const wm_config& c, const wm_cache& cache, int32_t layer, const void* q,
+                         const int32_t* page_table, const int32_t* lens, int32_t B, int32_t max_pages,
+                         int32_t* dev_status) {
+  const size_t chan = (size_t)c.chan_of_layer[layer] * cache.num_pages * c.Hkv * c.page_size * c.d * elem_size(c.dtype);
+  RangeParams p{};
+  p.k_pool = (const char*)cache.k_pool + chan;
+  p.v_pool = (const char*)cache.v_pool + chan;
+  p.q = q;
+  p.page_table = page_table;
+  p.seq_lens = lens;
+  p.status = dev_status;
+  p.B = B;
+  p.Hq = c.Hq;
+  p.Hkv = c.Hkv;
+  p.G = c.Hq / c.Hkv;
+  p.P = c.page_size;
+  p.log2P = ilog2(c.page_size);
+  p.num_pages = cache.num_pages;
+  p.max_pages = max_pages;
+  p.rows = p.G;
+  p.pieces = 1;
+  p.rows_per_seq = 1;
+  p.qscale = (float)(1.4426950408889634 / sqrt((double)c.d));
+  return p;
+}
+
+// Split of a shared-prefix call and its workspace.
+struct PrefixPlan {
+  int groups, prefix_pieces, suffix_pieces;
+  size_t off_suffix, total;
+};
+
+PrefixPlan prefix_plan(const wm_config& c, int32_t B, int32_t max_pages, int32_t shared_pages) {
+  const int G = c.Hq / c.Hkv;
+  PrefixPlan pl{};
+  pl.groups = (int)(((int64_t)B * G + kRangeRows - 1) / kRangeRows);
+  pl.prefix_pieces = split_pieces((int64_t)pl.groups * c.Hkv, stages_of(c, (int64_t)shared_pages * c.page_size), 2);
+  pl.suffix_pieces =
+      split_pieces((int64_t)B * c.Hkv, stages_of(c, (int64_t)(max_pages - shared_pages) * c.page_size), 2);
+  pl.off_suffix = align256(sizeof(float) * (size_t)pl.groups * c.Hkv * pl.prefix_pieces * range_rec(kRangeRows, c.d));
+  pl.total = pl.off_suffix + align256(sizeof(float) * (size_t)B * c.Hkv * pl.suffix_pieces * range_rec(G, c.d));
+  return pl;
+}
+
+struct MassPlan {
+  int pieces;
+  int64_t score_stride;
+  size_t off_scores, total;
+};
+
+MassPlan mass_plan(const wm_config& c, int32_t B, int32_t max_pages) {
+  const int G = c.Hq / c.Hkv;
+  const int64_t slots = (int64_t)max_pages * c.page_size, units = (int64_t)B * c.Hkv;
+  MassPlan pl{};
+  pl.pieces = split_pieces(units, stages_of(c, slots), 6);
+  pl.score_stride = (slots + 31) / 32 * 32;
+  pl.off_scores = align256(sizeof(float) * (size_t)units * pl.pieces * range_rec(G, c.d));
+  pl.total = pl.off_scores + align256(sizeof(float) * (size_t)units * G * pl.score_stride);
+  return pl;
+}
+
+wm_status cuda_status(cudaError_t e) { return e == cudaSuccess ? WM_OK : WM_ERR_CUDA; }
+
+}  // namespace
+
+extern "C" {
+
+wm_status wm_window_attn(const wm_config* c, const wm_cache* cache, int32_t layer, const void* q,
+                         const int32_t* page_table, const int32_t* seq_lens, int32_t sinks, int32_t window,
+                         int32_t B, int32_t max_pages, void* out, int32_t* dev_status, void* stream) {
+  wm_status st = check_attn(c, cache, layer, B, max_pages);
+  if (st != WM_OK) return st;
+  if (sinks < 0 || window < 0) return WM_ERR_INVALID_ARG;
+  if (B == 0) return WM_OK;
+  if (B > kMaxBatch || (int64_t)B * c->Hq > INT32_MAX / 2) return WM_ERR_UNSUPPORTED;
+  if (!q || !page_table || !seq_lens || !out) return WM_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16)) return WM_ERR_INVALID_ARG;
+  const int64_t slots = (int64_t)max_pages * c->page_size, visible = (int64_t)sinks + window;
+  RangeParams p = range_params(*c, *cache, layer, q, page_table, seq_lens, B, max_pages, dev_status);
+  p.mode = kRangeWindow;
+  p.out = out;
+  p.sinks = sinks;
+  p.window = window;
+  p.pieces = window_cluster(*c, (int64_t)B * c->Hkv, visible < slots ? visible : slots);
+  return cuda_status(launch_range_attn(p, c->dtype, c->d, B * c->Hkv, (cudaStream_t)stream));
+}
+
+wm_status wm_window_prefill_attn(const wm_config* c, const wm_cache* cache, int32_t layer, const void* q,
+                                 const int32_t* pos, const int32_t* page_table, int32_t sinks, int32_t window,
+                                 int32_t B, int32_t Tq, int32_t max_pages, void* out, int32_t* dev_status,
+                                 void* stream) {
+  wm_status st = check_attn(c, cache, layer, B, max_pages);
+  if (st != WM_OK) return st;
+  if (Tq < 0 || sinks < 0 || window < 0) return WM_ERR_INVALID_ARG;
+  if (B == 0 || Tq == 0) return WM_OK;
+  if ((int64_t)B * Tq > INT32_MAX / 2 / c->Hq) return WM_ERR_UNSUPPORTED;
+  if (!q || !pos || !page_table || !out) return WM_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16)) return WM_ERR_INVALID_ARG;
+  RangeParams p = range_params(*c, *cache, layer, q, page_table, pos, B * Tq, max_pages, dev_status);
+  p.mode = kRangeWindow;
+  p.out = out;
+  p.sinks = sinks;
+  p.window = window;
+  p.rows_per_seq = Tq;
+  p.len_add = 1;  // the query at position i sees slots up to i
+  return cuda_status(launch_range_attn(p, c->dtype, c->d, B * Tq * c->Hkv, (cudaStream_t)stream));
+}
+
+size_t wm_prefix_attn_workspace(const wm_config* c, int32_t B, int32_t max_pages, int32_t shared_pages) {
+  if (wm_config_check(c) != WM_OK || B < 0 || max_pages < 1 || shared_pages < 0 || shared_pages > max_pages) return 0;
+  if (B == 0) return 256;
+  return prefix_plan(*c, B, max_pages, shared_pages).total;
+}
+
+wm_status wm_prefix_attn(const wm_config* c, const wm_cache* cache, int32_t layer, const void* q,
+                         const int32_t* page_table, const int32_t* seq_lens, int32_t shared_pages, int32_t B,
+                         int32_t max_pages, void* out, void* workspace, size_t ws_bytes, int32_t* dev_status,
+                         void* stream) {
+  wm_status st = check_attn(c, cache, layer, B, max_pages);
+  if (st != WM_OK) return st;
+  if (shared_pages < 0 || shared_pages > max_pages) return WM_ERR_INVALID_ARG;
+  if (B == 0) return WM_OK;
+  if (B > kMaxBatch || (int64_t)B * c->Hq > INT32_MAX / 2) return WM_ERR_UNSUPPORTED;
+  if (!q || !page_table || !seq_lens || !out || !workspace) return WM_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256)) return WM_ERR_INVALID_ARG;
+  const PrefixPlan pl = prefix_plan(*c, B, max_pages, shared_pages);
+  if (ws_bytes < pl.total) return WM_ERR_INVALID_ARG;
+  RangeParams p = range_params(*c, *cache, layer, q, page_table, seq_lens, B, max_pages, dev_status);
+  p.begin = shared_pages * c->page_size;
+  p.part = (float*)workspace;
+  p.mode = kRangePrefix;
+  p.rows = kRangeRows;
+  p.pieces = pl.prefix_pieces;
+  cudaError_t e = launch_range_attn(p, c->dtype, c->d, pl.groups * c->Hkv, (cudaStream_t)stream);
+  if (e != cudaSuccess) return WM_ERR_CUDA;
+  p.part = (float*)((char*)workspace + pl.off_suffix);
+  p.mode = kRangeSuffix;
+  p.rows = p.G;
+  p.pieces = pl.suffix_pieces;
+  e = launch_range_attn(p, c->dtype, c->d, B * c->Hkv, (cudaStream_t)stream);
+  if (e != cudaSuccess) return WM_ERR_CUDA;
+  PrefixJoinParams j{};
+  j.prefix = (const float*)workspace;
+  j.suffix = p.part;
+  j.out = out;
+  j.B = B;
+  j.Hq = c->Hq;
+  j.Hkv = c->Hkv;
+  j.G = p.G;
+  j.prefix_pieces = pl.prefix_pieces;
+  j.suffix_pieces = pl.suffix_pieces;
+  return cuda_status(launch_prefix_join(j, c->dtype, c->d, (cudaStream_t)stream));
+}
+
+size_t wm_decode_attn_mass_workspace(const wm_config* c, int32_t B, int32_t max_pages) {
+  if (wm_config_check(c) != WM_OK || B < 0 || max_pages < 1) return 0;
+  if (B == 0) return 256;
+  return mass_plan(*c, B, max_pages).total;
+}
+
+wm_status wm_decode_attn_mass(const wm_config* c, const wm_cache* cache, int32_t layer, const void* q,
+                              const int32_t* page_table, const int32_t* seq_lens, float* mass, int32_t B,
+                              int32_t max_pages, void* out, void* workspace, size_t ws_bytes,
+                              int32_t* dev_status, void* stream) {
+  wm_status st = check_attn(c, cache, layer, B, max_pages);
+  if (st != WM_OK) return st;
+  if (B == 0) return WM_OK;
+  if (B > kMaxBatch || (int64_t)B * c->Hq > INT32_MAX / 2) return WM_ERR_UNSUPPORTED;
+  if (!q || !page_table || !seq_lens || !mass || !out || !workspace) return WM_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(mass, 4) || !aligned(workspace, 256)) return WM_ERR_INVALID_ARG;
+  const MassPlan pl = mass_plan(*c, B, max_pages);
+  if (ws_bytes < pl.total) return WM_ERR_INVALID_ARG;
+  RangeParams p = range_params(*c, *cache, layer, q, page_table, seq_lens, B, max_pages, dev_status);
+  p.mode = kRangeScores;
+  p.pieces = pl.pieces;
+  p.part = (float*)workspace;
+  p.scores = (float*)((char*)workspace + pl.off_scores);
+  p.score_stride = pl.score_stride;
+  const cudaError_t e = launch_range_attn(p, c->dtype, c->d, B * c->Hkv, (cudaStream_t)stream);
+  if (e != cudaSuccess) return WM_ERR_CUDA;
+  MassParams m{};
+  m.part = p.part;
+  m.scores = p.scores;
+  m.seq_lens = seq_lens;
+  m.max_slots = max_pages * c->page_size;
+  m.mass = mass + (size_t)c->chan_of_layer[layer] * B * c->Hkv * m.max_slots;
+  m.out = out;
+  m.score_stride = pl.score_stride;
+  m.B = B;
+  m.Hq = c->Hq;
+  m.Hkv = c->Hkv;
+  m.G = p.G;
+  m.pieces = pl.pieces;
+  return cuda_status(launch_mass_add(m, c->dtype, c->d, (cudaStream_t)stream));
+}
+
+wm_status wm_cache_evict(const wm_config* c, const wm_cache* cache, const float* mass, float* mass_out,
+                         const int32_t* page_table, const int32_t* seq_lens, int32_t budget, int32_t sinks,
+                         int32_t recent, int32_t B, int32_t max_pages, int32_t* kept, int32_t* new_lens,
+                         int32_t* dev_status, void* stream) {
+  wm_status st = check_attn(c, cache, 0, B, max_pages);
+  if (st != WM_OK) return st;
+  if (budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget) return WM_ERR_INVALID_ARG;
+  if (budget > max_pages * c->page_size) return WM_ERR_INVALID_ARG;
+  if (B == 0) return WM_OK;
+  if ((int64_t)c->k * B * c->Hkv > INT32_MAX) return WM_ERR_UNSUPPORTED;
+  if (!mass || !mass_out || !page_table || !seq_lens || !kept || !new_lens) return WM_ERR_INVALID_ARG;
+  if (!aligned(mass, 4) || !aligned(mass_out, 4) || new_lens == seq_lens) return WM_ERR_INVALID_ARG;
+  EvictParams p{};
+  p.k_pool = cache->k_pool;
+  p.v_pool = cache->v_pool;
+  p.mass = mass;
+  p.mass_out = mass_out;
+  p.page_table = page_table;
+  p.seq_lens = seq_lens;
+  p.kept = kept;
+  p.new_lens = new_lens;
+  p.status = dev_status;
+  p.B = B;
+  p.k = c->k;
+  p.Hkv = c->Hkv;
+  p.P = c->page_size;
+  p.log2P = ilog2(c->page_size);
+  p.num_pages = cache->num_pages;
+  p.max_pages = max_pages;
+  p.budget = budget;
+  p.sinks = sinks;
+  p.recent = recent;
+  return cuda_status(launch_cache_evict(p, c->dtype, c->d, (cudaStream_t)stream));
+}
+
+}  // extern "C"

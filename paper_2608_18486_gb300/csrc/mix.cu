@@ -4,7 +4,7 @@
 // Kernels, in launch order:
 //   1. prenorm   : per (token, layer) inverse RMS of h_l; writes the router
 //                  input xi = [hhat_{L-1}, hhat_{L-1-p}, ...] for both branches;
-//                  per token the RoPE cos/sin at pos = slot - 1.
+//                  per token the RoPE cos/sin at pos = slot - 1 (or a given pos).
 //   2. router    : z = Wr[X] xi (split over the L'D reduction), fp32 partials;
 //                  tcgen05 for bf16 (proj_tc.cu), SIMT FMA for fp32.
 //   3. mix       : alpha = reshape(z + br), htilde_j = sum_l alpha[j][l] hhat_l,
@@ -132,8 +132,7 @@ __global__ void __launch_bounds__(kMixThreads) prenorm_kernel(const MixParams p)
   }
   if (l == 0) {
     // RoPE angle pos * theta^(-2i/d) in fp64, reduced to [-pi, pi] before sincosf
-    const int s = p.slot[b];
-    const double pos = (double)(s - 1);
+    const double pos = (double)(p.pos ? p.pos[b] : p.slot[b] - 1);
     for (int i = tid; i < p.d / 2; i += kMixThreads) {
       const double a = pos * p.inv_freq[i];
       const double two_pi = 6.283185307179586476925286766559;
@@ -185,7 +184,7 @@ __global__ void __launch_bounds__(kMixThreads) prenorm_rows_kernel(const MixPara
   }
   if (l == 0) {
     // RoPE angle pos * theta^(-2i/d) in fp64, reduced to [-pi, pi] before sincosf
-    const double pos = (double)(p.slot[b] - 1);
+    const double pos = (double)(p.pos ? p.pos[b] : p.slot[b] - 1);
     for (int i = lane; i < p.d / 2; i += 32) {
       const double a = pos * p.inv_freq[i];
       const double two_pi = 6.283185307179586476925286766559;

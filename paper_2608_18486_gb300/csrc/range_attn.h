@@ -1,0 +1,93 @@
+// Launch interface of the attention over part of a sequence's slots: sliding
+// windows with sinks, shared prefixes and their suffixes, and decode attention
+// that keeps its scores (range_attn.cuh, range_attn.cu).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "wm.h"
+
+namespace wm {
+
+// What a unit (one group of query rows that read the same K/V rows) covers.
+enum RangeMode : int32_t {
+  kRangeWindow = 0,  // (sequence, kv head): the sinks and the window, written to out
+  kRangeSuffix = 1,  // (sequence, kv head): slots begin .. S-1, partial records
+  kRangePrefix = 2,  // (8 query rows of any sequences, kv head): slots 0 .. begin-1 of
+                     // sequence 0's pages, partial records
+  kRangeScores = 3   // (sequence, kv head): every slot, partial records and scores
+};
+
+constexpr int kRangeRows = 8;        // most query rows of a unit
+constexpr int kRangeWarps = 4;       // warps per CTA
+constexpr int kRangeMaxCluster = 8;
+
+struct RangeParams {
+  const void* k_pool;         // channel base of the K pool
+  const void* v_pool;
+  const void* q;              // [B][Hq][d]
+  void* out;                  // [B][Hq][d] (kRangeWindow)
+  const int32_t* page_table;  // [B][max_pages]
+  const int32_t* seq_lens;    // [B]
+  int32_t* status;
+  float* part;                // [units][pieces][range_rec(rows, d)]
+  float* scores;              // [units][G][score_stride] log2-scaled scores (kRangeScores)
+  int64_t score_stride;
+  int32_t mode, B, Hq, Hkv, G, P, log2P, num_pages, max_pages;
+  int32_t rows_per_seq;       // "sequences" per page-table row (many query positions of one), 1 for decode
+  int32_t len_add;            // slots of sequence b: seq_lens[b] + len_add
+  int32_t sinks, window;      // kRangeWindow
+  int32_t begin;              // kRangeSuffix / kRangePrefix: slots in the shared prefix
+  int32_t rows;               // query rows per unit: G, or kRangeRows for kRangePrefix
+  int32_t pieces;             // CTAs per unit
+  float qscale;               // log2(e) / sqrt(d)
+};
+
+// floats of one partial record: rows x d unnormalised outputs, then (max, sum)
+// per row in log2 units
+constexpr int range_rec(int rows, int d) { return rows * (d + 2); }
+
+// Slots of one pipeline stage (the grain the planner splits by).
+int range_stage_slots(int dtype, int d);
+// CTAs of the kernel that fit one SM (the planner's unit of residency).
+constexpr int kRangeCtasPerSm = 2;
+cudaError_t launch_range_attn(const RangeParams& p, int dtype, int d, int units, cudaStream_t s);
+
+// Joins the partial records of the shared prefix and of each sequence's suffix.
+struct PrefixJoinParams {
+  const float* prefix;  // [row groups][Hkv][prefix_pieces][range_rec(8, d)]
+  const float* suffix;  // [B][Hkv][suffix_pieces][range_rec(G, d)]
+  void* out;
+  int32_t B, Hq, Hkv, G, prefix_pieces, suffix_pieces;
+};
+cudaError_t launch_prefix_join(const PrefixJoinParams& p, int dtype, int d, cudaStream_t s);
+
+// Joins the partial records of kRangeScores and adds the weights to mass.
+struct MassParams {
+  const float* part;     // [B][Hkv][pieces][range_rec(G, d)]
+  const float* scores;   // [B][Hkv][G][score_stride]
+  const int32_t* seq_lens;
+  float* mass;           // [B][Hkv][max_slots], the call's channel
+  void* out;             // [B][Hq][d]
+  int64_t score_stride;
+  int32_t B, Hq, Hkv, G, pieces, max_slots;
+};
+cudaError_t launch_mass_add(const MassParams& p, int dtype, int d, cudaStream_t s);
+
+// Cache eviction (evict.cu).
+struct EvictParams {
+  void* k_pool;               // whole pools: [k][num_pages][Hkv][P][d]
+  void* v_pool;
+  const float* mass;          // [k][B][Hkv][max_slots]
+  float* mass_out;
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+  int32_t* kept;              // [k][B][Hkv][budget]
+  int32_t* new_lens;
+  int32_t* status;
+  int32_t B, k, Hkv, P, log2P, num_pages, max_pages, budget, sinks, recent;
+};
+cudaError_t launch_cache_evict(const EvictParams& p, int dtype, int d, cudaStream_t s);
+
+}  // namespace wm

@@ -6,35 +6,30 @@
 #include <atomic>
 #include <mutex>
 
+#include "api_util.h"
 #include "common.cuh"
 #include "internal.h"
 #include "wm.h"
 
-namespace {
-
-constexpr int kMaxDevices = 64;
-int g_sm_count[kMaxDevices];  // per-device attribute cache (0 = not yet read)
+namespace wm {
 
 int sm_count() {
+  static int cached[kMaxDevices];  // per-device attribute (0 = not yet read)
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 148;
-  if (dev < kMaxDevices && g_sm_count[dev] > 0) return g_sm_count[dev];
+  if (dev < kMaxDevices && cached[dev] > 0) return cached[dev];
   int n = 0;
   if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
     n = 148;
-  if (dev < kMaxDevices) g_sm_count[dev] = n;
+  if (dev < kMaxDevices) cached[dev] = n;
   return n;
 }
 
-bool is_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
-int ilog2(int x) {
-  int r = 0;
-  while ((1 << r) < x) ++r;
-  return r;
-}
-size_t elem_size(int dtype) { return dtype == WM_DT_F32 ? 4 : 2; }
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+}  // namespace wm
+
+namespace {
+
+using namespace wm;
 
 // Persistent grid of one attention launch and its workspace layout.
 struct AttnPlan {
@@ -205,15 +200,6 @@ int32_t next_attn_epoch() {
   return (int32_t)(e & 0x7FFFFFFFu);
 }
 
-wm_status check_cache(const wm_config& c, const wm_cache* cache) {
-  if (!cache || !cache->k_pool || !cache->v_pool || cache->num_pages < 1) return WM_ERR_INVALID_ARG;
-  if (cache->k != c.k || cache->Hkv != c.Hkv || cache->page_size != c.page_size ||
-      cache->d != c.d || cache->dtype != c.dtype)
-    return WM_ERR_INVALID_ARG;
-  if (!aligned(cache->k_pool, 16) || !aligned(cache->v_pool, 16)) return WM_ERR_INVALID_ARG;
-  return WM_OK;
-}
-
 // Checks, plans and launches one decode-attention call.  clear_workspace:
 // zero the span of the workspace the launch uses (counters and records) on
 // the stream just before the launch, after every argument check passed; the
@@ -275,6 +261,65 @@ wm_status decode_attn_impl(const wm_config* c, const wm_cache* cache, int32_t la
                                         B * c->Hkv, pl.unit_ctas, (cudaStream_t)stream)
           : wm::launch_decode_attn(p, pl.stage_bytes, c->dtype, c->d, c->Hq / c->Hkv, pl.grid,
                                    (cudaStream_t)stream);
+  return e == cudaSuccess ? WM_OK : WM_ERR_CUDA;
+}
+
+// Checks and launches one pool call; pos: the tokens' positions, or NULL for
+// slot - 1.
+wm_status kv_mix_impl(const wm_config* c, const wm_cache* cache, const wm_mix_weights* w,
+                      const void* h, const int32_t* page_table, const int32_t* slot,
+                      const int32_t* pos, int32_t B, int32_t max_pages, void* workspace,
+                      size_t ws_bytes, int32_t* dev_status, void* stream) {
+  wm_status st = wm_config_check(c);
+  if (st != WM_OK) return st;
+  if ((st = check_cache(*c, cache)) != WM_OK) return st;
+  if (B < 0 || max_pages < 1 || !w) return WM_ERR_INVALID_ARG;
+  if ((int64_t)max_pages * c->page_size > INT32_MAX / 2) return WM_ERR_INVALID_ARG;
+  if (B == 0) return WM_OK;
+  if (B > 65535) return WM_ERR_UNSUPPORTED;
+  if (!h || !page_table || !slot || !workspace || !w->qk_g) return WM_ERR_INVALID_ARG;
+  for (int X = 0; X < 2; ++X)
+    if (!w->pre_g[X] || !w->Wr[X] || !w->br[X] || !w->ch_g[X] || !w->Wkv[X])
+      return WM_ERR_INVALID_ARG;
+  for (int X = 0; X < 2; ++X)
+    if (!aligned(w->Wr[X], 16) || !aligned(w->Wkv[X], 16) || !aligned(w->pre_g[X], 16) ||
+        !aligned(w->ch_g[X], 16))
+      return WM_ERR_INVALID_ARG;
+  if (!aligned(h, 16)) return WM_ERR_INVALID_ARG;
+  if (!aligned(workspace, 256)) return WM_ERR_INVALID_ARG;
+  const wm::MixWorkspace ws = wm::mix_workspace_layout(*c, B, sm_count());
+  if (ws_bytes < ws.total) return WM_ERR_INVALID_ARG;
+
+  wm::MixParams p{};
+  mix_shape(*c, B, p);
+  p.num_pages = cache->num_pages;
+  p.max_pages = max_pages;
+  p.h = h;
+  for (int X = 0; X < 2; ++X) {
+    p.pre_g[X] = w->pre_g[X];
+    p.Wr[X] = w->Wr[X];
+    p.br[X] = w->br[X];
+    p.ch_g[X] = w->ch_g[X];
+    p.Wkv[X] = w->Wkv[X];
+  }
+  p.qk_g = w->qk_g;
+  p.page_table = page_table;
+  p.slot = slot;
+  p.pos = pos;
+  p.k_pool = cache->k_pool;
+  p.v_pool = cache->v_pool;
+  char* base = (char*)workspace;
+  p.inv_rms = (float*)(base + ws.inv_rms);
+  p.xi = base + ws.xi;
+  p.zpart = (float*)(base + ws.zpart);
+  p.rope_cs = (float*)(base + ws.rope_cs);
+  p.xop = base + ws.xop;
+  p.proj = (float*)(base + ws.proj);
+  p.nsplit_r = ws.nsplit_r;
+  p.status = dev_status;
+  for (int i = 0; i < c->d / 2 && i < wm::kMaxRopeHalf; ++i)
+    p.inv_freq[i] = pow(c->rope_theta, -2.0 * i / c->d);
+  cudaError_t e = wm::launch_kv_mix(p, c->dtype, (cudaStream_t)stream);
   return e == cudaSuccess ? WM_OK : WM_ERR_CUDA;
 }
 
@@ -436,56 +481,17 @@ wm_status wm_kv_mix(const wm_config* c, const wm_cache* cache, const wm_mix_weig
                     const void* h, const int32_t* page_table, const int32_t* slot, int32_t B,
                     int32_t max_pages, void* workspace, size_t ws_bytes, int32_t* dev_status,
                     void* stream) {
-  wm_status st = wm_config_check(c);
-  if (st != WM_OK) return st;
-  if ((st = check_cache(*c, cache)) != WM_OK) return st;
-  if (B < 0 || max_pages < 1 || !w) return WM_ERR_INVALID_ARG;
-  if ((int64_t)max_pages * c->page_size > INT32_MAX / 2) return WM_ERR_INVALID_ARG;
-  if (B == 0) return WM_OK;
-  if (B > 65535) return WM_ERR_UNSUPPORTED;
-  if (!h || !page_table || !slot || !workspace || !w->qk_g) return WM_ERR_INVALID_ARG;
-  for (int X = 0; X < 2; ++X)
-    if (!w->pre_g[X] || !w->Wr[X] || !w->br[X] || !w->ch_g[X] || !w->Wkv[X])
-      return WM_ERR_INVALID_ARG;
-  for (int X = 0; X < 2; ++X)
-    if (!aligned(w->Wr[X], 16) || !aligned(w->Wkv[X], 16) || !aligned(w->pre_g[X], 16) ||
-        !aligned(w->ch_g[X], 16))
-      return WM_ERR_INVALID_ARG;
-  if (!aligned(h, 16)) return WM_ERR_INVALID_ARG;
-  if (!aligned(workspace, 256)) return WM_ERR_INVALID_ARG;
-  const wm::MixWorkspace ws = wm::mix_workspace_layout(*c, B, sm_count());
-  if (ws_bytes < ws.total) return WM_ERR_INVALID_ARG;
+  return kv_mix_impl(c, cache, w, h, page_table, slot, nullptr, B, max_pages, workspace, ws_bytes,
+                     dev_status, stream);
+}
 
-  wm::MixParams p{};
-  mix_shape(*c, B, p);
-  p.num_pages = cache->num_pages;
-  p.max_pages = max_pages;
-  p.h = h;
-  for (int X = 0; X < 2; ++X) {
-    p.pre_g[X] = w->pre_g[X];
-    p.Wr[X] = w->Wr[X];
-    p.br[X] = w->br[X];
-    p.ch_g[X] = w->ch_g[X];
-    p.Wkv[X] = w->Wkv[X];
-  }
-  p.qk_g = w->qk_g;
-  p.page_table = page_table;
-  p.slot = slot;
-  p.k_pool = cache->k_pool;
-  p.v_pool = cache->v_pool;
-  char* base = (char*)workspace;
-  p.inv_rms = (float*)(base + ws.inv_rms);
-  p.xi = base + ws.xi;
-  p.zpart = (float*)(base + ws.zpart);
-  p.rope_cs = (float*)(base + ws.rope_cs);
-  p.xop = base + ws.xop;
-  p.proj = (float*)(base + ws.proj);
-  p.nsplit_r = ws.nsplit_r;
-  p.status = dev_status;
-  for (int i = 0; i < c->d / 2 && i < wm::kMaxRopeHalf; ++i)
-    p.inv_freq[i] = pow(c->rope_theta, -2.0 * i / c->d);
-  cudaError_t e = wm::launch_kv_mix(p, c->dtype, (cudaStream_t)stream);
-  return e == cudaSuccess ? WM_OK : WM_ERR_CUDA;
+wm_status wm_kv_mix_at(const wm_config* c, const wm_cache* cache, const wm_mix_weights* w,
+                       const void* h, const int32_t* page_table, const int32_t* slot,
+                       const int32_t* pos, int32_t B, int32_t max_pages, void* workspace,
+                       size_t ws_bytes, int32_t* dev_status, void* stream) {
+  if (B != 0 && !pos) return WM_ERR_INVALID_ARG;
+  return kv_mix_impl(c, cache, w, h, page_table, slot, pos, B, max_pages, workspace, ws_bytes,
+                     dev_status, stream);
 }
 
 }  // extern "C"

@@ -20,7 +20,9 @@ def torch_dtype(dtype: str):
 
 class DecodeSession:
     def __init__(self, cfg: W.wm_config, B: int, num_pages: int, max_pages: int,
-                 device: str | torch.device = "cuda:0"):
+                 device: str | torch.device = "cuda:0", cache_buf: torch.Tensor | None = None):
+        """cache_buf: a contiguous uint8 tensor that holds the cache (K pool,
+        then V pool, as wm_cache_alloc lays them out); allocated if None."""
         rc = W.wm_config_check(cfg)
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_config_check")
@@ -31,7 +33,14 @@ class DecodeSession:
         nbytes = W.wm_cache_bytes(cfg, num_pages)
         if nbytes == 0:
             raise W.WMError(W.WM_ERR_INVALID_ARG, "wm_cache_bytes")
-        self.cache_buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        if cache_buf is None:
+            cache_buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        elif cache_buf.dtype != torch.uint8 or not cache_buf.is_contiguous() or \
+                cache_buf.device.type != self.device.type:
+            raise ValueError("cache_buf must be a contiguous uint8 tensor on the session's device")
+        elif cache_buf.numel() < nbytes:
+            raise W.WMError(W.WM_ERR_INVALID_ARG, "wm_cache_alloc")
+        self.cache_buf = cache_buf
         self.cache = W.wm_cache_alloc(cfg, self.cache_buf, nbytes, num_pages)
         shape = (cfg.k, num_pages, cfg.Hkv, cfg.page_size, cfg.d)
         esz = 4 if cfg.dtype == W.WM_DT_F32 else 2
@@ -48,6 +57,7 @@ class DecodeSession:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._weights = None
         self._weight_refs = None
+        self._scratch = {}
 
     # ------------------------------------------------------------------ setup
     def set_weights(self, pre_g, Wr, br, ch_g, Wkv, qk_g) -> None:
@@ -89,15 +99,95 @@ class DecodeSession:
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_prefill_attn")
 
-    def kv_mix(self, h, page_table, slot, B: int | None = None, stream=None) -> None:
+    def kv_mix(self, h, page_table, slot, B: int | None = None, stream=None, pos=None) -> None:
+        """pos: int32 positions of the tokens where they are not slot - 1
+        (after an eviction)."""
         if self._weights is None:
             raise RuntimeError("set_weights() first")
         B = self.B if B is None else B
+        if pos is not None:
+            rc = W.wm_kv_mix_at(self.cfg, self.cache, self._weights, h, page_table, slot, pos, B,
+                                self.max_pages, self.mix_ws, self.mix_ws_bytes, self.status,
+                                self._stream(stream))
+            if rc != W.WM_OK:
+                raise W.WMError(rc, "wm_kv_mix_at")
+            return
         rc = W.wm_kv_mix(self.cfg, self.cache, self._weights, h, page_table, slot, B,
                          self.max_pages, self.mix_ws, self.mix_ws_bytes, self.status,
                          self._stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_kv_mix")
+
+    # ---------------------------------------------------------- long contexts
+    def window_attn(self, layer: int, q, page_table, seq_lens, out, *, sinks: int, window: int,
+                    B: int | None = None, stream=None) -> None:
+        """Decode attention over the first ``sinks`` slots and the last
+        ``window`` slots of each sequence."""
+        rc = W.wm_window_attn(self.cfg, self.cache, layer, q, page_table, seq_lens, sinks, window,
+                              self.B if B is None else B, self.max_pages, out, self.status,
+                              self._stream(stream))
+        if rc != W.WM_OK:
+            raise W.WMError(rc, "wm_window_attn")
+
+    def window_prefill_attn(self, layer: int, q, pos, page_table, out, *, sinks: int, window: int,
+                            stream=None) -> None:
+        """window_attn's mask for query rows q [B][Tq][Hq][d] at positions pos
+        [B][Tq]: position i sees slots t <= i, t < sinks or t > i - window."""
+        rc = W.wm_window_prefill_attn(self.cfg, self.cache, layer, q, pos, page_table, sinks, window,
+                                      int(q.shape[0]), int(q.shape[1]), self.max_pages, out,
+                                      self.status, self._stream(stream))
+        if rc != W.WM_OK:
+            raise W.WMError(rc, "wm_window_prefill_attn")
+
+    def _scratch_for(self, nbytes: int, stream):
+        # one buffer per stream for the calls below (they need nothing in it,
+        # so calls on one stream share it), kept at the largest size asked for
+        # and allocated on that stream.  The first call of a size may allocate:
+        # make it before a graph capture.
+        if nbytes == 0:
+            raise W.WMError(W.WM_ERR_INVALID_ARG, "workspace query")
+        s = torch.cuda.current_stream(self.device) if stream is None else stream
+        buf = self._scratch.get(s.cuda_stream)
+        if buf is None or buf.numel() < nbytes:
+            with torch.cuda.stream(s):
+                buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self._scratch[s.cuda_stream] = buf
+        return buf
+
+    def prefix_attn(self, layer: int, q, page_table, seq_lens, out, *, shared_pages: int,
+                    B: int | None = None, stream=None) -> None:
+        """Decode attention of sequences whose first ``shared_pages`` pages are
+        the same ones: those are read once for the batch."""
+        B = self.B if B is None else B
+        need = W.wm_prefix_attn_workspace(self.cfg, B, self.max_pages, shared_pages)
+        rc = W.wm_prefix_attn(self.cfg, self.cache, layer, q, page_table, seq_lens, shared_pages, B,
+                              self.max_pages, out, self._scratch_for(need, stream), need, self.status,
+                              self._stream(stream))
+        if rc != W.WM_OK:
+            raise W.WMError(rc, "wm_prefix_attn")
+
+    def decode_attn_mass(self, layer: int, q, page_table, seq_lens, mass, out, *,
+                         B: int | None = None, stream=None) -> None:
+        """Decode attention that adds every slot's softmax weight, summed over
+        the query heads of a kv head, to mass [k][B][Hkv][slots] (fp32)."""
+        B = self.B if B is None else B
+        need = W.wm_decode_attn_mass_workspace(self.cfg, B, self.max_pages)
+        rc = W.wm_decode_attn_mass(self.cfg, self.cache, layer, q, page_table, seq_lens, mass, B,
+                                   self.max_pages, out, self._scratch_for(need, stream), need, self.status,
+                                   self._stream(stream))
+        if rc != W.WM_OK:
+            raise W.WMError(rc, "wm_decode_attn_mass")
+
+    def evict(self, mass, page_table, seq_lens, mass_out, kept, new_lens, *, budget: int,
+              sinks: int, recent: int, B: int | None = None, stream=None) -> None:
+        """Cut every (channel, sequence, kv head) to ``budget`` slots: the
+        first ``sinks``, the last ``recent`` and those with the largest mass.
+        Writes mass_out (may be mass), kept [k][B][Hkv][budget] and new_lens."""
+        rc = W.wm_cache_evict(self.cfg, self.cache, mass, mass_out, page_table, seq_lens, budget,
+                              sinks, recent, self.B if B is None else B, self.max_pages, kept,
+                              new_lens, self.status, self._stream(stream))
+        if rc != W.WM_OK:
+            raise W.WMError(rc, "wm_cache_evict")
 
     def read_status(self, reset: bool = True) -> int:
         v = int(self.status.item())
