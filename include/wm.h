@@ -303,7 +303,8 @@ wm_status wm_prefill_attn(const wm_config* cfg, const wm_cache* cache, int32_t l
  * bf16 probabilities enter the P V product as bf16.  A sequence may hold no
  * slot at all (length 0): its rows are zeros, and so is any row whose mask
  * leaves nothing.  A negative length, or one past the page table, zero-fills
- * the row and sets WM_ERR_BOUNDS.  Page-table entries of pages without a
+ * the row and sets WM_ERR_BOUNDS.  So does a bad page id, whose slots are
+ * left out.  Page-table entries of pages without a
  * visible slot are not read into anything: the pages may be gone.  Slots that
  * are not visible may hold anything, NaN included.
  */

@@ -84,11 +84,65 @@ RangeParams range_params(const wm_config& c, const wm_cache& cache, int32_t laye
   return p;
 }
 
-// Split of a shared-prefix call and its workspace.
+// The tensor-core kernel is built for bf16 and pages of at least 8 slots (a TMA
+// box is a whole 8-row swizzle atom); its tensor maps take 32-bit rows over all
+// channels.  Everything else runs on the range kernel.
+bool tiles_ok(const wm_config& c, int32_t num_pages) {
+  return c.dtype == WM_DT_BF16 && c.page_size >= 8 && tma_available() &&
+         (int64_t)c.k * num_pages * c.Hkv * c.page_size < INT32_MAX;
+}
+
+TileParams tile_params(const wm_config& c, const wm_cache& cache, int32_t layer, const int32_t* page_table,
+                       int32_t max_pages, int32_t* dev_status) {
+  TileParams p{};
+  p.page_table = page_table;
+  p.status = dev_status;
+  p.Hq = c.Hq;
+  p.G = c.Hq / c.Hkv;
+  p.Hkv = c.Hkv;
+  p.chan = c.chan_of_layer[layer];
+  p.num_pages = cache.num_pages;
+  p.max_pages = max_pages;
+  p.P = c.page_size;
+  p.log2P = ilog2(c.page_size);
+  p.splits = 1;
+  p.qscale = (float)(1.4426950408889634 / sqrt((double)c.d));
+  return p;
+}
+
+wm_status launch_tiles(const TileParams& p, const wm_config& c, const wm_cache& cache, const void* q, int32_t B,
+                       void* stream) {
+  const TileInputs in{q, cache.k_pool, cache.v_pool, B, c.k, c.d};
+  const cudaError_t e = launch_tile_attn(p, in, sm_count(), (cudaStream_t)stream);
+  if (e == cudaErrorInvalidValue) return WM_ERR_INVALID_ARG;  // the tensor-map encoder refused
+  return e == cudaSuccess ? WM_OK : WM_ERR_CUDA;
+}
+
+// Split of a shared-prefix call and its workspace.  The prefix runs either on
+// the tensor cores (row blocks of 256, or of 128 if there are no more, times
+// `splits` parts of its KV tiles) or on the range kernel (groups of 8 rows,
+// times prefix_pieces).
 struct PrefixPlan {
-  int groups, prefix_pieces, suffix_pieces;
+  int blocks, pair, splits, records;         // tensor cores
+  int groups, prefix_pieces, suffix_pieces;  // range kernel
   size_t off_suffix, total;
 };
+
+// KV parts of the tensor-core prefix: the count with the shortest last CTA,
+// counting a CTA's fixed cost as two KV tiles and each further record's join.
+int prefix_splits(int64_t units, int64_t tiles, int sms) {
+  int best = 1;
+  double least = 1e30;
+  for (int n = 1; n <= 64 && n <= tiles; ++n) {
+    const double waves = (double)((units * n + sms - 1) / sms);
+    const double cost = waves * ((double)((tiles + n - 1) / n) + 2.0) + 0.05 * n;
+    if (cost < least) {
+      least = cost;
+      best = n;
+    }
+  }
+  return best;
+}
 
 PrefixPlan prefix_plan(const wm_config& c, int32_t B, int32_t max_pages, int32_t shared_pages) {
   const int G = c.Hq / c.Hkv;
@@ -97,7 +151,17 @@ PrefixPlan prefix_plan(const wm_config& c, int32_t B, int32_t max_pages, int32_t
   pl.prefix_pieces = split_pieces((int64_t)pl.groups * c.Hkv, stages_of(c, (int64_t)shared_pages * c.page_size), 2);
   pl.suffix_pieces =
       split_pieces((int64_t)B * c.Hkv, stages_of(c, (int64_t)(max_pages - shared_pages) * c.page_size), 2);
-  pl.off_suffix = align256(sizeof(float) * (size_t)pl.groups * c.Hkv * pl.prefix_pieces * range_rec(kRangeRows, c.d));
+  const int64_t rows = (int64_t)B * G;
+  pl.pair = rows <= kTileRows ? 1 : 0;
+  pl.blocks = pl.pair ? 1 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
+  pl.splits = prefix_splits((int64_t)pl.blocks * c.Hkv,
+                            ((int64_t)shared_pages * c.page_size + kTileSlots - 1) / kTileSlots, sm_count());
+  pl.records = pl.splits * (pl.pair ? 2 : 1);
+  const size_t tile_bytes = sizeof(float) * (size_t)c.Hkv * rows * pl.records * tile_rec(c.d);
+  const size_t range_bytes =
+      sizeof(float) * (size_t)pl.groups * c.Hkv * pl.prefix_pieces * range_rec(kRangeRows, c.d);
+  // (room for either: which one runs depends on the cache too)
+  pl.off_suffix = align256(tile_bytes > range_bytes ? tile_bytes : range_bytes);
   pl.total = pl.off_suffix + align256(sizeof(float) * (size_t)B * c.Hkv * pl.suffix_pieces * range_rec(G, c.d));
   return pl;
 }
@@ -156,6 +220,20 @@ wm_status wm_window_prefill_attn(const wm_config* c, const wm_cache* cache, int3
   if ((int64_t)B * Tq > INT32_MAX / 2 / c->Hq) return WM_ERR_UNSUPPORTED;
   if (!q || !pos || !page_table || !out) return WM_ERR_INVALID_ARG;
   if (!aligned(q, 16) || !aligned(out, 16)) return WM_ERR_INVALID_ARG;
+  if (tiles_ok(*c, cache->num_pages)) {
+    const int64_t slots = (int64_t)max_pages * c->page_size;
+    TileParams t = tile_params(*c, *cache, layer, page_table, max_pages, dev_status);
+    t.pos = pos;
+    t.out = out;
+    t.rows = Tq;
+    t.sinks = (int32_t)(sinks < slots ? sinks : slots);
+    t.window = (int32_t)(window < slots ? window : slots);
+    t.pair = t.G % 2 == 0 ? 1 : 0;
+    const int block = t.pair ? kTileRows : 2 * kTileRows;
+    t.blocks = (Tq + block - 1) / block;
+    t.items = B * (t.pair ? c->Hq / 2 : c->Hq) * t.blocks;
+    return launch_tiles(t, *c, *cache, q, B, stream);
+  }
   RangeParams p = range_params(*c, *cache, layer, q, page_table, pos, B * Tq, max_pages, dev_status);
   p.mode = kRangeWindow;
   p.out = out;
@@ -187,18 +265,31 @@ wm_status wm_prefix_attn(const wm_config* c, const wm_cache* cache, int32_t laye
   if (ws_bytes < pl.total) return WM_ERR_INVALID_ARG;
   RangeParams p = range_params(*c, *cache, layer, q, page_table, seq_lens, B, max_pages, dev_status);
   p.begin = shared_pages * c->page_size;
-  p.part = (float*)workspace;
-  p.mode = kRangePrefix;
-  p.rows = kRangeRows;
-  p.pieces = pl.prefix_pieces;
-  cudaError_t e = launch_range_attn(p, c->dtype, c->d, pl.groups * c->Hkv, (cudaStream_t)stream);
-  if (e != cudaSuccess) return WM_ERR_CUDA;
+  const bool tiles = tiles_ok(*c, cache->num_pages);
+  if (shared_pages > 0 && tiles) {
+    TileParams t = tile_params(*c, *cache, layer, page_table, max_pages, dev_status);
+    t.pos = seq_lens;
+    t.part = (float*)workspace;
+    t.rows = B * p.G;
+    t.prefix_slots = p.begin;
+    t.pair = pl.pair;
+    t.splits = pl.splits;
+    t.records = pl.records;
+    t.items = pl.blocks * c->Hkv * pl.splits;
+    if ((st = launch_tiles(t, *c, *cache, q, B, stream)) != WM_OK) return st;
+  } else if (shared_pages > 0) {
+    p.part = (float*)workspace;
+    p.mode = kRangePrefix;
+    p.rows = kRangeRows;
+    p.pieces = pl.prefix_pieces;
+    if (launch_range_attn(p, c->dtype, c->d, pl.groups * c->Hkv, (cudaStream_t)stream) != cudaSuccess)
+      return WM_ERR_CUDA;
+  }
   p.part = (float*)((char*)workspace + pl.off_suffix);
   p.mode = kRangeSuffix;
   p.rows = p.G;
   p.pieces = pl.suffix_pieces;
-  e = launch_range_attn(p, c->dtype, c->d, B * c->Hkv, (cudaStream_t)stream);
-  if (e != cudaSuccess) return WM_ERR_CUDA;
+  if (launch_range_attn(p, c->dtype, c->d, B * c->Hkv, (cudaStream_t)stream) != cudaSuccess) return WM_ERR_CUDA;
   PrefixJoinParams j{};
   j.prefix = (const float*)workspace;
   j.suffix = p.part;
@@ -207,7 +298,8 @@ wm_status wm_prefix_attn(const wm_config* c, const wm_cache* cache, int32_t laye
   j.Hq = c->Hq;
   j.Hkv = c->Hkv;
   j.G = p.G;
-  j.prefix_pieces = pl.prefix_pieces;
+  j.tiles = tiles ? 1 : 0;
+  j.prefix_pieces = shared_pages == 0 ? 0 : tiles ? pl.records : pl.prefix_pieces;
   j.suffix_pieces = pl.suffix_pieces;
   return cuda_status(launch_prefix_join(j, c->dtype, c->d, (cudaStream_t)stream));
 }

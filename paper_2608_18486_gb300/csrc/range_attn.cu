@@ -57,18 +57,19 @@ __global__ void __launch_bounds__(kJoinWarps * 32) prefix_join_kernel(const Pref
   const int row = (int)blockIdx.x * kJoinWarps + (int)(threadIdx.x >> 5);
   if (row >= p.B * p.Hq) return;
   const int b = row / p.Hq, hq = row - b * p.Hq, h = hq / p.G, g = hq - h * p.G;
-  // the row's records: its place in its group of 8 rows, then its suffix
+  // the row's records: of the prefix, then of its suffix
+  const int np = p.prefix_pieces, srec = range_rec(p.G, HD);
   const int x = b * p.G + g, grp = x / kRangeRows, xr = x - grp * kRangeRows;
-  const int prec = range_rec(kRangeRows, HD), srec = range_rec(p.G, HD);
-  const float* pre = p.prefix + ((int64_t)grp * p.Hkv + h) * p.prefix_pieces * prec;
+  const int prec = p.tiles ? tile_rec(HD) : range_rec(kRangeRows, HD);
+  const float* pre = p.prefix + (p.tiles ? ((int64_t)h * p.B * p.G + x) * np * prec
+                                         : ((int64_t)grp * p.Hkv + h) * np * prec + xr * HD);
+  const int pml = p.tiles ? HD : kRangeRows * HD + 2 * xr - xr * HD;  // (max, sum) of a record, from its outputs
   const float* suf = p.suffix + ((int64_t)b * p.Hkv + h) * p.suffix_pieces * srec;
-  const int np = p.prefix_pieces;
   auto rec = [&](int i) -> const float* {
-    return i < np ? pre + (int64_t)i * prec + xr * HD : suf + (int64_t)(i - np) * srec + g * HD;
+    return i < np ? pre + (int64_t)i * prec : suf + (int64_t)(i - np) * srec + g * HD;
   };
   auto ml = [&](int i) -> float2 {
-    const float* r = i < np ? pre + (int64_t)i * prec + kRangeRows * HD + 2 * xr
-                            : suf + (int64_t)(i - np) * srec + p.G * HD + 2 * g;
+    const float* r = i < np ? pre + (int64_t)i * prec + pml : suf + (int64_t)(i - np) * srec + p.G * HD + 2 * g;
     return make_float2(__ldcg(r), __ldcg(r + 1));
   };
   join_row<T, HD>(reinterpret_cast<T*>(p.out) + (int64_t)row * HD, np + p.suffix_pieces, lane, rec, ml);

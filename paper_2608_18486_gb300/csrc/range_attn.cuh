@@ -15,7 +15,8 @@
 // stored there reaches the sums).  The work reads about one byte per FLOP and
 // is bound by HBM, so the math only has to stay out of the way:
 //  * bf16: mma.sync m16n8k16 with the query rows as the 16-row operand (8 used)
-//    for both products, K and V read from shared memory with ldmatrix (chunks
+//    for both products (in P V the 8 others carry the low parts of the
+//    probabilities), K and V read from shared memory with ldmatrix (chunks
 //    of 16 bytes XOR-swizzled by the slot, so that no read conflicts); the
 //    cost does not grow with the query heads of a kv head.
 //  * fp32: CUDA-core FMAs, 8 lanes per slot, queries in shared memory.
@@ -88,6 +89,16 @@ __device__ __forceinline__ void mma_rows8(float (&c)[2], uint32_t a0, uint32_t a
       : "r"(a0), "r"(0u), "r"(a2), "r"(b0), "r"(b1), "f"(0.f));
 }
 
+// c += A B, all 16 rows
+__device__ __forceinline__ void mma_rows16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                           uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
 // The visible slots of a unit: [0, a) and [w0, S), as stages of SS slots.
 struct Range {
   int S, a, w0, n0, f, n;  // n0 stages of the first part, then from stage f on; n in all
@@ -112,7 +123,8 @@ struct MmaMath {
   using SH = Shape<T, HD>;
   static constexpr int SS = SH::SS, NT = SS / 8;
   uint32_t qa[HD / 16][2];  // A operand: row lane / 4, features 16 kk + 2 (lane % 4) (+ 8)
-  float acc[HD / 8][2];     // row lane / 4, features 8 j + 2 (lane % 4) + {0, 1}
+  float acc[HD / 8][4];     // features 8 j + 2 (lane % 4) + {0, 1} of row lane / 4: from the
+                            // probabilities' high parts, then from their low parts
   float m, l;               // of row lane / 4 (l: this lane's slots only)
   int lim;                  // slots of the row: t < lim
 
@@ -125,7 +137,7 @@ struct MmaMath {
       qa[kk][1] = qrow ? __ldcg(reinterpret_cast<const uint32_t*>(qrow + 16 * kk + 8 + 2 * c)) : 0u;
     }
 #pragma unroll
-    for (int j = 0; j < HD / 8; ++j) acc[j][0] = acc[j][1] = 0.f;
+    for (int j = 0; j < HD / 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
     m = -INFINITY;
     l = 0.f;
     lim = lim_;
@@ -168,22 +180,24 @@ struct MmaMath {
       const float corr = m == -INFINITY ? 0.f : exp2f(m - mnew);
       l *= corr;
 #pragma unroll
-      for (int j = 0; j < HD / 8; ++j) {
-        acc[j][0] *= corr;
-        acc[j][1] *= corr;
-      }
+      for (int j = 0; j < HD / 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] *= corr;
       m = mnew;
     }
-    // probabilities; they enter P V as bf16 (like the prefill attention's), the
-    // row sum is kept from the unrounded ones
-    uint32_t pa[NT];
+    // Probabilities enter P V as two bf16 parts, p = hi + lo (16 bits of p): the
+    // low parts fill rows 8-15 of the A operand, which the query rows leave
+    // empty, so they cost no product.  The row sum is kept from p itself.
+    uint32_t hi[NT], lo[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const float p0 = s[nt][0] == -INFINITY ? 0.f : exp2f(s[nt][0] - m);
       const float p1 = s[nt][1] == -INFINITY ? 0.f : exp2f(s[nt][1] - m);
       l += p0 + p1;
       const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
-      pa[nt] = *reinterpret_cast<const uint32_t*>(&h);
+      const __nv_bfloat162 g = __floats2bfloat162_rn(p0 - __low2float(h), p1 - __high2float(h));
+      hi[nt] = *reinterpret_cast<const uint32_t*>(&h);
+      lo[nt] = *reinterpret_cast<const uint32_t*>(&g);
     }
 #pragma unroll
     for (int kt = 0; kt < NT / 2; ++kt) {
@@ -192,8 +206,8 @@ struct MmaMath {
       for (int u = 0; u < HD / 16; ++u) {
         uint32_t b[4];
         ldsm4_t(b, vs + slot * SH::ROW_BYTES + swz<T, HD>(slot, 2 * u + (lane >> 4)) * 16);
-        mma_rows8(acc[2 * u], pa[2 * kt], pa[2 * kt + 1], b[0], b[1]);
-        mma_rows8(acc[2 * u + 1], pa[2 * kt], pa[2 * kt + 1], b[2], b[3]);
+        mma_rows16(acc[2 * u], hi[2 * kt], lo[2 * kt], hi[2 * kt + 1], lo[2 * kt + 1], b[0], b[1]);
+        mma_rows16(acc[2 * u + 1], hi[2 * kt], lo[2 * kt], hi[2 * kt + 1], lo[2 * kt + 1], b[2], b[3]);
       }
     }
   }
@@ -206,7 +220,7 @@ struct MmaMath {
     if (r >= rows) return;
 #pragma unroll
     for (int j = 0; j < HD / 8; ++j)
-      *reinterpret_cast<float2*>(rec + r * HD + 8 * j + 2 * c) = make_float2(acc[j][0], acc[j][1]);
+      *reinterpret_cast<float2*>(rec + r * HD + 8 * j + 2 * c) = make_float2(acc[j][0] + acc[j][2], acc[j][1] + acc[j][3]);
     if (c == 0) {
       rec[rows * HD + 2 * r] = m;
       rec[rows * HD + 2 * r + 1] = l;

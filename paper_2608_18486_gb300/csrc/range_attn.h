@@ -56,10 +56,12 @@ cudaError_t launch_range_attn(const RangeParams& p, int dtype, int d, int units,
 
 // Joins the partial records of the shared prefix and of each sequence's suffix.
 struct PrefixJoinParams {
-  const float* prefix;  // [row groups][Hkv][prefix_pieces][range_rec(8, d)]
+  const float* prefix;  // tile records [Hkv][B * G][prefix_pieces][tile_rec(d)], or range
+                        // records [row groups][Hkv][prefix_pieces][range_rec(8, d)]
   const float* suffix;  // [B][Hkv][suffix_pieces][range_rec(G, d)]
   void* out;
   int32_t B, Hq, Hkv, G, prefix_pieces, suffix_pieces;
+  int32_t tiles;        // the prefix records' layout
 };
 cudaError_t launch_prefix_join(const PrefixJoinParams& p, int dtype, int d, cudaStream_t s);
 
@@ -74,6 +76,42 @@ struct MassParams {
   int32_t B, Hq, Hkv, G, pieces, max_slots;
 };
 cudaError_t launch_mass_add(const MassParams& p, int dtype, int d, cudaStream_t s);
+
+// Tensor-core attention of many rows (tile_attn.cu; bf16, pages of >= 8 slots):
+// under a window with sinks (part == NULL), or over a shared prefix into
+// partial records.
+struct TileParams {
+  const int32_t* pos;         // window: [B][rows] positions; prefix: [B] lengths
+  const int32_t* page_table;  // [B][max_pages]
+  void* out;                  // window: [B][rows][Hq][d]
+  float* part;                // prefix: [Hkv][rows][records][tile_rec(d)]
+  int32_t* status;
+  int32_t rows;               // window: query positions per sequence; prefix: B * G
+  int32_t Hq, G, Hkv, chan, num_pages, max_pages, P, log2P;
+  int32_t sinks, window;      // at most the page table's slots
+  int32_t prefix_slots;
+  int32_t pair;               // window: the two tiles are query heads h, h + 1 of the same
+                              // rows; prefix: they are the even and odd KV tiles of one
+  int32_t splits;             // prefix: parts of the KV tiles
+  int32_t records;            // prefix: partial records per row
+  int32_t blocks;             // window: row blocks per head
+  int32_t items;
+  float qscale;               // log2(e) / sqrt(d)
+};
+struct TileInputs {
+  const void* q;
+  const void* k_pool;         // whole pools, all channels
+  const void* v_pool;
+  int32_t B, k, d;
+};
+// floats of a partial record: d outputs, (max, sum), padded to 16 bytes
+constexpr int tile_rec(int d) { return d + 4; }
+constexpr int kTileRows = 128;
+constexpr int kTileSlots = 128;
+cudaError_t launch_tile_attn(TileParams p, const TileInputs& in, int sms, cudaStream_t s);
+// 3-D map of a bf16 array [n2][n1][n0], boxes of 64 x box1 x box2 elements,
+// 128-byte swizzle (rows of a box are its (n2, n1) pairs in order).
+bool tma_map_bf16_3d(void* tm, const void* ptr, uint64_t n2, uint64_t n1, uint64_t n0, uint32_t box2, uint32_t box1);
 
 // Cache eviction (evict.cu).
 struct EvictParams {

@@ -5,6 +5,7 @@
 #include <cudaTypedefs.h>
 
 #include "internal.h"
+#include "range_attn.h"
 
 namespace wm {
 namespace {
@@ -35,6 +36,20 @@ bool tma_map_bf16_2d(void* tm, const void* ptr, uint64_t rows, uint64_t cols, ui
   cuuint32_t box[2] = {64u, box_rows};
   cuuint32_t estr[2] = {1, 1};
   return fn(static_cast<CUtensorMap*>(tm), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+            const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool tma_map_bf16_3d(void* tm, const void* ptr, uint64_t n2, uint64_t n1, uint64_t n0, uint32_t box2,
+                     uint32_t box1) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {n0, n1, n2};
+  cuuint64_t strides[2] = {n0 * 2, n1 * n0 * 2};
+  cuuint32_t box[3] = {64u, box1, box2};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(static_cast<CUtensorMap*>(tm), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
             const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

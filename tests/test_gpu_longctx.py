@@ -181,6 +181,31 @@ def test_window_prefill_positions_in_any_order(order):
     check_prefill(c, pos[None], 3, 60, q, got, rows=range(0, len(pos), 5))
 
 
+@pytest.mark.parametrize("G", [1, 2])
+def test_window_prefill_of_scattered_positions_reads_only_visible_slots(G):
+    pos = np.array([300, 5, 171, 172, 40, 600, 601, 333] * 20, dtype=np.int32)
+    seen = sorted({t for i in set(pos.tolist()) for t in prefill_slots(i, 2, 6)})
+    c = Cache([602], Hkv=1, G=G, d=64, page=8, k=1, visible=lambda b: seen, seed=4)
+    for x in range(c.max_pages):
+        if x not in {t // 8 for t in seen}:
+            c.table[:, x] = [-1, BIG, c.num_pages][x % 3]
+    s, q, got = run_prefill(c, pos[None], 2, 6)
+    assert s.read_status() == 0
+    check_prefill(c, pos[None], 2, 6, q, got, rows=list(range(8)) + [127, 128, 159])
+
+
+@pytest.mark.parametrize("Hkv,G", [(32, 1), (16, 2), (8, 4)])
+@pytest.mark.parametrize("sinks,window", [(0, 40), (4, 200), (300, 1)])
+def test_window_prefill_more_tiles_than_sms(Hkv, G, sinks, window):
+    """Several items per CTA, items of a single step among them."""
+    n, B = 1000, 2
+    c = Cache([n] * B, Hkv=Hkv, G=G, d=64, page=64, k=1, seed=Hkv)
+    pos = np.stack([np.arange(n, dtype=np.int32)] * B)
+    s, q, got = run_prefill(c, pos, sinks, window)
+    assert s.read_status() == 0
+    check_prefill(c, pos, sinks, window, q, got, rows=[0, 100, 128, 255, 256, 511, 700, 999])
+
+
 def test_window_prefill_bad_positions_zero_their_rows():
     c = Cache([60], Hkv=1, G=2, d=64, page=16, k=1, seed=8)
     pos = np.arange(0, 60, dtype=np.int32)[None].copy()
@@ -189,6 +214,22 @@ def test_window_prefill_bad_positions_zero_their_rows():
     assert s.read_status() == W.WM_ERR_BOUNDS
     assert (got[0, [7, 30]] == 0).all()
     check_prefill(c, pos, 2, 9, q, got, rows=[0, 6, 8, 29, 31, 59])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_window_prefill_bad_pages_are_left_out(dtype):
+    c = Cache([200], Hkv=1, G=2, d=64, page=16, k=1, dtype=dtype, seed=8)
+    good = c.table.copy()
+    c.table[0, [0, 5]] = [-1, c.num_pages]  # slots 0 .. 15 and 80 .. 95
+    pos = np.arange(200, dtype=np.int32)[None]
+    s, q, got = run_prefill(c, pos, 20, 60)
+    assert s.read_status() == W.WM_ERR_BOUNDS
+    c.table = good
+    for r in (0, 15, 16, 90, 95, 96, 199):
+        ts = [t for t in prefill_slots(r, 20, 60) if t // 16 not in (0, 5)]
+        for hq in range(2):
+            want, _, ds, vmax = c.attend(0, 0, hq, q[0, r, hq], ts)
+            check_rows(c, got[0, r, hq], want, ds, vmax)
 
 
 def test_window_prefill_rows_equal_decode_rows():
