@@ -19,9 +19,12 @@
 // the softmax warps still write the previous item's rows.
 //
 //  * warps 0-3, 4-7: softmax of query tile 0, 1, one thread per row;
-//  * warp 8: TMA, and each item's ranges (from its rows' positions), passed on
-//    through shared memory with the query barrier;
-//  * warp 9: MMA issue.
+//  * warp 8: each item's ranges (from its rows' positions), passed on through
+//    shared memory, and the TMA loads of Q and K;
+//  * warp 9: MMA issue, by one elected lane;
+//  * warp 10: passes each V tile on to the MMA warp, its unseen rows zeroed
+//    where there are any;
+//  * warp 11: the TMA loads of V.
 //
 // The two query tiles of an item are two query heads of one kv head over the
 // same rows where the group size is even, else consecutive rows of one head.
@@ -47,7 +50,9 @@ constexpr int kQT = 2;                    // query tiles per item
 constexpr int kSoftWarps = 4 * kQT;
 constexpr int kLoadWarp = kSoftWarps;
 constexpr int kMmaWarp = kSoftWarps + 1;
-constexpr int kTThreads = (kSoftWarps + 2) * 32;
+constexpr int kFixWarp = kSoftWarps + 2;
+constexpr int kVWarp = kSoftWarps + 3;
+constexpr int kTThreads = (kSoftWarps + 4) * 32;
 constexpr uint32_t kBlock = 128u * 128u;  // bytes of a 64-column block of a 128-row tile
 constexpr uint32_t kTmemCols = 512;       // S_i at 128 i (P_i over its first 64), O_i at 256 + 128 i
 constexpr float kStaleMax = 8.f;          // log2 headroom before O is rescaled
@@ -254,14 +259,16 @@ __global__ void __launch_bounds__(kTThreads, 1)
   constexpr uint32_t TB = SH::TILE_BYTES;
   constexpr unsigned FULL = 0xFFFFFFFFu;
   extern __shared__ uint8_t smem_dyn[];
-  __shared__ uint64_t qfull[2], qempty, mfree[2], kfull[NSK], kempty[NSK], vfull[NSV], vempty[NSV];
+  __shared__ uint64_t qfull[2], qempty, mfull[2], mfree[2], kfull[NSK], kempty[NSK], vfull[NSV], vready[NSV],
+      vempty[NSV];
   __shared__ uint64_t sfull[kQT], pfull[kQT], odone[kQT];
   __shared__ uint32_t tmem_base;
   __shared__ Item items[2];
-  // Boxes of a step whose page does not exist, bit per box.  The TMA warp is at
-  // most NSV + 1 steps ahead of the softmax, so a ring of kBadRing is enough.
+  // Boxes of a step whose page does not exist, bit per box.  K tile j + NSK is
+  // loaded once S of step j is there, and S runs at most two steps ahead of the
+  // softmax, so a ring of kBadRing is enough.
   constexpr int kBadRing = 8;
-  static_assert(NSV + 2 <= kBadRing, "bad-page ring");
+  static_assert(NSK + 3 <= kBadRing, "bad-page ring");
   __shared__ uint32_t bad_boxes[kBadRing];
 
   const int tid = threadIdx.x, lane = tid & 31;
@@ -280,7 +287,8 @@ __global__ void __launch_bounds__(kTThreads, 1)
     mbar_init(&qempty, 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&qfull[s], 1);
-      mbar_init(&mfree[s], kSoftWarps + 1);
+      mbar_init(&mfull[s], 1);
+      mbar_init(&mfree[s], kSoftWarps + 3);
     }
     for (int s = 0; s < NSK; ++s) {
       mbar_init(&kfull[s], 1);
@@ -288,6 +296,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
     }
     for (int s = 0; s < NSV; ++s) {
       mbar_init(&vfull[s], 1);
+      mbar_init(&vready[s], 1);
       mbar_init(&vempty[s], 1);
     }
     for (int i = 0; i < kQT; ++i) {
@@ -315,17 +324,35 @@ __global__ void __launch_bounds__(kTThreads, 1)
   const int stride = (int)gridDim.x;
   bool ok = true;
 
-  if (warp == kLoadWarp) {
+  if (warp == kLoadWarp || warp == kVWarp) {
     // ================================================================ TMA
     // Lane t owns box t of every KV tile (one box per page, or one per 128
     // slots of a longer page) and fetches its page id one tile ahead.
     const int boxes = p.P >= kTN ? 1 : kTN >> p.log2P;  // <= 16 for pages of >= 8 slots
     const int brows = p.P >= kTN ? kTN : p.P;
-    int ks = 0, vs = 0;  // K and V tiles loaded
-    int no = 0;          // items of this CTA
+    const bool kq = warp == kLoadWarp;
+    const CUtensorMap* tm = kq ? &tmK : &tmV;
+    int n_tile = 0;  // tiles loaded
+    int no = 0;      // items of this CTA
     for (int it = (int)blockIdx.x; it < p.items && ok; it += stride, ++no) {
       const Work w = work_of<WIN>(p, it);
-      const Item I = item_of<WIN>(p, w, lane);
+      Item I;
+      if (kq) {
+        I = item_of<WIN>(p, w, lane);
+        if (no >= 2) ok = __all_sync(FULL, mbar_wait(&mfree[no & 1], ((no >> 1) - 1) & 1));
+        if (!ok) break;
+        if (lane == 0) {
+          items[no & 1] = I;
+          mbar_arrive(&mfull[no & 1]);
+        }
+        __syncwarp();
+      } else {
+        ok = __all_sync(FULL, mbar_wait(&mfull[no & 1], (no >> 1) & 1));
+        if (!ok) break;
+        I = items[no & 1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&mfree[no & 1]);
+      }
       const int hkv = WIN ? w.h / p.G : w.h;
       // tensor-map row of this lane's box of step j (-brows: read zeros; below
       // that: zeros, and the box has no page)
@@ -342,124 +369,74 @@ __global__ void __launch_bounds__(kTThreads, 1)
         }
         return row;
       };
-      int row_next = I.steps > 0 ? box_row(0) : 0;
-      if (no >= 2) ok = __all_sync(FULL, mbar_wait(&mfree[no & 1], ((no >> 1) - 1) & 1));
-      if (ok && no >= 1) ok = __all_sync(FULL, mbar_wait(&qempty, (no - 1) & 1));
-      if (!ok) break;
-      if (lane == 0) {
-        items[no & 1] = I;
+      // the queries go out behind the first two K tiles, whose slots free up
+      // before the previous item's queries do
+      auto load_q = [&]() {
+        if (no >= 1) ok = __all_sync(FULL, mbar_wait(&qempty, (no - 1) & 1));
+        if (!ok || lane != 0) return;
         const int nq = !WIN && p.pair ? 1 : kQT;
         if (I.steps == 0) {
           mbar_arrive(&qfull[no & 1]);
-        } else {
-          mbar_arrive_expect_tx(&qfull[no & 1], nq * TB);
-          for (int i = 0; i < nq; ++i)
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb) {
-              if (WIN)
-                tc::tma_load_2d(Qs + i * TB + cb * kBlock, &tmQ, (w.h + (p.pair ? i : 0)) * HD + cb * 64,
-                                w.b * p.rows + w.row0 + (p.pair ? 0 : i * kTM), &qfull[no & 1]);
-              else
-                tc::tma_load_3d(Qs + i * TB + cb * kBlock, &tmQ, cb * 64, w.h * p.G, (w.row0 + i * kTM) / p.G,
-                                &qfull[no & 1]);
-            }
+          return;
         }
-      }
-      __syncwarp();
-      auto load_tile = [&](const CUtensorMap* tm, uint8_t* dst, int row, uint64_t* bar) {
+        mbar_arrive_expect_tx(&qfull[no & 1], nq * TB);
+        for (int i = 0; i < nq; ++i)
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) {
+            if (WIN)
+              tc::tma_load_2d(Qs + i * TB + cb * kBlock, &tmQ, (w.h + (p.pair ? i : 0)) * HD + cb * 64,
+                              w.b * p.rows + w.row0 + (p.pair ? 0 : i * kTM), &qfull[no & 1]);
+            else
+              tc::tma_load_3d(Qs + i * TB + cb * kBlock, &tmQ, cb * 64, w.h * p.G, (w.row0 + i * kTM) / p.G,
+                              &qfull[no & 1]);
+          }
+      };
+      const int q_at = min(2, I.steps);
+      int row_next = I.steps > 0 ? box_row(0) : 0;
+      for (int j = 0; j < I.steps; ++j, ++n_tile) {
+        if (kq && j == q_at) {
+          load_q();
+          ok = __all_sync(FULL, ok);
+          if (!ok) break;
+        }
+        const int row = row_next;
+        if (j + 1 < I.steps) row_next = box_row(j + 1);
+        const int depth = kq ? NSK : NSV, slot = n_tile % depth, turn = n_tile / depth;
+        if (turn > 0) ok = __all_sync(FULL, mbar_wait(kq ? &kempty[slot] : &vempty[slot], (turn - 1) & 1));
+        if (!ok) break;
+        uint64_t* bar = kq ? &kfull[slot] : &vfull[slot];
+        uint8_t* dst = (kq ? Ks : Vs) + slot * TB;
+        if (kq) {
+          const uint32_t gone = __ballot_sync(FULL, row < -brows);
+          if (lane == 0) {
+            bad_boxes[n_tile % kBadRing] = gone;
+            if (gone) report(p.status, WM_ERR_BOUNDS);
+          }
+        }
         if (lane == 0) mbar_arrive_expect_tx(bar, TB);
         __syncwarp();
         if (lane < boxes)
 #pragma unroll
-          for (int cb = 0; cb < CB; ++cb)
-            tc::tma_load_2d(dst + cb * kBlock + lane * brows * 128, tm, cb * 64, row, bar);
-      };
-      for (int j = 0; j < I.steps; ++j, ++ks, ++vs) {
-        const int row = row_next;
-        if (j + 1 < I.steps) row_next = box_row(j + 1);
-        const int sk = ks % NSK, sv = vs % NSV;
-        if (ks >= NSK) ok = __all_sync(FULL, mbar_wait(&kempty[sk], (ks / NSK - 1) & 1));
-        if (!ok) break;
-        const uint32_t gone = __ballot_sync(FULL, row < -brows);
-        if (lane == 0) {
-          bad_boxes[ks % kBadRing] = gone;
-          if (gone) report(p.status, WM_ERR_BOUNDS);
-        }
-        load_tile(&tmK, Ks + sk * TB, row, &kfull[sk]);
-        if (vs >= NSV) ok = __all_sync(FULL, mbar_wait(&vempty[sv], (vs / NSV - 1) & 1));
-        if (!ok) break;
-        load_tile(&tmV, Vs + sv * TB, row, &vfull[sv]);
+          for (int cb = 0; cb < CB; ++cb) tc::tma_load_2d(dst + cb * kBlock + lane * brows * 128, tm, cb * 64, row, bar);
       }
+      if (kq && ok && I.steps == q_at) load_q();
+      ok = __all_sync(FULL, ok);
     }
     if (!ok && lane == 0) report(p.status, WM_ERR_TIMEOUT);
-  } else if (warp == kMmaWarp) {
-    // ================================================================ MMA
-    // every lane runs the schedule (all wait, all zero unseen V rows, wait
-    // outcomes made warp-uniform); one elected lane issues
-    const uint32_t idesc_o = tc::idesc_bf16_f32(kTM, HD) | tc::kIdescBMajorMN;
-    const int la = !WIN && p.pair ? 2 : 1;  // steps that S runs ahead of P V
-    const bool lead = elect_one();
-    // descriptors of the first tiles (a tile further on: plus its bytes / 16)
-    const uint64_t qd = tc::sdesc_kmajor_sw128(smem_u32(Qs)), kd0 = tc::sdesc_kmajor_sw128(smem_u32(Ks)),
-                   vd0 = tc::sdesc_mnmajor_sw128(smem_u32(Vs), kBlock, 1024);
-    auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL, mbar_wait(bar, parity)); };
-    int ks = 0, vs = 0;          // K tiles multiplied, V tiles multiplied
-    int cnt0 = 0, cnt1 = 0;      // P V products of each query tile
-    int no = 0;
+  } else if (warp == kFixWarp) {
+    // ================================================================ V tiles
+    int vs = 0, no = 0;
     for (int it = (int)blockIdx.x; it < p.items && ok; it += stride, ++no) {
-      ok = wait_all(&qfull[no & 1], (no >> 1) & 1);
+      ok = __all_sync(FULL, mbar_wait(&mfull[no & 1], (no >> 1) & 1));
       if (!ok) break;
-      Item I;
-      {
-        const int* src = reinterpret_cast<const int*>(&items[no & 1]);
-        int* to = reinterpret_cast<int*>(&I);
-#pragma unroll
-        for (int x = 0; x < (int)(sizeof(Item) / sizeof(int)); ++x) to[x] = uniform(src[x]);
-      }
-      const int steps = I.steps;
-      __syncwarp();  // every lane has read the item's ranges
-      if (lead) mbar_arrive(&mfree[no & 1]);
-      if (steps == 0) {
-        if (lead) mbar_arrive(&qempty);
-        continue;
-      }
+      const Item I = items[no & 1];
       const Work w = work_of<WIN>(p, it);
-      auto issue_s = [&](int i, int cols, uint64_t kd) {  // S_i = Q_i K^T
-        if (lead) {
-          const uint64_t qi = qd + (!WIN && p.pair ? 0 : i) * (TB >> 4);
-          const uint32_t idesc = tc::idesc_bf16_f32(kTM, cols);
-#pragma unroll
-          for (int kk = 0; kk < HD / 16; ++kk) {
-            const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;
-            tc::mma_bf16(tmem + 128 * i, qi + off, kd + off, idesc, kk > 0);
-          }
-          tc::mma_commit(&sfull[i]);
-        }
-      };
-      // S of step j for both query tiles (or one of them), then its K tile is free
-      auto wait_k = [&]() -> bool { return wait_all(&kfull[ks % NSK], (ks / NSK) & 1); };
-      auto free_k = [&](int j) {
-        if (lead) {
-          tc::mma_commit(&kempty[ks % NSK]);
-          if (j == steps - 1) tc::mma_commit(&qempty);
-        }
-        ++ks;
-      };
-      for (int j = 0; j < la && j < steps && ok; ++j) {
-        ok = wait_k();
-        if (!ok) break;
-        tc::fence_after_sync();
-        const int cols = columns<WIN>(p, I, tile_at<WIN>(I, j));
-#pragma unroll
-        for (int i = 0; i < kQT; ++i)
-          if (active<WIN>(p, I, i, j)) issue_s(i, cols, kd0 + (ks % NSK) * (TB >> 4));
-        free_k(j);
-      }
-      bool begun0 = false, begun1 = false;  // O_i holds this item's products
-      for (int j = 0; j < steps && ok; ++j, ++vs) {
+      __syncwarp();  // every lane has read the item's ranges
+      if (lane == 0) mbar_arrive(&mfree[no & 1]);
+      for (int j = 0; j < I.steps; ++j, ++vs) {
         const int sv = vs % NSV, kt = tile_at<WIN>(I, j), s0 = kt * kTN;
         const int cols = columns<WIN>(p, I, kt);
-        ok = wait_all(&vfull[sv], (vs / NSV) & 1);
+        ok = __all_sync(FULL, mbar_wait(&vfull[sv], (vs / NSV) & 1));
         if (!ok) break;
         if (s0 + cols - 1 > I.top || (WIN && s0 + cols > p.sinks && (s0 < I.wlo || I.sparse))) {
           // slots that no row sees may hold anything: zero their V rows
@@ -473,48 +450,108 @@ __global__ void __launch_bounds__(kTThreads, 1)
                 *reinterpret_cast<uint4*>(vt + cb * kBlock + row * 128 + u * 16) = make_uint4(0, 0, 0, 0);
           }
           fence_proxy_async_shared();
-          __syncwarp();
         }
-        const bool more = j + la < steps;
-        int cols_next = 0;
-        if (more) {
-          ok = wait_k();
-          if (!ok) break;
-          cols_next = columns<WIN>(p, I, tile_at<WIN>(I, j + la));
-        }
-        const uint64_t vd = vd0 + sv * (TB >> 4);
-#pragma unroll
-        for (int i = 0; i < kQT; ++i) {
-          if (active<WIN>(p, I, i, j)) {
-            int& cnt = i == 0 ? cnt0 : cnt1;
-            bool& begun = i == 0 ? begun0 : begun1;
-            ok = wait_all(&pfull[i], cnt & 1);
-            if (!ok) break;
-            tc::fence_after_sync();
-            if (lead) {  // O_i += P_i V
-              const uint32_t o = tmem + 256 + 128 * i, pa = tmem + 128 * i;
-              if (cols == kTN) {
-#pragma unroll
-                for (int kk = 0; kk < kTN / 16; ++kk)
-                  tc::mma_bf16_ts(o, pa + 8 * kk, vd + kk * (16 * 128 >> 4), idesc_o, begun || kk > 0);
-              } else {
-                for (int kk = 0; kk < cols / 16; ++kk)
-                  tc::mma_bf16_ts(o, pa + 8 * kk, vd + kk * (16 * 128 >> 4), idesc_o, begun || kk > 0);
-              }
-              tc::mma_commit(&odone[i]);
-            }
-            begun = true;
-            ++cnt;
-          }
-          if (more && active<WIN>(p, I, i, j + la)) issue_s(i, cols_next, kd0 + (ks % NSK) * (TB >> 4));
-        }
-        if (!ok) break;
-        if (lead) tc::mma_commit(&vempty[sv]);
-        if (more) free_k(j + la);
         __syncwarp();
+        if (lane == 0) mbar_arrive(&vready[sv]);
       }
     }
     if (!ok && lane == 0) report(p.status, WM_ERR_TIMEOUT);
+  } else if (warp == kMmaWarp) {
+    // ================================================================ MMA
+    const uint32_t idesc_o = tc::idesc_bf16_f32(kTM, HD) | tc::kIdescBMajorMN;
+    const int la = !WIN && p.pair ? 2 : 1;  // steps that S runs ahead of P V
+    const bool lead = elect_one();
+    // descriptors of the first tiles (a tile further on: plus its bytes / 16)
+    const uint64_t qd = tc::sdesc_kmajor_sw128(smem_u32(Qs)), kd0 = tc::sdesc_kmajor_sw128(smem_u32(Ks)),
+                   vd0 = tc::sdesc_mnmajor_sw128(smem_u32(Vs), kBlock, 1024);
+    int ks = 0, vs = 0;      // K tiles multiplied, V tiles multiplied
+    int cnt0 = 0, cnt1 = 0;  // P V products of each query tile
+    int no = 0;
+    for (int it = (int)blockIdx.x; it < p.items && ok; it += stride, ++no) {
+      ok = __all_sync(FULL, mbar_wait(&qfull[no & 1], (no >> 1) & 1));
+      if (!ok) break;
+      Item I;
+      {
+        const int* src = reinterpret_cast<const int*>(&items[no & 1]);
+        int* to = reinterpret_cast<int*>(&I);
+#pragma unroll
+        for (int x = 0; x < (int)(sizeof(Item) / sizeof(int)); ++x) to[x] = uniform(src[x]);
+      }
+      const int steps = I.steps;
+      __syncwarp();  // every lane has read the item's ranges
+      if (lead) {
+        mbar_arrive(&mfree[no & 1]);
+        if (steps == 0) mbar_arrive(&qempty);
+        auto issue_s = [&](int i, int cols) {  // S_i = Q_i K^T with the next K tile
+          const uint64_t qi = qd + (!WIN && p.pair ? 0 : i) * (TB >> 4), kd = kd0 + (ks % NSK) * (TB >> 4);
+          const uint32_t idesc = tc::idesc_bf16_f32(kTM, cols);
+#pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;
+            tc::mma_bf16(tmem + 128 * i, qi + off, kd + off, idesc, kk > 0);
+          }
+          tc::mma_commit(&sfull[i]);
+        };
+        auto issue_pv = [&](int i, int cols, uint64_t vd, bool begun) {  // O_i += P_i V
+          const uint32_t o = tmem + 256 + 128 * i, pa = tmem + 128 * i;
+          if (cols == kTN) {
+#pragma unroll
+            for (int kk = 0; kk < kTN / 16; ++kk)
+              tc::mma_bf16_ts(o, pa + 8 * kk, vd + kk * (16 * 128 >> 4), idesc_o, begun || kk > 0);
+          } else {
+            for (int kk = 0; kk < cols / 16; ++kk)
+              tc::mma_bf16_ts(o, pa + 8 * kk, vd + kk * (16 * 128 >> 4), idesc_o, begun || kk > 0);
+          }
+          tc::mma_commit(&odone[i]);
+        };
+        auto wait_k = [&]() -> bool { return mbar_wait(&kfull[ks % NSK], (ks / NSK) & 1); };
+        // the K tile of step j is free once the S issued so far are done
+        auto free_k = [&](int j) {
+          tc::mma_commit(&kempty[ks % NSK]);
+          if (j == steps - 1) tc::mma_commit(&qempty);
+          ++ks;
+        };
+        for (int j = 0; j < la && j < steps && ok; ++j) {
+          ok = wait_k();
+          if (!ok) break;
+          tc::fence_after_sync();
+          const int cols = columns<WIN>(p, I, tile_at<WIN>(I, j));
+#pragma unroll
+          for (int i = 0; i < kQT; ++i)
+            if (active<WIN>(p, I, i, j)) issue_s(i, cols);
+          free_k(j);
+        }
+        bool begun0 = false, begun1 = false;  // O_i holds this item's products
+        for (int j = 0; j < steps && ok; ++j, ++vs) {
+          const int sv = vs % NSV;
+          const int cols = columns<WIN>(p, I, tile_at<WIN>(I, j));
+          const bool more = j + la < steps;
+          const int cols_next = more ? columns<WIN>(p, I, tile_at<WIN>(I, j + la)) : 0;
+          ok = mbar_wait(&vready[sv], (vs / NSV) & 1) && (!more || wait_k());
+          if (!ok) break;
+          const uint64_t vd = vd0 + sv * (TB >> 4);
+#pragma unroll
+          for (int i = 0; i < kQT; ++i) {
+            if (active<WIN>(p, I, i, j)) {
+              int& cnt = i == 0 ? cnt0 : cnt1;
+              bool& begun = i == 0 ? begun0 : begun1;
+              ok = mbar_wait(&pfull[i], cnt & 1);
+              if (!ok) break;
+              tc::fence_after_sync();
+              issue_pv(i, cols, vd, begun);
+              begun = true;
+              ++cnt;
+            }
+            if (more && active<WIN>(p, I, i, j + la)) issue_s(i, cols_next);
+          }
+          if (!ok) break;
+          tc::mma_commit(&vempty[sv]);
+          if (more) free_k(j + la);
+        }
+      }
+      ok = __all_sync(FULL, ok);
+    }
+    if (!ok && lead) report(p.status, WM_ERR_TIMEOUT);
   } else {
     // ================================================================ softmax
     const int i = warp >> 2;             // query tile
