@@ -96,6 +96,7 @@ struct TileParams {
   int32_t records;            // prefix: partial records per row
   int32_t blocks;             // window: row blocks per head
   int32_t items;
+  int32_t wide_out;           // out is 32-byte aligned
   float qscale;               // log2(e) / sqrt(d)
 };
 struct TileInputs {
@@ -104,8 +105,8 @@ struct TileInputs {
   const void* v_pool;
   int32_t B, k, d;
 };
-// floats of a partial record: d outputs, (max, sum), padded to 16 bytes
-constexpr int tile_rec(int d) { return d + 4; }
+// floats of a partial record: d outputs, (max, sum), padded to 32 bytes
+constexpr int tile_rec(int d) { return d + 8; }
 constexpr int kTileRows = 128;
 constexpr int kTileSlots = 128;
 cudaError_t launch_tile_attn(TileParams p, const TileInputs& in, int sms, cudaStream_t s);

@@ -32,7 +32,7 @@
 // softmax groups take its even and odd KV tiles instead.
 //
 // A KV tile whose visible slots end early (the sinks, the end of a prefix) is
-// only multiplied as far as they go, in steps of 32 columns.  Slots that no
+// only multiplied as far as they go, in steps of 64 columns.  Slots that no
 // row of an item sees are never used: their pages are not fetched where a
 // whole box is unseen, their V rows are zeroed, their scores replaced.
 #include <math.h>
@@ -89,6 +89,18 @@ __device__ __forceinline__ void tmem_wait_for(uint32_t (&r)[32]) {
                  "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
                  "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]),
                  "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
+}
+
+// 32 bytes to global memory (wide: dst is 32-byte aligned).
+__device__ __forceinline__ void store32(void* dst, const uint32_t (&u)[8], int wide) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(u[0]), "r"(u[1]),
+                 "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(dst)[0] = make_uint4(u[0], u[1], u[2], u[3]);
+    reinterpret_cast<uint4*>(dst)[1] = make_uint4(u[4], u[5], u[6], u[7]);
+  }
 }
 
 // KV tiles of a query tile, or of the whole item: [0, sn) and [wf, we).
@@ -227,12 +239,12 @@ __device__ __forceinline__ bool active(const TileParams& p, const Item& I, int i
   if (!WIN && p.pair) return (j & 1) == i;
   return I.tile[i].has(tile_at<WIN>(I, j));
 }
-// Columns of step j that may be seen, a multiple of 32.
+// Columns of step j that may be seen: 64 or 128.
 template <bool WIN>
 __device__ __forceinline__ int columns(const TileParams& p, const Item& I, int kt) {
   int hi = I.top + 1 - kt * kTN;
   if (WIN && kt < I.all.sn && (kt + 1) * kTN <= I.wlo) hi = min(hi, p.sinks - kt * kTN);
-  return min(kTN, (hi + 31) & ~31);
+  return hi > kTN / 2 ? kTN : kTN / 2;
 }
 // No row of the item sees a slot of t0 .. t1.
 template <bool WIN>
@@ -261,7 +273,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
   extern __shared__ uint8_t smem_dyn[];
   __shared__ uint64_t qfull[2], qempty, mfull[2], mfree[2], kfull[NSK], kempty[NSK], vfull[NSV], vready[NSV],
       vempty[NSV];
-  __shared__ uint64_t sfull[kQT], pfull[kQT], odone[kQT];
+  __shared__ uint64_t sfull[kQT], pfull[2 * kQT], odone[kQT];
   __shared__ uint32_t tmem_base;
   __shared__ Item items[2];
   // Boxes of a step whose page does not exist, bit per box.  K tile j + NSK is
@@ -302,6 +314,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
     for (int i = 0; i < kQT; ++i) {
       mbar_init(&sfull[i], 1);
       mbar_init(&pfull[i], kTM);
+      mbar_init(&pfull[kQT + i], kTM);
       mbar_init(&odone[i], 1);
     }
     fence_mbar_init();
@@ -369,8 +382,8 @@ __global__ void __launch_bounds__(kTThreads, 1)
         }
         return row;
       };
-      // the queries go out behind the first two K tiles, whose slots free up
-      // before the previous item's queries do
+      // the queries go out behind the first two K tiles (whose slots free up
+      // before the previous item's queries do), but first of all in the first item
       auto load_q = [&]() {
         if (no >= 1) ok = __all_sync(FULL, mbar_wait(&qempty, (no - 1) & 1));
         if (!ok || lane != 0) return;
@@ -391,7 +404,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
                               &qfull[no & 1]);
           }
       };
-      const int q_at = min(2, I.steps);
+      const int q_at = no == 0 ? 0 : min(2, I.steps);
       int row_next = I.steps > 0 ? box_row(0) : 0;
       for (int j = 0; j < I.steps; ++j, ++n_tile) {
         if (kq && j == q_at) {
@@ -419,7 +432,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb) tc::tma_load_2d(dst + cb * kBlock + lane * brows * 128, tm, cb * 64, row, bar);
       }
-      if (kq && ok && I.steps == q_at) load_q();
+      if (kq && ok && I.steps <= q_at) load_q();
       ok = __all_sync(FULL, ok);
     }
     if (!ok && lane == 0) report(p.status, WM_ERR_TIMEOUT);
@@ -492,17 +505,23 @@ __global__ void __launch_bounds__(kTThreads, 1)
           }
           tc::mma_commit(&sfull[i]);
         };
-        auto issue_pv = [&](int i, int cols, uint64_t vd, bool begun) {  // O_i += P_i V
+        // O_i += P_i V; the second half of P follows on its own barrier
+        auto issue_pv = [&](int i, int cols, uint64_t vd, bool begun, uint32_t parity) -> bool {
           const uint32_t o = tmem + 256 + 128 * i, pa = tmem + 128 * i;
-          if (cols == kTN) {
 #pragma unroll
-            for (int kk = 0; kk < kTN / 16; ++kk)
-              tc::mma_bf16_ts(o, pa + 8 * kk, vd + kk * (16 * 128 >> 4), idesc_o, begun || kk > 0);
-          } else {
-            for (int kk = 0; kk < cols / 16; ++kk)
-              tc::mma_bf16_ts(o, pa + 8 * kk, vd + kk * (16 * 128 >> 4), idesc_o, begun || kk > 0);
+          for (int kk = 0; kk < kTN / 32; ++kk)
+            tc::mma_bf16_ts(o, pa + 8 * kk, vd + kk * (16 * 128 >> 4), idesc_o, begun || kk > 0);
+          if (cols == kTN) {
+            if (!mbar_wait(&pfull[kQT + i], parity)) return false;
+            tc::fence_after_sync();
+#pragma unroll
+            for (int kk = kTN / 32; kk < kTN / 16; ++kk)
+              tc::mma_bf16_ts(o, pa + 8 * kk, vd + kk * (16 * 128 >> 4), idesc_o, 1);
+          } else if (!mbar_wait(&pfull[kQT + i], parity)) {
+            return false;
           }
           tc::mma_commit(&odone[i]);
+          return true;
         };
         auto wait_k = [&]() -> bool { return mbar_wait(&kfull[ks % NSK], (ks / NSK) & 1); };
         // the K tile of step j is free once the S issued so far are done
@@ -538,7 +557,8 @@ __global__ void __launch_bounds__(kTThreads, 1)
               ok = mbar_wait(&pfull[i], cnt & 1);
               if (!ok) break;
               tc::fence_after_sync();
-              issue_pv(i, cols, vd, begun);
+              ok = issue_pv(i, cols, vd, begun, cnt & 1);
+              if (!ok) break;
               begun = true;
               ++cnt;
             }
@@ -562,16 +582,20 @@ __global__ void __launch_bounds__(kTThreads, 1)
     int done = 0;                        // steps of the CTA before this item
     const int log2b = p.P >= kTN ? 7 : p.log2P;  // slots per box
     int no = 0;
+    // largest slot this thread's row of item `it` sees, fetched an item ahead
+    auto row_top = [&](int it) -> int {
+      const Work w = work_of<WIN>(p, it);
+      bool bad;
+      const int t = top_of<WIN>(p, w, w.row0 + (p.pair ? 0 : i * kTM) + lr, bad);
+      if (bad) report(p.status, WM_ERR_BOUNDS);
+      return t;
+    };
+    int top_next = (int)blockIdx.x < p.items ? row_top((int)blockIdx.x) : -1;
     // tcgen05.ld / st are warp-collective: every lane of the warp issues each
     // one, and the wait outcomes are made warp-uniform before any branch
     for (int it = (int)blockIdx.x; it < p.items && ok; it += stride, ++no) {
-      int mytop;  // largest slot this thread's row sees
-      {
-        const Work w = work_of<WIN>(p, it);
-        bool bad;
-        mytop = top_of<WIN>(p, w, w.row0 + (p.pair ? 0 : i * kTM) + lr, bad);
-        if (bad) report(p.status, WM_ERR_BOUNDS);
-      }
+      const int mytop = top_next;  // largest slot this thread's row sees
+      if (it + stride < p.items) top_next = row_top(it + stride);
       ok = __all_sync(FULL, mbar_wait(&qfull[no & 1], (no >> 1) & 1));
       if (!ok) break;
       const Item& I = items[no & 1];
@@ -585,7 +609,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
         ok = __all_sync(FULL, mbar_wait(&sfull[i], cnt & 1));
         if (!ok) break;
         tc::fence_after_sync();
-        const int nc = columns<WIN>(p, I, kt) / 32;  // 32-column parts of the step
+        const int nc = columns<WIN>(p, I, kt) / 32;  // 32-column parts of the step: 2 or 4
         // Visible columns of this row: e < vis, and under a window e < es (sinks)
         // or e >= el (the row's window).  Masked scores become -inf.
         const int vis = mytop - s0 + 1;
@@ -608,17 +632,25 @@ __global__ void __launch_bounds__(kTThreads, 1)
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = (see >> e) & 1u ? v[e] : 0xFF800000u;
         };
-        // The row is read from TMEM twice, 32 columns at a time: for its maximum,
-        // then for the probabilities (the other warps of the SM cover the loads).
+        // The row is read from TMEM twice, 64 columns at a time: for its maximum,
+        // then for the probabilities.  (A whole row of 128 registers spills, and
+        // unrolled loops or separate ones for masked steps cost more in the
+        // instruction cache than they save.)
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
-        for (int c = 0; c < nc; ++c) {
-          uint32_t v[32];
+        for (int c = 0; c < nc; c += 2) {
+          uint32_t v[32], u[32];
           tc::tmem_ld32(lane_base + scol + 32 * c, v);
+          tc::tmem_ld32(lane_base + scol + 32 * c + 32, u);
           tmem_wait_for(v);
-          if (masked) mask_part(c, v);
+          tmem_wait_for(u);
+          if (masked) {
+            mask_part(c, v);
+            mask_part(c + 1, u);
+          }
 #pragma unroll
-          for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(v[e]));
+          for (int e = 0; e < 32; ++e)
+            mx[e & 3] = fmaxf(mx[e & 3], fmaxf(__uint_as_float(v[e]), __uint_as_float(u[e])));
         }
         const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.qscale;  // qscale > 0
         float scale = 1.f;
@@ -627,35 +659,11 @@ __global__ void __launch_bounds__(kTThreads, 1)
           scale = (m == -INFINITY) ? 0.f : ex2(m - mt);
           m = mt;
         }
-        // p = 2^(s * qscale - m) in pairs; masked slots give 0, and so do rows
-        // that have seen nothing yet.  P enters the product as bf16 (the tensor
-        // cores' operand); the row sum is kept in fp32 from the unrounded values.
-        const float nm = m == -INFINITY ? 0.f : -m;
-        const float2 qs2 = make_float2(p.qscale, p.qscale), nm2 = make_float2(nm, nm);
-        float2 sum2 = make_float2(0.f, 0.f);
-#pragma unroll 1
-        for (int c = 0; c < nc; ++c) {
-          uint32_t v[32], pk[16];
-          tc::tmem_ld32(lane_base + scol + 32 * c, v);
-          tmem_wait_for(v);
-          if (masked) mask_part(c, v);
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), qs2, nm2);
-            const float2 pr = make_float2(ex2(y.x), ex2(y.y));
-            sum2 = __fadd2_rn(sum2, pr);
-            const __nv_bfloat162 h = __floats2bfloat162_rn(pr.x, pr.y);
-            pk[e / 2] = *reinterpret_cast<const uint32_t*>(&h);
-          }
-          // P over S columns that have been read: packed pairs, columns 16c .. 16c+15
-          tc::tmem_st16(lane_base + scol + 16 * c, pk);
-        }
-        l = l * scale + (sum2.x + sum2.y);
         if (__any_sync(FULL, raise && x > 0)) {
           // a row's max grew past the headroom: rescale O (every lane of the
           // warp takes part; rows that did not raise their max scale by 1)
           // once P V of the previous step has landed in it
-          if (!(raise && x > 0)) scale = 1.f;
+          const float fac = raise && x > 0 ? scale : 1.f;
           ok = __all_sync(FULL, mbar_wait(&odone[i], (cnt - 1) & 1));
           if (!ok) break;
           tc::fence_after_sync();
@@ -667,16 +675,54 @@ __global__ void __launch_bounds__(kTThreads, 1)
             uint32_t w0[16], w1[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              w0[e] = __float_as_uint(__uint_as_float(o[e]) * scale);
-              w1[e] = __float_as_uint(__uint_as_float(o[16 + e]) * scale);
+              w0[e] = __float_as_uint(__uint_as_float(o[e]) * fac);
+              w1[e] = __float_as_uint(__uint_as_float(o[16 + e]) * fac);
             }
             tc::tmem_st16(lane_base + ocol + 32 * c, w0);
             tc::tmem_st16(lane_base + ocol + 32 * c + 16, w1);
           }
         }
-        tc::tmem_st_wait();
-        tc::fence_before_sync();
-        mbar_arrive(&pfull[i]);
+        // p = 2^(s * qscale - m) in pairs; masked slots give 0, and so do rows
+        // that have seen nothing yet.  P enters the product as bf16 (the tensor
+        // cores' operand); the row sum is kept in fp32 from the unrounded values.
+        const float nm = m == -INFINITY ? 0.f : -m;
+        const float2 qs2 = make_float2(p.qscale, p.qscale), nm2 = make_float2(nm, nm);
+        float2 sum2 = make_float2(0.f, 0.f);
+        float2 sum2b = make_float2(0.f, 0.f);
+#pragma unroll 1
+        for (int c = 0; c < nc; c += 2) {
+          uint32_t v[32], u[32], pv[16], pu[16];
+          tc::tmem_ld32(lane_base + scol + 32 * c, v);
+          tc::tmem_ld32(lane_base + scol + 32 * c + 32, u);
+          tmem_wait_for(v);
+          tmem_wait_for(u);
+          if (masked) {
+            mask_part(c, v);
+            mask_part(c + 1, u);
+          }
+          auto prob = [&](uint32_t x0, uint32_t x1, float2& sum) -> uint32_t {
+            const float2 y = __ffma2_rn(make_float2(__uint_as_float(x0), __uint_as_float(x1)), qs2, nm2);
+            const float2 pr = make_float2(ex2(y.x), ex2(y.y));
+            sum = __fadd2_rn(sum, pr);
+            const __nv_bfloat162 h = __floats2bfloat162_rn(pr.x, pr.y);
+            return *reinterpret_cast<const uint32_t*>(&h);
+          };
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            pv[e / 2] = prob(v[e], v[e + 1], sum2);
+            pu[e / 2] = prob(u[e], u[e + 1], sum2b);
+          }
+          // P over S columns that have been read: packed pairs, columns 16c .. 16c+31.
+          // P V of the first 64 slots starts while the others' are computed.
+          tc::tmem_st16(lane_base + scol + 16 * c, pv);
+          tc::tmem_st16(lane_base + scol + 16 * c + 16, pu);
+          tc::tmem_st_wait();
+          tc::fence_before_sync();
+          mbar_arrive(&pfull[c == 0 ? i : kQT + i]);
+        }
+        if (nc == 2) mbar_arrive(&pfull[kQT + i]);
+        sum2 = __fadd2_rn(sum2, sum2b);
+        l = l * scale + (sum2.x + sum2.y);
         ++cnt;
         ++x;
       }
@@ -709,21 +755,25 @@ __global__ void __launch_bounds__(kTThreads, 1)
         if (!live) continue;
         if (WIN) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            uint32_t u[4];
+          for (int e = 0; e < 32; e += 16) {
+            uint32_t u[8];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
+            for (int t = 0; t < 8; ++t) {
               const float f0 = x > 0 ? __uint_as_float(o[e + 2 * t]) * inv : 0.f;
               const float f1 = x > 0 ? __uint_as_float(o[e + 2 * t + 1]) * inv : 0.f;
               const __nv_bfloat162 h = __floats2bfloat162_rn(f0, f1);
               u[t] = *reinterpret_cast<const uint32_t*>(&h);
             }
-            *reinterpret_cast<uint4*>(dst + 32 * c + e) = make_uint4(u[0], u[1], u[2], u[3]);
+            store32(dst + 32 * c + e, u, p.wide_out);
           }
         } else if (x > 0) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            *reinterpret_cast<uint4*>(rec + 32 * c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          for (int e = 0; e < 32; e += 8) {
+            uint32_t u[8];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) u[t] = o[e + t];
+            store32(rec + 32 * c + e, u, 1);
+          }
         }
       }
       if (!WIN && live) *reinterpret_cast<float2*>(rec + HD) = make_float2(m, l);
@@ -764,6 +814,7 @@ cudaError_t launch_t(const CUtensorMap& q, const CUtensorMap& k, const CUtensorM
 
 cudaError_t launch_tile_attn(TileParams p, const TileInputs& in, int sms, cudaStream_t s) {
   const bool win = p.part == nullptr;
+  p.wide_out = ((uintptr_t)p.out & 31) == 0 ? 1 : 0;
   CUtensorMap tq, tk, tv;
   const uint64_t pool_rows = (uint64_t)in.k * p.num_pages * p.Hkv * p.P;
   const uint32_t box_rows = p.P >= kTN ? (uint32_t)kTN : (uint32_t)p.P;
