@@ -27,7 +27,7 @@ int clamp_int(int64_t x, int64_t lo, int64_t hi) { return (int)(x < lo ? lo : x 
 int split_pieces(int64_t units, int64_t stages, int waves) {
   const int64_t by_work = stages / (kRangeWarps * kMinStagesPerWarp);
   const int64_t by_sms = ((int64_t)sm_count() * kRangeCtasPerSm * waves + units - 1) / units;
-  return clamp_int(by_work < by_sms ? by_work : by_sms, 1, 64);
+  return clamp_int(by_work < by_sms ? by_work : by_sms, 1, kMassMaxPieces);
 }
 
 int64_t stages_of(const wm_config& c, int64_t slots) {
@@ -35,9 +35,9 @@ int64_t stages_of(const wm_config& c, int64_t slots) {
   return (slots + ss - 1) / ss;
 }
 
-// CTAs per unit (one cluster, joined on chip) of a window launch: as many as
-// keep every CTA resident and leave each warp a stage.
-int window_cluster(const wm_config& c, int64_t units, int64_t visible) {
+// CTAs per unit (one cluster, joined on chip) of a launch that writes its
+// outputs itself: as many as keep every CTA resident and leave each warp a stage.
+int range_cluster(const wm_config& c, int64_t units, int64_t visible) {
   const int64_t stages = stages_of(c, visible) + 1;
   int C = 1;
   while (C < kRangeMaxCluster && units * C * 2 <= (int64_t)sm_count() * kRangeCtasPerSm &&
@@ -123,9 +123,10 @@ wm_status launch_tiles(const TileParams& p, const wm_config& c, const wm_cache& 
 // `splits` parts of its KV tiles) or on the range kernel (groups of 8 rows,
 // times prefix_pieces).
 struct PrefixPlan {
-  int blocks, pair, splits, records;         // tensor cores
-  int groups, prefix_pieces, suffix_pieces;  // range kernel
-  size_t off_suffix, total;
+  int blocks, pair, splits, records;  // tensor cores
+  int groups, prefix_pieces;          // range kernel
+  int suffix_cluster;
+  size_t total;
 };
 
 // KV parts of the tensor-core prefix: the count with the shortest last CTA,
@@ -149,8 +150,7 @@ PrefixPlan prefix_plan(const wm_config& c, int32_t B, int32_t max_pages, int32_t
   PrefixPlan pl{};
   pl.groups = (int)(((int64_t)B * G + kRangeRows - 1) / kRangeRows);
   pl.prefix_pieces = split_pieces((int64_t)pl.groups * c.Hkv, stages_of(c, (int64_t)shared_pages * c.page_size), 2);
-  pl.suffix_pieces =
-      split_pieces((int64_t)B * c.Hkv, stages_of(c, (int64_t)(max_pages - shared_pages) * c.page_size), 2);
+  pl.suffix_cluster = range_cluster(c, (int64_t)B * c.Hkv, (int64_t)(max_pages - shared_pages) * c.page_size);
   const int64_t rows = (int64_t)B * G;
   pl.pair = rows <= kTileRows ? 1 : 0;
   pl.blocks = pl.pair ? 1 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
@@ -161,22 +161,37 @@ PrefixPlan prefix_plan(const wm_config& c, int32_t B, int32_t max_pages, int32_t
   const size_t range_bytes =
       sizeof(float) * (size_t)pl.groups * c.Hkv * pl.prefix_pieces * range_rec(kRangeRows, c.d);
   // (room for either: which one runs depends on the cache too)
-  pl.off_suffix = align256(tile_bytes > range_bytes ? tile_bytes : range_bytes);
-  pl.total = pl.off_suffix + align256(sizeof(float) * (size_t)B * c.Hkv * pl.suffix_pieces * range_rec(G, c.d));
+  pl.total = align256(tile_bytes > range_bytes ? tile_bytes : range_bytes);
+  if (pl.total == 0) pl.total = 256;
   return pl;
 }
 
+// Split of a mass call.  Where a CTA's scores fit beside its ring without
+// costing the SM its second CTA, one launch does it all (clusters join on chip
+// and add their own slots' weights); else partial records and scores go through
+// the workspace to a second kernel.
 struct MassPlan {
+  int cluster, mass_slots;  // one launch: CTAs per unit (0: two launches), slots per CTA
   int pieces;
   int64_t score_stride;
   size_t off_scores, total;
 };
+constexpr int kMassSmemBytes = 4096;
 
 MassPlan mass_plan(const wm_config& c, int32_t B, int32_t max_pages) {
   const int G = c.Hq / c.Hkv;
   const int64_t slots = (int64_t)max_pages * c.page_size, units = (int64_t)B * c.Hkv;
   MassPlan pl{};
-  pl.pieces = split_pieces(units, stages_of(c, slots), 6);
+  const int64_t stages = stages_of(c, slots);
+  const int C = range_cluster(c, units, slots);
+  const int64_t per_cta = (stages + C * kRangeWarps - 1) / (C * kRangeWarps) * kRangeWarps * range_stage_slots(c.dtype, c.d);
+  if (per_cta * G * (int64_t)sizeof(float) <= kMassSmemBytes) {
+    pl.cluster = C;
+    pl.mass_slots = (int)per_cta;
+    pl.total = 256;
+    return pl;
+  }
+  pl.pieces = split_pieces(units, stages, 6);
   pl.score_stride = (slots + 31) / 32 * 32;
   pl.off_scores = align256(sizeof(float) * (size_t)units * pl.pieces * range_rec(G, c.d));
   pl.total = pl.off_scores + align256(sizeof(float) * (size_t)units * G * pl.score_stride);
@@ -205,7 +220,7 @@ wm_status wm_window_attn(const wm_config* c, const wm_cache* cache, int32_t laye
   p.out = out;
   p.sinks = sinks;
   p.window = window;
-  p.pieces = window_cluster(*c, (int64_t)B * c->Hkv, visible < slots ? visible : slots);
+  p.pieces = range_cluster(*c, (int64_t)B * c->Hkv, visible < slots ? visible : slots);
   return cuda_status(launch_range_attn(p, c->dtype, c->d, B * c->Hkv, (cudaStream_t)stream));
 }
 
@@ -277,7 +292,7 @@ wm_status wm_prefix_attn(const wm_config* c, const wm_cache* cache, int32_t laye
     t.records = pl.records;
     t.items = pl.blocks * c->Hkv * pl.splits;
     if ((st = launch_tiles(t, *c, *cache, q, B, stream)) != WM_OK) return st;
-  } else if (shared_pages > 0) {
+  } else if (shared_pages > 0) {  // every other form of the prefix
     p.part = (float*)workspace;
     p.mode = kRangePrefix;
     p.rows = kRangeRows;
@@ -285,23 +300,15 @@ wm_status wm_prefix_attn(const wm_config* c, const wm_cache* cache, int32_t laye
     if (launch_range_attn(p, c->dtype, c->d, pl.groups * c->Hkv, (cudaStream_t)stream) != cudaSuccess)
       return WM_ERR_CUDA;
   }
-  p.part = (float*)((char*)workspace + pl.off_suffix);
+  p.part = nullptr;
   p.mode = kRangeSuffix;
+  p.out = out;
+  p.prefix = (const float*)workspace;
+  p.records = shared_pages == 0 ? 0 : tiles ? pl.records : pl.prefix_pieces;
+  p.tile_records = tiles ? 1 : 0;
   p.rows = p.G;
-  p.pieces = pl.suffix_pieces;
-  if (launch_range_attn(p, c->dtype, c->d, B * c->Hkv, (cudaStream_t)stream) != cudaSuccess) return WM_ERR_CUDA;
-  PrefixJoinParams j{};
-  j.prefix = (const float*)workspace;
-  j.suffix = p.part;
-  j.out = out;
-  j.B = B;
-  j.Hq = c->Hq;
-  j.Hkv = c->Hkv;
-  j.G = p.G;
-  j.tiles = tiles ? 1 : 0;
-  j.prefix_pieces = shared_pages == 0 ? 0 : tiles ? pl.records : pl.prefix_pieces;
-  j.suffix_pieces = pl.suffix_pieces;
-  return cuda_status(launch_prefix_join(j, c->dtype, c->d, (cudaStream_t)stream));
+  p.pieces = pl.suffix_cluster;
+  return cuda_status(launch_range_attn(p, c->dtype, c->d, B * c->Hkv, (cudaStream_t)stream));
 }
 
 size_t wm_decode_attn_mass_workspace(const wm_config* c, int32_t B, int32_t max_pages) {
@@ -324,6 +331,15 @@ wm_status wm_decode_attn_mass(const wm_config* c, const wm_cache* cache, int32_t
   if (ws_bytes < pl.total) return WM_ERR_INVALID_ARG;
   RangeParams p = range_params(*c, *cache, layer, q, page_table, seq_lens, B, max_pages, dev_status);
   p.mode = kRangeScores;
+  const int32_t max_slots = max_pages * c->page_size;
+  float* chan_mass = mass + (size_t)c->chan_of_layer[layer] * B * c->Hkv * max_slots;
+  if (pl.cluster > 0) {
+    p.out = out;
+    p.mass = chan_mass;
+    p.mass_slots = pl.mass_slots;
+    p.pieces = pl.cluster;
+    return cuda_status(launch_range_attn(p, c->dtype, c->d, B * c->Hkv, (cudaStream_t)stream));
+  }
   p.pieces = pl.pieces;
   p.part = (float*)workspace;
   p.scores = (float*)((char*)workspace + pl.off_scores);
@@ -334,8 +350,8 @@ wm_status wm_decode_attn_mass(const wm_config* c, const wm_cache* cache, int32_t
   m.part = p.part;
   m.scores = p.scores;
   m.seq_lens = seq_lens;
-  m.max_slots = max_pages * c->page_size;
-  m.mass = mass + (size_t)c->chan_of_layer[layer] * B * c->Hkv * m.max_slots;
+  m.max_slots = max_slots;
+  m.mass = chan_mass;
   m.out = out;
   m.score_stride = pl.score_stride;
   m.B = B;
@@ -355,7 +371,7 @@ wm_status wm_cache_evict(const wm_config* c, const wm_cache* cache, const float*
   if (budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget) return WM_ERR_INVALID_ARG;
   if (budget > max_pages * c->page_size) return WM_ERR_INVALID_ARG;
   if (B == 0) return WM_OK;
-  if ((int64_t)c->k * B * c->Hkv > INT32_MAX) return WM_ERR_UNSUPPORTED;
+  if ((int64_t)c->k * B * c->Hkv > INT32_MAX / 8) return WM_ERR_UNSUPPORTED;
   if (!mass || !mass_out || !page_table || !seq_lens || !kept || !new_lens) return WM_ERR_INVALID_ARG;
   if (!aligned(mass, 4) || !aligned(mass_out, 4) || new_lens == seq_lens) return WM_ERR_INVALID_ARG;
   EvictParams p{};
@@ -378,7 +394,7 @@ wm_status wm_cache_evict(const wm_config* c, const wm_cache* cache, const float*
   p.budget = budget;
   p.sinks = sinks;
   p.recent = recent;
-  return cuda_status(launch_cache_evict(p, c->dtype, c->d, (cudaStream_t)stream));
+  return cuda_status(launch_cache_evict(p, c->dtype, c->d, sm_count(), (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,6 +1,6 @@
-// Host side of the range attention (kernel in range_attn.cuh) and the kernels
-// that join its partial records: of a shared prefix with each sequence's
-// suffix, and of decode attention with the weights added to the slots' sums.
+// Host side of the range attention (kernel in range_attn.cuh), and the kernel
+// that joins the partial records of a long decode attention and adds its
+// weights to the slots' sums.
 #include <math.h>
 
 #include "common.cuh"
@@ -23,105 +23,94 @@ cudaError_t launch_range_attn(const RangeParams& p, int dtype, int d, int units,
 
 namespace {
 
-// Joins n partial records of one row: out_e = sum_i 2^(m_i - M) O_i,e / sum_i 2^(m_i - M) l_i.
-// rec(i): the i-th record's row of HD outputs; ml(i): its (max, sum).  One warp per row.
-template <typename T, int HD, typename Rec, typename Ml>
-__device__ __forceinline__ void join_row(T* out, int n, int lane, Rec rec, Ml ml) {
-  float M = -INFINITY;
-  for (int i = lane; i < n; i += 32) M = fmaxf(M, ml(i).x);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
-  float L = 0.f, O[HD / 32] = {};
-  for (int i = 0; i < n; ++i) {
-    const float2 x = ml(i);
-    if (x.x == -INFINITY) continue;
-    const float w = exp2f(x.x - M);
-    L = fmaf(w, x.y, L);
-    const float* r = rec(i);
-#pragma unroll
-    for (int e = 0; e < HD / 32; ++e) O[e] = fmaf(w, __ldcg(r + lane + 32 * e), O[e]);
-  }
-  const float inv = L > 0.f ? 1.f / L : 0.f;
-#pragma unroll
-  for (int e = 0; e < HD / 32; ++e) out[lane + 32 * e] = Elem<T>::from_f(O[e] * inv);
-}
-
-constexpr int kJoinWarps = 4;
-
-// One warp per output row (sequence b, query head hq).
-template <typename T, int HD>
-__global__ void __launch_bounds__(kJoinWarps * 32) prefix_join_kernel(const PrefixJoinParams p) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int lane = threadIdx.x & 31;
-  const int row = (int)blockIdx.x * kJoinWarps + (int)(threadIdx.x >> 5);
-  if (row >= p.B * p.Hq) return;
-  const int b = row / p.Hq, hq = row - b * p.Hq, h = hq / p.G, g = hq - h * p.G;
-  // the row's records: of the prefix, then of its suffix
-  const int np = p.prefix_pieces, srec = range_rec(p.G, HD);
-  const int x = b * p.G + g, grp = x / kRangeRows, xr = x - grp * kRangeRows;
-  const int prec = p.tiles ? tile_rec(HD) : range_rec(kRangeRows, HD);
-  const float* pre = p.prefix + (p.tiles ? ((int64_t)h * p.B * p.G + x) * np * prec
-                                         : ((int64_t)grp * p.Hkv + h) * np * prec + xr * HD);
-  const int pml = p.tiles ? HD : kRangeRows * HD + 2 * xr - xr * HD;  // (max, sum) of a record, from its outputs
-  const float* suf = p.suffix + ((int64_t)b * p.Hkv + h) * p.suffix_pieces * srec;
-  auto rec = [&](int i) -> const float* {
-    return i < np ? pre + (int64_t)i * prec : suf + (int64_t)(i - np) * srec + g * HD;
-  };
-  auto ml = [&](int i) -> float2 {
-    const float* r = i < np ? pre + (int64_t)i * prec + pml : suf + (int64_t)(i - np) * srec + p.G * HD + 2 * g;
-    return make_float2(__ldcg(r), __ldcg(r + 1));
-  };
-  join_row<T, HD>(reinterpret_cast<T*>(p.out) + (int64_t)row * HD, np + p.suffix_pieces, lane, rec, ml);
-}
-
 // mass[t] += sum_g 2^(s_g[t] - m_g) / l_g over the G query heads of a unit
-// (sequence, kv head).  Every slot is added to by one thread, so the sums do
-// not depend on the order of anything.  blockIdx.y: part of the slots; part 0
-// also joins the output rows.
+// (sequence, kv head), after the unit's partial records are joined:
+//   out_e = sum_i 2^(m_i - M) O_i,e / sum_i 2^(m_i - M) l_i.
+// Every slot is added to by one thread, so the sums do not depend on the order
+// of anything.  blockIdx.y 0 writes the output rows, the others add a part of
+// the slots each: bound by HBM / L2 (G + 2 floats per slot), four slots per
+// 16-byte access.
 constexpr int kMassThreads = 256;
+constexpr int kMassSlots = kMassThreads * 16;  // per CTA
 template <typename T, int HD>
 __global__ void __launch_bounds__(kMassThreads) mass_add_kernel(const MassParams p) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  __shared__ float lse_s[kRangeRows], inv_s[kRangeRows];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  __shared__ float m_s[kRangeRows], inv_s[kRangeRows], w_s[kRangeRows][kMassMaxPieces];
   const int unit = blockIdx.x, b = unit / p.Hkv, h = unit - b * p.Hkv;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int recf = range_rec(p.G, HD);
   const float* part = p.part + (int64_t)unit * p.pieces * recf;
-  if (warp < p.G) {
+  const int S_in = __ldg(p.seq_lens + b);
+  const int S = S_in >= 0 && S_in <= p.max_slots ? S_in : 0;
+  const int t0 = ((int)blockIdx.y - 1) * kMassSlots;
+  if (t0 >= S) return;
+  if (warp < p.G) {  // 8 warps: one per query head
+    const float* ml = part + p.G * HD + 2 * warp;
     float M = -INFINITY, L = 0.f;
-    for (int i = 0; i < p.pieces; ++i) M = fmaxf(M, __ldcg(part + (int64_t)i * recf + p.G * HD + 2 * warp));
-    for (int i = 0; i < p.pieces; ++i) {
-      const float* r = part + (int64_t)i * recf + p.G * HD + 2 * warp;
-      const float m = __ldcg(r);
-      if (m != -INFINITY) L = fmaf(exp2f(m - M), __ldcg(r + 1), L);
+    for (int i = lane; i < p.pieces; i += 32) M = fmaxf(M, __ldcg(ml + (int64_t)i * recf));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
+    for (int i = lane; i < p.pieces; i += 32) {
+      const float m = __ldcg(ml + (int64_t)i * recf);
+      const float w = m == -INFINITY ? 0.f : exp2f(m - M);
+      w_s[warp][i] = w;
+      if (w != 0.f) L = fmaf(w, __ldcg(ml + (int64_t)i * recf + 1), L);
     }
+    L = warp_sum(L);
     if (lane == 0) {
-      lse_s[warp] = M;
+      m_s[warp] = M;
       inv_s[warp] = L > 0.f ? 1.f / L : 0.f;
-    }
-    if (blockIdx.y == 0) {
-      auto rec = [&](int i) -> const float* { return part + (int64_t)i * recf + warp * HD; };
-      auto ml = [&](int i) -> float2 {
-        const float* r = part + (int64_t)i * recf + p.G * HD + 2 * warp;
-        return make_float2(__ldcg(r), __ldcg(r + 1));
-      };
-      join_row<T, HD>(reinterpret_cast<T*>(p.out) + ((int64_t)b * p.Hq + h * p.G + warp) * HD, p.pieces, lane, rec, ml);
     }
   }
   __syncthreads();
-  const int S_in = __ldg(p.seq_lens + b);
-  const int S = S_in >= 0 && S_in <= p.max_slots ? S_in : 0;
+  if (blockIdx.y == 0) {
+    T* out = reinterpret_cast<T*>(p.out) + ((int64_t)b * p.Hq + h * p.G) * HD;
+    for (int e = tid; e < p.G * HD; e += kMassThreads) {
+      float O = 0.f;
+      for (int i0 = 0; i0 < p.pieces; i0 += 8) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i0 + i < p.pieces ? __ldcg(part + (int64_t)(i0 + i) * recf + e) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i0 + i < p.pieces) O = fmaf(w_s[e / HD][i0 + i], v[i], O);
+      }
+      out[e] = Elem<T>::from_f(O * inv_s[e / HD]);
+    }
+    return;
+  }
   const float* sc = p.scores + (int64_t)unit * p.G * p.score_stride;
   float* mass = p.mass + (int64_t)unit * p.max_slots;
-  for (int t = (int)blockIdx.y * kMassThreads + tid; t < S; t += (int)gridDim.y * kMassThreads) {
-    float w = 0.f;
-    for (int g = 0; g < p.G; ++g) {
-      const float s = __ldcg(sc + (int64_t)g * p.score_stride + t);
-      if (s != -INFINITY) w = fmaf(exp2f(s - lse_s[g]), inv_s[g], w);
+  auto weight = [&](float s, int g, float w) { return s == -INFINITY ? w : fmaf(exp2f(s - m_s[g]), inv_s[g], w); };
+  const int64_t step = (int64_t)(gridDim.y - 1) * kMassSlots;
+  for (int64_t base = t0; base < S; base += step) {
+    const int t1 = (int)min((int64_t)S, base + kMassSlots);
+    if (p.vec4) {
+      for (int t = (int)base + tid * 4; t < t1; t += kMassThreads * 4) {
+        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int g = 0; g < p.G; ++g) {  // (scores past S are not weights: not added below)
+          const float4 s = __ldcg(reinterpret_cast<const float4*>(sc + (int64_t)g * p.score_stride + t));
+          w.x = weight(s.x, g, w.x);
+          w.y = weight(s.y, g, w.y);
+          w.z = weight(s.z, g, w.z);
+          w.w = weight(s.w, g, w.w);
+        }
+        float4* at = reinterpret_cast<float4*>(mass + t);
+        float4 a = *at;
+        a.x += w.x;
+        if (t + 1 < S) a.y += w.y;
+        if (t + 2 < S) a.z += w.z;
+        if (t + 3 < S) a.w += w.w;
+        *at = a;
+      }
+    } else {
+      for (int t = (int)base + tid; t < t1; t += kMassThreads) {
+        float w = 0.f;
+        for (int g = 0; g < p.G; ++g) w = weight(__ldcg(sc + (int64_t)g * p.score_stride + t), g, w);
+        mass[t] += w;
+      }
     }
-    mass[t] += w;
   }
 }
 
@@ -141,24 +130,11 @@ cudaError_t launch_chained(Kern kern, const P& p, dim3 grid, int threads, cudaSt
 
 }  // namespace
 
-cudaError_t launch_prefix_join(const PrefixJoinParams& p, int dtype, int d, cudaStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)p.B * p.Hq + kJoinWarps - 1) / kJoinWarps));
-  const int n = kJoinWarps * 32;
-  if (dtype == WM_DT_F32) {
-    if (d == 64) return launch_chained(prefix_join_kernel<float, 64>, p, grid, n, s);
-    if (d == 96) return launch_chained(prefix_join_kernel<float, 96>, p, grid, n, s);
-    return launch_chained(prefix_join_kernel<float, 128>, p, grid, n, s);
-  }
-  if (d == 64) return launch_chained(prefix_join_kernel<__nv_bfloat16, 64>, p, grid, n, s);
-  if (d == 96) return launch_chained(prefix_join_kernel<__nv_bfloat16, 96>, p, grid, n, s);
-  return launch_chained(prefix_join_kernel<__nv_bfloat16, 128>, p, grid, n, s);
-}
-
-cudaError_t launch_mass_add(const MassParams& p, int dtype, int d, cudaStream_t s) {
-  // four slots per thread and pass at most
-  int ny = (p.max_slots + 4 * kMassThreads - 1) / (4 * kMassThreads);
-  if (ny > 65535) ny = 65535;
-  const dim3 grid((unsigned)(p.B * p.Hkv), (unsigned)ny);
+cudaError_t launch_mass_add(MassParams p, int dtype, int d, cudaStream_t s) {
+  // rows of mass on 16-byte boundaries
+  p.vec4 = p.max_slots % 4 == 0 && ((uintptr_t)p.mass & 15) == 0 ? 1 : 0;
+  const int parts = (p.max_slots + kMassSlots - 1) / kMassSlots;
+  const dim3 grid((unsigned)(p.B * p.Hkv), (unsigned)(1 + (parts < 65534 ? parts : 65534)));
   const int n = kMassThreads;
   if (dtype == WM_DT_F32) {
     if (d == 64) return launch_chained(mass_add_kernel<float, 64>, p, grid, n, s);

@@ -342,6 +342,8 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ uint32_t live_s[kRangeWarps][kStages];
   __shared__ int lims[kRangeRows];
+  __shared__ float wts[kRangeRows][kRangeMaxCluster + kRangeMaxRecords];  // weights of the records joined
+  __shared__ float row_m[kRangeRows], row_inv[kRangeRows];                // joined max and 1 / sum
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int C = p.pieces;
@@ -351,8 +353,14 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
   unsigned char* ring = smem_raw + warp * kStages * SH::STAGE_BYTES;
   float* crec = reinterpret_cast<float*>(smem_raw + kRangeWarps * kStages * SH::STAGE_BYTES);
 
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // A suffix runs behind the prefix kernel of the same call, which lets it start
+  // only after its own wait: everything before that call is visible already, and
+  // only the prefix's records have to be waited for, at the end.
+  const bool late = p.records > 0;
+  if (!late) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  }
 
   // ---- this unit's rows and slots.  Row i is query head h G + g of sequence b.
   const bool shared_prefix = p.mode == kRangePrefix;
@@ -452,7 +460,14 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
     fm.init();
   }
 
-  float* srows = SCORES ? p.scores + (int64_t)unit * p.G * p.score_stride : nullptr;
+  // scores: in global memory, or this CTA's slots of them in shared memory
+  const bool own_mass = SCORES && p.mass != nullptr;
+  const int jA = (int)((int64_t)piece * kRangeWarps * R.n / npieces);
+  const int jB = (int)((int64_t)(piece + 1) * kRangeWarps * R.n / npieces);  // (kRangeScores: R is [0, S))
+  const int64_t sstride = own_mass ? p.mass_slots : p.score_stride;
+  float* smass = qs + (MMA ? 0 : kRangeRows * HD);
+  float* srows = nullptr;
+  if (SCORES) srows = own_mass ? smass - jA * SS : p.scores + (int64_t)unit * p.G * p.score_stride;
   for (int i = 0; i < nmine; ++i) {
     cp_async_wait<kStages - 1>();
     __syncwarp();
@@ -461,11 +476,11 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
     const int t0 = first_slot(j0 + i);
     if constexpr (MMA) {
       const uint32_t ks = smem_u32(st);
-      float* srow = SCORES && (lane >> 2) < rows ? srows + (lane >> 2) * p.score_stride : nullptr;
+      float* srow = SCORES && (lane >> 2) < rows ? srows + (lane >> 2) * sstride : nullptr;
       mm.template stage<SCORES>(ks, ks + SH::HALF_BYTES, lane, t0, live, p.qscale, srow);
     } else {
       fm.template stage<SCORES>(reinterpret_cast<const float*>(st), reinterpret_cast<const float*>(st + SH::HALF_BYTES),
-                                qs, lims, lane, t0, live, p.qscale, srows, p.score_stride);
+                                qs, lims, lane, t0, live, p.qscale, srows, sstride);
     }
     __syncwarp();  // every lane is done with this ring slot
     const int row = row_next;
@@ -487,7 +502,8 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
   };
   T* outp = reinterpret_cast<T*>(p.out) + ((int64_t)grp * p.Hq + h * p.G) * HD;  // kRangeWindow
   float* gpart = p.part + (int64_t)blockIdx.x * range_rec(rows, HD);
-  const bool window = p.mode == kRangeWindow;
+  const bool final_out = p.mode == kRangeWindow || p.mode == kRangeSuffix || own_mass;
+  const bool direct = final_out && C == 1 && p.records == 0 && !own_mass;
   for (int e = tid; e < E; e += kThreads) {
     const int r = e / HD;
     float M = -INFINITY, L = 0.f, O = 0.f;
@@ -500,10 +516,10 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
       L = fmaf(wt, warp_rec(w)[E + 2 * r + 1], L);
       O = fmaf(wt, warp_rec(w)[e], O);
     }
-    if (window && C == 1) {
+    if (direct) {
       outp[e] = Elem<T>::from_f(O * (L > 0.f ? 1.f / L : 0.f));
     } else {
-      float* rec = window ? crec : gpart;
+      float* rec = final_out ? crec : gpart;
       rec[e] = O;
       if (e == r * HD) {
         rec[E + 2 * r] = M;
@@ -511,36 +527,93 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
       }
     }
   }
-  if (!window || C == 1) return;
+  if (direct || !final_out) return;
 
-  // ---- join the cluster's CTAs through distributed shared memory: CTA
-  // `piece` finishes its share of the outputs; the second barrier keeps each
-  // CTA's shared memory until every reader is done
+  // ---- join the cluster's CTAs through distributed shared memory, and the
+  // records of the shared prefix: CTA `piece` finishes its share of the outputs.
+  // The last barrier keeps each CTA's shared memory until every reader is done.
   cg::cluster_group cluster = cg::this_cluster();
-  cluster.sync();
+  if (C > 1) cluster.sync();
+  else __syncthreads();
+  const int np = p.records;
+  if (late) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  }
+  // record i of the prefix for row r: outputs, and (max, sum) at offset `pml`
+  auto prefix_rec = [&](int r, int i, int& pml) -> const float* {
+    const int x = grp * p.G + r;  // the row among the batch's rows of this kv head
+    if (p.tile_records) {
+      pml = HD;
+      return p.prefix + (((int64_t)h * p.B * p.G + x) * np + i) * tile_rec(HD);
+    }
+    const int g8 = x / kRangeRows, xr = x - g8 * kRangeRows;
+    pml = kRangeRows * HD + 2 * xr - xr * HD;
+    return p.prefix + (((int64_t)g8 * p.Hkv + h) * np + i) * range_rec(kRangeRows, HD) + xr * HD;
+  };
+  for (int r = warp; r < rows; r += kRangeWarps) {
+    auto ml = [&](int i) -> float2 {
+      if (i < C) {
+        const float* cr = C > 1 ? cluster.map_shared_rank(crec, i) : crec;
+        return make_float2(cr[E + 2 * r], cr[E + 2 * r + 1]);
+      }
+      int pml;
+      const float* rec = prefix_rec(r, i - C, pml);
+      return make_float2(__ldcg(rec + pml), __ldcg(rec + pml + 1));
+    };
+    float M = -INFINITY, L = 0.f;
+    for (int i = lane; i < C + np; i += 32) M = fmaxf(M, ml(i).x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(FULL, M, o));
+    for (int i = lane; i < C + np; i += 32) {
+      const float2 x = ml(i);
+      const float w = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
+      wts[r][i] = w;
+      if (w != 0.f) L = fmaf(w, x.y, L);
+    }
+    L = warp_sum(L);
+    if (lane == 0) {
+      row_m[r] = M;
+      row_inv[r] = L > 0.f ? 1.f / L : 0.f;
+    }
+  }
+  __syncthreads();
   const int e0 = piece * E / C, e1 = (piece + 1) * E / C;
   for (int e = e0 + tid; e < e1; e += kThreads) {
-    const int r = e / HD;
-    float mq[kRangeMaxCluster], lq[kRangeMaxCluster], oq[kRangeMaxCluster];
-#pragma unroll
-    for (int c = 0; c < kRangeMaxCluster; ++c) {
-      const float* cr = cluster.map_shared_rank(crec, c < C ? c : 0);
-      mq[c] = c < C ? cr[E + 2 * r] : -INFINITY;
-      lq[c] = c < C ? cr[E + 2 * r + 1] : 0.f;
-      oq[c] = c < C ? cr[e] : 0.f;
+    const int r = e / HD, x = e - r * HD;
+    float O = 0.f;
+    for (int c = 0; c < C; ++c) {
+      const float* cr = C > 1 ? cluster.map_shared_rank(crec, c) : crec;
+      O = fmaf(wts[r][c], cr[e], O);
     }
-    float M = -INFINITY, L = 0.f, O = 0.f;
+    // (a record without a visible slot may hold no outputs: weight 0, not read)
+    int pml;
+    const float* rec = np > 0 ? prefix_rec(r, 0, pml) : nullptr;
+    const int64_t rstride = p.tile_records ? tile_rec(HD) : range_rec(kRangeRows, HD);
+    for (int i0 = 0; i0 < np; i0 += 8) {
+      float v[8];
 #pragma unroll
-    for (int c = 0; c < kRangeMaxCluster; ++c) M = fmaxf(M, mq[c]);
+      for (int i = 0; i < 8; ++i)
+        v[i] = i0 + i < np && wts[r][C + i0 + i] != 0.f ? __ldcg(rec + (i0 + i) * rstride + x) : 0.f;
 #pragma unroll
-    for (int c = 0; c < kRangeMaxCluster; ++c) {
-      const float wt = mq[c] == -INFINITY ? 0.f : exp2f(mq[c] - M);
-      L = fmaf(wt, lq[c], L);
-      O = fmaf(wt, oq[c], O);
+      for (int i = 0; i < 8; ++i)
+        if (i0 + i < np) O = fmaf(wts[r][C + i0 + i], v[i], O);
     }
-    outp[e] = Elem<T>::from_f(O * (L > 0.f ? 1.f / L : 0.f));
+    outp[e] = Elem<T>::from_f(O * row_inv[r]);
   }
-  cluster.sync();
+  if (own_mass) {
+    // mass[t] += sum_r 2^(s_r[t] - m_r) / l_r over this CTA's slots
+    float* mass = p.mass + (int64_t)unit * max_slots;
+    for (int t = jA * SS + tid; t < min(jB * SS, R.S); t += kThreads) {
+      float w = 0.f;
+      for (int r = 0; r < rows; ++r) {
+        const float x = srows[r * sstride + t];
+        if (x != -INFINITY) w = fmaf(exp2f(x - row_m[r]), row_inv[r], w);
+      }
+      mass[t] += w;
+    }
+  }
+  if (C > 1) cluster.sync();
 }
 
 template <typename T, int HD>
@@ -553,7 +626,7 @@ template <typename T, int HD, int NR, bool SCORES>
 inline cudaError_t launch_t(const RangeParams& p, int units, cudaStream_t stream) {
   static size_t smem_set[kSmemOptDevices] = {};
   auto kern = range_attn_kernel<T, HD, NR, SCORES>;
-  constexpr size_t smem = range_smem<T, HD>();
+  const size_t smem = range_smem<T, HD>() + (p.mass ? (size_t)p.G * p.mass_slots * sizeof(float) : 0);
   if (cudaError_t e = opt_in_smem(kern, smem, smem_set); e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)units * (unsigned)p.pieces);
@@ -568,7 +641,7 @@ inline cudaError_t launch_t(const RangeParams& p, int units, cudaStream_t stream
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = p.mode == kRangeWindow ? 2 : 1;
+  cfg.numAttrs = p.mode == kRangeWindow || p.mode == kRangeSuffix || p.mass ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, p);
 }
 

@@ -13,15 +13,18 @@ namespace wm {
 // What a unit (one group of query rows that read the same K/V rows) covers.
 enum RangeMode : int32_t {
   kRangeWindow = 0,  // (sequence, kv head): the sinks and the window, written to out
-  kRangeSuffix = 1,  // (sequence, kv head): slots begin .. S-1, partial records
+  kRangeSuffix = 1,  // (sequence, kv head): slots begin .. S-1, joined with the
+                     // prefix's records and written to out
   kRangePrefix = 2,  // (8 query rows of any sequences, kv head): slots 0 .. begin-1 of
                      // sequence 0's pages, partial records
-  kRangeScores = 3   // (sequence, kv head): every slot, partial records and scores
+  kRangeScores = 3   // (sequence, kv head): every slot; partial records and scores, or
+                     // (mass != NULL) out and the weights added to mass
 };
 
 constexpr int kRangeRows = 8;        // most query rows of a unit
 constexpr int kRangeWarps = 4;       // warps per CTA
 constexpr int kRangeMaxCluster = 8;
+constexpr int kRangeMaxRecords = 128;  // most records of a shared prefix per row
 
 struct RangeParams {
   const void* k_pool;         // channel base of the K pool
@@ -31,6 +34,11 @@ struct RangeParams {
   const int32_t* page_table;  // [B][max_pages]
   const int32_t* seq_lens;    // [B]
   int32_t* status;
+  const float* prefix;        // kRangeSuffix: records of the shared prefix, tile_rec or
+                              // range_rec (8 rows) ones
+  int32_t records, tile_records;  // of them per row (0: no prefix), and their layout
+  float* mass;                // [units][max_slots] of the channel, or NULL
+  int32_t mass_slots;         // mass: most slots of one CTA
   float* part;                // [units][pieces][range_rec(rows, d)]
   float* scores;              // [units][G][score_stride] log2-scaled scores (kRangeScores)
   int64_t score_stride;
@@ -44,6 +52,9 @@ struct RangeParams {
   float qscale;               // log2(e) / sqrt(d)
 };
 
+// floats of a partial record of the tile kernel: d outputs, (max, sum), padded
+// to 32 bytes
+constexpr int tile_rec(int d) { return d + 8; }
 // floats of one partial record: rows x d unnormalised outputs, then (max, sum)
 // per row in log2 units
 constexpr int range_rec(int rows, int d) { return rows * (d + 2); }
@@ -54,17 +65,6 @@ int range_stage_slots(int dtype, int d);
 constexpr int kRangeCtasPerSm = 2;
 cudaError_t launch_range_attn(const RangeParams& p, int dtype, int d, int units, cudaStream_t s);
 
-// Joins the partial records of the shared prefix and of each sequence's suffix.
-struct PrefixJoinParams {
-  const float* prefix;  // tile records [Hkv][B * G][prefix_pieces][tile_rec(d)], or range
-                        // records [row groups][Hkv][prefix_pieces][range_rec(8, d)]
-  const float* suffix;  // [B][Hkv][suffix_pieces][range_rec(G, d)]
-  void* out;
-  int32_t B, Hq, Hkv, G, prefix_pieces, suffix_pieces;
-  int32_t tiles;        // the prefix records' layout
-};
-cudaError_t launch_prefix_join(const PrefixJoinParams& p, int dtype, int d, cudaStream_t s);
-
 // Joins the partial records of kRangeScores and adds the weights to mass.
 struct MassParams {
   const float* part;     // [B][Hkv][pieces][range_rec(G, d)]
@@ -74,8 +74,10 @@ struct MassParams {
   void* out;             // [B][Hq][d]
   int64_t score_stride;
   int32_t B, Hq, Hkv, G, pieces, max_slots;
+  int32_t vec4;          // rows of mass are 16-byte aligned (set by the launch)
 };
-cudaError_t launch_mass_add(const MassParams& p, int dtype, int d, cudaStream_t s);
+constexpr int kMassMaxPieces = 64;
+cudaError_t launch_mass_add(MassParams p, int dtype, int d, cudaStream_t s);
 
 // Tensor-core attention of many rows (tile_attn.cu; bf16, pages of >= 8 slots):
 // under a window with sinks (part == NULL), or over a shared prefix into
@@ -105,8 +107,6 @@ struct TileInputs {
   const void* v_pool;
   int32_t B, k, d;
 };
-// floats of a partial record: d outputs, (max, sum), padded to 32 bytes
-constexpr int tile_rec(int d) { return d + 8; }
 constexpr int kTileRows = 128;
 constexpr int kTileSlots = 128;
 cudaError_t launch_tile_attn(TileParams p, const TileInputs& in, int sms, cudaStream_t s);
@@ -126,7 +126,8 @@ struct EvictParams {
   int32_t* new_lens;
   int32_t* status;
   int32_t B, k, Hkv, P, log2P, num_pages, max_pages, budget, sinks, recent;
+  int32_t cluster;            // CTAs per unit (set by the launch)
 };
-cudaError_t launch_cache_evict(const EvictParams& p, int dtype, int d, cudaStream_t s);
+cudaError_t launch_cache_evict(EvictParams p, int dtype, int d, int sms, cudaStream_t s);
 
 }  // namespace wm
