@@ -356,10 +356,11 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
   // A suffix runs behind the prefix kernel of the same call, which lets it start
   // only after its own wait: everything before that call is visible already, and
   // only the prefix's records have to be waited for, at the end.
-  const bool late = p.records > 0;
+  const bool late = p.records > 0, prefix_pass = p.mode == kRangePrefix;
   if (!late) {
+    if (!prefix_pass) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (prefix_pass) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   }
 
   // ---- this unit's rows and slots.  Row i is query head h G + g of sequence b.
@@ -536,6 +537,32 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
   if (C > 1) cluster.sync();
   else __syncthreads();
   const int np = p.records;
+  const int e0 = piece * E / C, e1 = (piece + 1) * E / C;
+  if (np == 0 && !own_mass) {
+    for (int e = e0 + tid; e < e1; e += kThreads) {
+      const int r = e / HD;
+      float mq[kRangeMaxCluster], lq[kRangeMaxCluster], oq[kRangeMaxCluster];
+#pragma unroll
+      for (int c = 0; c < kRangeMaxCluster; ++c) {
+        const float* cr = cluster.map_shared_rank(crec, c < C ? c : 0);
+        mq[c] = c < C ? cr[E + 2 * r] : -INFINITY;
+        lq[c] = c < C ? cr[E + 2 * r + 1] : 0.f;
+        oq[c] = c < C ? cr[e] : 0.f;
+      }
+      float M = -INFINITY, L = 0.f, O = 0.f;
+#pragma unroll
+      for (int c = 0; c < kRangeMaxCluster; ++c) M = fmaxf(M, mq[c]);
+#pragma unroll
+      for (int c = 0; c < kRangeMaxCluster; ++c) {
+        const float wt = mq[c] == -INFINITY ? 0.f : exp2f(mq[c] - M);
+        L = fmaf(wt, lq[c], L);
+        O = fmaf(wt, oq[c], O);
+      }
+      outp[e] = Elem<T>::from_f(O * (L > 0.f ? 1.f / L : 0.f));
+    }
+    cluster.sync();
+    return;
+  }
   if (late) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -578,7 +605,6 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
     }
   }
   __syncthreads();
-  const int e0 = piece * E / C, e1 = (piece + 1) * E / C;
   for (int e = e0 + tid; e < e1; e += kThreads) {
     const int r = e / HD, x = e - r * HD;
     float O = 0.f;

@@ -57,7 +57,13 @@ class DecodeSession:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._weights = None
         self._weight_refs = None
-        self._scratch = {}
+        self._scratch = {}   # per stream
+        self._need = {}      # workspace bytes by call and shape
+        # argument-independent parts of the long-context calls, made once: a
+        # small launch takes about as long on the GPU as its call on the host
+        self._refs = (ctypes.byref(self.cfg), ctypes.byref(self.cache))
+        self._lib = W.lib()
+        self._status_ptr = self.status.data_ptr()
 
     # ------------------------------------------------------------------ setup
     def set_weights(self, pre_g, Wr, br, ch_g, Wkv, qk_g) -> None:
@@ -119,13 +125,42 @@ class DecodeSession:
             raise W.WMError(rc, "wm_kv_mix")
 
     # ---------------------------------------------------------- long contexts
+    def _raw_stream(self, stream) -> int:
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self.device.index or 0)
+        return stream.cuda_stream
+
+    def _scratch_for(self, nbytes: int, raw: int, stream):
+        # one buffer per stream for the calls below (they need nothing in it,
+        # so calls on one stream share it), kept at the largest size asked for
+        # and allocated on that stream.  The first call of a size may allocate:
+        # make it before a graph capture.
+        buf = self._scratch.get(raw)
+        if buf is None or buf.numel() < nbytes:
+            s = torch.cuda.current_stream(self.device) if stream is None else stream
+            with torch.cuda.stream(s):
+                buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self._scratch[raw] = buf
+        return buf.data_ptr()
+
+    def _bytes(self, key, query, *args) -> int:
+        n = self._need.get(key)
+        if n is None:
+            n = query(self.cfg, *args)
+            if n == 0:
+                raise W.WMError(W.WM_ERR_INVALID_ARG, query.__name__)
+            self._need[key] = n
+        return n
+
     def window_attn(self, layer: int, q, page_table, seq_lens, out, *, sinks: int, window: int,
                     B: int | None = None, stream=None) -> None:
         """Decode attention over the first ``sinks`` slots and the last
         ``window`` slots of each sequence."""
-        rc = W.wm_window_attn(self.cfg, self.cache, layer, q, page_table, seq_lens, sinks, window,
-                              self.B if B is None else B, self.max_pages, out, self.status,
-                              self._stream(stream))
+        cfg, cache = self._refs
+        rc = self._lib.wm_window_attn(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
+                                      seq_lens.data_ptr(), sinks, window, self.B if B is None else B,
+                                      self.max_pages, out.data_ptr(), self._status_ptr,
+                                      self._raw_stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_window_attn")
 
@@ -133,36 +168,28 @@ class DecodeSession:
                             stream=None) -> None:
         """window_attn's mask for query rows q [B][Tq][Hq][d] at positions pos
         [B][Tq]: position i sees slots t <= i, t < sinks or t > i - window."""
-        rc = W.wm_window_prefill_attn(self.cfg, self.cache, layer, q, pos, page_table, sinks, window,
-                                      int(q.shape[0]), int(q.shape[1]), self.max_pages, out,
-                                      self.status, self._stream(stream))
+        cfg, cache = self._refs
+        B, Tq = q.shape[:2]
+        rc = self._lib.wm_window_prefill_attn(cfg, cache, layer, q.data_ptr(), pos.data_ptr(),
+                                              page_table.data_ptr(), sinks, window, B, Tq,
+                                              self.max_pages, out.data_ptr(), self._status_ptr,
+                                              self._raw_stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_window_prefill_attn")
-
-    def _scratch_for(self, nbytes: int, stream):
-        # one buffer per stream for the calls below (they need nothing in it,
-        # so calls on one stream share it), kept at the largest size asked for
-        # and allocated on that stream.  The first call of a size may allocate:
-        # make it before a graph capture.
-        if nbytes == 0:
-            raise W.WMError(W.WM_ERR_INVALID_ARG, "workspace query")
-        s = torch.cuda.current_stream(self.device) if stream is None else stream
-        buf = self._scratch.get(s.cuda_stream)
-        if buf is None or buf.numel() < nbytes:
-            with torch.cuda.stream(s):
-                buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-            self._scratch[s.cuda_stream] = buf
-        return buf
 
     def prefix_attn(self, layer: int, q, page_table, seq_lens, out, *, shared_pages: int,
                     B: int | None = None, stream=None) -> None:
         """Decode attention of sequences whose first ``shared_pages`` pages are
         the same ones: those are read once for the batch."""
+        cfg, cache = self._refs
         B = self.B if B is None else B
-        need = W.wm_prefix_attn_workspace(self.cfg, B, self.max_pages, shared_pages)
-        rc = W.wm_prefix_attn(self.cfg, self.cache, layer, q, page_table, seq_lens, shared_pages, B,
-                              self.max_pages, out, self._scratch_for(need, stream), need, self.status,
-                              self._stream(stream))
+        need = self._bytes(("prefix", B, shared_pages), W.wm_prefix_attn_workspace, B,
+                           self.max_pages, shared_pages)
+        raw = self._raw_stream(stream)
+        rc = self._lib.wm_prefix_attn(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
+                                      seq_lens.data_ptr(), shared_pages, B, self.max_pages,
+                                      out.data_ptr(), self._scratch_for(need, raw, stream), need,
+                                      self._status_ptr, raw)
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_prefix_attn")
 
@@ -170,11 +197,14 @@ class DecodeSession:
                          B: int | None = None, stream=None) -> None:
         """Decode attention that adds every slot's softmax weight, summed over
         the query heads of a kv head, to mass [k][B][Hkv][slots] (fp32)."""
+        cfg, cache = self._refs
         B = self.B if B is None else B
-        need = W.wm_decode_attn_mass_workspace(self.cfg, B, self.max_pages)
-        rc = W.wm_decode_attn_mass(self.cfg, self.cache, layer, q, page_table, seq_lens, mass, B,
-                                   self.max_pages, out, self._scratch_for(need, stream), need, self.status,
-                                   self._stream(stream))
+        need = self._bytes(("mass", B), W.wm_decode_attn_mass_workspace, B, self.max_pages)
+        raw = self._raw_stream(stream)
+        rc = self._lib.wm_decode_attn_mass(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
+                                           seq_lens.data_ptr(), mass.data_ptr(), B, self.max_pages,
+                                           out.data_ptr(), self._scratch_for(need, raw, stream),
+                                           need, self._status_ptr, raw)
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_decode_attn_mass")
 
@@ -183,9 +213,12 @@ class DecodeSession:
         """Cut every (channel, sequence, kv head) to ``budget`` slots: the
         first ``sinks``, the last ``recent`` and those with the largest mass.
         Writes mass_out (may be mass), kept [k][B][Hkv][budget] and new_lens."""
-        rc = W.wm_cache_evict(self.cfg, self.cache, mass, mass_out, page_table, seq_lens, budget,
-                              sinks, recent, self.B if B is None else B, self.max_pages, kept,
-                              new_lens, self.status, self._stream(stream))
+        cfg, cache = self._refs
+        rc = self._lib.wm_cache_evict(cfg, cache, mass.data_ptr(), mass_out.data_ptr(),
+                                      page_table.data_ptr(), seq_lens.data_ptr(), budget, sinks,
+                                      recent, self.B if B is None else B, self.max_pages,
+                                      kept.data_ptr(), new_lens.data_ptr(), self._status_ptr,
+                                      self._raw_stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_cache_evict")
 
