@@ -605,27 +605,43 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
     }
   }
   __syncthreads();
-  for (int e = e0 + tid; e < e1; e += kThreads) {
-    const int r = e / HD, x = e - r * HD;
-    float O = 0.f;
+  // four outputs per thread; a record without a visible slot may hold no
+  // outputs: weight 0, not read
+  const int64_t rstride = p.tile_records ? tile_rec(HD) : range_rec(kRangeRows, HD);
+  for (int q = piece * (E / 4) / C + tid; q < (piece + 1) * (E / 4) / C; q += kThreads) {
+    const int r = q / (HD / 4), x = (q - r * (HD / 4)) * 4;
+    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float w, const float4& v) {
+      O.x = fmaf(w, v.x, O.x);
+      O.y = fmaf(w, v.y, O.y);
+      O.z = fmaf(w, v.z, O.z);
+      O.w = fmaf(w, v.w, O.w);
+    };
     for (int c = 0; c < C; ++c) {
       const float* cr = C > 1 ? cluster.map_shared_rank(crec, c) : crec;
-      O = fmaf(wts[r][c], cr[e], O);
+      add(wts[r][c], *reinterpret_cast<const float4*>(cr + r * HD + x));
     }
-    // (a record without a visible slot may hold no outputs: weight 0, not read)
     int pml;
-    const float* rec = np > 0 ? prefix_rec(r, 0, pml) : nullptr;
-    const int64_t rstride = p.tile_records ? tile_rec(HD) : range_rec(kRangeRows, HD);
-    for (int i0 = 0; i0 < np; i0 += 8) {
-      float v[8];
+    const float* rec = np > 0 ? prefix_rec(r, 0, pml) + x : nullptr;
+    constexpr int NB = 10;  // records in flight
+    for (int i0 = 0; i0 < np; i0 += NB) {
+      float4 v[NB];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        v[i] = i0 + i < np && wts[r][C + i0 + i] != 0.f ? __ldcg(rec + (i0 + i) * rstride + x) : 0.f;
+      for (int i = 0; i < NB; ++i) {
+        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i0 + i < np && wts[r][C + i0 + i] != 0.f)
+          v[i] = __ldcg(reinterpret_cast<const float4*>(rec + (i0 + i) * rstride));
+      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i0 + i < np) O = fmaf(wts[r][C + i0 + i], v[i], O);
+      for (int i = 0; i < NB; ++i)
+        if (i0 + i < np) add(wts[r][C + i0 + i], v[i]);
     }
-    outp[e] = Elem<T>::from_f(O * row_inv[r]);
+    const float inv = row_inv[r];
+    T* to = outp + r * HD + x;
+    to[0] = Elem<T>::from_f(O.x * inv);
+    to[1] = Elem<T>::from_f(O.y * inv);
+    to[2] = Elem<T>::from_f(O.z * inv);
+    to[3] = Elem<T>::from_f(O.w * inv);
   }
   if (own_mass) {
     // mass[t] += sum_r 2^(s_r[t] - m_r) / l_r over this CTA's slots
