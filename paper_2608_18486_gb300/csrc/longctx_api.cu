@@ -372,6 +372,8 @@ wm_status wm_cache_evict(const wm_config* c, const wm_cache* cache, const float*
   if (budget > max_pages * c->page_size) return WM_ERR_INVALID_ARG;
   if (B == 0) return WM_OK;
   if ((int64_t)c->k * B * c->Hkv > INT32_MAX / 8) return WM_ERR_UNSUPPORTED;
+  // 32-bit cache rows over all channels
+  if ((int64_t)c->k * cache->num_pages * c->Hkv * c->page_size > INT32_MAX) return WM_ERR_UNSUPPORTED;
   if (!mass || !mass_out || !page_table || !seq_lens || !kept || !new_lens) return WM_ERR_INVALID_ARG;
   if (!aligned(mass, 4) || !aligned(mass_out, 4) || new_lens == seq_lens) return WM_ERR_INVALID_ARG;
   EvictParams p{};

@@ -471,6 +471,23 @@ def test_evict_long_sequence():
     assert same_bits(s.k_pool, kd) and same_bits(s.v_pool, vd)
 
 
+@pytest.mark.parametrize("B,k,Hkv,d", [(30, 3, 4, 64), (3, 2, 5, 96)])
+def test_evict_many_units_and_clusters(B, k, Hkv, d):
+    """More units than two per SM, and few enough for clusters, several waves each."""
+    lens = [500 - 7 * b for b in range(B)]
+    c = Cache(lens, Hkv=Hkv, G=1, d=d, page=16, k=k, seed=B)
+    mass = np.abs(c.rng.standard_normal((k, B, Hkv, c.T))).astype(np.float32)
+    s = c.session()
+    table, dl = c.dev()
+    m = torch.from_numpy(mass).cuda()
+    kept, nl = torch.empty((k, B, Hkv, 260), dtype=torch.int32, device="cuda"), torch.empty_like(dl)
+    s.evict(m, table, dl, m, kept, nl, budget=260, sinks=4, recent=30)
+    kd, vd, out, want, wl = evict_reference(c, mass, 260, 4, 30)
+    assert s.read_status() == 0
+    assert np.array_equal(kept.cpu().numpy(), want) and np.array_equal(m.cpu().numpy(), out)
+    assert same_bits(s.k_pool, kd) and same_bits(s.v_pool, vd)
+
+
 def test_evict_bad_lengths_and_pages_are_reported():
     c = Cache([60, 60, 60], Hkv=1, G=1, d=64, page=16, k=1, seed=2)
     s = c.session()
