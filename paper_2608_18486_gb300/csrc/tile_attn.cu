@@ -18,13 +18,15 @@
 // item's queries and first K tiles, and the MMA warp issues its first S, while
 // the softmax warps still write the previous item's rows.
 //
-//  * warps 0-3, 4-7: softmax of query tile 0, 1, one thread per row;
-//  * warp 8: each item's ranges (from its rows' positions), passed on through
+//  * warps 0-7, 8-15: softmax of query tile 0, 1, two threads per row, each over
+//    64 columns (one thread's chain of a whole row was longer than the products
+//    of both tiles);
+//  * warp 16: each item's ranges (from its rows' positions), passed on through
 //    shared memory, and the TMA loads of Q and K;
-//  * warp 9: MMA issue, by one elected lane;
-//  * warp 10: passes each V tile on to the MMA warp, its unseen rows zeroed
+//  * warp 17: MMA issue, by its elected lane;
+//  * warp 18: passes each V tile on to the MMA warp, its unseen rows zeroed
 //    where there are any;
-//  * warp 11: the TMA loads of V.
+//  * warp 19: the TMA loads of V.
 //
 // The two query tiles of an item are two query heads of one kv head over the
 // same rows where the group size is even, else consecutive rows of one head.
@@ -47,14 +49,15 @@ namespace {
 constexpr int kTM = 128;                  // query rows per tile (MMA M)
 constexpr int kTN = 128;                  // slots per KV tile
 constexpr int kQT = 2;                    // query tiles per item
-constexpr int kSoftWarps = 4 * kQT;
+constexpr int kTileWarps = 8;             // softmax warps per query tile: two threads per row
+constexpr int kSoftWarps = kTileWarps * kQT;
 constexpr int kLoadWarp = kSoftWarps;
 constexpr int kMmaWarp = kSoftWarps + 1;
 constexpr int kFixWarp = kSoftWarps + 2;
 constexpr int kVWarp = kSoftWarps + 3;
 constexpr int kTThreads = (kSoftWarps + 4) * 32;
 constexpr uint32_t kBlock = 128u * 128u;  // bytes of a 64-column block of a 128-row tile
-constexpr uint32_t kTmemCols = 512;       // S_i at 128 i (P_i over its first 64), O_i at 256 + 128 i
+constexpr uint32_t kTmemCols = 512;       // S_i at 128 i (P_i at its columns 0-31 and 64-95), O_i at 256 + 128 i
 constexpr float kStaleMax = 8.f;          // log2 headroom before O is rescaled
 
 template <int HD>
@@ -63,8 +66,7 @@ struct TShape {
   static constexpr int NSK = HD <= 64 ? 4 : 3;
   static constexpr int NSV = HD <= 64 ? 4 : 2;
   static constexpr uint32_t TILE_BYTES = CB * kBlock;  // one Q, K or V tile
-  static constexpr uint32_t SMEM = (kQT + NSK + NSV) * TILE_BYTES + 1024;  // + alignment
-  static_assert(SMEM <= 227 * 1024, "shared memory");
+  static constexpr uint32_t TILES = (kQT + NSK + NSV) * TILE_BYTES;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -80,6 +82,38 @@ __device__ __forceinline__ bool elect_one() {
   return e != 0;
 }
 
+// The MMA warp runs as a whole, with every tensor instruction predicated on its
+// elected lane: inside a branch of one lane the operands would not stay in
+// uniform registers.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate,
+                                       uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 e, %5, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(lead)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate,
+                                       uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 e, %5, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(lead)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t* bar, uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "setp.ne.b32 e, %1, 0;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)),
+      "r"(lead)
+      : "memory");
+}
+
 // Wait for this thread's TMEM loads; the registers of the one that is used next
 // are operands, so that no use moves up across the wait.
 __device__ __forceinline__ void tmem_wait_for(uint32_t (&r)[32]) {
@@ -89,6 +123,13 @@ __device__ __forceinline__ void tmem_wait_for(uint32_t (&r)[32]) {
                  "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
                  "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]),
                  "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
+}
+
+__device__ __forceinline__ void tmem_wait_for(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]),
+                 "+r"(r[15])::"memory");
 }
 
 // 32 bytes to global memory (wide: dst is 32-byte aligned).
@@ -116,6 +157,24 @@ struct Item {
   int top;     // largest visible slot (-1: none)
   int wlo;     // smallest window start of a row
   int sparse;  // rows may leave slots between wlo and top that none of them sees
+};
+
+// Boxes of a step whose page does not exist, bit per box: K tile j + NSK is
+// loaded once S of step j is there, and S runs at most two steps ahead of the
+// softmax, so a ring of kBadRing is enough.
+constexpr int kBadRing = 8;
+
+// Shared memory behind the tiles.  (Nothing is static, so that the tiles start
+// at the 1024-byte boundary that the swizzle needs: there is no room to align.)
+template <int NSK, int NSV>
+struct Shared {
+  uint64_t qfull[2], qempty, mfull[2], mfree[2], kfull[NSK], kempty[NSK], vfull[NSV], vready[NSV], vempty[NSV];
+  uint64_t sfull[kQT], pfull[2 * kQT], odone[kQT];
+  uint64_t xbar[kQT * 4];       // the two warps of a quadrant of a tile
+  float xval[kQT][2][kTM];      // what their threads tell each other
+  Item items[2];
+  uint32_t bad_boxes[kBadRing];
+  uint32_t tmem_base;
 };
 
 struct Work {  // place of an item
@@ -270,18 +329,30 @@ __global__ void __launch_bounds__(kTThreads, 1)
   constexpr int CB = SH::CB, NSK = SH::NSK, NSV = SH::NSV;
   constexpr uint32_t TB = SH::TILE_BYTES;
   constexpr unsigned FULL = 0xFFFFFFFFu;
-  extern __shared__ uint8_t smem_dyn[];
-  __shared__ uint64_t qfull[2], qempty, mfull[2], mfree[2], kfull[NSK], kempty[NSK], vfull[NSV], vready[NSV],
-      vempty[NSV];
-  __shared__ uint64_t sfull[kQT], pfull[2 * kQT], odone[kQT];
-  __shared__ uint32_t tmem_base;
-  __shared__ Item items[2];
-  // Boxes of a step whose page does not exist, bit per box.  K tile j + NSK is
-  // loaded once S of step j is there, and S runs at most two steps ahead of the
-  // softmax, so a ring of kBadRing is enough.
-  constexpr int kBadRing = 8;
   static_assert(NSK + 3 <= kBadRing, "bad-page ring");
-  __shared__ uint32_t bad_boxes[kBadRing];
+  using Sh = Shared<NSK, NSV>;
+  static_assert(SH::TILES + sizeof(Sh) <= 227 * 1024, "shared memory");
+  extern __shared__ __align__(1024) uint8_t smem_dyn[];
+  Sh& sh = *reinterpret_cast<Sh*>(smem_dyn + SH::TILES);
+  if ((smem_u32(smem_dyn) & 1023u) != 0) {  // (cannot happen)
+    report(p.status, WM_ERR_CUDA);
+    return;
+  }
+  auto& qfull = sh.qfull;
+  auto& mfull = sh.mfull;
+  auto& mfree = sh.mfree;
+  auto& kfull = sh.kfull;
+  auto& kempty = sh.kempty;
+  auto& vfull = sh.vfull;
+  auto& vready = sh.vready;
+  auto& vempty = sh.vempty;
+  auto& sfull = sh.sfull;
+  auto& pfull = sh.pfull;
+  auto& odone = sh.odone;
+  auto& xbar = sh.xbar;
+  uint64_t& qempty = sh.qempty;
+  auto& items = sh.items;
+  auto& bad_boxes = sh.bad_boxes;
 
   const int tid = threadIdx.x, lane = tid & 31;
   // Warp-uniform by construction (here and wherever a value of the MMA warp's
@@ -289,9 +360,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
   // from uniform registers, and a value the compiler cannot prove uniform costs
   // a move each, about 85 cycles per MMA against the 64 it takes to run.
   const int warp = uniform(tid >> 5);
-  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) &
-                                             ~static_cast<uintptr_t>(1023));
-  uint8_t* Qs = base;
+  uint8_t* Qs = smem_dyn;
   uint8_t* Ks = Qs + kQT * TB;
   uint8_t* Vs = Ks + NSK * TB;
 
@@ -313,8 +382,9 @@ __global__ void __launch_bounds__(kTThreads, 1)
     }
     for (int i = 0; i < kQT; ++i) {
       mbar_init(&sfull[i], 1);
-      mbar_init(&pfull[i], kTM);
-      mbar_init(&pfull[kQT + i], kTM);
+      mbar_init(&pfull[i], kTileWarps);
+      mbar_init(&pfull[kQT + i], kTileWarps / 2);
+      for (int x = 0; x < 4; ++x) mbar_init(&xbar[4 * i + x], 2);
       mbar_init(&odone[i], 1);
     }
     fence_mbar_init();
@@ -323,7 +393,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
     tc::prefetch_tensormap(&tmV);
   }
   if (warp == 0) {
-    tc::tmem_alloc(&tmem_base, kTmemCols);
+    tc::tmem_alloc(&sh.tmem_base, kTmemCols);
     tc::tmem_relinquish();
   }
   // Dependents may start once this grid has waited for the work before it:
@@ -333,7 +403,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmem = (uint32_t)uniform((int)tmem_base);
+  const uint32_t tmem = (uint32_t)uniform((int)sh.tmem_base);
   const int stride = (int)gridDim.x;
   bool ok = true;
 
@@ -473,10 +543,11 @@ __global__ void __launch_bounds__(kTThreads, 1)
     // ================================================================ MMA
     const uint32_t idesc_o = tc::idesc_bf16_f32(kTM, HD) | tc::kIdescBMajorMN;
     const int la = !WIN && p.pair ? 2 : 1;  // steps that S runs ahead of P V
-    const bool lead = elect_one();
+    const uint32_t lead = elect_one();
     // descriptors of the first tiles (a tile further on: plus its bytes / 16)
     const uint64_t qd = tc::sdesc_kmajor_sw128(smem_u32(Qs)), kd0 = tc::sdesc_kmajor_sw128(smem_u32(Ks)),
                    vd0 = tc::sdesc_mnmajor_sw128(smem_u32(Vs), kBlock, 1024);
+    auto all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL, mbar_wait(bar, parity)) != 0; };
     int ks = 0, vs = 0;      // K tiles multiplied, V tiles multiplied
     int cnt0 = 0, cnt1 = 0;  // P V products of each query tile
     int no = 0;
@@ -495,39 +566,42 @@ __global__ void __launch_bounds__(kTThreads, 1)
       if (lead) {
         mbar_arrive(&mfree[no & 1]);
         if (steps == 0) mbar_arrive(&qempty);
+      }
+      __syncwarp();
+      {  // (a scope of its own: the item's schedule)
         auto issue_s = [&](int i, int cols) {  // S_i = Q_i K^T with the next K tile
           const uint64_t qi = qd + (!WIN && p.pair ? 0 : i) * (TB >> 4), kd = kd0 + (ks % NSK) * (TB >> 4);
           const uint32_t idesc = tc::idesc_bf16_f32(kTM, cols);
 #pragma unroll
           for (int kk = 0; kk < HD / 16; ++kk) {
             const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;
-            tc::mma_bf16(tmem + 128 * i, qi + off, kd + off, idesc, kk > 0);
+            mma_ss(tmem + 128 * i, qi + off, kd + off, idesc, kk > 0, lead);
           }
-          tc::mma_commit(&sfull[i]);
+          commit(&sfull[i], lead);
         };
         // O_i += P_i V; the second half of P follows on its own barrier
         auto issue_pv = [&](int i, int cols, uint64_t vd, bool begun, uint32_t parity) -> bool {
           const uint32_t o = tmem + 256 + 128 * i, pa = tmem + 128 * i;
 #pragma unroll
           for (int kk = 0; kk < kTN / 32; ++kk)
-            tc::mma_bf16_ts(o, pa + 8 * kk, vd + kk * (16 * 128 >> 4), idesc_o, begun || kk > 0);
+            mma_ts(o, pa + 8 * kk, vd + kk * (16 * 128 >> 4), idesc_o, begun || kk > 0, lead);
           if (cols == kTN) {
-            if (!mbar_wait(&pfull[kQT + i], parity)) return false;
+            if (!all(&pfull[kQT + i], parity)) return false;
             tc::fence_after_sync();
 #pragma unroll
             for (int kk = kTN / 32; kk < kTN / 16; ++kk)
-              tc::mma_bf16_ts(o, pa + 8 * kk, vd + kk * (16 * 128 >> 4), idesc_o, 1);
-          } else if (!mbar_wait(&pfull[kQT + i], parity)) {
+              mma_ts(o, pa + 64 + 8 * (kk - kTN / 32), vd + kk * (16 * 128 >> 4), idesc_o, 1, lead);
+          } else if (!all(&pfull[kQT + i], parity)) {
             return false;
           }
-          tc::mma_commit(&odone[i]);
+          commit(&odone[i], lead);
           return true;
         };
-        auto wait_k = [&]() -> bool { return mbar_wait(&kfull[ks % NSK], (ks / NSK) & 1); };
+        auto wait_k = [&]() -> bool { return all(&kfull[ks % NSK], (ks / NSK) & 1); };
         // the K tile of step j is free once the S issued so far are done
         auto free_k = [&](int j) {
-          tc::mma_commit(&kempty[ks % NSK]);
-          if (j == steps - 1) tc::mma_commit(&qempty);
+          commit(&kempty[ks % NSK], lead);
+          if (j == steps - 1) commit(&qempty, lead);
           ++ks;
         };
         for (int j = 0; j < la && j < steps && ok; ++j) {
@@ -546,7 +620,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
           const int cols = columns<WIN>(p, I, tile_at<WIN>(I, j));
           const bool more = j + la < steps;
           const int cols_next = more ? columns<WIN>(p, I, tile_at<WIN>(I, j + la)) : 0;
-          ok = mbar_wait(&vready[sv], (vs / NSV) & 1) && (!more || wait_k());
+          ok = all(&vready[sv], (vs / NSV) & 1) && (!more || wait_k());
           if (!ok) break;
           const uint64_t vd = vd0 + sv * (TB >> 4);
 #pragma unroll
@@ -554,7 +628,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
             if (active<WIN>(p, I, i, j)) {
               int& cnt = i == 0 ? cnt0 : cnt1;
               bool& begun = i == 0 ? begun0 : begun1;
-              ok = mbar_wait(&pfull[i], cnt & 1);
+              ok = all(&pfull[i], cnt & 1);
               if (!ok) break;
               tc::fence_after_sync();
               ok = issue_pv(i, cols, vd, begun, cnt & 1);
@@ -565,19 +639,35 @@ __global__ void __launch_bounds__(kTThreads, 1)
             if (more && active<WIN>(p, I, i, j + la)) issue_s(i, cols_next);
           }
           if (!ok) break;
-          tc::mma_commit(&vempty[sv]);
+          commit(&vempty[sv], lead);
           if (more) free_k(j + la);
         }
       }
-      ok = __all_sync(FULL, ok);
     }
     if (!ok && lead) report(p.status, WM_ERR_TIMEOUT);
   } else {
     // ================================================================ softmax
-    const int i = warp >> 2;             // query tile
-    const int lr = tid - i * kTM;        // row in the tile
+    const int i = warp / kTileWarps;     // query tile
+    const int half = (warp >> 2) & 1;    // columns 64 half .. 64 half + 63
+    const int lr = (warp & 3) * 32 + lane;  // row in the tile: the warp's quadrant of TMEM lanes
     const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t scol = 128 * i, ocol = 256 + 128 * i;
+    const uint32_t scol = 128 * i + 64 * half, ocol = 256 + 128 * i + HD / 2 * half;
+    // The other half's value of the row: written to shared memory, then a barrier
+    // of the two warps.  A step's value is overwritten only after the next S is
+    // there, which was issued after both warps handed on this step's P.
+    uint64_t* xb = &xbar[4 * i + (warp & 3)];
+    int xn = 0;  // barriers passed
+    auto meet = [&]() -> bool {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(xb);
+      return __all_sync(FULL, mbar_wait(xb, xn++ & 1));
+    };
+    auto exchange = [&](float mine, float& other) -> bool {
+      sh.xval[i][half][lr] = mine;
+      if (!meet()) return false;
+      other = sh.xval[i][half ^ 1][lr];
+      return true;
+    };
     int cnt = 0;                         // steps of this tile, over all items
     int done = 0;                        // steps of the CTA before this item
     const int log2b = p.P >= kTN ? 7 : p.log2P;  // slots per box
@@ -632,27 +722,27 @@ __global__ void __launch_bounds__(kTThreads, 1)
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = (see >> e) & 1u ? v[e] : 0xFF800000u;
         };
-        // The row is read from TMEM twice, 64 columns at a time: for its maximum,
-        // then for the probabilities.  (A whole row of 128 registers spills, and
-        // unrolled loops or separate ones for masked steps cost more in the
-        // instruction cache than they save.)
+        // The thread's part of the row is read from TMEM twice, 32 columns at a
+        // time: for its maximum, then for the probabilities.  (Unrolled loops, or
+        // separate ones for masked steps, cost more in the instruction cache than
+        // they save.)
+        const bool mine_too = nc > 2 * half;  // (a step of 64 columns is the lower half's)
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        if (mine_too) {
 #pragma unroll 1
-        for (int c = 0; c < nc; c += 2) {
-          uint32_t v[32], u[32];
-          tc::tmem_ld32(lane_base + scol + 32 * c, v);
-          tc::tmem_ld32(lane_base + scol + 32 * c + 32, u);
-          tmem_wait_for(v);
-          tmem_wait_for(u);
-          if (masked) {
-            mask_part(c, v);
-            mask_part(c + 1, u);
-          }
+          for (int c = 0; c < 2; ++c) {
+            uint32_t v[32];
+            tc::tmem_ld32(lane_base + scol + 32 * c, v);
+            tmem_wait_for(v);
+            if (masked) mask_part(2 * half + c, v);
 #pragma unroll
-          for (int e = 0; e < 32; ++e)
-            mx[e & 3] = fmaxf(mx[e & 3], fmaxf(__uint_as_float(v[e]), __uint_as_float(u[e])));
+            for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(v[e]));
+          }
         }
-        const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.qscale;  // qscale > 0
+        float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), mo = 0.f;
+        ok = exchange(mt, mo);
+        if (!ok) break;
+        mt = fmaxf(mt, mo) * p.qscale;  // qscale > 0: the max commutes with the scale
         float scale = 1.f;
         const bool raise = (m == -INFINITY) ? (mt != -INFINITY) : (mt > m + kStaleMax);
         if (raise) {
@@ -667,21 +757,22 @@ __global__ void __launch_bounds__(kTThreads, 1)
           ok = __all_sync(FULL, mbar_wait(&odone[i], (cnt - 1) & 1));
           if (!ok) break;
           tc::fence_after_sync();
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < HD / 32; ++c) {
-            uint32_t o[32];
-            tc::tmem_ld32(lane_base + ocol + 32 * c, o);
+            uint32_t o[16];
+            tc::tmem_ld16(lane_base + ocol + 16 * c, o);
             tmem_wait_for(o);
-            uint32_t w0[16], w1[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              w0[e] = __float_as_uint(__uint_as_float(o[e]) * fac);
-              w1[e] = __float_as_uint(__uint_as_float(o[16 + e]) * fac);
-            }
-            tc::tmem_st16(lane_base + ocol + 32 * c, w0);
-            tc::tmem_st16(lane_base + ocol + 32 * c + 16, w1);
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fac);
+            tc::tmem_st16(lane_base + ocol + 16 * c, o);
           }
+          tc::tmem_st_wait();
         }
+        // P V of the first 64 slots starts while the others' P is computed; it
+        // needs the lower half's P, and O rescaled by both.
+        tc::fence_before_sync();
+        __syncwarp();
+        if (half == 1 && lane == 0) mbar_arrive(&pfull[i]);
         // p = 2^(s * qscale - m) in pairs; masked slots give 0, and so do rows
         // that have seen nothing yet.  P enters the product as bf16 (the tensor
         // cores' operand); the row sum is kept in fp32 from the unrounded values.
@@ -689,44 +780,41 @@ __global__ void __launch_bounds__(kTThreads, 1)
         const float2 qs2 = make_float2(p.qscale, p.qscale), nm2 = make_float2(nm, nm);
         float2 sum2 = make_float2(0.f, 0.f);
         float2 sum2b = make_float2(0.f, 0.f);
+        if (mine_too) {
 #pragma unroll 1
-        for (int c = 0; c < nc; c += 2) {
-          uint32_t v[32], u[32], pv[16], pu[16];
-          tc::tmem_ld32(lane_base + scol + 32 * c, v);
-          tc::tmem_ld32(lane_base + scol + 32 * c + 32, u);
-          tmem_wait_for(v);
-          tmem_wait_for(u);
-          if (masked) {
-            mask_part(c, v);
-            mask_part(c + 1, u);
-          }
-          auto prob = [&](uint32_t x0, uint32_t x1, float2& sum) -> uint32_t {
-            const float2 y = __ffma2_rn(make_float2(__uint_as_float(x0), __uint_as_float(x1)), qs2, nm2);
-            const float2 pr = make_float2(ex2(y.x), ex2(y.y));
-            sum = __fadd2_rn(sum, pr);
-            const __nv_bfloat162 h = __floats2bfloat162_rn(pr.x, pr.y);
-            return *reinterpret_cast<const uint32_t*>(&h);
-          };
+          for (int c = 0; c < 2; ++c) {
+            uint32_t v[32], pk[16];
+            tc::tmem_ld32(lane_base + scol + 32 * c, v);
+            tmem_wait_for(v);
+            if (masked) mask_part(2 * half + c, v);
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            pv[e / 2] = prob(v[e], v[e + 1], sum2);
-            pu[e / 2] = prob(u[e], u[e + 1], sum2b);
+            for (int e = 0; e < 32; e += 2) {
+              const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), qs2, nm2);
+              const float2 pr = make_float2(ex2(y.x), ex2(y.y));
+              if (e & 2) sum2b = __fadd2_rn(sum2b, pr);
+              else sum2 = __fadd2_rn(sum2, pr);
+              const __nv_bfloat162 h = __floats2bfloat162_rn(pr.x, pr.y);
+              pk[e / 2] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            // P over this thread's own S columns that have been read
+            tc::tmem_st16(lane_base + scol + 16 * c, pk);
           }
-          // P over S columns that have been read: packed pairs, columns 16c .. 16c+31.
-          // P V of the first 64 slots starts while the others' are computed.
-          tc::tmem_st16(lane_base + scol + 16 * c, pv);
-          tc::tmem_st16(lane_base + scol + 16 * c + 16, pu);
           tc::tmem_st_wait();
           tc::fence_before_sync();
-          mbar_arrive(&pfull[c == 0 ? i : kQT + i]);
         }
-        if (nc == 2) mbar_arrive(&pfull[kQT + i]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&pfull[half == 0 ? i : kQT + i]);
         sum2 = __fadd2_rn(sum2, sum2b);
         l = l * scale + (sum2.x + sum2.y);
         ++cnt;
         ++x;
       }
       if (ok && x > 0) ok = __all_sync(FULL, mbar_wait(&odone[i], (cnt - 1) & 1));
+      if (ok && x > 0) {  // both halves' sums (the same in both threads: addition commutes)
+        float lo = 0.f;
+        ok = exchange(l, lo) && meet();  // (the next item's first value waits for both reads)
+        l += lo;
+      }
       if (!ok) break;
       __syncwarp();  // every lane is done with the item's ranges
       if (lane == 0) mbar_arrive(&mfree[no & 1]);
@@ -745,38 +833,36 @@ __global__ void __launch_bounds__(kTThreads, 1)
               (((int64_t)w.b * p.rows + r) * p.Hq + w.h + (p.pair ? i : 0)) * HD;
       else
         rec = p.part + (((int64_t)w.h * p.rows + r) * p.records + (p.pair ? w.split * kQT + i : w.split)) * tile_rec(HD);
-#pragma unroll
-      for (int c = 0; c < HD / 32; ++c) {
-        uint32_t o[32];
+#pragma unroll 1
+      for (int c = 0; c < HD / 32; ++c) {  // 16 columns of this thread's half
+        uint32_t o[16];
         if (x > 0) {  // the same for the whole warp group
-          tc::tmem_ld32(lane_base + ocol + 32 * c, o);
+          tc::tmem_ld16(lane_base + ocol + 16 * c, o);
           tmem_wait_for(o);
         }
         if (!live) continue;
+        const int col = HD / 2 * half + 16 * c;
         if (WIN) {
+          uint32_t u[8];
 #pragma unroll
-          for (int e = 0; e < 32; e += 16) {
-            uint32_t u[8];
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-              const float f0 = x > 0 ? __uint_as_float(o[e + 2 * t]) * inv : 0.f;
-              const float f1 = x > 0 ? __uint_as_float(o[e + 2 * t + 1]) * inv : 0.f;
-              const __nv_bfloat162 h = __floats2bfloat162_rn(f0, f1);
-              u[t] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            store32(dst + 32 * c + e, u, p.wide_out);
+          for (int t = 0; t < 8; ++t) {
+            const float f0 = x > 0 ? __uint_as_float(o[2 * t]) * inv : 0.f;
+            const float f1 = x > 0 ? __uint_as_float(o[2 * t + 1]) * inv : 0.f;
+            const __nv_bfloat162 h = __floats2bfloat162_rn(f0, f1);
+            u[t] = *reinterpret_cast<const uint32_t*>(&h);
           }
+          store32(dst + col, u, p.wide_out);
         } else if (x > 0) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
+          for (int e = 0; e < 16; e += 8) {
             uint32_t u[8];
 #pragma unroll
             for (int t = 0; t < 8; ++t) u[t] = o[e + t];
-            store32(rec + 32 * c + e, u, 1);
+            store32(rec + col + e, u, 1);
           }
         }
       }
-      if (!WIN && live) *reinterpret_cast<float2*>(rec + HD) = make_float2(m, l);
+      if (!WIN && live && half == 0) *reinterpret_cast<float2*>(rec + HD) = make_float2(m, l);
       tc::fence_before_sync();
     }
     if (!ok) report(p.status, WM_ERR_TIMEOUT);
@@ -796,11 +882,12 @@ cudaError_t launch_t(const CUtensorMap& q, const CUtensorMap& k, const CUtensorM
                      cudaStream_t s) {
   static size_t smem_set[kSmemOptDevices] = {};
   auto kern = tile_attn_kernel<HD, WIN>;
-  if (cudaError_t e = opt_in_smem(kern, (size_t)TShape<HD>::SMEM, smem_set); e != cudaSuccess) return e;
+  constexpr size_t smem = TShape<HD>::TILES + sizeof(Shared<TShape<HD>::NSK, TShape<HD>::NSV>);
+  if (cudaError_t e = opt_in_smem(kern, smem, smem_set); e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.items < sms ? p.items : sms));
   cfg.blockDim = dim3(kTThreads);
-  cfg.dynamicSmemBytes = TShape<HD>::SMEM;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
