@@ -711,16 +711,27 @@ __global__ void __launch_bounds__(kTThreads, 1)
         }
         const uint32_t gone = bad_boxes[(done + j) % kBadRing];
         const bool masked = __any_sync(FULL, vis < 32 * nc || el > 0 || gone != 0);
-        auto mask_part = [&](int c, uint32_t (&v)[32]) {
-          auto below = [&](int n) -> uint32_t {  // bits e < n of this part
-            return n >= 32 * c + 32 ? 0xFFFFFFFFu : n <= 32 * c ? 0u : (1u << (n - 32 * c)) - 1u;
-          };
-          uint32_t see = below(vis) & (below(es) | ~below(el));
-          if (gone)
-            for (int e = 0; e < 32; ++e)
-              if ((gone >> ((32 * c + e) >> log2b)) & 1u) see &= ~(1u << e);
+        // The warp's two parts of 32 columns: nothing of one is seen (0), some (1) or
+        // all of it (2); a diagonal or a window's edge leaves most of them whole.
+        uint32_t see[2] = {0xFFFFFFFFu, 0xFFFFFFFFu};  // bit per column
+        int kind[2] = {2, 2};
+        if (masked) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = (see >> e) & 1u ? v[e] : 0xFF800000u;
+          for (int c = 0; c < 2; ++c) {
+            const int c0 = 64 * half + 32 * c;
+            auto below = [&](int n) -> uint32_t {  // columns e < n
+              return n >= c0 + 32 ? 0xFFFFFFFFu : n <= c0 ? 0u : (1u << (n - c0)) - 1u;
+            };
+            see[c] = below(vis) & (below(es) | ~below(el));
+            if (gone)
+              for (int e = 0; e < 32; ++e)
+                if ((gone >> ((c0 + e) >> log2b)) & 1u) see[c] &= ~(1u << e);
+            kind[c] = __all_sync(FULL, see[c] == 0xFFFFFFFFu) ? 2 : __any_sync(FULL, see[c] != 0u) ? 1 : 0;
+          }
+        }
+        auto mask_part = [&](uint32_t bits, uint32_t (&v)[32]) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = (bits >> e) & 1u ? v[e] : 0xFF800000u;
         };
         // The thread's part of the row is read from TMEM twice, 32 columns at a
         // time: for its maximum, then for the probabilities.  (Unrolled loops, or
@@ -731,10 +742,12 @@ __global__ void __launch_bounds__(kTThreads, 1)
         if (mine_too) {
 #pragma unroll 1
           for (int c = 0; c < 2; ++c) {
+            const int k = c == 0 ? kind[0] : kind[1];
+            if (k == 0) continue;
             uint32_t v[32];
             tc::tmem_ld32(lane_base + scol + 32 * c, v);
             tmem_wait_for(v);
-            if (masked) mask_part(2 * half + c, v);
+            if (k == 1) mask_part(c == 0 ? see[0] : see[1], v);
 #pragma unroll
             for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(v[e]));
           }
@@ -783,10 +796,17 @@ __global__ void __launch_bounds__(kTThreads, 1)
         if (mine_too) {
 #pragma unroll 1
           for (int c = 0; c < 2; ++c) {
+            const int k = c == 0 ? kind[0] : kind[1];
             uint32_t v[32], pk[16];
+            if (k == 0) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) pk[e] = 0u;
+              tc::tmem_st16(lane_base + scol + 16 * c, pk);
+              continue;
+            }
             tc::tmem_ld32(lane_base + scol + 32 * c, v);
             tmem_wait_for(v);
-            if (masked) mask_part(2 * half + c, v);
+            if (k == 1) mask_part(c == 0 ? see[0] : see[1], v);
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
               const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), qs2, nm2);
