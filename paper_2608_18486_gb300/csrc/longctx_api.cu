@@ -129,6 +129,38 @@ struct PrefixPlan {
   size_t total;
 };
 
+// Which kernel reads the prefix.  The range kernel reads it once per 8 rows, from
+// L2 after the first, and starts in about 5 us less; the tensor-core kernel reads
+// it once.  Measured side by side (us per call, range / tensor): 4.7 MB of K/V
+// and 8 rows 11.0 / 15.4, 37 MB and 8 rows 22.2 / 28.3, 5.9 MB and 16 rows 11.2 /
+// 14.8, 5.9 MB and 32 rows 18.6 / 17.8, 49 MB and 16 rows 32.8 / 25.5, 134 MB and
+// 8 rows 44.5 / 39.3.
+constexpr int64_t kPrefixRangeBytes = 40 << 20;
+
+bool prefix_on_tiles(const wm_config& c, int32_t num_pages, int32_t shared_pages, int groups) {
+  const int64_t bytes = (int64_t)shared_pages * c.page_size * c.Hkv * c.d * 2 * (int64_t)elem_size(c.dtype);
+  return tiles_ok(c, num_pages) && bytes * groups > kPrefixRangeBytes;
+}
+
+// Pieces of a unit of the range kernel's prefix: streaming takes time as
+// stages / pieces, the join behind it as pieces, so about sqrt(stages) of them
+// within the SMs' residency.  More than half the SMs' worth of CTAs keeps the
+// suffix from starting beside them: then no more (bf16) than leave each warp 4
+// stages.  Measured (us per call, 3 / 8 pieces): 16 sequences of 12 heads behind
+// 1920 slots 11.3 / 12.5; 4 sequences of 3 heads behind 512 slots, 2 / 6 pieces,
+// 9.4 / 8.0.
+int prefix_pieces(const wm_config& c, int64_t units, int64_t slots) {
+  const int64_t stages = stages_of(c, slots), sms = sm_count();
+  int64_t n = (int64_t)(sqrt((double)stages) + 0.5);
+  if (n > kRangeCtasPerSm * sms / units) n = kRangeCtasPerSm * sms / units;
+  if (c.dtype == WM_DT_BF16 && 2 * units * n > sms) {
+    const int64_t by_work = stages / (kRangeWarps * kMinStagesPerWarp), beside = sms / 2 / units;
+    const int64_t most = by_work > beside ? by_work : beside;
+    if (n > most) n = most;
+  }
+  return clamp_int(n, 1, 64);
+}
+
 // KV parts of the tensor-core prefix: the count with the shortest last CTA,
 // counting a CTA's fixed cost as two KV tiles and each further record's join.
 int prefix_splits(int64_t units, int64_t tiles, int sms) {
@@ -149,7 +181,7 @@ PrefixPlan prefix_plan(const wm_config& c, int32_t B, int32_t max_pages, int32_t
   const int G = c.Hq / c.Hkv;
   PrefixPlan pl{};
   pl.groups = (int)(((int64_t)B * G + kRangeRows - 1) / kRangeRows);
-  pl.prefix_pieces = split_pieces((int64_t)pl.groups * c.Hkv, stages_of(c, (int64_t)shared_pages * c.page_size), 2);
+  pl.prefix_pieces = prefix_pieces(c, (int64_t)pl.groups * c.Hkv, (int64_t)shared_pages * c.page_size);
   pl.suffix_cluster = range_cluster(c, (int64_t)B * c.Hkv, (int64_t)(max_pages - shared_pages) * c.page_size);
   const int64_t rows = (int64_t)B * G;
   pl.pair = rows <= kTileRows ? 1 : 0;
@@ -280,7 +312,7 @@ wm_status wm_prefix_attn(const wm_config* c, const wm_cache* cache, int32_t laye
   if (ws_bytes < pl.total) return WM_ERR_INVALID_ARG;
   RangeParams p = range_params(*c, *cache, layer, q, page_table, seq_lens, B, max_pages, dev_status);
   p.begin = shared_pages * c->page_size;
-  const bool tiles = tiles_ok(*c, cache->num_pages);
+  const bool tiles = prefix_on_tiles(*c, cache->num_pages, shared_pages, pl.groups);
   if (shared_pages > 0 && tiles) {
     TileParams t = tile_params(*c, *cache, layer, page_table, max_pages, dev_status);
     t.pos = seq_lens;

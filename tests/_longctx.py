@@ -41,13 +41,15 @@ class Cache:
         kp, vp = torch.full(shape, float("nan"), dtype=tdt), torch.full(shape, float("nan"), dtype=tdt)
         # visible(b): the slots of sequence b that hold values (default: all)
         for b in range(self.B):
-            ts = range(int(self.lens[b])) if visible is None else visible(b)
-            for t in ts:
-                pg = self.table[b, t // page]
-                if shared and t < shared * page and not torch.isnan(kp[0, pg, 0, t % page, 0]):
-                    continue
-                kp[:, pg, :, t % page] = torch.from_numpy(rng.standard_normal((k, Hkv, d))).to(tdt)
-                vp[:, pg, :, t % page] = torch.from_numpy(rng.standard_normal((k, Hkv, d))).to(tdt)
+            ts = np.asarray(list(range(int(self.lens[b])) if visible is None else visible(b)), dtype=np.int64)
+            if shared and len(ts):  # slots of the shared pages are written once
+                first = torch.from_numpy(self.table[b, ts // page].astype(np.int64)), torch.from_numpy(ts % page)
+                ts = ts[torch.isnan(kp[0, first[0], 0, first[1], 0]).numpy()]
+            at = torch.from_numpy(self.table[b, ts // page].astype(np.int64)), torch.from_numpy(ts % page)
+            for pool in (kp, vp):
+                for ch in range(k):
+                    rows = rng.standard_normal((len(ts), Hkv, d), dtype=np.float32)
+                    pool[ch].transpose(1, 2)[at[0], at[1]] = torch.from_numpy(rows).to(tdt)
         self.kp, self.vp, self.T = kp, vp, T
         self.kd, self.vd = kp.double().numpy(), vp.double().numpy()
 

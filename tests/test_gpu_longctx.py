@@ -308,6 +308,31 @@ def test_prefix_of_nothing_and_of_everything(shared):
             check_rows(c, got[b, hq], want, ds, vmax)
 
 
+# Prefixes large enough for the tensor-core kernel (over 40 MB of K/V times
+# groups of 8 rows): more and fewer than 128 rows per kv head, several row
+# blocks, sequences that end inside the prefix, a page that does not exist.
+@pytest.mark.parametrize("B,G,Hkv,d,page,shared,drop", [
+    (64, 8, 1, 64, 16, 210, None), (37, 4, 2, 96, 8, 401, 100), (100, 1, 4, 64, 64, 53, None),
+    (75, 4, 1, 128, 256, 10, None), (4, 2, 4, 128, 64, 330, 7), (9, 8, 2, 96, 128, 50, None)])
+def test_prefix_on_the_tensor_cores(B, G, Hkv, d, page, shared, drop):
+    base = shared * page
+    lens = [base + (7 * b) % 29 for b in range(B)]
+    lens[1], lens[B // 2], lens[B - 1] = base // 2 + 3, 5, 0  # (sequence 0 holds the whole prefix)
+    assert base * Hkv * d * 4 * -(-B * G // 8) > 40 << 20
+    c = Cache(lens, Hkv=Hkv, G=G, d=d, page=page, shared=shared, k=1, seed=B)
+    good = c.table.copy()
+    if drop is not None:
+        c.table[:, drop] = c.num_pages
+    s, q, got = run_prefix(c, shared)
+    assert s.read_status() == (0 if drop is None else W.WM_ERR_BOUNDS)
+    c.table = good
+    for b in sorted({0, 1, 2, B // 2, B - 1, B - 2, B // 3}):
+        ts = [t for t in range(lens[b]) if drop is None or t // page != drop]
+        for hq in {0, G - 1, c.Hq - 1}:
+            want, _, ds, vmax = c.attend(0, b, hq, q[b, hq], ts)
+            check_rows(c, got[b, hq], want, ds, vmax)
+
+
 def test_prefix_peaked_queries():
     c = Cache([500, 433, 401], Hkv=2, G=2, d=128, page=16, shared=25, k=1, seed=12)
     s, q, got = run_prefix(c, 25, scale=20.0)
