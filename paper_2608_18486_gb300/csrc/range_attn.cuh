@@ -19,7 +19,15 @@
 //    probabilities), K and V read from shared memory with ldmatrix (chunks
 //    of 16 bytes XOR-swizzled by the slot, so that no read conflicts); the
 //    cost does not grow with the query heads of a kv head.
-//  * fp32: CUDA-core FMAs, 8 lanes per slot, queries in shared memory.
+//  * fp32, up to 4 rows: CUDA-core FMAs, 8 lanes per slot, queries in shared
+//    memory.
+//  * fp32, 8 rows: the bf16 products on operands split into three bf16 parts (8
+//    bits of the 24 each): x = h + m + l, and q k = (qh + qm)(kh + km + kl) +
+//    ql kh up to 2^-23 of |q||k|.  h and m of the query rows fill the 16 rows of
+//    one operand, so four matrix instructions do what one does for bf16; the
+//    splitting of K and V bounds it (about 4.4 TB/s whatever the rows).  us per
+//    call over 1028 slots of 32 sequences, 32 query heads of 128 (FMAs / split): 1
+//    row per unit 159 / 229, 2 rows 87 / 123, 4 rows 56 / 63, 8 rows 64 / 40.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -47,11 +55,12 @@ struct Shape {
   static_assert(CHUNKS % 32 == 0, "whole warp copies");
 };
 
-// Place of 16-byte chunk c of slot row `slot`: any 8 consecutive slots have a
-// given chunk on 8 different 16-byte bank groups.
+// Place of 16-byte chunk c of slot row `slot`.  bf16: any 8 consecutive slots have
+// a given chunk on 8 different 16-byte bank groups (ldmatrix).  fp32: so have
+// two neighbouring slots with 4 chunks each, and 4 slots two apart with 2.
 template <typename T, int HD>
 __device__ __forceinline__ int swz(int slot, int c) {
-  if (sizeof(T) == 4) return c;
+  if (sizeof(T) == 4) return c ^ (slot & 6) ^ ((slot & 1) << 2);
   if (HD == 96) return c ^ ((slot >> 1) & 3);  // rows of 192 bytes alternate halves already
   return c ^ (slot & 7);
 }
@@ -228,7 +237,148 @@ struct MmaMath {
   }
 };
 
-// ------------------------------------------------------------ fp32: FMAs
+// ------------------------------------------------------------ fp32: three bf16 parts
+// x0 and x1 as packed pairs of parts: h rounded, m the next 8 bits, l the rest.
+struct Split {
+  uint32_t h, m, l;
+};
+__device__ __forceinline__ Split split2(float x0, float x1) {
+  const uint32_t a = __float_as_uint(x0) + 0x8000u, b = __float_as_uint(x1) + 0x8000u;
+  const float r0 = x0 - __uint_as_float(a & 0xFFFF0000u), r1 = x1 - __uint_as_float(b & 0xFFFF0000u);
+  const uint32_t c = __float_as_uint(r0), d = __float_as_uint(r1);
+  const float l0 = r0 - __uint_as_float(c & 0xFFFF0000u), l1 = r1 - __uint_as_float(d & 0xFFFF0000u);
+  Split s;
+  s.h = __byte_perm(a, b, 0x7632);
+  s.m = __byte_perm(c, d, 0x7632);
+  s.l = __byte_perm(__float_as_uint(l0), __float_as_uint(l1), 0x7632);
+  return s;
+}
+__device__ __forceinline__ void mma_k8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5}, {%6}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(b));
+}
+__device__ __forceinline__ float4 lds128(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+template <int HD>
+struct SplitMath {
+  using T = float;
+  using SH = Shape<T, HD>;
+  static constexpr int SS = SH::SS, NT = SS / 8;
+  Split q0[HD / 16], q1[HD / 16];  // row lane / 4, features 16 j + 4 (lane % 4) + {0, 1} and {2, 3}
+  float acc[HD / 8][4];            // tile 4 u + t: features 4 (2 (lane % 4) + {0, 1} + 8 u) + t, from h and
+                                   // from m of the probabilities
+  float m, l;
+  int lim;
+
+  __device__ __forceinline__ void init(const T* qrow, int lane, int lim_) {
+    const int c = lane & 3;
+#pragma unroll
+    for (int j = 0; j < HD / 16; ++j) {
+      const float4 x = qrow ? __ldcg(reinterpret_cast<const float4*>(qrow + 16 * j + 4 * c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      q0[j] = split2(x.x, x.y);
+      q1[j] = split2(x.z, x.w);
+    }
+#pragma unroll
+    for (int j = 0; j < HD / 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+    lim = lim_;
+  }
+
+  template <bool SCORES>
+  __device__ __forceinline__ void stage(uint32_t ks, uint32_t vs, int lane, int t0, uint32_t live, float qscale,
+                                        float* srow) {
+    const int c = lane & 3, n = lane >> 2;
+    float s[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float z[4] = {0.f, 0.f, 0.f, 0.f};
+      const int slot = nt * 8 + n;
+#pragma unroll
+      for (int j = 0; j < HD / 16; ++j) {
+        const float4 k = lds128(ks + slot * SH::ROW_BYTES + swz<T, HD>(slot, c + 4 * j) * 16);
+        const Split b0 = split2(k.x, k.y), b1 = split2(k.z, k.w);
+        mma_rows16(z, q0[j].h, q0[j].m, q1[j].h, q1[j].m, b0.l, b1.l);
+        mma_rows16(z, q0[j].l, 0u, q1[j].l, 0u, b0.h, b1.h);
+        mma_rows16(z, q0[j].h, q0[j].m, q1[j].h, q1[j].m, b0.m, b1.m);
+        mma_rows16(z, q0[j].h, q0[j].m, q1[j].h, q1[j].m, b0.h, b1.h);
+      }
+      s[nt][0] = z[0] + z[2];
+      s[nt][1] = z[1] + z[3];
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int slot = nt * 8 + 2 * c + i;
+        const bool see = ((live >> slot) & 1u) && t0 + slot < lim;
+        s[nt][i] = see ? s[nt][i] * qscale : -INFINITY;
+        mx = fmaxf(mx, s[nt][i]);
+        if (SCORES && srow && t0 + slot < lim) srow[t0 + slot] = s[nt][i];
+      }
+    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 2));
+    const float mnew = fmaxf(m, mx);
+    if (__any_sync(0xFFFFFFFFu, mnew > m)) {
+      const float corr = m == -INFINITY ? 0.f : exp2f(m - mnew);
+      l *= corr;
+#pragma unroll
+      for (int j = 0; j < HD / 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] *= corr;
+      m = mnew;
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float p0 = s[nt][0] == -INFINITY ? 0.f : exp2f(s[nt][0] - m);
+      const float p1 = s[nt][1] == -INFINITY ? 0.f : exp2f(s[nt][1] - m);
+      l += p0 + p1;
+      const Split p = split2(p0, p1);
+      const int slot = nt * 8 + 2 * c;
+#pragma unroll
+      for (int u = 0; u < HD / 32; ++u) {
+        const float4 x = lds128(vs + slot * SH::ROW_BYTES + swz<T, HD>(slot, n + 8 * u) * 16);
+        const float4 y = lds128(vs + (slot + 1) * SH::ROW_BYTES + swz<T, HD>(slot + 1, n + 8 * u) * 16);
+        const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const Split b = split2(xs[t], ys[t]);
+          mma_k8(acc[4 * u + t], p.h, p.m, b.l);
+          mma_k8(acc[4 * u + t], p.l, 0u, b.h);
+          mma_k8(acc[4 * u + t], p.h, p.m, b.m);
+          mma_k8(acc[4 * u + t], p.h, p.m, b.h);
+        }
+      }
+    }
+  }
+
+  __device__ __forceinline__ void store(float* rec, int rows, int lane) {
+    l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
+    l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
+    const int r = lane >> 2, c = lane & 3;
+    if (r >= rows) return;
+#pragma unroll
+    for (int u = 0; u < HD / 32; ++u)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        *reinterpret_cast<float4*>(rec + r * HD + 4 * (2 * c + i + 8 * u)) =
+            make_float4(acc[4 * u][i] + acc[4 * u][2 + i], acc[4 * u + 1][i] + acc[4 * u + 1][2 + i],
+                        acc[4 * u + 2][i] + acc[4 * u + 2][2 + i], acc[4 * u + 3][i] + acc[4 * u + 3][2 + i]);
+    if (c == 0) {
+      rec[rows * HD + 2 * r] = m;
+      rec[rows * HD + 2 * r + 1] = l;
+    }
+  }
+};
+
+// ------------------------------------------------------------ fp32, up to 4 rows: FMAs
 template <int HD, int NR>
 struct FmaMath {
   using T = float;
@@ -257,7 +407,7 @@ struct FmaMath {
       const int slot = it * 4 + (lane >> 3);
       float4 k[NV];
 #pragma unroll
-      for (int v = 0; v < NV; ++v) k[v] = *reinterpret_cast<const float4*>(ks + slot * HD + (v * 8 + lp) * 4);
+      for (int v = 0; v < NV; ++v) k[v] = *reinterpret_cast<const float4*>(ks + slot * HD + swz<T, HD>(slot, v * 8 + lp) * 4);
       float s[NR];
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
@@ -277,7 +427,7 @@ struct FmaMath {
       }
       float4 w[NV];
 #pragma unroll
-      for (int v = 0; v < NV; ++v) w[v] = *reinterpret_cast<const float4*>(vs + slot * HD + (v * 8 + lp) * 4);
+      for (int v = 0; v < NV; ++v) w[v] = *reinterpret_cast<const float4*>(vs + slot * HD + swz<T, HD>(slot, v * 8 + lp) * 4);
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
         if (s[r] == -INFINITY) continue;
@@ -332,13 +482,27 @@ struct FmaMath {
   }
 };
 
-// NR: rows per unit (fp32: the register tile; bf16: 8 rows in any case)
+// The math of NR rows per unit.
+template <typename T, int HD, int NR>
+struct MathOf {
+  using type = FmaMath<HD, NR>;
+};
+template <int HD, int NR>
+struct MathOf<__nv_bfloat16, HD, NR> {
+  using type = MmaMath<HD>;
+};
+template <int HD>
+struct MathOf<float, HD, kRangeRows> {
+  using type = SplitMath<HD>;
+};
+
+// NR: rows per unit (bf16: 8 in any case, of which p.rows are used)
 template <typename T, int HD, int NR, bool SCORES>
 __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(const RangeParams p) {
   using SH = Shape<T, HD>;
   constexpr int SS = SH::SS, ROWV = SH::ROWV, VEC = SH::VEC;
   constexpr unsigned FULL = 0xFFFFFFFFu;
-  constexpr bool MMA = sizeof(T) == 2;
+  constexpr bool FMA = sizeof(T) == 4 && NR < kRangeRows;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ uint32_t live_s[kRangeWarps][kStages];
   __shared__ int lims[kRangeRows];
@@ -440,14 +604,9 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
 
   // ---- queries and per-row limits
   const T* qbase = reinterpret_cast<const T*>(p.q);
-  float* qs = crec + range_rec(kRangeRows, HD);  // fp32: [NR][HD]
-  MmaMath<HD> mm;
-  FmaMath<HD, MMA ? 1 : NR> fm;
-  if constexpr (MMA) {
-    int b, g;
-    const bool in = row_of(lane >> 2, b, g);
-    mm.init(in ? qbase + ((int64_t)b * p.Hq + h * p.G + g) * HD : nullptr, lane, in ? length(b, bad) : 0);
-  } else {
+  typename MathOf<T, HD, NR>::type mm;
+  float* qs = crec + range_rec(kRangeRows, HD);  // FMA: queries [NR][HD]
+  if constexpr (FMA) {
     for (int e = tid; e < NR * HD; e += kThreads) {
       int b, g;
       const bool in = row_of(e / HD, b, g);
@@ -458,7 +617,11 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
       lims[tid] = row_of(tid, b, g) ? length(b, bad) : 0;
     }
     __syncthreads();
-    fm.init();
+    mm.init();
+  } else {
+    int b, g;
+    const bool in = row_of(lane >> 2, b, g);
+    mm.init(in ? qbase + ((int64_t)b * p.Hq + h * p.G + g) * HD : nullptr, lane, in ? length(b, bad) : 0);
   }
 
   // scores: in global memory, or this CTA's slots of them in shared memory
@@ -466,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
   const int jA = (int)((int64_t)piece * kRangeWarps * R.n / npieces);
   const int jB = (int)((int64_t)(piece + 1) * kRangeWarps * R.n / npieces);  // (kRangeScores: R is [0, S))
   const int64_t sstride = own_mass ? p.mass_slots : p.score_stride;
-  float* smass = qs + (MMA ? 0 : kRangeRows * HD);
+  float* smass = qs + (FMA ? NR * HD : 0);
   float* srows = nullptr;
   if (SCORES) srows = own_mass ? smass - jA * SS : p.scores + (int64_t)unit * p.G * p.score_stride;
   for (int i = 0; i < nmine; ++i) {
@@ -475,13 +638,13 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
     unsigned char* st = ring + (i % kStages) * SH::STAGE_BYTES;
     const uint32_t live = live_s[warp][i % kStages];
     const int t0 = first_slot(j0 + i);
-    if constexpr (MMA) {
+    if constexpr (FMA) {
+      mm.template stage<SCORES>(reinterpret_cast<const float*>(st), reinterpret_cast<const float*>(st + SH::HALF_BYTES),
+                                qs, lims, lane, t0, live, p.qscale, srows, sstride);
+    } else {
       const uint32_t ks = smem_u32(st);
       float* srow = SCORES && (lane >> 2) < rows ? srows + (lane >> 2) * sstride : nullptr;
       mm.template stage<SCORES>(ks, ks + SH::HALF_BYTES, lane, t0, live, p.qscale, srow);
-    } else {
-      fm.template stage<SCORES>(reinterpret_cast<const float*>(st), reinterpret_cast<const float*>(st + SH::HALF_BYTES),
-                                qs, lims, lane, t0, live, p.qscale, srows, sstride);
     }
     __syncwarp();  // every lane is done with this ring slot
     const int row = row_next;
@@ -494,8 +657,8 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
 
   // ---- join the CTA's warps (each warp's state in its idle ring)
   float* wrec = reinterpret_cast<float*>(ring);
-  if constexpr (MMA) mm.store(wrec, rows, lane);
-  else fm.store(wrec, lane);
+  if constexpr (FMA) mm.store(wrec, lane);
+  else mm.store(wrec, rows, lane);
   __syncthreads();
   const int E = rows * HD;
   auto warp_rec = [&](int w) -> const float* {
@@ -658,17 +821,17 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
   if (C > 1) cluster.sync();
 }
 
-template <typename T, int HD>
+template <typename T, int HD, int NR>
 constexpr size_t range_smem() {
   return (size_t)kRangeWarps * kStages * Shape<T, HD>::STAGE_BYTES +
-         (range_rec(kRangeRows, HD) + (sizeof(T) == 4 ? kRangeRows * HD : 0)) * sizeof(float);
+         (range_rec(kRangeRows, HD) + (sizeof(T) == 4 && NR < kRangeRows ? NR * HD : 0)) * sizeof(float);
 }
 
 template <typename T, int HD, int NR, bool SCORES>
 inline cudaError_t launch_t(const RangeParams& p, int units, cudaStream_t stream) {
   static size_t smem_set[kSmemOptDevices] = {};
   auto kern = range_attn_kernel<T, HD, NR, SCORES>;
-  const size_t smem = range_smem<T, HD>() + (p.mass ? (size_t)p.G * p.mass_slots * sizeof(float) : 0);
+  const size_t smem = range_smem<T, HD, NR>() + (p.mass ? (size_t)p.G * p.mass_slots * sizeof(float) : 0);
   if (cudaError_t e = opt_in_smem(kern, smem, smem_set); e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)units * (unsigned)p.pieces);
@@ -687,26 +850,19 @@ inline cudaError_t launch_t(const RangeParams& p, int units, cudaStream_t stream
   return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
-template <int HD>
-inline cudaError_t launch_bf16_d(const RangeParams& p, int units, cudaStream_t s) {
-  return p.mode == kRangeScores ? launch_t<__nv_bfloat16, HD, kRangeRows, true>(p, units, s)
-                                : launch_t<__nv_bfloat16, HD, kRangeRows, false>(p, units, s);
+template <typename T, int HD, int NR>
+inline cudaError_t launch_n(const RangeParams& p, int units, cudaStream_t s) {
+  return p.mode == kRangeScores ? launch_t<T, HD, NR, true>(p, units, s) : launch_t<T, HD, NR, false>(p, units, s);
 }
 
-template <int HD, bool SCORES>
-inline cudaError_t launch_f32_n(const RangeParams& p, int units, cudaStream_t s) {
-  switch (p.rows) {
-    case 1: return launch_t<float, HD, 1, SCORES>(p, units, s);
-    case 2: return launch_t<float, HD, 2, SCORES>(p, units, s);
-    case 4: return launch_t<float, HD, 4, SCORES>(p, units, s);
-    case 8: return launch_t<float, HD, 8, SCORES>(p, units, s);
-    default: return cudaErrorInvalidValue;
+template <typename T, int HD>
+inline cudaError_t launch_d(const RangeParams& p, int units, cudaStream_t s) {
+  if constexpr (sizeof(T) == 4) {
+    if (p.rows == 1) return launch_n<T, HD, 1>(p, units, s);
+    if (p.rows == 2) return launch_n<T, HD, 2>(p, units, s);
+    if (p.rows == 4) return launch_n<T, HD, 4>(p, units, s);
   }
-}
-
-template <int HD>
-inline cudaError_t launch_f32_d(const RangeParams& p, int units, cudaStream_t s) {
-  return p.mode == kRangeScores ? launch_f32_n<HD, true>(p, units, s) : launch_f32_n<HD, false>(p, units, s);
+  return launch_n<T, HD, kRangeRows>(p, units, s);
 }
 
 }  // namespace range_detail
