@@ -299,14 +299,19 @@ wm_status wm_prefill_attn(const wm_config* cfg, const wm_cache* cache, int32_t l
 /*
  * Attention over part of the cache, for long contexts (no counterpart in the
  * paper).  All of it reads channel c(layer) as wm_decode_attn does, for both
- * dtypes, every page size and group size, with fp32 softmax and accumulation;
- * bf16 probabilities enter the P V product as bf16.  A sequence may hold no
- * slot at all (length 0): its rows are zeros, and so is any row whose mask
- * leaves nothing.  A negative length, or one past the page table, zero-fills
- * the row and sets WM_ERR_BOUNDS.  So does a bad page id, whose slots are
- * left out.  Page-table entries of pages without a
- * visible slot are not read into anything: the pages may be gone.  Slots that
- * are not visible may hold anything, NaN included.
+ * dtypes, every page size and group size, with softmax and accumulation in
+ * fp32.  bf16: the tensor-core kernels (many rows, long shared prefixes) round
+ * the probabilities to bf16 for the P V product, the others keep 16 bits of
+ * them.  fp32 units of 8 query rows multiply operands split into three bf16
+ * parts (exact to 2^-23 of the products' magnitude); everything else in fp32 is
+ * FMA arithmetic.  A sequence may hold no slot at all (length 0): its rows are
+ * zeros, and so is any row whose mask leaves nothing.  A negative length, or one
+ * past the page table, zero-fills the row and sets WM_ERR_BOUNDS.  So does a
+ * bad page id, whose slots are
+ * left out.  Page-table entries of pages without a visible slot are not read
+ * into anything: the pages may be gone.  Slots that no row of a call sees may
+ * hold anything, NaN included; one that a row of a many-row call sees (or any
+ * sequence behind a shared prefix) must be finite.
  */
 
 /*

@@ -271,8 +271,7 @@ struct SplitMath {
   using SH = Shape<T, HD>;
   static constexpr int SS = SH::SS, NT = SS / 8;
   Split q0[HD / 16], q1[HD / 16];  // row lane / 4, features 16 j + 4 (lane % 4) + {0, 1} and {2, 3}
-  float acc[HD / 8][4];            // tile 4 u + t: features 4 (2 (lane % 4) + {0, 1} + 8 u) + t, from h and
-                                   // from m of the probabilities
+  float acc[HD / 8][2];            // tile 4 u + t: features 4 (2 (lane % 4) + {0, 1} + 8 u) + t
   float m, l;
   int lim;
 
@@ -285,7 +284,7 @@ struct SplitMath {
       q1[j] = split2(x.z, x.w);
     }
 #pragma unroll
-    for (int j = 0; j < HD / 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+    for (int j = 0; j < HD / 8; ++j) acc[j][0] = acc[j][1] = 0.f;
     m = -INFINITY;
     l = 0.f;
     lim = lim_;
@@ -298,19 +297,23 @@ struct SplitMath {
     float s[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float z[4] = {0.f, 0.f, 0.f, 0.f};
       const int slot = nt * 8 + n;
+      s[nt][0] = s[nt][1] = 0.f;
 #pragma unroll
       for (int j = 0; j < HD / 16; ++j) {
+        // A matrix instruction truncates its sums: each group of four starts at
+        // zero, smallest terms first, and is added with rounding (in one chain over
+        // all features and slots the error of a result reached 1e-6).
+        float z[4] = {0.f, 0.f, 0.f, 0.f};
         const float4 k = lds128(ks + slot * SH::ROW_BYTES + swz<T, HD>(slot, c + 4 * j) * 16);
         const Split b0 = split2(k.x, k.y), b1 = split2(k.z, k.w);
         mma_rows16(z, q0[j].h, q0[j].m, q1[j].h, q1[j].m, b0.l, b1.l);
         mma_rows16(z, q0[j].l, 0u, q1[j].l, 0u, b0.h, b1.h);
         mma_rows16(z, q0[j].h, q0[j].m, q1[j].h, q1[j].m, b0.m, b1.m);
         mma_rows16(z, q0[j].h, q0[j].m, q1[j].h, q1[j].m, b0.h, b1.h);
+        s[nt][0] += z[0] + z[2];
+        s[nt][1] += z[1] + z[3];
       }
-      s[nt][0] = z[0] + z[2];
-      s[nt][1] = z[1] + z[3];
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -332,7 +335,7 @@ struct SplitMath {
 #pragma unroll
       for (int j = 0; j < HD / 8; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[j][i] *= corr;
+        for (int i = 0; i < 2; ++i) acc[j][i] *= corr;
       m = mnew;
     }
 #pragma unroll
@@ -350,10 +353,13 @@ struct SplitMath {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const Split b = split2(xs[t], ys[t]);
-          mma_k8(acc[4 * u + t], p.h, p.m, b.l);
-          mma_k8(acc[4 * u + t], p.l, 0u, b.h);
-          mma_k8(acc[4 * u + t], p.h, p.m, b.m);
-          mma_k8(acc[4 * u + t], p.h, p.m, b.h);
+          float z[4] = {0.f, 0.f, 0.f, 0.f};
+          mma_k8(z, p.h, p.m, b.l);
+          mma_k8(z, p.l, 0u, b.h);
+          mma_k8(z, p.h, p.m, b.m);
+          mma_k8(z, p.h, p.m, b.h);
+          acc[4 * u + t][0] += z[0] + z[2];
+          acc[4 * u + t][1] += z[1] + z[3];
         }
       }
     }
@@ -369,8 +375,7 @@ struct SplitMath {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         *reinterpret_cast<float4*>(rec + r * HD + 4 * (2 * c + i + 8 * u)) =
-            make_float4(acc[4 * u][i] + acc[4 * u][2 + i], acc[4 * u + 1][i] + acc[4 * u + 1][2 + i],
-                        acc[4 * u + 2][i] + acc[4 * u + 2][2 + i], acc[4 * u + 3][i] + acc[4 * u + 3][2 + i]);
+            make_float4(acc[4 * u][i], acc[4 * u + 1][i], acc[4 * u + 2][i], acc[4 * u + 3][i]);
     if (c == 0) {
       rec[rows * HD + 2 * r] = m;
       rec[rows * HD + 2 * r + 1] = l;
@@ -517,14 +522,14 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
   unsigned char* ring = smem_raw + warp * kStages * SH::STAGE_BYTES;
   float* crec = reinterpret_cast<float*>(smem_raw + kRangeWarps * kStages * SH::STAGE_BYTES);
 
-  // A suffix runs behind the prefix kernel of the same call, which lets it start
-  // only after its own wait: everything before that call is visible already, and
-  // only the prefix's records have to be waited for, at the end.
-  const bool late = p.records > 0, prefix_pass = p.mode == kRangePrefix;
+  // Dependents start only after this grid's own wait, so that everything before
+  // it is visible to them whatever they wait for.  A suffix runs behind the prefix
+  // kernel of the same call and relies on that: it reads the cache at once and
+  // waits only for the prefix's records, at the end.
+  const bool late = p.records > 0;
   if (!late) {
-    if (!prefix_pass) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (prefix_pass) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   }
 
   // ---- this unit's rows and slots.  Row i is query head h G + g of sequence b.

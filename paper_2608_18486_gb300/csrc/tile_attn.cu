@@ -505,7 +505,14 @@ __global__ void __launch_bounds__(kTThreads, 1)
       if (kq && ok && I.steps <= q_at) load_q();
       ok = __all_sync(FULL, ok);
     }
-    if (!ok && lane == 0) report(p.status, WM_ERR_TIMEOUT);
+    if (!ok && lane == 0) {
+      report(p.status, WM_ERR_TIMEOUT);
+      // the copies still on their way to this CTA's shared memory (bounded)
+      const int depth = kq ? NSK : NSV;
+      for (int x = max(0, n_tile - depth); x < n_tile; ++x)
+        mbar_wait(kq ? &kfull[x % depth] : &vfull[x % depth], (x / depth) & 1);
+      if (kq && no > 0) mbar_wait(&qfull[(no - 1) & 1], ((no - 1) >> 1) & 1);
+    }
   } else if (warp == kFixWarp) {
     // ================================================================ V tiles
     int vs = 0, no = 0;

@@ -125,6 +125,14 @@ class DecodeSession:
             raise W.WMError(rc, "wm_kv_mix")
 
     # ---------------------------------------------------------- long contexts
+    @staticmethod
+    def _packed(*tensors) -> None:
+        # the library takes addresses: a view with gaps or another order of its
+        # dimensions would be read as if it had none
+        for t in tensors:
+            if not t.is_contiguous():
+                raise ValueError("the library reads contiguous tensors only")
+
     def _raw_stream(self, stream) -> int:
         if stream is None:
             return torch._C._cuda_getCurrentRawStream(self.device.index or 0)
@@ -157,6 +165,7 @@ class DecodeSession:
         """Decode attention over the first ``sinks`` slots and the last
         ``window`` slots of each sequence."""
         cfg, cache = self._refs
+        self._packed(q, page_table, seq_lens, out)
         rc = self._lib.wm_window_attn(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
                                       seq_lens.data_ptr(), sinks, window, self.B if B is None else B,
                                       self.max_pages, out.data_ptr(), self._status_ptr,
@@ -170,6 +179,7 @@ class DecodeSession:
         [B][Tq]: position i sees slots t <= i, t < sinks or t > i - window."""
         cfg, cache = self._refs
         B, Tq = q.shape[:2]
+        self._packed(q, pos, page_table, out)
         rc = self._lib.wm_window_prefill_attn(cfg, cache, layer, q.data_ptr(), pos.data_ptr(),
                                               page_table.data_ptr(), sinks, window, B, Tq,
                                               self.max_pages, out.data_ptr(), self._status_ptr,
@@ -183,6 +193,7 @@ class DecodeSession:
         the same ones: those are read once for the batch."""
         cfg, cache = self._refs
         B = self.B if B is None else B
+        self._packed(q, page_table, seq_lens, out)
         need = self._bytes(("prefix", B, shared_pages), W.wm_prefix_attn_workspace, B,
                            self.max_pages, shared_pages)
         raw = self._raw_stream(stream)
@@ -199,6 +210,7 @@ class DecodeSession:
         the query heads of a kv head, to mass [k][B][Hkv][slots] (fp32)."""
         cfg, cache = self._refs
         B = self.B if B is None else B
+        self._packed(q, page_table, seq_lens, mass, out)
         need = self._bytes(("mass", B), W.wm_decode_attn_mass_workspace, B, self.max_pages)
         raw = self._raw_stream(stream)
         rc = self._lib.wm_decode_attn_mass(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
@@ -214,6 +226,7 @@ class DecodeSession:
         first ``sinks``, the last ``recent`` and those with the largest mass.
         Writes mass_out (may be mass), kept [k][B][Hkv][budget] and new_lens."""
         cfg, cache = self._refs
+        self._packed(mass, page_table, seq_lens, mass_out, kept, new_lens)
         rc = self._lib.wm_cache_evict(cfg, cache, mass.data_ptr(), mass_out.data_ptr(),
                                       page_table.data_ptr(), seq_lens.data_ptr(), budget, sinks,
                                       recent, self.B if B is None else B, self.max_pages,

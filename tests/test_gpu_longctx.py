@@ -617,3 +617,20 @@ def test_pool_at_given_positions(name, B):
     pg = int(prob.page_table[1, 37 // w.page])
     assert np.array_equal(to_f64(s.k_pool[w.k - 1, pg, :, 37 % w.page]), k2)
     assert s.read_status() == 0
+
+
+def test_views_with_gaps_are_refused():
+    c = Cache([40, 20], Hkv=2, G=2, d=64, page=16, k=1, seed=1)
+    s = c.session()
+    table, lens = c.dev()
+    wide = torch.zeros((2, 4, 128), dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros((2, 4, 64), dtype=torch.bfloat16, device="cuda")
+    mass = torch.zeros((1, 2, 2, c.T), device="cuda")
+    for call in (lambda: s.window_attn(0, wide[..., :64], table, lens, out, sinks=1, window=4),
+                 lambda: s.window_attn(0, out, table, lens, wide[..., ::2], sinks=1, window=4),
+                 lambda: s.prefix_attn(0, wide[..., :64], table, lens, out, shared_pages=0),
+                 lambda: s.window_prefill_attn(0, wide[:, None, :, :64], lens[:, None], table, out, sinks=1, window=4),
+                 lambda: s.decode_attn_mass(0, out, table, lens, mass[..., ::2], out),
+                 lambda: s.evict(mass, table.t(), lens, mass, table, lens, budget=8, sinks=1, recent=1)):
+        with pytest.raises(ValueError):
+            call()
