@@ -32,21 +32,21 @@ namespace {
 // 16-byte access.
 constexpr int kMassThreads = 256;
 constexpr int kMassSlots = kMassThreads * 16;  // per CTA
-template <typename T, int HD>
-__global__ void __launch_bounds__(kMassThreads) mass_add_kernel(const MassParams p) {
+template <typename T, int HD, int G>
+__global__ void __launch_bounds__(kMassThreads, G <= 2 ? 8 : 4) mass_add_kernel(const MassParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __shared__ float m_s[kRangeRows], inv_s[kRangeRows], w_s[kRangeRows][kMassMaxPieces];
   const int unit = blockIdx.x, b = unit / p.Hkv, h = unit - b * p.Hkv;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int recf = range_rec(p.G, HD);
+  const int recf = range_rec(G, HD);
   const float* part = p.part + (int64_t)unit * p.pieces * recf;
   const int S_in = __ldg(p.seq_lens + b);
   const int S = S_in >= 0 && S_in <= p.max_slots ? S_in : 0;
   const int t0 = ((int)blockIdx.y - 1) * kMassSlots;
   if (t0 >= S) return;
-  if (warp < p.G) {  // 8 warps: one per query head
-    const float* ml = part + p.G * HD + 2 * warp;
+  if (warp < G) {  // 8 warps: one per query head
+    const float* ml = part + G * HD + 2 * warp;
     float M = -INFINITY, L = 0.f;
     for (int i = lane; i < p.pieces; i += 32) M = fmaxf(M, __ldcg(ml + (int64_t)i * recf));
 #pragma unroll
@@ -65,22 +65,35 @@ __global__ void __launch_bounds__(kMassThreads) mass_add_kernel(const MassParams
   }
   __syncthreads();
   if (blockIdx.y == 0) {
-    T* out = reinterpret_cast<T*>(p.out) + ((int64_t)b * p.Hq + h * p.G) * HD;
-    for (int e = tid; e < p.G * HD; e += kMassThreads) {
-      float O = 0.f;
-      for (int i0 = 0; i0 < p.pieces; i0 += 8) {
-        float v[8];
+    T* out = reinterpret_cast<T*>(p.out) + ((int64_t)b * p.Hq + h * G) * HD;
+    for (int q = tid; q < G * HD / 4; q += kMassThreads) {  // four outputs, NB records in flight
+      const int r = q / (HD / 4);
+      constexpr int NB = G <= 2 ? 4 : 10;
+      float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i0 = 0; i0 < p.pieces; i0 += NB) {
+        float4 v[NB];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i0 + i < p.pieces ? __ldcg(part + (int64_t)(i0 + i) * recf + e) : 0.f;
+        for (int i = 0; i < NB; ++i)
+          if (i0 + i < p.pieces) v[i] = __ldcg(reinterpret_cast<const float4*>(part + (int64_t)(i0 + i) * recf) + q);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i0 + i < p.pieces) O = fmaf(w_s[e / HD][i0 + i], v[i], O);
+        for (int i = 0; i < NB; ++i) {
+          if (i0 + i >= p.pieces) continue;
+          const float w = w_s[r][i0 + i];
+          O.x = fmaf(w, v[i].x, O.x);
+          O.y = fmaf(w, v[i].y, O.y);
+          O.z = fmaf(w, v[i].z, O.z);
+          O.w = fmaf(w, v[i].w, O.w);
+        }
       }
-      out[e] = Elem<T>::from_f(O * inv_s[e / HD]);
+      const float inv = inv_s[r];
+      out[4 * q] = Elem<T>::from_f(O.x * inv);
+      out[4 * q + 1] = Elem<T>::from_f(O.y * inv);
+      out[4 * q + 2] = Elem<T>::from_f(O.z * inv);
+      out[4 * q + 3] = Elem<T>::from_f(O.w * inv);
     }
     return;
   }
-  const float* sc = p.scores + (int64_t)unit * p.G * p.score_stride;
+  const float* sc = p.scores + (int64_t)unit * G * p.score_stride;
   float* mass = p.mass + (int64_t)unit * p.max_slots;
   auto weight = [&](float s, int g, float w) { return s == -INFINITY ? w : fmaf(exp2f(s - m_s[g]), inv_s[g], w); };
   const int64_t step = (int64_t)(gridDim.y - 1) * kMassSlots;
@@ -89,15 +102,18 @@ __global__ void __launch_bounds__(kMassThreads) mass_add_kernel(const MassParams
     if (p.vec4) {
       for (int t = (int)base + tid * 4; t < t1; t += kMassThreads * 4) {
         float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int g = 0; g < p.G; ++g) {  // (scores past S are not weights: not added below)
-          const float4 s = __ldcg(reinterpret_cast<const float4*>(sc + (int64_t)g * p.score_stride + t));
-          w.x = weight(s.x, g, w.x);
-          w.y = weight(s.y, g, w.y);
-          w.z = weight(s.z, g, w.z);
-          w.w = weight(s.w, g, w.w);
-        }
         float4* at = reinterpret_cast<float4*>(mass + t);
-        float4 a = *at;
+        float4 a = *at, s[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g)  // (scores past S are not weights: not added below)
+          s[g] = __ldcg(reinterpret_cast<const float4*>(sc + (int64_t)g * p.score_stride + t));
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          w.x = weight(s[g].x, g, w.x);
+          w.y = weight(s[g].y, g, w.y);
+          w.z = weight(s[g].z, g, w.z);
+          w.w = weight(s[g].w, g, w.w);
+        }
         a.x += w.x;
         if (t + 1 < S) a.y += w.y;
         if (t + 2 < S) a.z += w.z;
@@ -107,7 +123,7 @@ __global__ void __launch_bounds__(kMassThreads) mass_add_kernel(const MassParams
     } else {
       for (int t = (int)base + tid; t < t1; t += kMassThreads) {
         float w = 0.f;
-        for (int g = 0; g < p.G; ++g) w = weight(__ldcg(sc + (int64_t)g * p.score_stride + t), g, w);
+        for (int g = 0; g < G; ++g) w = weight(__ldcg(sc + (int64_t)g * p.score_stride + t), g, w);
         mass[t] += w;
       }
     }
@@ -128,6 +144,17 @@ cudaError_t launch_chained(Kern kern, const P& p, dim3 grid, int threads, cudaSt
   return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
+template <typename T, int HD>
+cudaError_t launch_mass_g(const MassParams& p, dim3 grid, cudaStream_t s) {
+  switch (p.G) {
+    case 1: return launch_chained(mass_add_kernel<T, HD, 1>, p, grid, kMassThreads, s);
+    case 2: return launch_chained(mass_add_kernel<T, HD, 2>, p, grid, kMassThreads, s);
+    case 4: return launch_chained(mass_add_kernel<T, HD, 4>, p, grid, kMassThreads, s);
+    case 8: return launch_chained(mass_add_kernel<T, HD, 8>, p, grid, kMassThreads, s);
+    default: return cudaErrorInvalidValue;
+  }
+}
+
 }  // namespace
 
 cudaError_t launch_mass_add(MassParams p, int dtype, int d, cudaStream_t s) {
@@ -135,15 +162,14 @@ cudaError_t launch_mass_add(MassParams p, int dtype, int d, cudaStream_t s) {
   p.vec4 = p.max_slots % 4 == 0 && ((uintptr_t)p.mass & 15) == 0 ? 1 : 0;
   const int parts = (p.max_slots + kMassSlots - 1) / kMassSlots;
   const dim3 grid((unsigned)(p.B * p.Hkv), (unsigned)(1 + (parts < 65534 ? parts : 65534)));
-  const int n = kMassThreads;
   if (dtype == WM_DT_F32) {
-    if (d == 64) return launch_chained(mass_add_kernel<float, 64>, p, grid, n, s);
-    if (d == 96) return launch_chained(mass_add_kernel<float, 96>, p, grid, n, s);
-    return launch_chained(mass_add_kernel<float, 128>, p, grid, n, s);
+    if (d == 64) return launch_mass_g<float, 64>(p, grid, s);
+    if (d == 96) return launch_mass_g<float, 96>(p, grid, s);
+    return launch_mass_g<float, 128>(p, grid, s);
   }
-  if (d == 64) return launch_chained(mass_add_kernel<__nv_bfloat16, 64>, p, grid, n, s);
-  if (d == 96) return launch_chained(mass_add_kernel<__nv_bfloat16, 96>, p, grid, n, s);
-  return launch_chained(mass_add_kernel<__nv_bfloat16, 128>, p, grid, n, s);
+  if (d == 64) return launch_mass_g<__nv_bfloat16, 64>(p, grid, s);
+  if (d == 96) return launch_mass_g<__nv_bfloat16, 96>(p, grid, s);
+  return launch_mass_g<__nv_bfloat16, 128>(p, grid, s);
 }
 
 }  // namespace wm

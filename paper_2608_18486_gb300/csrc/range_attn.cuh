@@ -108,6 +108,12 @@ __device__ __forceinline__ void mma_rows16(float (&c)[4], uint32_t a0, uint32_t 
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// Two neighbouring scores of a row (t even) that has `lim` slots.
+__device__ __forceinline__ void put_scores(float* row, int t, int lim, float a, float b) {
+  if (t + 1 < lim) *reinterpret_cast<float2*>(row + t) = make_float2(a, b);
+  else if (t < lim) row[t] = a;
+}
+
 // The visible slots of a unit: [0, a) and [w0, S), as stages of SS slots.
 struct Range {
   int S, a, w0, n0, f, n;  // n0 stages of the first part, then from stage f on; n in all
@@ -180,8 +186,10 @@ struct MmaMath {
         const bool see = ((live >> slot) & 1u) && t0 + slot < lim;
         s[nt][i] = see ? s[nt][i] * qscale : -INFINITY;
         mx = fmaxf(mx, s[nt][i]);
-        if (SCORES && srow && t0 + slot < lim) srow[t0 + slot] = s[nt][i];
       }
+    if (SCORES && srow)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) put_scores(srow, t0 + nt * 8 + 2 * c, lim, s[nt][0], s[nt][1]);
     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 1));
     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 2));
     const float mnew = fmaxf(m, mx);
@@ -324,8 +332,10 @@ struct SplitMath {
         const bool see = ((live >> slot) & 1u) && t0 + slot < lim;
         s[nt][i] = see ? s[nt][i] * qscale : -INFINITY;
         mx = fmaxf(mx, s[nt][i]);
-        if (SCORES && srow && t0 + slot < lim) srow[t0 + slot] = s[nt][i];
       }
+    if (SCORES && srow)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) put_scores(srow, t0 + nt * 8 + 2 * c, lim, s[nt][0], s[nt][1]);
     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 1));
     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 2));
     const float mnew = fmaxf(m, mx);

@@ -56,8 +56,8 @@ struct RangeParams {
 // to 32 bytes
 constexpr int tile_rec(int d) { return d + 8; }
 // floats of one partial record: rows x d unnormalised outputs, then (max, sum)
-// per row in log2 units
-constexpr int range_rec(int rows, int d) { return rows * (d + 2); }
+// per row in log2 units, padded to 16 bytes
+constexpr int range_rec(int rows, int d) { return rows * d + (2 * rows + 3) / 4 * 4; }
 
 // Slots of one pipeline stage (the grain the planner splits by).
 int range_stage_slots(int dtype, int d);

@@ -96,5 +96,7 @@ def test_workspace_queries():
     assert W.wm_decode_attn_mass_workspace(c, 2, 0) == 0 and W.wm_decode_attn_mass_workspace(c, -1, 4) == 0
     for b in (1, 3, 64):
         assert W.wm_prefix_attn_workspace(c, b, 40, 7) % 256 == 0
-        # a score per query head and slot, and at least one record per unit
-        assert W.wm_decode_attn_mass_workspace(c, b, 40) >= 4 * b * (c.Hq * 40 * c.page_size + c.Hkv * (c.d + 2))
+        # short contexts keep their scores on chip
+        assert W.wm_decode_attn_mass_workspace(c, b, 40) % 256 == 0 < W.wm_decode_attn_mass_workspace(c, b, 40)
+        # long ones: a score per query head and slot, and at least one record per unit
+        assert W.wm_decode_attn_mass_workspace(c, b, 8192) >= 4 * b * (c.Hq * 8192 * c.page_size + c.Hkv * (c.d + 2))
