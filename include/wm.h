@@ -306,12 +306,11 @@ wm_status wm_prefill_attn(const wm_config* cfg, const wm_cache* cache, int32_t l
  * parts (exact to 2^-23 of the products' magnitude); everything else in fp32 is
  * FMA arithmetic.  A sequence may hold no slot at all (length 0): its rows are
  * zeros, and so is any row whose mask leaves nothing.  A negative length, or one
- * past the page table, zero-fills the row and sets WM_ERR_BOUNDS.  So does a
- * bad page id, whose slots are
- * left out.  Page-table entries of pages without a visible slot are not read
- * into anything: the pages may be gone.  Slots that no row of a call sees may
- * hold anything, NaN included; one that a row of a many-row call sees (or any
- * sequence behind a shared prefix) must be finite.
+ * past the page table, zero-fills the row and sets WM_ERR_BOUNDS; a bad page id
+ * sets it too, and its slots are left out.  Page-table entries of pages without
+ * a visible slot are not read into anything: the pages may be gone.  Slots that
+ * no row of a call sees may hold anything, NaN included; one that a row of a
+ * many-row call sees (or any sequence behind a shared prefix) must be finite.
  */
 
 /*

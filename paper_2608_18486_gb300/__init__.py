@@ -5,6 +5,8 @@
 computation of the path runs in the CUDA kernels of libwm.so.
 """
 from . import _lib  # noqa: F401
-from ._lib import (WMError, make_config, wm_cache_alloc, wm_cache_bytes, wm_config_check,  # noqa: F401
-                   wm_decode_attn, wm_decode_attn_workspace, wm_kv_mix, wm_kv_mix_workspace,
-                   wm_status_string)
+from ._lib import (WMError, make_config, wm_cache_alloc, wm_cache_bytes, wm_cache_evict,  # noqa: F401
+                   wm_config_check, wm_decode_attn, wm_decode_attn_mass,
+                   wm_decode_attn_mass_workspace, wm_decode_attn_workspace, wm_kv_mix, wm_kv_mix_at,
+                   wm_kv_mix_workspace, wm_prefix_attn, wm_prefix_attn_workspace, wm_status_string,
+                   wm_window_attn, wm_window_prefill_attn)

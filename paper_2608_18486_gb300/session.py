@@ -58,12 +58,9 @@ class DecodeSession:
         self._weights = None
         self._weight_refs = None
         self._scratch = {}   # per stream
+        self._outgrown = []  # scratch replaced by larger: graphs captured before may use it
         self._need = {}      # workspace bytes by call and shape
-        # argument-independent parts of the long-context calls, made once: a
-        # small launch takes about as long on the GPU as its call on the host
-        self._refs = (ctypes.byref(self.cfg), ctypes.byref(self.cache))
         self._lib = W.lib()
-        self._status_ptr = self.status.data_ptr()
 
     # ------------------------------------------------------------------ setup
     def set_weights(self, pre_g, Wr, br, ch_g, Wkv, qk_g) -> None:
@@ -142,9 +139,12 @@ class DecodeSession:
         # one buffer per stream for the calls below (they need nothing in it,
         # so calls on one stream share it), kept at the largest size asked for
         # and allocated on that stream.  The first call of a size may allocate:
-        # make it before a graph capture.
+        # make it before a graph capture.  Graphs captured on one stream share
+        # its buffer: their replays must not overlap.
         buf = self._scratch.get(raw)
         if buf is None or buf.numel() < nbytes:
+            if buf is not None:
+                self._outgrown.append(buf)
             s = torch.cuda.current_stream(self.device) if stream is None else stream
             with torch.cuda.stream(s):
                 buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
@@ -164,11 +164,11 @@ class DecodeSession:
                     B: int | None = None, stream=None) -> None:
         """Decode attention over the first ``sinks`` slots and the last
         ``window`` slots of each sequence."""
-        cfg, cache = self._refs
+        cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         self._packed(q, page_table, seq_lens, out)
         rc = self._lib.wm_window_attn(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
                                       seq_lens.data_ptr(), sinks, window, self.B if B is None else B,
-                                      self.max_pages, out.data_ptr(), self._status_ptr,
+                                      self.max_pages, out.data_ptr(), self.status.data_ptr(),
                                       self._raw_stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_window_attn")
@@ -177,12 +177,12 @@ class DecodeSession:
                             stream=None) -> None:
         """window_attn's mask for query rows q [B][Tq][Hq][d] at positions pos
         [B][Tq]: position i sees slots t <= i, t < sinks or t > i - window."""
-        cfg, cache = self._refs
+        cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         B, Tq = q.shape[:2]
         self._packed(q, pos, page_table, out)
         rc = self._lib.wm_window_prefill_attn(cfg, cache, layer, q.data_ptr(), pos.data_ptr(),
                                               page_table.data_ptr(), sinks, window, B, Tq,
-                                              self.max_pages, out.data_ptr(), self._status_ptr,
+                                              self.max_pages, out.data_ptr(), self.status.data_ptr(),
                                               self._raw_stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_window_prefill_attn")
@@ -191,16 +191,16 @@ class DecodeSession:
                     B: int | None = None, stream=None) -> None:
         """Decode attention of sequences whose first ``shared_pages`` pages are
         the same ones: those are read once for the batch."""
-        cfg, cache = self._refs
+        cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         B = self.B if B is None else B
         self._packed(q, page_table, seq_lens, out)
-        need = self._bytes(("prefix", B, shared_pages), W.wm_prefix_attn_workspace, B,
+        need = self._bytes(("prefix", B, self.max_pages, shared_pages), W.wm_prefix_attn_workspace, B,
                            self.max_pages, shared_pages)
         raw = self._raw_stream(stream)
         rc = self._lib.wm_prefix_attn(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
                                       seq_lens.data_ptr(), shared_pages, B, self.max_pages,
                                       out.data_ptr(), self._scratch_for(need, raw, stream), need,
-                                      self._status_ptr, raw)
+                                      self.status.data_ptr(), raw)
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_prefix_attn")
 
@@ -208,15 +208,15 @@ class DecodeSession:
                          B: int | None = None, stream=None) -> None:
         """Decode attention that adds every slot's softmax weight, summed over
         the query heads of a kv head, to mass [k][B][Hkv][slots] (fp32)."""
-        cfg, cache = self._refs
+        cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         B = self.B if B is None else B
         self._packed(q, page_table, seq_lens, mass, out)
-        need = self._bytes(("mass", B), W.wm_decode_attn_mass_workspace, B, self.max_pages)
+        need = self._bytes(("mass", B, self.max_pages), W.wm_decode_attn_mass_workspace, B, self.max_pages)
         raw = self._raw_stream(stream)
         rc = self._lib.wm_decode_attn_mass(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
                                            seq_lens.data_ptr(), mass.data_ptr(), B, self.max_pages,
                                            out.data_ptr(), self._scratch_for(need, raw, stream),
-                                           need, self._status_ptr, raw)
+                                           need, self.status.data_ptr(), raw)
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_decode_attn_mass")
 
@@ -225,12 +225,12 @@ class DecodeSession:
         """Cut every (channel, sequence, kv head) to ``budget`` slots: the
         first ``sinks``, the last ``recent`` and those with the largest mass.
         Writes mass_out (may be mass), kept [k][B][Hkv][budget] and new_lens."""
-        cfg, cache = self._refs
+        cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         self._packed(mass, page_table, seq_lens, mass_out, kept, new_lens)
         rc = self._lib.wm_cache_evict(cfg, cache, mass.data_ptr(), mass_out.data_ptr(),
                                       page_table.data_ptr(), seq_lens.data_ptr(), budget, sinks,
                                       recent, self.B if B is None else B, self.max_pages,
-                                      kept.data_ptr(), new_lens.data_ptr(), self._status_ptr,
+                                      kept.data_ptr(), new_lens.data_ptr(), self.status.data_ptr(),
                                       self._raw_stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_cache_evict")

@@ -634,3 +634,33 @@ def test_views_with_gaps_are_refused():
                  lambda: s.evict(mass, table.t(), lens, mass, table, lens, budget=8, sinks=1, recent=1)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_scratch_outgrown_by_a_later_call_stays_with_its_graph():
+    c = Cache([90] * 6, Hkv=2, G=2, d=64, page=16, shared=3, seed=8)
+    s = c.session()
+    table, lens = c.dev()
+    q = c.queries(6).cuda()
+    want, out = torch.empty_like(q), torch.empty_like(q)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+
+    def call(B, out, stream=None):
+        s.prefix_attn(1, q, table, lens, out, shared_pages=3, B=B, stream=stream)
+
+    call(1, want, stream)  # (allocates before the capture)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=stream):
+        call(1, out)
+    small = s._scratch[stream.cuda_stream].numel()
+    call(6, want, stream)
+    torch.cuda.synchronize()
+    assert s._scratch[stream.cuda_stream].numel() > small
+    with torch.cuda.stream(stream):  # what the allocator hands out next is not the graph's
+        others = [torch.full((small,), 77, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    torch.cuda.synchronize()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], want[0])
+    assert all(bool((x == 77).all()) for x in others)
