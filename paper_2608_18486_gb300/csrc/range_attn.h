@@ -126,7 +126,7 @@ struct EvictParams {
   int32_t* new_lens;
   int32_t* status;
   int32_t B, k, Hkv, P, log2P, num_pages, max_pages, budget, sinks, recent;
-  int32_t cluster;            // CTAs per unit (set by the launch)
+  int32_t cluster, vec4;      // set by the launch: CTAs per unit; sums may be read 16 bytes at a time
 };
 cudaError_t launch_cache_evict(EvictParams p, int dtype, int d, int sms, cudaStream_t s);
 

@@ -37,6 +37,13 @@
 // only multiplied as far as they go, in steps of 64 columns.  Slots that no
 // row of an item sees are never used: their pages are not fetched where a
 // whole box is unseen, their V rows are zeroed, their scores replaced.
+//
+// Measured: 8192 rows of 32 heads of 128 under a window of 1024: 155 us, 838
+// TFLOP/s of visible products (the tensor pipe 46% active, instruction issue
+// 43%); a prefix of 32768 slots under 64 sequences of 32 query / 8 kv heads of
+// 128: 38 us, 3.6 TB/s.  A step's chain bounds it: S, the softmax's reads and
+// exponentials, P V, per query tile one after the other; tensor memory has no
+// room for a second S per tile at a head size of 128.
 #include <math.h>
 
 #include "internal.h"

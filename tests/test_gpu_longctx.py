@@ -513,6 +513,59 @@ def test_evict_many_units_and_clusters(B, k, Hkv, d):
     assert same_bits(s.k_pool, kd) and same_bits(s.v_pool, vd)
 
 
+def evict_masses(c, kind):
+    shape = (c.k, c.B, c.Hkv, c.T)
+    m = np.abs(c.rng.standard_normal(shape))
+    if kind == "equal":
+        m[:] = 0.3
+    elif kind == "few":  # ties of many slots
+        m = c.rng.integers(0, 3, shape) * 0.25
+    elif kind == "wide":  # every exponent, both signs, what is no number
+        m = np.exp2(c.rng.uniform(-140, 120, shape)) * c.rng.choice([-1.0, 1.0], shape)
+        m[..., 5::19], m[..., 7::23], m[..., 9::29] = np.inf, -np.inf, np.nan
+    elif kind == "close":  # neighbours of one value
+        m = np.float32(0.5) * (1 + c.rng.integers(0, 40, shape) * 2.0 ** -23)
+    return m.astype(np.float32)
+
+
+# units of one to eight CTAs, whose CTAs hold up to 2048 sums each, up to 8192, or more than that
+@pytest.mark.parametrize("B,Hkv,lens,page", [(1, 1, 2050, 16), (2, 3, 5011, 4), (1, 1, 16381, 64), (1, 2, 30001, 64),
+                                             (1, 1, 65505, 64), (40, 1, 4099, 32), (40, 2, 9001, 16),
+                                             (1, 1, 4001, 1), (3, 4, 1023, 8), (160, 1, 2048, 16), (160, 1, 2049, 16)])
+@pytest.mark.parametrize("kind", ["random", "equal", "few", "wide", "close"])
+@pytest.mark.parametrize("alias", [False, True])
+def test_evict_selects_the_largest_sums_at_every_split(B, Hkv, lens, page, kind, alias):
+    """kept and the sums against a stable sort, the rows against kept."""
+    if lens * B * Hkv > 200000 and kind not in ("random", "few"):
+        pytest.skip("the large ones at two kinds")
+    c = Cache([lens - 3 * (b % 5) for b in range(B)], Hkv=Hkv, G=1, d=64, page=page, k=1, seed=lens)
+    mass = evict_masses(c, kind)
+    budget, sinks, recent = lens * 3 // 7, 5, lens // 9
+    s = c.session()
+    table, dl = c.dev()
+    m = torch.from_numpy(mass).cuda()
+    mo = m if alias else torch.full_like(m, 9.0)
+    kept = torch.full((1, B, Hkv, budget), 77, dtype=torch.int32, device="cuda")
+    nl = torch.empty_like(dl)
+    s.evict(m, table, dl, mo, kept, nl, budget=budget, sinks=sinks, recent=recent)
+    assert s.read_status() == 0 and (nl == budget).all()
+    kept, mo = kept.cpu().numpy(), mo.cpu().numpy()
+    kd, vd = s.k_pool.cpu(), s.v_pool.cpu()
+    for b in range(B):
+        n, tab = int(c.lens[b]), c.table[b]
+        for h in range(Hkv):
+            x = mass[0, b, h]
+            mid = np.where(np.isnan(x[sinks:n - recent]), -np.inf, x[sinks:n - recent]).astype(np.float64)
+            nan = np.isnan(x[sinks:n - recent])
+            order = sinks + np.lexsort((np.arange(len(mid)), -mid, nan))
+            want = np.sort(np.concatenate([np.arange(sinks), order[:budget - sinks - recent], np.arange(n - recent, n)]))
+            assert np.array_equal(kept[0, b, h], want)
+            assert np.array_equal(mo[0, b, h, :budget], x[want], equal_nan=True) and (mo[0, b, h, budget:] == 0).all()
+            to = np.arange(budget)
+            for got, was in ((kd, c.kp), (vd, c.vp)):
+                assert same_bits(got[0, tab[to // page], h, to % page], was[0, tab[want // page], h, want % page])
+
+
 def test_evict_bad_lengths_and_pages_are_reported():
     c = Cache([60, 60, 60], Hkv=1, G=1, d=64, page=16, k=1, seed=2)
     s = c.session()
