@@ -29,6 +29,9 @@ class DecodeSession:
         self.cfg = cfg
         self.B, self.num_pages, self.max_pages = int(B), int(num_pages), int(max_pages)
         self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            # one device for the session's buffers, streams and checks
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.dtype = torch.float32 if cfg.dtype == W.WM_DT_F32 else torch.bfloat16
         nbytes = W.wm_cache_bytes(cfg, num_pages)
         if nbytes == 0:
@@ -36,7 +39,7 @@ class DecodeSession:
         if cache_buf is None:
             cache_buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         elif cache_buf.dtype != torch.uint8 or not cache_buf.is_contiguous() or \
-                cache_buf.device.type != self.device.type:
+                cache_buf.device != self.device:
             raise ValueError("cache_buf must be a contiguous uint8 tensor on the session's device")
         elif cache_buf.numel() < nbytes:
             raise W.WMError(W.WM_ERR_INVALID_ARG, "wm_cache_alloc")
@@ -68,9 +71,8 @@ class DecodeSession:
         self._weight_refs = (pre_g, Wr, br, ch_g, Wkv, qk_g)
         self._weights = W.mix_weights(pre_g, Wr, br, ch_g, Wkv, qk_g)
 
-    @staticmethod
-    def _stream(stream) -> ctypes.c_void_p:
-        s = torch.cuda.current_stream() if stream is None else stream
+    def _stream(self, stream) -> ctypes.c_void_p:
+        s = torch.cuda.current_stream(self.device) if stream is None else stream
         return ctypes.c_void_p(s.cuda_stream)
 
     # ------------------------------------------------------------------ calls
@@ -132,7 +134,7 @@ class DecodeSession:
 
     def _raw_stream(self, stream) -> int:
         if stream is None:
-            return torch._C._cuda_getCurrentRawStream(self.device.index or 0)
+            return torch._C._cuda_getCurrentRawStream(self.device.index)
         return stream.cuda_stream
 
     def _scratch_for(self, nbytes: int, raw: int, stream):
