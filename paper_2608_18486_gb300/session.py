@@ -139,14 +139,17 @@ class DecodeSession:
 
     def _scratch_for(self, nbytes: int, raw: int, stream):
         # one buffer per stream for the calls below (they need nothing in it,
-        # so calls on one stream share it), kept at the largest size asked for
-        # and allocated on that stream.  The first call of a size may allocate:
-        # make it before a graph capture.  Graphs captured on one stream share
-        # its buffer: their replays must not overlap.
+        # so calls on one stream share it), allocated on that stream.  One that
+        # is too small is replaced by one of at least twice its size, so that
+        # all the outgrown ones together are smaller than the live one, which is
+        # less than twice the largest size asked for.  The first call of a size
+        # may allocate: make it before a graph capture.  Graphs captured on one
+        # stream share its buffer: their replays must not overlap.
         buf = self._scratch.get(raw)
         if buf is None or buf.numel() < nbytes:
             if buf is not None:
                 self._outgrown.append(buf)
+                nbytes = max(nbytes, 2 * buf.numel())
             s = torch.cuda.current_stream(self.device) if stream is None else stream
             with torch.cuda.stream(s):
                 buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
