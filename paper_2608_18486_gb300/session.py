@@ -13,6 +13,8 @@ import torch
 
 from . import _lib as W
 
+_I32 = torch.int32
+
 
 def torch_dtype(dtype: str):
     return {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
@@ -64,6 +66,11 @@ class DecodeSession:
         self._outgrown = []  # scratch replaced by larger: graphs captured before may use it
         self._need = {}      # workspace bytes by call and shape
         self._lib = W.lib()
+        # what the long-context calls check their tensors against
+        self._index = -1 if self.device.type == "cpu" else self.device.index
+        self._row_bytes = cfg.Hq * cfg.d * esz  # of q and out
+        self._units = cfg.k * cfg.Hkv           # (channel, kv head) pairs of a sequence
+        self._slots = self.max_pages * cfg.page_size
 
     # ------------------------------------------------------------------ setup
     def set_weights(self, pre_g, Wr, br, ch_g, Wkv, qk_g) -> None:
@@ -111,6 +118,7 @@ class DecodeSession:
             raise RuntimeError("set_weights() first")
         B = self.B if B is None else B
         if pos is not None:
+            self._check((pos, _I32, B))
             rc = W.wm_kv_mix_at(self.cfg, self.cache, self._weights, h, page_table, slot, pos, B,
                                 self.max_pages, self.mix_ws, self.mix_ws_bytes, self.status,
                                 self._stream(stream))
@@ -124,13 +132,47 @@ class DecodeSession:
             raise W.WMError(rc, "wm_kv_mix")
 
     # ---------------------------------------------------------- long contexts
-    @staticmethod
-    def _packed(*tensors) -> None:
-        # the library takes addresses: a view with gaps or another order of its
-        # dimensions would be read as if it had none
-        for t in tensors:
+    # The library takes addresses: a view with gaps or another order of its
+    # dimensions, another type, fewer rows or another device's memory would be
+    # read as if they were right.  The calls' checks are written out, since a
+    # loop over the tensors takes about twice as long (1.6 against 0.9 us a call).
+    def _check(self, *needs) -> None:
+        """needs: (tensor, type, elements it holds at least)."""
+        for t, dtype, n in needs:
             if not t.is_contiguous():
                 raise ValueError("the library reads contiguous tensors only")
+            if t.dtype is not dtype:
+                raise ValueError(f"the library reads {dtype} here, not {t.dtype}")
+            if t.numel() < n:
+                raise ValueError(f"{t.numel()} elements where the call reads or writes {n}")
+            if t.get_device() != self._index:
+                raise ValueError(f"a tensor on {t.device} in a session on {self.device}")
+
+    def _check_rows(self, q, index, page_table, out, B: int, n: int) -> None:
+        """n query rows of B sequences; index: lengths or positions, one per row."""
+        dt, dev, row, pages = self.dtype, self._index, n * self._row_bytes, self.max_pages
+        if not (q.is_contiguous() and index.is_contiguous() and page_table.is_contiguous() and out.is_contiguous()
+                and q.dtype is dt and out.dtype is dt and index.dtype is _I32 and page_table.dtype is _I32
+                and q.nbytes >= row and out.nbytes >= row and index.nbytes >= 4 * n
+                and page_table.nbytes >= 4 * B * pages
+                and q.get_device() == index.get_device() == page_table.get_device() == out.get_device() == dev):
+            e = n * self.cfg.Hq * self.cfg.d
+            self._check((q, dt, e), (index, _I32, n), (page_table, _I32, B * pages), (out, dt, e))
+        if page_table.shape[-1] != pages:
+            self._check_width(page_table)
+
+    def _check_width(self, page_table) -> None:
+        if page_table.dim() > 1 and page_table.shape[-1] != self.max_pages:
+            raise ValueError(f"rows of {page_table.shape[-1]} pages in a session of {self.max_pages}")
+
+    def _check_slots(self, t, dtype, B: int, per: int) -> None:
+        """t holds `per` elements of every (channel, sequence, kv head) of a call of
+        B sequences: one made for more sequences is laid out otherwise."""
+        n = self._units * B * per
+        if not (t.is_contiguous() and t.dtype is dtype and t.get_device() == self._index):
+            self._check((t, dtype, n))
+        if t.numel() != n:
+            raise ValueError(f"{t.numel()} elements where the call's sizes make {n}")
 
     def _raw_stream(self, stream) -> int:
         if stream is None:
@@ -170,11 +212,11 @@ class DecodeSession:
         """Decode attention over the first ``sinks`` slots and the last
         ``window`` slots of each sequence."""
         cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
-        self._packed(q, page_table, seq_lens, out)
+        B = self.B if B is None else B
+        self._check_rows(q, seq_lens, page_table, out, B, B)
         rc = self._lib.wm_window_attn(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
-                                      seq_lens.data_ptr(), sinks, window, self.B if B is None else B,
-                                      self.max_pages, out.data_ptr(), self.status.data_ptr(),
-                                      self._raw_stream(stream))
+                                      seq_lens.data_ptr(), sinks, window, B, self.max_pages,
+                                      out.data_ptr(), self.status.data_ptr(), self._raw_stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_window_attn")
 
@@ -184,7 +226,7 @@ class DecodeSession:
         [B][Tq]: position i sees slots t <= i, t < sinks or t > i - window."""
         cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         B, Tq = q.shape[:2]
-        self._packed(q, pos, page_table, out)
+        self._check_rows(q, pos, page_table, out, B, B * Tq)
         rc = self._lib.wm_window_prefill_attn(cfg, cache, layer, q.data_ptr(), pos.data_ptr(),
                                               page_table.data_ptr(), sinks, window, B, Tq,
                                               self.max_pages, out.data_ptr(), self.status.data_ptr(),
@@ -198,7 +240,7 @@ class DecodeSession:
         the same ones: those are read once for the batch."""
         cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         B = self.B if B is None else B
-        self._packed(q, page_table, seq_lens, out)
+        self._check_rows(q, seq_lens, page_table, out, B, B)
         need = self._bytes(("prefix", B, self.max_pages, shared_pages), W.wm_prefix_attn_workspace, B,
                            self.max_pages, shared_pages)
         raw = self._raw_stream(stream)
@@ -215,7 +257,8 @@ class DecodeSession:
         the query heads of a kv head, to mass [k][B][Hkv][slots] (fp32)."""
         cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         B = self.B if B is None else B
-        self._packed(q, page_table, seq_lens, mass, out)
+        self._check_rows(q, seq_lens, page_table, out, B, B)
+        self._check_slots(mass, torch.float32, B, self._slots)
         need = self._bytes(("mass", B, self.max_pages), W.wm_decode_attn_mass_workspace, B, self.max_pages)
         raw = self._raw_stream(stream)
         rc = self._lib.wm_decode_attn_mass(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
@@ -231,10 +274,15 @@ class DecodeSession:
         first ``sinks``, the last ``recent`` and those with the largest mass.
         Writes mass_out (may be mass), kept [k][B][Hkv][budget] and new_lens."""
         cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
-        self._packed(mass, page_table, seq_lens, mass_out, kept, new_lens)
+        B = self.B if B is None else B
+        self._check((seq_lens, _I32, B), (new_lens, _I32, B), (page_table, _I32, B * self.max_pages))
+        self._check_width(page_table)
+        self._check_slots(mass, torch.float32, B, self._slots)
+        self._check_slots(mass_out, torch.float32, B, self._slots)
+        self._check_slots(kept, _I32, B, budget)
         rc = self._lib.wm_cache_evict(cfg, cache, mass.data_ptr(), mass_out.data_ptr(),
                                       page_table.data_ptr(), seq_lens.data_ptr(), budget, sinks,
-                                      recent, self.B if B is None else B, self.max_pages,
+                                      recent, B, self.max_pages,
                                       kept.data_ptr(), new_lens.data_ptr(), self.status.data_ptr(),
                                       self._raw_stream(stream))
         if rc != W.WM_OK:

@@ -1,4 +1,4 @@
-"""DecodeSession's host side: devices and streams (no GPU, nothing launched)."""
+"""DecodeSession's host side: devices, streams, scratch and checks (no GPU, nothing launched)."""
 import contextlib
 
 import pytest
@@ -85,3 +85,137 @@ def test_scratch_kept_for_graphs_stays_below_what_is_in_use(monkeypatch):
     for n in reversed(needs):  # (smaller requests share what is there)
         s._scratch_for(n, 7, None)
     assert [x.data_ptr() for x in s._scratch.values()] == again
+
+
+class Calls:
+    """The long-context calls of a session of B sequences on right tensors, any of
+    them replaced; what reaches the library is recorded, and not called."""
+
+    def __init__(self, monkeypatch, B=3, dtype="bf16"):
+        cfg = config(k=2, dtype=dtype)
+        self.s = s = host_session(cfg, B, 16, 4)
+        monkeypatch.setattr(s, "_raw_stream", lambda stream: 0)
+        monkeypatch.setattr(s, "_scratch_for", lambda n, raw, stream: 0)
+        self.reached = []
+
+        class Library:
+            def __getattr__(_, name):
+                return lambda *a: self.reached.append((name, a)) or W.WM_OK
+        s._lib = Library()
+        i32 = torch.int32
+        self.B, self.t = B, dict(
+            q=torch.zeros(B, 4, 64, dtype=s.dtype), out=torch.zeros(B, 4, 64, dtype=s.dtype),
+            table=torch.zeros(B, 4, dtype=i32), lens=torch.zeros(B, dtype=i32),
+            rows=torch.zeros(B, 5, 4, 64, dtype=s.dtype), rows_out=torch.zeros(B, 5, 4, 64, dtype=s.dtype),
+            pos=torch.zeros(B, 5, dtype=i32), mass=torch.zeros(2, B, 2, 64), mass_out=torch.zeros(2, B, 2, 64),
+            kept=torch.zeros(2, B, 2, 24, dtype=i32), new_lens=torch.zeros(B, dtype=i32))
+
+    def __call__(self, name, B=None, sinks=1, window=8, budget=24, recent=2, **other):
+        t, s = {**self.t, **other}, self.s
+        if name == "window":
+            s.window_attn(0, t["q"], t["table"], t["lens"], t["out"], sinks=sinks, window=window, B=B)
+        if name == "rows":
+            s.window_prefill_attn(0, t["rows"], t["pos"], t["table"], t["rows_out"], sinks=sinks, window=window)
+        if name == "prefix":
+            s.prefix_attn(0, t["q"], t["table"], t["lens"], t["out"], shared_pages=1, B=B)
+        if name == "mass":
+            s.decode_attn_mass(0, t["q"], t["table"], t["lens"], t["mass"], t["out"], B=B)
+        if name == "evict":
+            s.evict(t["mass"], t["table"], t["lens"], t["mass_out"], t["kept"], t["new_lens"], budget=budget,
+                    sinks=sinks, recent=recent, B=B)
+
+
+READ = {"window": ["q", "table", "lens", "out"], "rows": ["rows", "pos", "table", "rows_out"],
+        "prefix": ["q", "table", "lens", "out"], "mass": ["q", "table", "lens", "mass", "out"],
+        "evict": ["mass", "table", "lens", "mass_out", "kept", "new_lens"]}
+EACH = [(name, what) for name in READ for what in READ[name]]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", list(READ))
+def test_right_tensors_reach_the_library(monkeypatch, name, dtype):
+    c = Calls(monkeypatch, dtype=dtype)
+    c(name)
+    assert len(c.reached) == 1
+    if name not in ("rows", "mass", "evict"):  # part of a batch, in tensors made for all of it
+        c(name, B=2)
+        assert len(c.reached) == 2
+    if name in ("mass", "evict"):
+        small = {"mass": torch.zeros(2, 2, 2, 64), "mass_out": torch.zeros(2, 2, 2, 64),
+                 "kept": torch.zeros(2, 2, 2, 24, dtype=torch.int32)}
+        c(name, B=2, **small)
+        assert len(c.reached) == 2
+    flat = c.t["table"].reshape(-1)  # (the table's rows one behind the other)
+    c(name, table=flat)
+
+
+@pytest.mark.parametrize("name,what", EACH)
+def test_another_type_is_refused(monkeypatch, name, what):
+    c = Calls(monkeypatch)
+    t = c.t[what]
+    for dtype in (torch.int64, torch.float64, torch.float16, torch.uint8):
+        with pytest.raises(ValueError):
+            c(name, **{what: torch.zeros(4 * t.numel(), dtype=dtype).view(4, *t.shape)})
+    assert not c.reached
+
+
+@pytest.mark.parametrize("name,what", EACH)
+def test_too_few_elements_and_gaps_are_refused(monkeypatch, name, what):
+    c = Calls(monkeypatch)
+    t = c.t[what]
+    wide = torch.zeros(*t.shape, 2, dtype=t.dtype)[..., 0]
+    fewer = t[1:] if what != "rows" else t[..., :63].contiguous()  # (the rows themselves give that call's sizes)
+    for bad in (wide, fewer):
+        with pytest.raises(ValueError):
+            c(name, **{what: bad})
+    assert not c.reached
+
+
+class Far(torch.Tensor):
+    """A tensor that says it is on device 1."""
+
+    def get_device(self):
+        return 1
+
+
+@pytest.mark.parametrize("name,what", EACH)
+def test_another_device_is_refused(monkeypatch, name, what):
+    c = Calls(monkeypatch)
+    with pytest.raises(ValueError):
+        c(name, **{what: c.t[what].as_subclass(Far)})
+    assert not c.reached
+
+
+@pytest.mark.parametrize("name", list(READ))
+def test_tables_of_another_width_are_refused(monkeypatch, name):
+    c = Calls(monkeypatch)
+    with pytest.raises(ValueError):
+        c(name, table=torch.zeros(3, 6, dtype=torch.int32))
+    assert not c.reached
+
+
+@pytest.mark.parametrize("name,what", [("mass", "mass"), ("evict", "mass"), ("evict", "mass_out"), ("evict", "kept")])
+def test_sums_made_for_another_batch_are_refused(monkeypatch, name, what):
+    """Their channels lie where the call's own batch puts them."""
+    c = Calls(monkeypatch)
+    small = {"mass": torch.zeros(2, 2, 2, 64), "mass_out": torch.zeros(2, 2, 2, 64),
+             "kept": torch.zeros(2, 2, 2, 24, dtype=torch.int32)}
+    del small[what]
+    with pytest.raises(ValueError):
+        c(name, B=2, **small)
+    assert not c.reached
+
+
+def test_pool_positions_are_checked(monkeypatch):
+    s = host_session(config(), 3, 16, 4)
+    s._weights = W.wm_mix_weights()
+    ran = []
+    monkeypatch.setattr(W, "wm_kv_mix_at", lambda *a: ran.append(a) or W.WM_OK)
+    monkeypatch.setattr(s, "_stream", lambda stream: None)
+    s.kv_mix(None, None, None, pos=torch.zeros(3, dtype=torch.int32))
+    assert len(ran) == 1
+    for bad in (torch.zeros(3, dtype=torch.int64), torch.zeros(2, dtype=torch.int32),
+                torch.zeros(3, 2, dtype=torch.int32)[:, 0], torch.zeros(3, dtype=torch.int32).as_subclass(Far)):
+        with pytest.raises(ValueError):
+            s.kv_mix(None, None, None, pos=bad)
+    assert len(ran) == 1
