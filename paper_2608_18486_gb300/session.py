@@ -174,6 +174,11 @@ class DecodeSession:
         if t.numel() != n:
             raise ValueError(f"{t.numel()} elements where the call's sizes make {n}")
 
+    @staticmethod
+    def _counts(*counts: int):
+        # the binding would keep the low 32 bits; no sequence has as many slots
+        return (min(max(n, -1), 0x7FFFFFFF) for n in counts)
+
     def _raw_stream(self, stream) -> int:
         if stream is None:
             return torch._C._cuda_getCurrentRawStream(self.device.index)
@@ -214,6 +219,8 @@ class DecodeSession:
         cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         B = self.B if B is None else B
         self._check_rows(q, seq_lens, page_table, out, B, B)
+        if (sinks | window) >> 31:
+            sinks, window = self._counts(sinks, window)
         rc = self._lib.wm_window_attn(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
                                       seq_lens.data_ptr(), sinks, window, B, self.max_pages,
                                       out.data_ptr(), self.status.data_ptr(), self._raw_stream(stream))
@@ -227,6 +234,8 @@ class DecodeSession:
         cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         B, Tq = q.shape[:2]
         self._check_rows(q, pos, page_table, out, B, B * Tq)
+        if (sinks | window) >> 31:
+            sinks, window = self._counts(sinks, window)
         rc = self._lib.wm_window_prefill_attn(cfg, cache, layer, q.data_ptr(), pos.data_ptr(),
                                               page_table.data_ptr(), sinks, window, B, Tq,
                                               self.max_pages, out.data_ptr(), self.status.data_ptr(),
@@ -280,6 +289,8 @@ class DecodeSession:
         self._check_slots(mass, torch.float32, B, self._slots)
         self._check_slots(mass_out, torch.float32, B, self._slots)
         self._check_slots(kept, _I32, B, budget)
+        if (budget | sinks | recent) >> 31:
+            budget, sinks, recent = self._counts(budget, sinks, recent)
         rc = self._lib.wm_cache_evict(cfg, cache, mass.data_ptr(), mass_out.data_ptr(),
                                       page_table.data_ptr(), seq_lens.data_ptr(), budget, sinks,
                                       recent, B, self.max_pages,

@@ -219,3 +219,23 @@ def test_pool_positions_are_checked(monkeypatch):
         with pytest.raises(ValueError):
             s.kv_mix(None, None, None, pos=bad)
     assert len(ran) == 1
+
+
+@pytest.mark.parametrize("n", [2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 40 + 1, 10 ** 30, -1, -2 ** 32, -2 ** 32 + 5])
+@pytest.mark.parametrize("name,at", [("window", (6, 7)), ("rows", (6, 7))])
+def test_counts_of_slots_past_32_bits_are_every_slot(monkeypatch, name, at, n):
+    """Windows and sinks may be of any size; a negative one reaches the library as one, which refuses it."""
+    c = Calls(monkeypatch)
+    c(name, sinks=n, window=3)
+    c(name, sinks=3, window=n)
+    want = 2 ** 31 - 1 if n > 0 else -1
+    assert [a[at[0]] for _, a in c.reached] == [want, 3] and [a[at[1]] for _, a in c.reached] == [3, want]
+
+
+@pytest.mark.parametrize("what,at", [("sinks", 7), ("recent", 8)])
+@pytest.mark.parametrize("n", [2 ** 31, 2 ** 32, 2 ** 32 + 1, -2 ** 32, -2 ** 32 + 1])
+def test_evictions_of_counts_past_32_bits_are_refused_by_the_library(monkeypatch, what, at, n):
+    c = Calls(monkeypatch)
+    c("evict", **{what: n})
+    (name, args), = c.reached
+    assert name == "wm_cache_evict" and args[at] == (2 ** 31 - 1 if n > 0 else -1)  # over the budget, or below 0
