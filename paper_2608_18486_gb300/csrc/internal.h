@@ -4,22 +4,35 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <mutex>
+
 #include "wm.h"
 
 namespace wm {
 
 // Opt kernel `kern` into `smem` bytes of dynamic shared memory on the current
 // device (the limit is a per-device attribute of the function).  `done`
-// holds, per device, the largest value set so far.
+// holds, per device, the largest value set so far.  Threads may call it at
+// once, for different sizes of one kernel too: the attribute is set under a
+// lock and only ever raised, and `done` follows it, so that whoever reads a
+// large enough value there launches under a large enough limit.
 constexpr int kSmemOptDevices = 64;
+inline std::mutex& opt_in_lock() {
+  static std::mutex m;
+  return m;
+}
 template <typename Kern>
 inline cudaError_t opt_in_smem(Kern kern, size_t smem, size_t (&done)[kSmemOptDevices]) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
   const bool cached = dev >= 0 && dev < kSmemOptDevices;
-  if (cached && smem <= done[dev]) return cudaSuccess;
+  if (!cached)  // (past the table: set every time)
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (smem <= __atomic_load_n(&done[dev], __ATOMIC_ACQUIRE)) return cudaSuccess;
+  std::lock_guard<std::mutex> held(opt_in_lock());
+  if (smem <= done[dev]) return cudaSuccess;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e == cudaSuccess && cached) done[dev] = smem;
+  if (e == cudaSuccess) __atomic_store_n(&done[dev], smem, __ATOMIC_RELEASE);
   return e;
 }
 
