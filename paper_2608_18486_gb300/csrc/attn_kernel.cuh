@@ -256,15 +256,18 @@ __global__ void __launch_bounds__(kThreads, attn_ctas_per_sm(SB, G)) decode_attn
   const int B = p.B, Hkv = p.Hkv;
   const int max_slots = p.max_pages * p.P;
 
-  // Programmatic dependent launch: the next grid on the stream may be
-  // scheduled now.  This grid waits for the previous one (finished and
-  // flushed) before reading anything it may have written.  With the caller's
-  // promise that the previous grid wrote neither the cache, the page table,
-  // the lengths nor the workspace (inputs_ready), the wait moves down to just
-  // before the query is read, and the first K/V copies overlap its tail.
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // Programmatic dependent launch.  This grid waits for the previous one
+  // (finished and flushed) before reading anything it may have written, and
+  // only then lets the next grid on the stream start: with the caller's promise
+  // that the grid just before wrote neither the cache, the page table nor the
+  // lengths (inputs_ready), that one reads them at once, and what wrote them (a
+  // pool update, an eviction) may be the grid before this one.  A grid with the
+  // promise started after such a wait itself, so it passes the start on at once;
+  // its own wait moves down to just before the query is read, and the first K/V
+  // copies overlap the previous grid's tail.
   const bool early = p.inputs_ready != 0;
   if (!early) asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // ---- stages per sequence and their prefix sums (every CTA, all threads)
   {

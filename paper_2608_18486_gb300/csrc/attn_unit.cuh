@@ -93,10 +93,11 @@ __global__ void __launch_bounds__(unit_warps<T, HD, G, SB>() * 32,
 
   // Programmatic dependent launch, as in the stream-K kernel: with the
   // caller's inputs_ready promise the cache, table and lengths are read
-  // before the dependency wait, and only the query after it.
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // before the dependency wait, and only the query after it; without it the
+  // next grid starts after the wait.
   const bool early = p.inputs_ready != 0;
   if (!early) asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   if (tid == 0) {
     for (int w = 0; w < NW; ++w)

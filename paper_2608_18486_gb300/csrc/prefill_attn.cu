@@ -136,9 +136,10 @@ __global__ void __launch_bounds__(kPThreads, 1)
     tc::tmem_relinquish();
   }
   // programmatic dependent launch: positions, table, queries and cache may
-  // come from the previous grid
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // come from the previous grid; the next grid starts after the wait, since a
+  // decode attention told that its inputs are ready reads the cache at once
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // ---- positions of the softmax threads' rows; the largest of each tile
   const int max_slots = p.max_pages * p.P;
