@@ -13,7 +13,7 @@ import torch
 
 from . import _lib as W
 
-_I32 = torch.int32
+_I32, _F32 = torch.int32, torch.float32
 
 
 def torch_dtype(dtype: str):
@@ -165,14 +165,14 @@ class DecodeSession:
         if page_table.dim() > 1 and page_table.shape[-1] != self.max_pages:
             raise ValueError(f"rows of {page_table.shape[-1]} pages in a session of {self.max_pages}")
 
-    def _check_slots(self, t, dtype, B: int, per: int) -> None:
-        """t holds `per` elements of every (channel, sequence, kv head) of a call of
-        B sequences: one made for more sequences is laid out otherwise."""
-        n = self._units * B * per
-        if not (t.is_contiguous() and t.dtype is dtype and t.get_device() == self._index):
+    def _check_sums(self, B: int, *needs) -> None:
+        """needs: (tensor, type, elements of every (channel, sequence, kv head) of a
+        call of B sequences).  One made for more sequences is laid out otherwise."""
+        for t, dtype, per in needs:
+            n = self._units * B * per
             self._check((t, dtype, n))
-        if t.numel() != n:
-            raise ValueError(f"{t.numel()} elements where the call's sizes make {n}")
+            if t.numel() != n:
+                raise ValueError(f"{t.numel()} elements where the call's sizes make {n}")
 
     @staticmethod
     def _counts(*counts: int):
@@ -267,7 +267,10 @@ class DecodeSession:
         cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         B = self.B if B is None else B
         self._check_rows(q, seq_lens, page_table, out, B, B)
-        self._check_slots(mass, torch.float32, B, self._slots)
+        need = 4 * self._units * B * self._slots
+        if not (mass.is_contiguous() and mass.dtype is _F32 and mass.nbytes == need
+                and mass.get_device() == self._index):
+            self._check_sums(B, (mass, _F32, self._slots))
         need = self._bytes(("mass", B, self.max_pages), W.wm_decode_attn_mass_workspace, B, self.max_pages)
         raw = self._raw_stream(stream)
         rc = self._lib.wm_decode_attn_mass(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
@@ -284,11 +287,19 @@ class DecodeSession:
         Writes mass_out (may be mass), kept [k][B][Hkv][budget] and new_lens."""
         cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
         B = self.B if B is None else B
-        self._check((seq_lens, _I32, B), (new_lens, _I32, B), (page_table, _I32, B * self.max_pages))
-        self._check_width(page_table)
-        self._check_slots(mass, torch.float32, B, self._slots)
-        self._check_slots(mass_out, torch.float32, B, self._slots)
-        self._check_slots(kept, _I32, B, budget)
+        dev, pages, units = self._index, self.max_pages, 4 * self._units * B
+        if not (mass.is_contiguous() and mass_out.is_contiguous() and kept.is_contiguous() and seq_lens.is_contiguous()
+                and new_lens.is_contiguous() and page_table.is_contiguous()
+                and mass.dtype is _F32 and mass_out.dtype is _F32 and kept.dtype is _I32 and seq_lens.dtype is _I32
+                and new_lens.dtype is _I32 and page_table.dtype is _I32
+                and mass.nbytes == mass_out.nbytes == units * self._slots and kept.nbytes == units * budget
+                and seq_lens.nbytes >= 4 * B and new_lens.nbytes >= 4 * B and page_table.nbytes >= 4 * B * pages
+                and mass.get_device() == mass_out.get_device() == kept.get_device() == seq_lens.get_device()
+                == new_lens.get_device() == page_table.get_device() == dev):
+            self._check((seq_lens, _I32, B), (new_lens, _I32, B), (page_table, _I32, B * pages))
+            self._check_sums(B, (mass, _F32, self._slots), (mass_out, _F32, self._slots), (kept, _I32, budget))
+        if page_table.shape[-1] != pages:
+            self._check_width(page_table)
         if (budget | sinks | recent) >> 31:
             budget, sinks, recent = self._counts(budget, sinks, recent)
         rc = self._lib.wm_cache_evict(cfg, cache, mass.data_ptr(), mass_out.data_ptr(),
