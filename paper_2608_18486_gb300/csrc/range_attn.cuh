@@ -776,7 +776,8 @@ __global__ void __launch_bounds__(kThreads, kRangeCtasPerSm) range_attn_kernel(c
     for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(FULL, M, o));
     for (int i = lane; i < C + np; i += 32) {
       const float2 x = ml(i);
-      const float w = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
+      // a record whose every score is NaN has no maximum either, but its sum is NaN
+      const float w = x.x == -INFINITY ? (x.y == x.y ? 0.f : 1.f) : exp2f(x.x - M);
       wts[r][i] = w;
       if (w != 0.f) L = fmaf(w, x.y, L);
     }
