@@ -229,7 +229,11 @@ wm_status wm_decode_attn(const wm_config* cfg, const wm_cache* cache, int32_t la
  *     Within one decode step this holds for layers 1..L-1 (the previous
  *     layer's attention may share the workspace); it does NOT hold for the
  *     first layer after wm_kv_mix or after any update of seq_lens / the page
- *     table.
+ *     table.  What wrote them may be the work before that work: this
+ *     library's attention calls let the next launch start only when all that
+ *     precedes them is done.  wm_kv_mix passes the start on at once, so the
+ *     promise does not hold right after a wm_kv_mix of another cache either,
+ *     while an update of this one may still run.
  *   WM_ATTN_DYNAMIC_SPLIT: hand the KV stream out in chunks from a device
  *     counter (about 8 chunks per warp, warps that stream faster take more)
  *     whatever the launch size.  Without it only launches reading at least
@@ -302,7 +306,10 @@ wm_status wm_prefill_attn(const wm_config* cfg, const wm_cache* cache, int32_t l
  * dtypes, every page size and group size, with softmax and accumulation in
  * fp32.  bf16: the tensor-core kernels (many rows, long shared prefixes) round
  * the probabilities to bf16 for the P V product, the others keep 16 bits of
- * them.  fp32 units of 8 query rows multiply operands split into three bf16
+ * them (relative errors of bf16 results 0.0021 to 0.0023 and 0.0016 to 0.0017,
+ * of which the rounding of the result is 0.0016); a shared prefix takes the
+ * tensor cores from 40 MB of K/V times groups of 8 query rows on, so one more
+ * page or sequence may change the last bits.  fp32 units of 8 query rows multiply operands split into three bf16
  * parts (exact to 2^-23 of the products' magnitude); everything else in fp32 is
  * FMA arithmetic.  A sequence may hold no slot at all (length 0): its rows are
  * zeros, and so is any row whose mask leaves nothing.  A negative length, or one
@@ -332,7 +339,13 @@ wm_status wm_window_attn(const wm_config* cfg, const wm_cache* cache, int32_t la
  * query at position i = pos[b][r] sees the slots t <= i with t < sinks or
  * t > i - window.
  *   q, out  device [B][Tq][Hq][d], 16-byte aligned
- *   pos     device int32 [B][Tq], 0 <= pos < max_pages*page_size, any order
+ *   pos     device int32 [B][Tq], 0 <= pos < max_pages*page_size, any order.
+ *           The tensor-core kernel (bf16, pages of at least 8 slots) works
+ *           best on positions that rise by at most the window from row to
+ *           row: others make it look up which slots are seen, and rows that
+ *           lie together but see different slots share no work (2048 rows of
+ *           32 heads of 128, window 1024: 50 us in order, 214 us shuffled).
+ *           The others (fp32, smaller pages) read the window anew per row.
  * No workspace.  A bad position zero-fills that row and sets WM_ERR_BOUNDS.
  */
 wm_status wm_window_prefill_attn(const wm_config* cfg, const wm_cache* cache, int32_t layer,
