@@ -78,7 +78,14 @@ class DecodeSession:
         self._weight_refs = (pre_g, Wr, br, ch_g, Wkv, qk_g)
         self._weights = W.mix_weights(pre_g, Wr, br, ch_g, Wkv, qk_g)
 
+    def _check_device(self) -> None:
+        # a launch goes to the current device, whatever its stream and pointers
+        if self._index >= 0 and torch._C._cuda_getDevice() != self._index:
+            raise ValueError(f"the session is on {self.device}, the current device is "
+                             f"{torch._C._cuda_getDevice()}")
+
     def _stream(self, stream) -> ctypes.c_void_p:
+        self._check_device()
         s = torch.cuda.current_stream(self.device) if stream is None else stream
         return ctypes.c_void_p(s.cuda_stream)
 
@@ -180,6 +187,7 @@ class DecodeSession:
         return (min(max(n, -1), 0x7FFFFFFF) for n in counts)
 
     def _raw_stream(self, stream) -> int:
+        self._check_device()
         if stream is None:
             return torch._C._cuda_getCurrentRawStream(self.device.index)
         return stream.cuda_stream

@@ -20,9 +20,14 @@ def host_session(cfg, B, pages, max_pages):
     return DecodeSession(cfg, B, pages, max_pages, "cpu", cache_buf=buf[at:at + n])
 
 
+class Devices:
+    current = 1
+
+
 @pytest.fixture
 def two_devices(monkeypatch):
-    """A process whose current device is 1; what it allocates lies in host memory."""
+    """A process whose current device is 1 at first; what it allocates lies in host memory."""
+    devices = Devices()
     zeros = torch.zeros
 
     def on_host(n, dtype, device):  # on a 256-byte boundary, as device memory is
@@ -31,8 +36,9 @@ def two_devices(monkeypatch):
         return x[at:at + n]
     monkeypatch.setattr(torch, "empty", on_host)
     monkeypatch.setattr(torch, "zeros", on_host)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
-    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 1000 + index)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: devices.current)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: devices.current, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 1000 + index, raising=False)
 
     class Stream:
         def __init__(self, index):
@@ -40,16 +46,30 @@ def two_devices(monkeypatch):
 
     def current_stream(device=None):
         index = None if device is None else torch.device(device).index
-        return Stream(1 if index is None else index)
+        return Stream(devices.current if index is None else index)
     monkeypatch.setattr(torch.cuda, "current_stream", current_stream)
+    return devices
 
 
 @pytest.mark.parametrize("device,index", [("cuda", 1), ("cuda:0", 0), ("cuda:1", 1)])
 def test_every_call_takes_the_stream_of_the_sessions_device(two_devices, device, index):
     s = DecodeSession(config(), 2, 4, 2, device)
     assert s.device == torch.device("cuda", index)
+    two_devices.current = index
     assert s._raw_stream(None) == 1000 + index
     assert s._stream(None).value == 1000 + index
+
+
+@pytest.mark.parametrize("device,current", [("cuda", 0), ("cuda:0", 1), ("cuda:1", 0)])
+def test_calls_while_another_device_is_current_are_refused(two_devices, device, current):
+    """They would launch there, on this device's addresses."""
+    s = DecodeSession(config(), 2, 4, 2, device)
+    two_devices.current = current
+    for stream in (None, torch.cuda.current_stream(s.device)):
+        with pytest.raises(ValueError):
+            s._raw_stream(stream)
+        with pytest.raises(ValueError):
+            s._stream(stream)
 
 
 def test_a_cache_on_another_device_is_refused(two_devices):
