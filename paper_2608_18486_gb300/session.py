@@ -66,6 +66,10 @@ class DecodeSession:
         self._outgrown = []  # scratch replaced by larger: graphs captured before may use it
         self._need = {}      # workspace bytes by call and shape
         self._lib = W.lib()
+        # the session's own arguments of the long-context calls, made once: a small
+        # launch takes about as long on the GPU as its call on the host
+        self._refs = (ctypes.byref(self.cfg), ctypes.byref(self.cache))
+        self._status_ptr = self.status.data_ptr()
         # what the long-context calls check their tensors against
         self._index = -1 if self.device.type == "cpu" else self.device.index
         self._row_bytes = cfg.Hq * cfg.d * esz  # of q and out
@@ -143,6 +147,7 @@ class DecodeSession:
     # dimensions, another type, fewer rows or another device's memory would be
     # read as if they were right.  The calls' checks are written out, since a
     # loop over the tensors takes about twice as long (1.6 against 0.9 us a call).
+    # A page table of exactly the call's bytes is taken for [B][max_pages].
     def _check(self, *needs) -> None:
         """needs: (tensor, type, elements it holds at least)."""
         for t, dtype, n in needs:
@@ -161,14 +166,14 @@ class DecodeSession:
         if not (q.is_contiguous() and index.is_contiguous() and page_table.is_contiguous() and out.is_contiguous()
                 and q.dtype is dt and out.dtype is dt and index.dtype is _I32 and page_table.dtype is _I32
                 and q.nbytes >= row and out.nbytes >= row and index.nbytes >= 4 * n
-                and page_table.nbytes >= 4 * B * pages
+                and page_table.nbytes == 4 * B * pages
                 and q.get_device() == index.get_device() == page_table.get_device() == out.get_device() == dev):
             e = n * self.cfg.Hq * self.cfg.d
-            self._check((q, dt, e), (index, _I32, n), (page_table, _I32, B * pages), (out, dt, e))
-        if page_table.shape[-1] != pages:
-            self._check_width(page_table)
+            self._check((q, dt, e), (index, _I32, n), (out, dt, e))
+            self._check_table(page_table, B)
 
-    def _check_width(self, page_table) -> None:
+    def _check_table(self, page_table, B: int) -> None:
+        self._check((page_table, _I32, B * self.max_pages))
         if page_table.dim() > 1 and page_table.shape[-1] != self.max_pages:
             raise ValueError(f"rows of {page_table.shape[-1]} pages in a session of {self.max_pages}")
 
@@ -187,7 +192,8 @@ class DecodeSession:
         return (min(max(n, -1), 0x7FFFFFFF) for n in counts)
 
     def _raw_stream(self, stream) -> int:
-        self._check_device()
+        if torch._C._cuda_getDevice() != self._index:
+            self._check_device()
         if stream is None:
             return torch._C._cuda_getCurrentRawStream(self.device.index)
         return stream.cuda_stream
@@ -224,14 +230,14 @@ class DecodeSession:
                     B: int | None = None, stream=None) -> None:
         """Decode attention over the first ``sinks`` slots and the last
         ``window`` slots of each sequence."""
-        cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
+        cfg, cache = self._refs
         B = self.B if B is None else B
         self._check_rows(q, seq_lens, page_table, out, B, B)
         if (sinks | window) >> 31:
             sinks, window = self._counts(sinks, window)
         rc = self._lib.wm_window_attn(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
                                       seq_lens.data_ptr(), sinks, window, B, self.max_pages,
-                                      out.data_ptr(), self.status.data_ptr(), self._raw_stream(stream))
+                                      out.data_ptr(), self._status_ptr, self._raw_stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_window_attn")
 
@@ -239,14 +245,14 @@ class DecodeSession:
                             stream=None) -> None:
         """window_attn's mask for query rows q [B][Tq][Hq][d] at positions pos
         [B][Tq]: position i sees slots t <= i, t < sinks or t > i - window."""
-        cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
+        cfg, cache = self._refs
         B, Tq = q.shape[:2]
         self._check_rows(q, pos, page_table, out, B, B * Tq)
         if (sinks | window) >> 31:
             sinks, window = self._counts(sinks, window)
         rc = self._lib.wm_window_prefill_attn(cfg, cache, layer, q.data_ptr(), pos.data_ptr(),
                                               page_table.data_ptr(), sinks, window, B, Tq,
-                                              self.max_pages, out.data_ptr(), self.status.data_ptr(),
+                                              self.max_pages, out.data_ptr(), self._status_ptr,
                                               self._raw_stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_window_prefill_attn")
@@ -255,7 +261,7 @@ class DecodeSession:
                     B: int | None = None, stream=None) -> None:
         """Decode attention of sequences whose first ``shared_pages`` pages are
         the same ones: those are read once for the batch."""
-        cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
+        cfg, cache = self._refs
         B = self.B if B is None else B
         self._check_rows(q, seq_lens, page_table, out, B, B)
         need = self._bytes(("prefix", B, self.max_pages, shared_pages), W.wm_prefix_attn_workspace, B,
@@ -264,7 +270,7 @@ class DecodeSession:
         rc = self._lib.wm_prefix_attn(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
                                       seq_lens.data_ptr(), shared_pages, B, self.max_pages,
                                       out.data_ptr(), self._scratch_for(need, raw, stream), need,
-                                      self.status.data_ptr(), raw)
+                                      self._status_ptr, raw)
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_prefix_attn")
 
@@ -272,7 +278,7 @@ class DecodeSession:
                          B: int | None = None, stream=None) -> None:
         """Decode attention that adds every slot's softmax weight, summed over
         the query heads of a kv head, to mass [k][B][Hkv][slots] (fp32)."""
-        cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
+        cfg, cache = self._refs
         B = self.B if B is None else B
         self._check_rows(q, seq_lens, page_table, out, B, B)
         need = 4 * self._units * B * self._slots
@@ -284,7 +290,7 @@ class DecodeSession:
         rc = self._lib.wm_decode_attn_mass(cfg, cache, layer, q.data_ptr(), page_table.data_ptr(),
                                            seq_lens.data_ptr(), mass.data_ptr(), B, self.max_pages,
                                            out.data_ptr(), self._scratch_for(need, raw, stream),
-                                           need, self.status.data_ptr(), raw)
+                                           need, self._status_ptr, raw)
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_decode_attn_mass")
 
@@ -293,7 +299,7 @@ class DecodeSession:
         """Cut every (channel, sequence, kv head) to ``budget`` slots: the
         first ``sinks``, the last ``recent`` and those with the largest mass.
         Writes mass_out (may be mass), kept [k][B][Hkv][budget] and new_lens."""
-        cfg, cache = ctypes.byref(self.cfg), ctypes.byref(self.cache)
+        cfg, cache = self._refs
         B = self.B if B is None else B
         dev, pages, units = self._index, self.max_pages, 4 * self._units * B
         if not (mass.is_contiguous() and mass_out.is_contiguous() and kept.is_contiguous() and seq_lens.is_contiguous()
@@ -301,19 +307,18 @@ class DecodeSession:
                 and mass.dtype is _F32 and mass_out.dtype is _F32 and kept.dtype is _I32 and seq_lens.dtype is _I32
                 and new_lens.dtype is _I32 and page_table.dtype is _I32
                 and mass.nbytes == mass_out.nbytes == units * self._slots and kept.nbytes == units * budget
-                and seq_lens.nbytes >= 4 * B and new_lens.nbytes >= 4 * B and page_table.nbytes >= 4 * B * pages
+                and seq_lens.nbytes >= 4 * B and new_lens.nbytes >= 4 * B and page_table.nbytes == 4 * B * pages
                 and mass.get_device() == mass_out.get_device() == kept.get_device() == seq_lens.get_device()
                 == new_lens.get_device() == page_table.get_device() == dev):
-            self._check((seq_lens, _I32, B), (new_lens, _I32, B), (page_table, _I32, B * pages))
+            self._check((seq_lens, _I32, B), (new_lens, _I32, B))
             self._check_sums(B, (mass, _F32, self._slots), (mass_out, _F32, self._slots), (kept, _I32, budget))
-        if page_table.shape[-1] != pages:
-            self._check_width(page_table)
+            self._check_table(page_table, B)
         if (budget | sinks | recent) >> 31:
             budget, sinks, recent = self._counts(budget, sinks, recent)
         rc = self._lib.wm_cache_evict(cfg, cache, mass.data_ptr(), mass_out.data_ptr(),
                                       page_table.data_ptr(), seq_lens.data_ptr(), budget, sinks,
                                       recent, B, self.max_pages,
-                                      kept.data_ptr(), new_lens.data_ptr(), self.status.data_ptr(),
+                                      kept.data_ptr(), new_lens.data_ptr(), self._status_ptr,
                                       self._raw_stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_cache_evict")
