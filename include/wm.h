@@ -427,6 +427,119 @@ wm_status wm_cache_evict(const wm_config* cfg, const wm_cache* cache, const floa
                          int32_t* dev_status, void* stream);
 
 /*
+ * A cache held in 4 bits (no counterpart in the paper): 9/32 of the bytes of a
+ * bf16 cache, to hold and to read.  A row of d elements (the key or the value of
+ * one slot and kv head) is d signed 4-bit floats and one scale per 16 of them:
+ * element = code * scale.
+ *   code   bit 3 the sign, bits 2-0 the magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6
+ *   scale  8 bits, 5 of exponent and 3 of mantissa: the fp16 with the bits
+ *          byte << 7; at most 10240 (byte 226).  0xFF: not a number
+ * Rounding: scale = the nearest one to (largest magnitude of the 16) / 6, code = the
+ * nearest one to element / scale, both with ties to the even bit pattern; larger
+ * magnitudes than 6 * 10240 become that, 16 elements below 6 * 2^-18 become zeros.
+ * A code's sign bit is its element's, also where the magnitude becomes 0 (not where the
+ * scale is 0).  16 elements of which one is NaN or infinite become NaN.  An element of
+ * normal rows is off by 9.5% of their root mean square, in the root mean square.
+ * Every value is exact in fp16, bf16 and fp32: attention reads what wm_q4_read returns,
+ * and (for scales from 2^-15 on) writing that again holds the same.
+ *
+ * Layout, for channel c, page and kv head h, from byte
+ *   ((c * num_pages + page) * Hkv + h) * (P / n) * tile
+ * on, with P = page_size, n = min(P, 16) slots per tile and tile = n * (d + d / 8)
+ * bytes, padded to a multiple of 16: P / n tiles, each
+ *   codes of n K rows [n][d / 2] (element 2 i in bits 3-0 of byte i, 2 i + 1 in bits
+ *   7-4), codes of n V rows, scales of n K rows [n][d / 16], scales of n V rows.
+ * Slots, page tables and channels are those of wm_cache; element types of rows,
+ * queries and outputs are the config's.  The calls below work for both types, every
+ * head size, group size and page size; num_pages * Hkv * page_size / n is at most
+ * 2^31 - 1 (else WM_ERR_UNSUPPORTED).
+ */
+typedef struct {
+  void* pool;                            /* device                              */
+  int32_t num_pages;                     /* physical pages per channel          */
+  int32_t k, Hkv, page_size, d;          /* copied from the config, checked per call */
+} wm_q4_cache;
+
+/* Bytes of a 4-bit cache of num_pages pages per channel (0: bad arguments). */
+size_t wm_q4_cache_bytes(const wm_config* cfg, int32_t num_pages);
+
+/* Describe a 4-bit cache in a caller buffer, 256-byte aligned; nothing is
+ * written to it.  Errors as wm_cache_alloc. */
+wm_status wm_q4_cache_alloc(const wm_config* cfg, void* dev_buf, size_t bytes, int32_t num_pages,
+                            wm_q4_cache* out);
+
+/*
+ * Write rows of a cache to a 4-bit cache: slots first[b] .. last[b] - 1 of every
+ * sequence, all channels and heads, K and V.  For prompts behind their prefill, and
+ * for tokens as they are appended (wm_q4_kv_mix does both steps of that).
+ *   page_table   device int32 [B][max_pages]: pages of the cache
+ *   q4_table     device int32 [B][max_pages]: pages of the 4-bit cache
+ *   first, last  device int32 [B], 0 <= first <= last <= max_pages*page_size
+ *   span         no range is longer; the launch is sized by it (1: one token per
+ *                sequence).  A longer range is cut to it and sets WM_ERR_BOUNDS
+ * Other slots of the 4-bit cache keep what they hold.  A bad range is left out, a
+ * bad page id (in either table) leaves its slots out; both set WM_ERR_BOUNDS.
+ * B = 0 or span = 0 is a no-op.
+ */
+wm_status wm_q4_write(const wm_config* cfg, const wm_cache* cache, const int32_t* page_table,
+                      const wm_q4_cache* q4, const int32_t* q4_table, const int32_t* first,
+                      const int32_t* last, int32_t span, int32_t B, int32_t max_pages,
+                      int32_t* dev_status, void* stream);
+
+/* The reverse: slots first[b] .. last[b] - 1 of the 4-bit cache as rows of a cache,
+ * whose other slots keep what they hold.  Arguments as wm_q4_write. */
+wm_status wm_q4_read(const wm_config* cfg, const wm_q4_cache* q4, const int32_t* q4_table,
+                     const wm_cache* cache, const int32_t* page_table, const int32_t* first,
+                     const int32_t* last, int32_t span, int32_t B, int32_t max_pages,
+                     int32_t* dev_status, void* stream);
+
+/* Workspace bytes of wm_q4_decode_attn (0 for bad arguments). */
+size_t wm_q4_decode_attn_workspace(const wm_config* cfg, int32_t B, int32_t max_pages);
+
+/*
+ * Decode attention of one layer over a 4-bit cache: as wm_decode_attn, of the
+ * values that the codes stand for; softmax and accumulation in fp32.  bf16
+ * configs round the softmax weights to fp16 for the products (weights below 2^-22 of the
+ * largest to a multiple of 2^-32 of it).
+ *   q, out      device [B][Hq][d], 16-byte aligned
+ *   page_table  device int32 [B][max_pages]
+ *   seq_lens    device int32 [B], 0 <= seq_lens[b] <= max_pages*page_size; 0 gives
+ *               rows of zeros
+ *   workspace   device, >= wm_q4_decode_attn_workspace(cfg, B, max_pages) bytes,
+ *               256-byte aligned, no contents required; calls that share one must
+ *               not overlap on the GPU
+ * A bad length zero-fills its rows, a bad page id leaves its slots out; both set
+ * WM_ERR_BOUNDS.  Slots at or beyond seq_lens[b] may hold anything.  B = 0 is a no-op;
+ * B above 4096 returns WM_ERR_UNSUPPORTED.
+ */
+wm_status wm_q4_decode_attn(const wm_config* cfg, const wm_q4_cache* q4, int32_t layer, const void* q,
+                            const int32_t* page_table, const int32_t* seq_lens, int32_t B,
+                            int32_t max_pages, void* out, void* workspace, size_t ws_bytes,
+                            int32_t* dev_status, void* stream);
+
+/* Workspace bytes of wm_q4_rows_attn (0 for bad arguments). */
+size_t wm_q4_rows_attn_workspace(const wm_config* cfg, int32_t B, int32_t Tq, int32_t max_pages);
+
+/*
+ * Causal attention of several positions per sequence over a 4-bit cache, as
+ * wm_prefill_attn: the query at position i = pos[b][r] sees slots 0 .. i.  For drafted
+ * tokens that are checked at once, and for a prompt's next tokens.
+ *   q, out     device [B][Tq][Hq][d], 16-byte aligned
+ *   pos        device int32 [B][Tq], 0 <= pos < max_pages*page_size, any order
+ *   workspace  device, >= wm_q4_rows_attn_workspace(cfg, B, Tq, max_pages) bytes,
+ *              256-byte aligned, no contents required; calls that share one must
+ *              not overlap on the GPU
+ * A bad position zero-fills its row, a bad page id leaves its slots out; both set
+ * WM_ERR_BOUNDS.  Slots that no row of the call sees may hold anything, one that a row
+ * sees must hold numbers.  B = 0 or Tq = 0 is a no-op; B above 4096 returns
+ * WM_ERR_UNSUPPORTED.
+ */
+wm_status wm_q4_rows_attn(const wm_config* cfg, const wm_q4_cache* q4, int32_t layer, const void* q,
+                          const int32_t* pos, const int32_t* page_table, int32_t B, int32_t Tq,
+                          int32_t max_pages, void* out, void* workspace, size_t ws_bytes,
+                          int32_t* dev_status, void* stream);
+
+/*
  * Self-test of the kernels' failure detection (no counterpart in the paper).
  * Every pipeline wait in this library is bounded; when a wait runs out the
  * kernel writes WM_ERR_TIMEOUT to the status word and returns instead of

@@ -21,7 +21,9 @@ EXPORTED = ["wm_status_string", "wm_config_check", "wm_cache_bytes", "wm_cache_a
             "wm_decode_attn_flags", "wm_decode_attn_plan", "wm_prefill_attn",
             "wm_kv_mix_launches", "wm_kv_mix_at", "wm_window_attn", "wm_window_prefill_attn",
             "wm_prefix_attn_workspace", "wm_prefix_attn", "wm_decode_attn_mass_workspace",
-            "wm_decode_attn_mass", "wm_cache_evict"]
+            "wm_decode_attn_mass", "wm_cache_evict", "wm_q4_cache_bytes", "wm_q4_cache_alloc",
+            "wm_q4_write", "wm_q4_read", "wm_q4_decode_attn_workspace", "wm_q4_decode_attn",
+            "wm_q4_rows_attn_workspace", "wm_q4_rows_attn"]
 WM_ATTN_INPUTS_READY = 1
 WM_ATTN_DYNAMIC_SPLIT = 2
 WM_ATTN_UNIT_SPLIT = 4
@@ -40,6 +42,11 @@ class wm_cache(ctypes.Structure):
     _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p),
                 ("num_pages", ctypes.c_int32), ("k", ctypes.c_int32), ("Hkv", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class wm_q4_cache(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("page_size", ctypes.c_int32), ("d", ctypes.c_int32)]
 
 
 class wm_mix_weights(ctypes.Structure):
@@ -113,6 +120,23 @@ def lib():
         L.wm_decode_attn_mass.argtypes = [cp, ccp, i32, vp, vp, vp, vp, i32, i32, vp, vp, sz, vp, vp]
         L.wm_cache_evict.restype = ctypes.c_int
         L.wm_cache_evict.argtypes = [cp, ccp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp]
+        qcp = ctypes.POINTER(wm_q4_cache)
+        L.wm_q4_cache_bytes.restype = sz
+        L.wm_q4_cache_bytes.argtypes = [cp, i32]
+        L.wm_q4_cache_alloc.restype = ctypes.c_int
+        L.wm_q4_cache_alloc.argtypes = [cp, vp, sz, i32, qcp]
+        L.wm_q4_write.restype = ctypes.c_int
+        L.wm_q4_write.argtypes = [cp, ccp, vp, qcp, vp, vp, vp, i32, i32, i32, vp, vp]
+        L.wm_q4_read.restype = ctypes.c_int
+        L.wm_q4_read.argtypes = [cp, qcp, vp, ccp, vp, vp, vp, i32, i32, i32, vp, vp]
+        L.wm_q4_decode_attn_workspace.restype = sz
+        L.wm_q4_decode_attn_workspace.argtypes = [cp, i32, i32]
+        L.wm_q4_decode_attn.restype = ctypes.c_int
+        L.wm_q4_decode_attn.argtypes = [cp, qcp, i32, vp, vp, vp, i32, i32, vp, vp, sz, vp, vp]
+        L.wm_q4_rows_attn_workspace.restype = sz
+        L.wm_q4_rows_attn_workspace.argtypes = [cp, i32, i32, i32]
+        L.wm_q4_rows_attn.restype = ctypes.c_int
+        L.wm_q4_rows_attn.argtypes = [cp, qcp, i32, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp, vp]
         _lib = L
     return _lib
 
@@ -272,6 +296,55 @@ def wm_cache_evict(cfg, cache, mass, mass_out, page_table, seq_lens, budget, sin
     return lib().wm_cache_evict(ctypes.byref(cfg), ctypes.byref(cache), _p(mass), _p(mass_out),
                                 _p(page_table), _p(seq_lens), budget, sinks, recent, B, max_pages,
                                 _p(kept), _p(new_lens), _p(dev_status), stream)
+
+
+def wm_q4_cache_bytes(cfg, num_pages) -> int:
+    return int(lib().wm_q4_cache_bytes(ctypes.byref(cfg), int(num_pages)))
+
+
+def wm_q4_cache_alloc(cfg, dev_buf, nbytes, num_pages) -> wm_q4_cache:
+    out = wm_q4_cache()
+    rc = lib().wm_q4_cache_alloc(ctypes.byref(cfg), _p(dev_buf), int(nbytes), int(num_pages),
+                                 ctypes.byref(out))
+    if rc != WM_OK:
+        raise WMError(rc, "wm_q4_cache_alloc")
+    return out
+
+
+def wm_q4_write(cfg, cache, page_table, q4, q4_table, first, last, span, B, max_pages, dev_status,
+                stream) -> int:
+    return lib().wm_q4_write(ctypes.byref(cfg), ctypes.byref(cache), _p(page_table), ctypes.byref(q4),
+                             _p(q4_table), _p(first), _p(last), span, B, max_pages, _p(dev_status),
+                             stream)
+
+
+def wm_q4_read(cfg, q4, q4_table, cache, page_table, first, last, span, B, max_pages, dev_status,
+               stream) -> int:
+    return lib().wm_q4_read(ctypes.byref(cfg), ctypes.byref(q4), _p(q4_table), ctypes.byref(cache),
+                            _p(page_table), _p(first), _p(last), span, B, max_pages, _p(dev_status),
+                            stream)
+
+
+def wm_q4_decode_attn_workspace(cfg, B, max_pages) -> int:
+    return int(lib().wm_q4_decode_attn_workspace(ctypes.byref(cfg), int(B), int(max_pages)))
+
+
+def wm_q4_decode_attn(cfg, q4, layer, q, page_table, seq_lens, B, max_pages, out, workspace, ws_bytes,
+                      dev_status, stream) -> int:
+    return lib().wm_q4_decode_attn(ctypes.byref(cfg), ctypes.byref(q4), layer, _p(q), _p(page_table),
+                                   _p(seq_lens), B, max_pages, _p(out), _p(workspace), ws_bytes,
+                                   _p(dev_status), stream)
+
+
+def wm_q4_rows_attn_workspace(cfg, B, Tq, max_pages) -> int:
+    return int(lib().wm_q4_rows_attn_workspace(ctypes.byref(cfg), int(B), int(Tq), int(max_pages)))
+
+
+def wm_q4_rows_attn(cfg, q4, layer, q, pos, page_table, B, Tq, max_pages, out, workspace, ws_bytes,
+                    dev_status, stream) -> int:
+    return lib().wm_q4_rows_attn(ctypes.byref(cfg), ctypes.byref(q4), layer, _p(q), _p(pos),
+                                 _p(page_table), B, Tq, max_pages, _p(out), _p(workspace), ws_bytes,
+                                 _p(dev_status), stream)
 
 
 def wm_decode_attn_noalloc(cfg, cache, layer, q, page_table, seq_lens, B, max_pages, out,

@@ -1,0 +1,90 @@
+// The 4-bit paged cache: layout and launch interfaces (q4_copy.cu, q4_attn.cuh).
+//
+// A row of d elements (a key or a value of one slot and kv head) is d signed
+// 4-bit floats and a scale per 16 of them; value = code * scale.
+//   code    bit 3 the sign, bits 2-0 the magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6
+//   scale   8 bits, 5 of exponent and 3 of mantissa: the fp16 of bits byte << 7,
+//           so 2^-17 .. 10240; 0xFF (NaN) for 16 elements that are not all finite
+// The scale is the nearest one (ties to even) to the largest magnitude of the 16
+// over 6, each code the nearest (ties to even) to its element over the scale.  A
+// code has 2 significant bits and a scale 4, so every value is exact in fp16 and in
+// bf16, whatever the element type the row came from.
+//
+// Slots are held in tiles of n = min(page_size, 16): codes of the K rows [n][d/2]
+// (element 2 i in the low half of byte i), codes of the V rows, scales of the K rows
+// [n][d/16], scales of the V rows, padded to 16 bytes.  So 16 slots (or a small
+// page) of one head are one contiguous piece (2304 bytes for d = 128) that one bulk
+// copy fetches, 9/32 of the bf16 cache's bytes.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "wm.h"
+
+namespace wm {
+
+constexpr int kQ4Group = 16;       // elements that share a scale
+constexpr int kQ4Step = 16;        // slots of a whole tile
+constexpr int kQ4MaxScale = 226;   // byte of 10240: 6 * 10240 is below the largest fp16
+
+inline int q4_tile_slots(int page_size) { return page_size < kQ4Step ? page_size : kQ4Step; }
+inline int64_t q4_tile_bytes(int page_size, int d) {
+  return ((int64_t)q4_tile_slots(page_size) * 2 * (d / 2 + d / kQ4Group) + 15) / 16 * 16;
+}
+inline int64_t q4_page_bytes(int page_size, int d) {  // of one kv head
+  return page_size / q4_tile_slots(page_size) * q4_tile_bytes(page_size, d);
+}
+
+// Where the rows of a copy are.
+enum Q4Rows : int32_t {
+  kQ4Paged = 0,   // a cache, through row_table
+  kQ4Staged = 1,  // [k][B][Hkv][d]: one row per sequence, of its slot `first`
+  kQ4Dense = 2    // one channel, pages b * max_pages + t / page_size
+};
+
+struct Q4CopyParams {
+  void* k_rows;               // rows of the element type
+  void* v_rows;
+  uint8_t* pool;              // 4-bit pool (read: of the first channel copied)
+  const int32_t* row_table;   // [B][max_pages] (kQ4Paged)
+  const int32_t* q4_table;    // [B][max_pages]
+  const int32_t* first;       // [B]: slots first .. last - 1 (NULL: from 0)
+  const int32_t* last;        // [B] (NULL: one slot, `first`, at least slot 1)
+  int32_t* status;
+  int64_t page_bytes;         // of one kv head
+  int32_t rows_at;            // Q4Rows
+  int32_t B, k, Hkv, P, log2P, tile, log2tile, tile_bytes, row_pages, q4_pages, max_pages;
+  int32_t span;               // slots of a range at most
+  int32_t steps;              // tiles of 16 slots that a range touches at most
+};
+cudaError_t launch_q4_write(const Q4CopyParams& p, int dtype, int d, int sms, cudaStream_t s);
+cudaError_t launch_q4_read(const Q4CopyParams& p, int dtype, int d, int sms, cudaStream_t s);
+
+// ------------------------------------------------------------ attention
+constexpr int kQ4Warps = 4;        // warps per CTA
+constexpr int kQ4MaxCluster = 8;
+constexpr int kQ4MaxPieces = 64;
+constexpr int kQ4CtasPerSm = 4;
+
+struct Q4AttnParams {
+  const uint8_t* pool;        // channel base
+  const void* q;              // [B][Tq][Hq][d]
+  void* out;
+  const int32_t* page_table;  // [B][max_pages]
+  const int32_t* lens;        // [B][Tq]: the row sees slots t < lens + len_add
+  int32_t* status;
+  float* part;                // [units][pieces][q4_rec] where a second kernel joins
+  int64_t page_bytes;         // of one kv head
+  int32_t len_add;
+  int32_t B, Tq, Hq, Hkv, G, P, log2P, tile, log2tile, tile_bytes, num_pages, max_pages;
+  int32_t col_blocks;         // units per (sequence, kv head): groups of 8 NB (row, head) columns
+  int32_t nb;                 // NB
+  int32_t pieces;             // CTAs per unit
+  float qscale;               // log2(e) / sqrt(d)
+};
+// floats of a partial record: cols x d unnormalised outputs, (reference, sum) per column
+constexpr int q4_rec(int cols, int d) { return cols * (d + 2); }
+cudaError_t launch_q4_attn(const Q4AttnParams& p, int dtype, int d, cudaStream_t s);
+
+}  // namespace wm

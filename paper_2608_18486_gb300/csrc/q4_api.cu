@@ -1,0 +1,244 @@
+// C ABI of the cache held in 4 bits (declared in include/wm.h): its layout, rows
+// of a cache to 4 bits and back, the pool appended in 4 bits, and attention over
+// it.  Argument checks, work splits and kernel dispatch; all device memory
+// belongs to the caller.
+#include <math.h>
+#include <string.h>
+
+#include "api_util.h"
+#include "internal.h"
+#include "q4.h"
+#include "range_attn.h"
+#include "wm.h"
+
+namespace wm {
+
+cudaError_t launch_q4_attn_bf16(const Q4AttnParams& p, int d, cudaStream_t s);
+cudaError_t launch_q4_attn_f32(const Q4AttnParams& p, int d, cudaStream_t s);
+
+cudaError_t launch_q4_attn(const Q4AttnParams& p, int dtype, int d, cudaStream_t s) {
+  return dtype == WM_DT_F32 ? launch_q4_attn_f32(p, d, s) : launch_q4_attn_bf16(p, d, s);
+}
+
+}  // namespace wm
+
+namespace {
+
+using namespace wm;
+
+constexpr int kMaxBatch = 4096;
+
+wm_status cuda_status(cudaError_t e) { return e == cudaSuccess ? WM_OK : WM_ERR_CUDA; }
+
+// The 4-bit cache belongs to the config and is usable.
+wm_status check_q4(const wm_config& c, const wm_q4_cache* q4) {
+  if (!q4 || !q4->pool || q4->num_pages < 1 || !aligned(q4->pool, 16)) return WM_ERR_INVALID_ARG;
+  if (q4->k != c.k || q4->Hkv != c.Hkv || q4->page_size != c.page_size || q4->d != c.d) return WM_ERR_INVALID_ARG;
+  // 32-bit tiles per channel
+  if ((int64_t)q4->num_pages * c.Hkv * (c.page_size / q4_tile_slots(c.page_size)) > INT32_MAX) return WM_ERR_UNSUPPORTED;
+  return WM_OK;
+}
+
+// Checks of every call that takes a 4-bit cache, its page table and a batch.
+wm_status check_call(const wm_config* c, const wm_q4_cache* q4, int32_t B, int32_t max_pages) {
+  wm_status st = wm_config_check(c);
+  if (st != WM_OK) return st;
+  if ((st = check_q4(*c, q4)) != WM_OK) return st;
+  if (B < 0 || max_pages < 1) return WM_ERR_INVALID_ARG;
+  if ((int64_t)max_pages * c->page_size > INT32_MAX / 2) return WM_ERR_INVALID_ARG;
+  return WM_OK;
+}
+
+size_t channel_bytes(const wm_config& c, int32_t num_pages) {
+  return (size_t)num_pages * c.Hkv * q4_page_bytes(c.page_size, c.d);
+}
+
+Q4CopyParams copy_params(const wm_config& c, const wm_q4_cache& q4, int32_t B, int32_t max_pages, int32_t span,
+                         int32_t* dev_status) {
+  Q4CopyParams p{};
+  p.pool = (uint8_t*)q4.pool;
+  p.status = dev_status;
+  p.page_bytes = q4_page_bytes(c.page_size, c.d);
+  p.B = B;
+  p.k = c.k;
+  p.Hkv = c.Hkv;
+  p.P = c.page_size;
+  p.log2P = ilog2(c.page_size);
+  p.tile = q4_tile_slots(c.page_size);
+  p.log2tile = ilog2(p.tile);
+  p.tile_bytes = (int32_t)q4_tile_bytes(c.page_size, c.d);
+  p.q4_pages = q4.num_pages;
+  p.max_pages = max_pages;
+  p.span = span;
+  p.steps = (span + 2 * kQ4Step - 2) / kQ4Step;  // a range may start and end inside a tile
+  return p;
+}
+
+wm_status copy_ranges(bool write, const wm_config* c, const wm_cache* cache, const int32_t* table,
+                      const wm_q4_cache* q4, const int32_t* q4_table, const int32_t* first, const int32_t* last,
+                      int32_t span, int32_t B, int32_t max_pages, int32_t* dev_status, void* stream) {
+  wm_status st = check_call(c, q4, B, max_pages);
+  if (st != WM_OK) return st;
+  if ((st = check_cache(*c, cache)) != WM_OK) return st;
+  if (span < 0) return WM_ERR_INVALID_ARG;
+  if (B == 0 || span == 0) return WM_OK;
+  if (!table || !q4_table || !first || !last) return WM_ERR_INVALID_ARG;
+  const int32_t slots = max_pages * c->page_size;
+  Q4CopyParams p = copy_params(*c, *q4, B, max_pages, span < slots ? span : slots, dev_status);
+  if ((int64_t)p.k * B * p.steps * p.Hkv > INT32_MAX / 2) return WM_ERR_UNSUPPORTED;
+  p.k_rows = cache->k_pool;
+  p.v_rows = cache->v_pool;
+  p.row_table = table;
+  p.q4_table = q4_table;
+  p.first = first;
+  p.last = last;
+  p.rows_at = kQ4Paged;
+  p.row_pages = cache->num_pages;
+  return cuda_status(write ? launch_q4_write(p, c->dtype, c->d, sm_count(), (cudaStream_t)stream)
+                           : launch_q4_read(p, c->dtype, c->d, sm_count(), (cudaStream_t)stream));
+}
+
+// Split of an attention call: columns per unit, CTAs per unit, and whether these
+// join on chip (a cluster) or through records in the workspace.
+struct Q4Plan {
+  int nb, col_blocks, pieces;
+  bool records;
+  size_t total;  // workspace
+};
+
+int clamp_int(int64_t x, int64_t lo, int64_t hi) { return (int)(x < lo ? lo : x > hi ? hi : x); }
+
+constexpr int kLongSteps = 24;  // steps of a warp from which a unit is cut into records
+constexpr int kMinSteps = 8;    // steps that a cut leaves each warp at least
+constexpr int kWaves = 4;       // waves of resident CTAs that a cut aims at
+
+Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
+  const int64_t cols = (int64_t)Tq * (c.Hq / c.Hkv);
+  Q4Plan pl{};
+  pl.nb = cols > 8 && c.dtype == WM_DT_BF16 ? 2 : 1;
+  pl.col_blocks = (int)((cols + 8 * pl.nb - 1) / (8 * pl.nb));
+  const int64_t units = (int64_t)B * c.Hkv * pl.col_blocks;
+  const int64_t steps = ((int64_t)max_pages * c.page_size + kQ4Step - 1) / kQ4Step;
+  const int64_t resident = (int64_t)sm_count() * (pl.nb == 1 && c.dtype == WM_DT_BF16 ? kQ4CtasPerSm : 2);
+  int C = 1;
+  while (C < kQ4MaxCluster && units * C * 2 <= resident && (int64_t)C * kQ4Warps < steps) C *= 2;
+  pl.pieces = C;
+  pl.total = 256;
+  if (steps > (int64_t)C * kQ4Warps * kLongSteps) {
+    const int64_t by_work = steps / (kQ4Warps * kMinSteps), by_sms = (resident * kWaves + units - 1) / units;
+    const int n = clamp_int(by_work < by_sms ? by_work : by_sms, 1, kQ4MaxPieces);
+    if (n > C) {
+      pl.pieces = n;
+      pl.records = true;
+      pl.total = align256(sizeof(float) * (size_t)units * n * q4_rec(8 * pl.nb, c.d));
+    }
+  }
+  return pl;
+}
+
+wm_status attn(const wm_config& c, const wm_q4_cache& q4, int32_t layer, const void* q, const int32_t* page_table,
+               const int32_t* lens, int32_t len_add, int32_t B, int32_t Tq, int32_t max_pages, void* out,
+               void* workspace, size_t ws_bytes, int32_t* dev_status, void* stream) {
+  if (!q || !page_table || !lens || !out || !workspace) return WM_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256)) return WM_ERR_INVALID_ARG;
+  const Q4Plan pl = attn_plan(c, B, Tq, max_pages);
+  if (ws_bytes < pl.total) return WM_ERR_INVALID_ARG;
+  Q4AttnParams p{};
+  p.pool = (const uint8_t*)q4.pool + c.chan_of_layer[layer] * channel_bytes(c, q4.num_pages);
+  p.q = q;
+  p.out = out;
+  p.page_table = page_table;
+  p.lens = lens;
+  p.status = dev_status;
+  p.part = pl.records ? (float*)workspace : nullptr;
+  p.page_bytes = q4_page_bytes(c.page_size, c.d);
+  p.len_add = len_add;
+  p.B = B;
+  p.Tq = Tq;
+  p.Hq = c.Hq;
+  p.Hkv = c.Hkv;
+  p.G = c.Hq / c.Hkv;
+  p.P = c.page_size;
+  p.log2P = ilog2(c.page_size);
+  p.tile = q4_tile_slots(c.page_size);
+  p.log2tile = ilog2(p.tile);
+  p.tile_bytes = (int32_t)q4_tile_bytes(c.page_size, c.d);
+  p.num_pages = q4.num_pages;
+  p.max_pages = max_pages;
+  p.col_blocks = pl.col_blocks;
+  p.nb = pl.nb;
+  p.pieces = pl.pieces;
+  p.qscale = (float)(1.4426950408889634 / sqrt((double)c.d));
+  return cuda_status(launch_q4_attn(p, c.dtype, c.d, (cudaStream_t)stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t wm_q4_cache_bytes(const wm_config* c, int32_t num_pages) {
+  if (wm_config_check(c) != WM_OK || num_pages < 1) return 0;
+  return align256(c->k * channel_bytes(*c, num_pages));
+}
+
+wm_status wm_q4_cache_alloc(const wm_config* c, void* dev_buf, size_t bytes, int32_t num_pages, wm_q4_cache* out) {
+  wm_status st = wm_config_check(c);
+  if (st != WM_OK) return st;
+  if (!dev_buf || !out || num_pages < 1 || !aligned(dev_buf, 256)) return WM_ERR_INVALID_ARG;
+  // (the padding behind the last channel is not read)
+  if (bytes < c->k * channel_bytes(*c, num_pages)) return WM_ERR_INVALID_ARG;
+  memset(out, 0, sizeof *out);
+  out->pool = dev_buf;
+  out->num_pages = num_pages;
+  out->k = c->k;
+  out->Hkv = c->Hkv;
+  out->page_size = c->page_size;
+  out->d = c->d;
+  return WM_OK;
+}
+
+wm_status wm_q4_write(const wm_config* c, const wm_cache* cache, const int32_t* page_table, const wm_q4_cache* q4,
+                      const int32_t* q4_table, const int32_t* first, const int32_t* last, int32_t span, int32_t B,
+                      int32_t max_pages, int32_t* dev_status, void* stream) {
+  return copy_ranges(true, c, cache, page_table, q4, q4_table, first, last, span, B, max_pages, dev_status, stream);
+}
+
+wm_status wm_q4_read(const wm_config* c, const wm_q4_cache* q4, const int32_t* q4_table, const wm_cache* cache,
+                     const int32_t* page_table, const int32_t* first, const int32_t* last, int32_t span, int32_t B,
+                     int32_t max_pages, int32_t* dev_status, void* stream) {
+  return copy_ranges(false, c, cache, page_table, q4, q4_table, first, last, span, B, max_pages, dev_status, stream);
+}
+
+size_t wm_q4_decode_attn_workspace(const wm_config* c, int32_t B, int32_t max_pages) {
+  return wm_q4_rows_attn_workspace(c, B, 1, max_pages);
+}
+
+wm_status wm_q4_decode_attn(const wm_config* c, const wm_q4_cache* q4, int32_t layer, const void* q,
+                            const int32_t* page_table, const int32_t* seq_lens, int32_t B, int32_t max_pages,
+                            void* out, void* workspace, size_t ws_bytes, int32_t* dev_status, void* stream) {
+  wm_status st = check_call(c, q4, B, max_pages);
+  if (st != WM_OK) return st;
+  if (layer < 0 || layer >= c->L) return WM_ERR_INVALID_ARG;
+  if (B == 0) return WM_OK;
+  if (B > kMaxBatch || (int64_t)B * c->Hq > INT32_MAX / 2) return WM_ERR_UNSUPPORTED;
+  return attn(*c, *q4, layer, q, page_table, seq_lens, 0, B, 1, max_pages, out, workspace, ws_bytes, dev_status, stream);
+}
+
+size_t wm_q4_rows_attn_workspace(const wm_config* c, int32_t B, int32_t Tq, int32_t max_pages) {
+  if (wm_config_check(c) != WM_OK || B < 0 || Tq < 0 || max_pages < 1) return 0;
+  if (B == 0 || Tq == 0) return 256;
+  return attn_plan(*c, B, Tq, max_pages).total;
+}
+
+wm_status wm_q4_rows_attn(const wm_config* c, const wm_q4_cache* q4, int32_t layer, const void* q, const int32_t* pos,
+                          const int32_t* page_table, int32_t B, int32_t Tq, int32_t max_pages, void* out,
+                          void* workspace, size_t ws_bytes, int32_t* dev_status, void* stream) {
+  wm_status st = check_call(c, q4, B, max_pages);
+  if (st != WM_OK) return st;
+  if (layer < 0 || layer >= c->L || Tq < 0) return WM_ERR_INVALID_ARG;
+  if (B == 0 || Tq == 0) return WM_OK;
+  if (B > kMaxBatch || (int64_t)B * Tq > INT32_MAX / 2 / c->Hq) return WM_ERR_UNSUPPORTED;
+  return attn(*c, *q4, layer, q, page_table, pos, 1, B, Tq, max_pages, out, workspace, ws_bytes, dev_status, stream);
+}
+
+}  // extern "C"

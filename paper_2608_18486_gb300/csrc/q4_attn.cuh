@@ -1,0 +1,739 @@
+#pragma once
+// Attention of a few query rows over a cache held in 4 bits (layout in q4.h):
+// decode attention, and several positions per sequence at once.
+//
+//   out_c = sum_t p_ct v_t,  p_ct = 2^(x_ct - m_c) / l_c,  x_ct = (q_c . k_t) log2(e) / sqrt(d)
+//   over the slots t below column c's limit.  A column is one (row, query head) pair
+//   that reads a kv head; sums (m, l, sum_t 2^(x - m) v_t) of disjoint slot sets
+//   join for any references m.
+//
+// A unit is one (sequence, kv head) and 8 NB of its columns.  `pieces` CTAs of 4
+// warps share a unit; each warp takes a contiguous part of its steps of 16 slots
+// through a private ring of bulk copies (one per step: a step is one contiguous
+// tile; one per page for pages below 16 slots).
+//
+// Both products are mma.sync m16n8k16 with the 8 columns as the narrow operand:
+//   S^T [16 slots x 8 columns] += K [16 x d] Q^T,   O^T [d x 8] += V^T [d x 16] P^T,
+// so a step costs d / 8 of them for up to 8 columns.  The values of the cache are exact
+// in fp16: a pair of codes becomes an fp16 pair in one conversion and one product
+// with the scale.  For S^T a lane takes consecutive features of one slot, for O^T the same
+// features of two slots, whose codes are first interleaved (byte = feature, halves =
+// slots).  P^T is the transpose of S^T's accumulators: movmatrix.
+//  * bf16: the columns' queries are scaled by a power of two so that they keep all
+//    8 bits in fp16; P is rounded to fp16 (11 bits) against a reference 2^8 below
+//    the running maximum, so that weights down to 2^-22 of the largest keep
+//    them, and the reference moves only when a score passes it by 2^15.
+//  * fp32: queries in three fp16 parts and P in two; each feature block's products
+//    start at zero and are added with rounding, since a matrix instruction
+//    truncates its sums.
+// One byte of cache costs 3.6 values to unpack: at HBM's rate the conversions take half of
+// the SM's rate (41 of 82 values a cycle), the matrix instructions a third.
+#include <cooperative_groups.h>
+#include <float.h>
+#include <math.h>
+
+#include "common.cuh"
+#include "internal.h"
+#include "q4.h"
+
+namespace wm {
+namespace q4_detail {
+
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = kQ4Warps * 32;
+constexpr int kStages = 4;         // ring depth per warp
+constexpr float kHead = 8.f;       // log2 of the weight of a new reference maximum
+constexpr float kRaise = 15.f;     // log2 of the weight that moves the reference
+constexpr unsigned FULL = 0xFFFFFFFFu;
+
+template <int HD>
+struct Shape {
+  static constexpr int KW = HD / 32;                 // words of 8 codes per lane and K row
+  static constexpr int MT = HD / 16;                 // 16-feature blocks
+  static constexpr int TILE = 16 * (HD + HD / 8);    // bytes of a whole tile
+  // a step of small pages: each tile is padded to 16 bytes
+  static constexpr int STEP = 16 * ((HD + HD / 8 + 15) / 16 * 16);
+};
+template <typename T>
+struct Parts {
+  static constexpr int Q = sizeof(T) == 4 ? 3 : 1, P = sizeof(T) == 4 ? 2 : 1;
+};
+
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                    uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The 8 x 8 matrix of 16-bit elements, row lane / 4, columns 2 (lane % 4) + {0, 1}, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// The four bytes of w, two codes each, to fp16 pairs (low half first).
+__device__ __forceinline__ void codes4(uint32_t w, uint32_t (&r)[4]) {
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "mov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+      : "r"(w));
+}
+__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float2 floats_of(uint32_t h) {
+  float2 f;
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}"
+      : "=f"(f.x), "=f"(f.y)
+      : "r"(h));
+  return f;
+}
+// Two neighbouring fp16 of the parts: hi + mid + lo = x to 2^-33 of the largest |x|.
+template <int N>
+__device__ __forceinline__ void split(float x, float y, uint32_t (&part)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    part[i] = half2_of(x, y);
+    if (i + 1 < N) {
+      const float2 f = floats_of(part[i]);
+      x -= f.x;
+      y -= f.y;
+    }
+  }
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+
+// First of the two neighbouring features of accumulator block m of lane row g.
+template <int HD>
+__device__ __forceinline__ int feature(int g, int m) {
+  if (HD == 128) return 16 * g + 2 * m;
+  if (HD == 64 || m < 4) return 8 * g + 2 * m;
+  return 64 + 4 * g + 2 * (m - 4);
+}
+
+// One warp's columns.  Lane: g = lane / 4, c = lane % 4.
+template <typename T, int HD, int NB>
+struct Math {
+  using SH = Shape<HD>;
+  static constexpr int NQ = Parts<T>::Q, NP = Parts<T>::P;
+  uint32_t q[NB][NQ][SH::MT][2];  // column g: features (HD / 4) c + 8 w + 4 u + {0, 1}, {2, 3} at [2 w + u]
+  float o[NB][SH::MT][4];         // features feature(g, m) (+ 1), columns 2 c, 2 c + 1
+  float ref[NB][2], l[NB][2];     // columns 2 c, 2 c + 1; l: this lane's slots only
+  float mul[NB][2];               // accumulator to score
+  int lim[NB][2];
+
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+#pragma unroll
+      for (int m = 0; m < SH::MT; ++m) o[n][m][0] = o[n][m][1] = o[n][m][2] = o[n][m][3] = 0.f;
+      ref[n][0] = ref[n][1] = -FLT_MAX;
+      l[n][0] = l[n][1] = 0.f;
+    }
+  }
+
+  // Column g of block n: row (NULL: none) and limit.
+  __device__ __forceinline__ void load(int n, const T* row, int limit, int lane, float qscale) {
+    const int c = lane & 3;
+    float x[HD / 4], top = 0.f;
+#pragma unroll
+    for (int i = 0; i < HD / 4; i += 16 / (int)sizeof(T)) {
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (row) v = __ldcg(reinterpret_cast<const uint4*>(row + HD / 4 * c + i));
+      Elem<T>::unpack(v, x + i);
+    }
+#pragma unroll
+    for (int i = 0; i < HD / 4; ++i) top = fmaxf(top, fabsf(x[i]));
+    top = fmaxf(top, __shfl_xor_sync(FULL, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(FULL, top, 2));
+    // largest magnitude to [2^14, 2^15): an exact product, undone by `mul`
+    const int field = min(268 - (int)(__float_as_uint(top) >> 23), 253);
+    const float up = __uint_as_float((uint32_t)field << 23);
+#pragma unroll
+    for (int j = 0; j < SH::MT; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint32_t part[NQ];
+        split(x[4 * j + 2 * i] * up, x[4 * j + 2 * i + 1] * up, part);
+#pragma unroll
+        for (int y = 0; y < NQ; ++y) q[n][y][j][i] = part[y];
+      }
+    const float down = qscale * __uint_as_float((uint32_t)(254 - field) << 23);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      mul[n][i] = __shfl_sync(FULL, down, 4 * (2 * c + i));
+      lim[n][i] = __shfl_sync(FULL, limit, 4 * (2 * c + i));
+    }
+  }
+
+  // Offsets of this lane's slots in a step (small pages), or for whole tiles.
+  struct At {
+    uint32_t k[2], ks[2], v[4], vs[4];
+  };
+  __device__ __forceinline__ static At offsets(int tile, int log2tile, int tile_bytes, int lane) {
+    const int g = lane >> 2, c = lane & 3;
+    At a;
+    auto put = [&](int slot, int X, uint32_t& codes, uint32_t& scales) {
+      const uint32_t base = (uint32_t)(slot >> log2tile) * tile_bytes;
+      const int r = slot & (tile - 1);
+      codes = base + (X * tile + r) * (HD / 2);
+      scales = base + tile * HD + (X * tile + r) * (HD / kQ4Group);
+    };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) put(g + 8 * i, 0, a.k[i], a.ks[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) put(2 * c + (i & 1) + 8 * (i >> 1), 1, a.v[i], a.vs[i]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      a.k[i] += HD / 8 * c;
+      a.ks[i] += HD == 128 ? 2 * c : HD == 64 ? c : (3 * c) >> 1;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a.v[i] += HD == 128 ? 8 * g : 4 * g;
+      a.vs[i] += HD == 128 ? g : g >> 1;
+    }
+    return a;
+  }
+
+  // One step at shared address st; t0: its first slot; live: bit per slot that is there
+  // and below the unit's largest limit; whole: every column sees every slot.
+  __device__ __forceinline__ void step(uint32_t st, const At& at, int lane, int t0, uint32_t live, bool whole) {
+    const int g = lane >> 2, c = lane & 3;
+    // ---- S^T
+    float s[NB][4];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+    uint32_t kw[2][SH::KW], sc[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t a = st + at.k[i];
+      if constexpr (HD == 128) {
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(kw[i][0]), "=r"(kw[i][1]), "=r"(kw[i][2]), "=r"(kw[i][3])
+                     : "r"(a)
+                     : "memory");
+        const uint32_t b = lds16(st + at.ks[i]);
+        sc[i][0] = __byte_perm(b, 0, 0x4040);  // byte 0 in both halves
+        sc[i][1] = __byte_perm(b, 0, 0x4141);
+      } else if constexpr (HD == 64) {
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(kw[i][0]), "=r"(kw[i][1]) : "r"(a) : "memory");
+        sc[i][0] = sc[i][1] = lds8(st + at.ks[i]) * 0x00010001u;
+      } else {
+#pragma unroll
+        for (int w = 0; w < SH::KW; ++w) kw[i][w] = lds32(a + 4 * w);
+        sc[i][0] = lds8(st + at.ks[i]) * 0x00010001u;
+        sc[i][1] = lds8(st + at.ks[i] + 1) * 0x00010001u;
+      }
+      sc[i][0] <<= 7;
+      sc[i][1] <<= 7;
+    }
+#pragma unroll
+    for (int w = 0; w < SH::KW; ++w) {
+      uint32_t r0[4], r1[4];
+      codes4(kw[0][w], r0);
+      codes4(kw[1][w], r1);
+      // which of the lane's scales: 96 features per row have 24 per lane, one and a half groups
+      uint32_t s0, s1;
+      if constexpr (HD == 96) {
+        const bool second = ((3 * c + w) >> 1) != ((3 * c) >> 1);
+        s0 = second ? sc[0][1] : sc[0][0];
+        s1 = second ? sc[1][1] : sc[1][0];
+      } else {
+        s0 = sc[0][w >> 1];
+        s1 = sc[1][w >> 1];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        r0[i] = times(r0[i], s0);
+        r1[i] = times(r1[i], s1);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          const int j = 2 * w + u;
+          if constexpr (NQ == 1) {
+            mma(s[n], r0[2 * u], r1[2 * u], r0[2 * u + 1], r1[2 * u + 1], q[n][0][j][0], q[n][0][j][1]);
+          } else {
+            float z[4] = {0.f, 0.f, 0.f, 0.f};  // (smallest parts first)
+#pragma unroll
+            for (int y = NQ - 1; y >= 0; --y)
+              mma(z, r0[2 * u], r1[2 * u], r0[2 * u + 1], r1[2 * u + 1], q[n][y][j][0], q[n][y][j][1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[n][i] += z[i];
+          }
+        }
+    }
+
+    // ---- weights: slots t0 + g + 8 (i / 2), columns 2 c + i % 2 of block n
+    bool raise = false;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int slot = g + 8 * (i >> 1);
+        s[n][i] *= mul[n][i & 1];
+        if (!whole && !(((live >> slot) & 1u) && t0 + slot < lim[n][i & 1])) s[n][i] = -INFINITY;
+        raise |= s[n][i] - ref[n][i & 1] > kRaise;
+      }
+    if (__any_sync(FULL, raise)) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float top = fmaxf(s[n][i], s[n][i + 2]);
+#pragma unroll
+          for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, d));
+          const float to = fmaxf(ref[n][i], top - kHead), corr = exp2f(ref[n][i] - to);
+          ref[n][i] = to;
+          l[n][i] *= corr;
+#pragma unroll
+          for (int m = 0; m < SH::MT; ++m) {
+            o[n][m][i] *= corr;
+            o[n][m][i + 2] *= corr;
+          }
+        }
+    }
+    uint32_t p[NB][NP][2];  // column g, slots 2 c + {0, 1} and 8 more
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float x = exp2f(s[n][2 * h] - ref[n][0]), y = exp2f(s[n][2 * h + 1] - ref[n][1]);
+        l[n][0] += x;
+        l[n][1] += y;
+        p[n][0][h] = half2_of(x, y);
+        if constexpr (NP == 2) {  // the rest, 2^11 larger so that it is no subnormal
+          const float2 f = floats_of(p[n][0][h]);
+          p[n][1][h] = transposed(half2_of((x - f.x) * 2048.f, (y - f.y) * 2048.f));
+        }
+        p[n][0][h] = transposed(p[n][0][h]);
+      }
+
+    // ---- O^T
+    uint32_t vs[2][2];  // scales of two slots, for the pairs 2 c + {0, 1} and 8 more
+    uint32_t b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = lds8(st + at.vs[i]);
+    if (live != 0xFFFFu)  // what lies in other slots must not reach the sums: 0 times any code
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!((live >> (2 * c + (i & 1) + 8 * (i >> 1))) & 1u)) b[i] = 0u;
+    vs[0][0] = (b[0] | b[1] << 16) << 7;
+    vs[0][1] = (b[2] | b[3] << 16) << 7;
+    if constexpr (HD == 96) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b[i] = lds8(st + at.vs[i] - (g >> 1) + 4 + (g >> 2));
+      if (live != 0xFFFFu)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!((live >> (2 * c + (i & 1) + 8 * (i >> 1))) & 1u)) b[i] = 0u;
+      vs[1][0] = (b[0] | b[1] << 16) << 7;
+      vs[1][1] = (b[2] | b[3] << 16) << 7;
+    } else {
+      vs[1][0] = vs[0][0];
+      vs[1][1] = vs[0][1];
+    }
+    uint32_t vw[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = st + at.v[i];
+      if constexpr (HD == 128) {
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(vw[i][0]), "=r"(vw[i][1]) : "r"(a) : "memory");
+      } else {
+        vw[i][0] = lds32(a);
+        vw[i][1] = HD == 96 ? lds16(a - 4 * g + 32 + 2 * g) : 0u;
+      }
+    }
+#pragma unroll
+    for (int w = 0; w < (HD == 64 ? 1 : 2); ++w) {
+      constexpr uint32_t M = 0x0F0F0F0Fu;
+      uint32_t e[2][4], f[2][4];  // slot pairs: even features, odd features
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t x = vw[2 * h][w], y = vw[2 * h + 1][w];
+        codes4((x & M) | (y << 4 & ~M), e[h]);
+        codes4((x >> 4 & M) | (y & ~M), f[h]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          e[h][i] = times(e[h][i], vs[w][h]);
+          f[h][i] = times(f[h][i], vs[w][h]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < (HD == 96 && w == 1 ? 2 : 4); ++i)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          float(&to)[4] = o[n][4 * w + i];
+          if constexpr (NP == 1) {
+            mma(to, e[0][i], f[0][i], e[1][i], f[1][i], p[n][0][0], p[n][0][1]);
+          } else {
+            float y[4] = {0.f, 0.f, 0.f, 0.f}, z[4] = {0.f, 0.f, 0.f, 0.f};
+            mma(y, e[0][i], f[0][i], e[1][i], f[1][i], p[n][NP - 1][0], p[n][NP - 1][1]);
+            mma(z, e[0][i], f[0][i], e[1][i], f[1][i], p[n][0][0], p[n][0][1]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) to[x] += fmaf(y[x], 1.f / 2048.f, z[x]);
+          }
+        }
+    }
+  }
+
+  // rec[col][HD], then (reference, sum) per column
+  __device__ __forceinline__ void store(float* rec, int cols, int lane) {
+    const int g = lane >> 2, c = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) l[n][i] += __shfl_xor_sync(FULL, l[n][i], d);
+        const int col = 8 * n + 2 * c + i;
+        if (col >= cols) continue;
+#pragma unroll
+        for (int m = 0; m < SH::MT; ++m)
+          *reinterpret_cast<float2*>(rec + col * HD + feature<HD>(g, m)) = make_float2(o[n][m][i], o[n][m][i + 2]);
+        if (g == 0) {
+          rec[cols * HD + 2 * col] = ref[n][i];
+          rec[cols * HD + 2 * col + 1] = l[n][i];
+        }
+      }
+  }
+};
+
+// BIG: pages of at least 16 slots
+template <typename T, int HD, int NB, bool BIG>
+__global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasPerSm : 2)
+    q4_attn_kernel(const Q4AttnParams p) {
+  using SH = Shape<HD>;
+  constexpr int STAGE = BIG ? SH::TILE : SH::STEP;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  __shared__ uint64_t full[kQ4Warps][kStages];
+  __shared__ uint32_t live_s[kQ4Warps][kStages];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int C = p.pieces;
+  const int unit = (int)(blockIdx.x / (unsigned)C), piece = (int)(blockIdx.x - (unsigned)unit * C);
+  const int bh = unit / p.col_blocks, x0 = (unit - bh * p.col_blocks) * 8 * NB;
+  const int b = bh / p.Hkv, h = bh - b * p.Hkv;
+  const int cols = min(8 * NB, p.Tq * p.G - x0), max_slots = p.max_pages * p.P;
+  unsigned char* ring = smem_raw + warp * kStages * STAGE;
+  float* crec = reinterpret_cast<float*>(smem_raw + kQ4Warps * kStages * STAGE);
+  if (lane == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(&full[warp][i], 1);
+    fence_mbar_init();
+  }
+  __syncwarp();
+
+  // Dependents start only after this grid's own wait, so that everything before
+  // it is visible to them whatever they wait for.
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // ---- limits: slots that column x sees (0: a bad length)
+  auto limit = [&](int x, bool& bad) -> int {
+    const int n = __ldg(p.lens + (int64_t)b * p.Tq + x / p.G);
+    bad = n < 0 || n > max_slots - p.len_add;
+    return bad ? 0 : n + p.len_add;
+  };
+  int S = 0, least = INT32_MAX;  // largest and smallest limit of the unit's columns
+  {
+    bool bad = false;
+    if (lane < cols) {
+      S = limit(x0 + lane, bad);
+      least = S;
+      if (bad && h == 0 && piece == 0 && warp == 0) report(p.status, WM_ERR_BOUNDS);
+    }
+    S = __reduce_max_sync(FULL, S);
+    least = __reduce_min_sync(FULL, least);
+  }
+  const int nsteps = (S + kQ4Step - 1) / kQ4Step;
+  const int nparts = C * kQ4Warps, mine = piece * kQ4Warps + warp;
+  const int j0 = (int)((int64_t)mine * nsteps / nparts);
+  const int nmine = (int)((int64_t)(mine + 1) * nsteps / nparts) - j0;
+
+  // lane i < tiles of a step: tile i of step j (-1: not seen, or no such page)
+  const int32_t* ptab = p.page_table + (int64_t)b * p.max_pages;
+  const int tiles = BIG ? 1 : kQ4Step >> p.log2tile, per_page = BIG ? p.P / kQ4Step : 1;
+  auto tile_at = [&](int j) -> int {
+    int at = -1;
+    if (lane < tiles && j < j0 + nmine) {
+      const int t = j * kQ4Step + (BIG ? 0 : lane << p.log2tile);
+      if (t < S) {
+        const int pg = __ldg(ptab + (t >> p.log2P));
+        if (pg >= 0 && pg < p.num_pages) at = (pg * p.Hkv + h) * per_page + (BIG ? (t & (p.P - 1)) / kQ4Step : 0);
+        else report(p.status, WM_ERR_BOUNDS);
+      }
+    }
+    return at;
+  };
+  const uint64_t policy = l2_evict_first_policy();
+  const uint32_t tile_bytes = BIG ? SH::TILE : p.tile_bytes;
+  auto issue = [&](int i, int at) {  // the warp's i-th step into ring slot i % kStages
+    const uint32_t mask = __ballot_sync(FULL, at >= 0);
+    uint64_t* bar = &full[warp][i % kStages];
+    if (lane == 0) {
+      uint32_t live = mask ? 0xFFFFu : 0u;
+      if (!BIG) {
+        live = 0;
+        for (int x = 0; x < tiles; ++x)
+          if ((mask >> x) & 1u) live |= ((1u << p.tile) - 1) << (x << p.log2tile);
+      }
+      const int rest = S - (j0 + i) * kQ4Step;
+      if (rest < kQ4Step) live &= (1u << rest) - 1;
+      live_s[warp][i % kStages] = live;
+      mbar_arrive_expect_tx(bar, __popc(mask) * tile_bytes);
+    }
+    __syncwarp();
+    if (at >= 0)
+      bulk_g2s(ring + (i % kStages) * STAGE + lane * tile_bytes, p.pool + (int64_t)at * tile_bytes, tile_bytes, bar, policy);
+  };
+  int next = tile_at(j0);
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) {
+    const int at = next;
+    next = tile_at(j0 + i + 1);
+    if (i < nmine) issue(i, at);
+  }
+
+  // ---- queries
+  Math<T, HD, NB> mm;
+  mm.init();
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    const int col = 8 * n + (lane >> 2), x = x0 + col;
+    const T* row = nullptr;
+    int lim = 0;
+    if (col < cols) {
+      bool bad;
+      row = reinterpret_cast<const T*>(p.q) + (((int64_t)b * p.Tq + x / p.G) * p.Hq + h * p.G + x % p.G) * HD;
+      lim = limit(x, bad);
+    }
+    mm.load(n, row, lim, lane, p.qscale);
+  }
+  const typename Math<T, HD, NB>::At at =
+      BIG ? Math<T, HD, NB>::offsets(kQ4Step, 4, SH::TILE, lane)
+          : Math<T, HD, NB>::offsets(p.tile, p.log2tile, p.tile_bytes, lane);
+
+  bool ok = true;
+  for (int i = 0; i < nmine; ++i) {
+    ok = __all_sync(FULL, mbar_wait(&full[warp][i % kStages], (i / kStages) & 1));
+    if (!ok) break;
+    const uint32_t live = live_s[warp][i % kStages];
+    const int t0 = (j0 + i) * kQ4Step;
+    mm.step(smem_u32(ring + (i % kStages) * STAGE), at, lane, t0, live, live == 0xFFFFu && t0 + kQ4Step <= least);
+    __syncwarp();  // every lane is done with this ring slot
+    const int to = next;
+    next = tile_at(j0 + i + kStages + 1);
+    if (i + kStages < nmine) issue(i + kStages, to);
+  }
+  if (!ok) {
+    // a copy never arrived: report it, and give the others their time before the ring is
+    // used for records
+    if (lane == 0) report(p.status, WM_ERR_TIMEOUT);
+    for (int i = 0; i < kStages; ++i) {
+      if (lane == 0) mbar_wait(&full[warp][i], 0, kWaitLimitNs / 100);
+      if (lane == 0) mbar_wait(&full[warp][i], 1, kWaitLimitNs / 100);
+      __syncwarp();
+    }
+  }
+
+  // ---- join the CTA's warps (each warp's state in its idle ring)
+  __syncwarp();
+  float* wrec = reinterpret_cast<float*>(ring);
+  mm.store(wrec, cols, lane);
+  __syncthreads();
+  const int E = cols * HD;
+  auto warp_rec = [&](int w) -> const float* {
+    return reinterpret_cast<const float*>(smem_raw + w * kStages * STAGE);
+  };
+  auto out_row = [&](int col) -> T* {
+    const int x = x0 + col;
+    return reinterpret_cast<T*>(p.out) + (((int64_t)b * p.Tq + x / p.G) * p.Hq + h * p.G + x % p.G) * HD;
+  };
+  float* gpart = p.part ? p.part + (int64_t)blockIdx.x * q4_rec(8 * NB, HD) : nullptr;
+  const bool direct = C == 1 && !gpart;
+  for (int e = tid; e < E; e += kThreads) {
+    const int r = e / HD;
+    float M = -FLT_MAX, L = 0.f, O = 0.f;
+#pragma unroll
+    for (int w = 0; w < kQ4Warps; ++w) M = fmaxf(M, warp_rec(w)[E + 2 * r]);
+#pragma unroll
+    for (int w = 0; w < kQ4Warps; ++w) {
+      const float wt = exp2f(warp_rec(w)[E + 2 * r] - M);
+      L = fmaf(wt, warp_rec(w)[E + 2 * r + 1], L);
+      O = fmaf(wt, warp_rec(w)[e], O);
+    }
+    if (direct) {
+      out_row(r)[e - r * HD] = Elem<T>::from_f(L == 0.f ? 0.f : O / L);
+    } else {
+      float* rec = gpart ? gpart : crec;
+      rec[e] = O;
+      if (e == r * HD) {
+        rec[(gpart ? 8 * NB * HD : E) + 2 * r] = M;
+        rec[(gpart ? 8 * NB * HD : E) + 2 * r + 1] = L;
+      }
+    }
+  }
+  if (direct || gpart) return;
+
+  // ---- join the cluster's CTAs through distributed shared memory: CTA `piece`
+  // finishes its share.  The last barrier keeps each CTA's shared memory until
+  // every reader is done.
+  cg::cluster_group cluster = cg::this_cluster();
+  cluster.sync();
+  for (int e = piece * E / C + tid; e < (piece + 1) * E / C; e += kThreads) {
+    const int r = e / HD;
+    float mq[kQ4MaxCluster], lq[kQ4MaxCluster], oq[kQ4MaxCluster];
+#pragma unroll
+    for (int c = 0; c < kQ4MaxCluster; ++c) {
+      const float* cr = cluster.map_shared_rank(crec, c < C ? c : 0);
+      mq[c] = c < C ? cr[E + 2 * r] : -FLT_MAX;
+      lq[c] = c < C ? cr[E + 2 * r + 1] : 0.f;
+      oq[c] = c < C ? cr[e] : 0.f;
+    }
+    float M = -FLT_MAX, L = 0.f, O = 0.f;
+#pragma unroll
+    for (int c = 0; c < kQ4MaxCluster; ++c) M = fmaxf(M, mq[c]);
+#pragma unroll
+    for (int c = 0; c < kQ4MaxCluster; ++c) {
+      const float wt = exp2f(mq[c] - M);
+      L = fmaf(wt, lq[c], L);
+      O = fmaf(wt, oq[c], O);
+    }
+    out_row(r)[e - r * HD] = Elem<T>::from_f(L == 0.f ? 0.f : O / L);
+  }
+  cluster.sync();
+}
+
+// Joins the records of a unit's pieces: out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i.
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) q4_join_kernel(const Q4AttnParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  constexpr int MAXC = 16;
+  __shared__ float w_s[MAXC][kQ4MaxPieces], inv_s[MAXC];
+  const int unit = blockIdx.x, most = 8 * p.nb;
+  const int bh = unit / p.col_blocks, x0 = (unit - bh * p.col_blocks) * most;
+  const int b = bh / p.Hkv, h = bh - b * p.Hkv, cols = min(most, p.Tq * p.G - x0);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, recf = q4_rec(most, HD);
+  const float* part = p.part + (int64_t)unit * p.pieces * recf;
+  for (int r = warp; r < cols; r += 8) {
+    const float* ml = part + most * HD + 2 * r;
+    float M = -FLT_MAX, L = 0.f;
+    for (int i = lane; i < p.pieces; i += 32) M = fmaxf(M, __ldcg(ml + (int64_t)i * recf));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(FULL, M, o));
+    for (int i = lane; i < p.pieces; i += 32) {
+      const float w = exp2f(__ldcg(ml + (int64_t)i * recf) - M);
+      w_s[r][i] = w;
+      L = fmaf(w, __ldcg(ml + (int64_t)i * recf + 1), L);
+    }
+    L = warp_sum(L);
+    if (lane == 0) inv_s[r] = L == 0.f ? 0.f : 1.f / L;
+  }
+  __syncthreads();
+  for (int y = tid; y < cols * HD / 4; y += 256) {
+    const int r = y / (HD / 4), e = (y - r * (HD / 4)) * 4, x = x0 + r;
+    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int NBUF = 8;
+    for (int i0 = 0; i0 < p.pieces; i0 += NBUF) {
+      float4 v[NBUF];
+#pragma unroll
+      for (int i = 0; i < NBUF; ++i)
+        if (i0 + i < p.pieces) v[i] = __ldcg(reinterpret_cast<const float4*>(part + (int64_t)(i0 + i) * recf) + y);
+#pragma unroll
+      for (int i = 0; i < NBUF; ++i) {
+        if (i0 + i >= p.pieces) continue;
+        const float w = w_s[r][i0 + i];
+        O.x = fmaf(w, v[i].x, O.x);
+        O.y = fmaf(w, v[i].y, O.y);
+        O.z = fmaf(w, v[i].z, O.z);
+        O.w = fmaf(w, v[i].w, O.w);
+      }
+    }
+    const float inv = inv_s[r];
+    T* out = reinterpret_cast<T*>(p.out) + (((int64_t)b * p.Tq + x / p.G) * p.Hq + h * p.G + x % p.G) * HD + e;
+    out[0] = Elem<T>::from_f(O.x * inv);
+    out[1] = Elem<T>::from_f(O.y * inv);
+    out[2] = Elem<T>::from_f(O.z * inv);
+    out[3] = Elem<T>::from_f(O.w * inv);
+  }
+}
+
+template <typename Kern>
+inline cudaError_t launch_chained(Kern kern, const Q4AttnParams& p, unsigned grid, int threads, size_t smem, int cluster,
+                                  cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 0 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, p);
+}
+
+template <typename T, int HD, int NB, bool BIG>
+inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
+  using SH = Shape<HD>;
+  static size_t smem_set[kSmemOptDevices] = {};
+  auto kern = q4_attn_kernel<T, HD, NB, BIG>;
+  constexpr size_t ring = (size_t)kStages * (BIG ? SH::TILE : SH::STEP), rec = q4_rec(8 * NB, HD) * sizeof(float);
+  static_assert(rec <= ring && ring % 16 == 0, "a warp's record goes into its ring");
+  const size_t smem = kQ4Warps * ring + (p.part ? 0 : rec);
+  if (cudaError_t e = opt_in_smem(kern, smem, smem_set); e != cudaSuccess) return e;
+  const unsigned units = (unsigned)p.B * p.Hkv * p.col_blocks;
+  const cudaError_t e = launch_chained(kern, p, units * (unsigned)p.pieces, kThreads, smem, p.part ? 0 : p.pieces, s);
+  if (e != cudaSuccess || !p.part) return e;
+  return launch_chained(q4_join_kernel<T, HD>, p, units, 256, 0, 0, s);
+}
+
+template <typename T, int HD>
+inline cudaError_t launch_d(const Q4AttnParams& p, cudaStream_t s) {
+  if constexpr (sizeof(T) == 2)
+    if (p.nb == 2) return p.P >= kQ4Step ? launch_t<T, HD, 2, true>(p, s) : launch_t<T, HD, 2, false>(p, s);
+  return p.P >= kQ4Step ? launch_t<T, HD, 1, true>(p, s) : launch_t<T, HD, 1, false>(p, s);
+}
+
+}  // namespace q4_detail
+
+// Per-dtype dispatch (one translation unit each, compiled in parallel).
+cudaError_t launch_q4_attn_bf16(const Q4AttnParams& p, int d, cudaStream_t s);
+cudaError_t launch_q4_attn_f32(const Q4AttnParams& p, int d, cudaStream_t s);
+
+}  // namespace wm

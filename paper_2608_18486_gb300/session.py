@@ -20,6 +20,33 @@ def torch_dtype(dtype: str):
     return {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
 
 
+class Q4Cache:
+    def __init__(self, cfg: W.wm_config, num_pages: int, device: str | torch.device = "cuda:0",
+                 cache_buf: torch.Tensor | None = None):
+        """The device memory of a cache held in 4 bits (wm_q4_cache), for the
+        q4_* calls of sessions of the same config.  cache_buf: a contiguous
+        uint8 tensor that holds it; allocated if None."""
+        rc = W.wm_config_check(cfg)
+        if rc != W.WM_OK:
+            raise W.WMError(rc, "wm_config_check")
+        self.cfg, self.num_pages = cfg, int(num_pages)
+        self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        nbytes = W.wm_q4_cache_bytes(cfg, num_pages)
+        if nbytes == 0:
+            raise W.WMError(W.WM_ERR_INVALID_ARG, "wm_q4_cache_bytes")
+        if cache_buf is None:
+            cache_buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        elif cache_buf.dtype != torch.uint8 or not cache_buf.is_contiguous() or \
+                cache_buf.device != self.device:
+            raise ValueError("cache_buf must be a contiguous uint8 tensor on the cache's device")
+        self.cache_buf = cache_buf
+        self.cache = W.wm_q4_cache_alloc(cfg, cache_buf, cache_buf.numel(), num_pages)
+        self._index = -1 if self.device.type == "cpu" else self.device.index
+        self._ref = ctypes.byref(self.cache)
+
+
 class DecodeSession:
     def __init__(self, cfg: W.wm_config, B: int, num_pages: int, max_pages: int,
                  device: str | torch.device = "cuda:0", cache_buf: torch.Tensor | None = None):
@@ -322,6 +349,76 @@ class DecodeSession:
                                       self._raw_stream(stream))
         if rc != W.WM_OK:
             raise W.WMError(rc, "wm_cache_evict")
+
+    # ------------------------------------------------------- caches held in 4 bits
+    def _q4_ref(self, q4: Q4Cache):
+        if q4._index != self._index:
+            raise ValueError(f"a 4-bit cache on {q4.device} in a session on {self.device}")
+        return q4._ref
+
+    def _q4_copy(self, call, name, q4, src_table, dst_table, first, last, span, B, stream, write):
+        cfg, cache = self._refs
+        q4r = self._q4_ref(q4)
+        B = self.B if B is None else B
+        dev, table = self._index, 4 * B * self.max_pages
+        if not (src_table.is_contiguous() and dst_table.is_contiguous() and first.is_contiguous()
+                and last.is_contiguous() and src_table.dtype is _I32 and dst_table.dtype is _I32
+                and first.dtype is _I32 and last.dtype is _I32 and src_table.nbytes == dst_table.nbytes == table
+                and first.nbytes >= 4 * B and last.nbytes >= 4 * B
+                and src_table.get_device() == dst_table.get_device() == first.get_device() == last.get_device() == dev):
+            self._check((first, _I32, B), (last, _I32, B))
+            self._check_table(src_table, B)
+            self._check_table(dst_table, B)
+        if span >> 31:
+            span, = self._counts(span)
+        src, dst = (cache, q4r) if write else (q4r, cache)
+        rc = call(cfg, src, src_table.data_ptr(), dst, dst_table.data_ptr(), first.data_ptr(),
+                  last.data_ptr(), span, B, self.max_pages, self._status_ptr, self._raw_stream(stream))
+        if rc != W.WM_OK:
+            raise W.WMError(rc, name)
+
+    def q4_write(self, q4: Q4Cache, page_table, q4_table, first, last, *, span: int,
+                 B: int | None = None, stream=None) -> None:
+        """Slots first[b] .. last[b] - 1 of the session's cache (page_table) to
+        the 4-bit cache (q4_table), all channels; no range longer than span."""
+        self._q4_copy(self._lib.wm_q4_write, "wm_q4_write", q4, page_table, q4_table, first, last, span, B,
+                      stream, True)
+
+    def q4_read(self, q4: Q4Cache, q4_table, page_table, first, last, *, span: int,
+                B: int | None = None, stream=None) -> None:
+        """Slots first[b] .. last[b] - 1 of the 4-bit cache (q4_table) back into
+        the session's cache (page_table), all channels."""
+        self._q4_copy(self._lib.wm_q4_read, "wm_q4_read", q4, q4_table, page_table, first, last, span, B,
+                      stream, False)
+
+    def q4_decode_attn(self, layer: int, q, q4: Q4Cache, page_table, seq_lens, out, *,
+                       B: int | None = None, stream=None) -> None:
+        """Decode attention of layer ``layer`` over a 4-bit cache (its pages:
+        page_table)."""
+        B = self.B if B is None else B
+        q4r = self._q4_ref(q4)
+        self._check_rows(q, seq_lens, page_table, out, B, B)
+        need = self._bytes(("q4", B, self.max_pages), W.wm_q4_decode_attn_workspace, B, self.max_pages)
+        raw = self._raw_stream(stream)
+        rc = self._lib.wm_q4_decode_attn(self._refs[0], q4r, layer, q.data_ptr(), page_table.data_ptr(),
+                                         seq_lens.data_ptr(), B, self.max_pages, out.data_ptr(),
+                                         self._scratch_for(need, raw, stream), need, self._status_ptr, raw)
+        if rc != W.WM_OK:
+            raise W.WMError(rc, "wm_q4_decode_attn")
+
+    def q4_rows_attn(self, layer: int, q, pos, q4: Q4Cache, page_table, out, *, stream=None) -> None:
+        """Causal attention of query rows q [B][Tq][Hq][d] at positions pos
+        [B][Tq] over a 4-bit cache: position i sees slots 0 .. i."""
+        B, Tq = q.shape[:2]
+        q4r = self._q4_ref(q4)
+        self._check_rows(q, pos, page_table, out, B, B * Tq)
+        need = self._bytes(("q4 rows", B, Tq, self.max_pages), W.wm_q4_rows_attn_workspace, B, Tq, self.max_pages)
+        raw = self._raw_stream(stream)
+        rc = self._lib.wm_q4_rows_attn(self._refs[0], q4r, layer, q.data_ptr(), pos.data_ptr(),
+                                       page_table.data_ptr(), B, Tq, self.max_pages, out.data_ptr(),
+                                       self._scratch_for(need, raw, stream), need, self._status_ptr, raw)
+        if rc != W.WM_OK:
+            raise W.WMError(rc, "wm_q4_rows_attn")
 
     def read_status(self, reset: bool = True) -> int:
         v = int(self.status.item())
