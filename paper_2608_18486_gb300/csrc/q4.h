@@ -63,6 +63,7 @@ cudaError_t launch_q4_read(const Q4CopyParams& p, int dtype, int d, int sms, cud
 
 // ------------------------------------------------------------ attention
 constexpr int kQ4Warps = 4;        // warps per CTA
+constexpr int kQ4Slots = 32;       // slots of a warp's step
 constexpr int kQ4MaxCluster = 8;
 constexpr int kQ4MaxPieces = 64;
 constexpr int kQ4CtasPerSm = 4;

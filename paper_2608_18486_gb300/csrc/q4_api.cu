@@ -108,8 +108,8 @@ struct Q4Plan {
 
 int clamp_int(int64_t x, int64_t lo, int64_t hi) { return (int)(x < lo ? lo : x > hi ? hi : x); }
 
-constexpr int kLongSteps = 24;  // steps of a warp from which a unit is cut into records
-constexpr int kMinSteps = 8;    // steps that a cut leaves each warp at least
+constexpr int kLongSteps = 12;  // steps of a warp from which a unit is cut into records
+constexpr int kMinSteps = 4;    // steps that a cut leaves each warp at least
 constexpr int kWaves = 4;       // waves of resident CTAs that a cut aims at
 
 Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
@@ -118,7 +118,7 @@ Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   pl.nb = cols > 8 && c.dtype == WM_DT_BF16 ? 2 : 1;
   pl.col_blocks = (int)((cols + 8 * pl.nb - 1) / (8 * pl.nb));
   const int64_t units = (int64_t)B * c.Hkv * pl.col_blocks;
-  const int64_t steps = ((int64_t)max_pages * c.page_size + kQ4Step - 1) / kQ4Step;
+  const int64_t steps = ((int64_t)max_pages * c.page_size + kQ4Slots - 1) / kQ4Slots;
   const int64_t resident = (int64_t)sm_count() * (pl.nb == 1 && c.dtype == WM_DT_BF16 ? kQ4CtasPerSm : 2);
   int C = 1;
   while (C < kQ4MaxCluster && units * C * 2 <= resident && (int64_t)C * kQ4Warps < steps) C *= 2;

@@ -8,13 +8,13 @@
 //   join for any references m.
 //
 // A unit is one (sequence, kv head) and 8 NB of its columns.  `pieces` CTAs of 4
-// warps share a unit; each warp takes a contiguous part of its steps of 16 slots
-// through a private ring of bulk copies (one per step: a step is one contiguous
-// tile; one per page for pages below 16 slots).
+// warps share a unit; each warp takes a contiguous part of its steps of 32 slots
+// through a private ring of bulk copies (a tile of 16 slots is contiguous: one copy,
+// or one per page for pages below 16 slots).
 //
 // Both products are mma.sync m16n8k16 with the 8 columns as the narrow operand:
 //   S^T [16 slots x 8 columns] += K [16 x d] Q^T,   O^T [d x 8] += V^T [d x 16] P^T,
-// so a step costs d / 8 of them for up to 8 columns.  The values of the cache are exact
+// so 16 slots cost d / 8 of them for up to 8 columns.  The values of the cache are exact
 // in fp16: a pair of codes becomes an fp16 pair in one conversion and one product
 // with the scale.  For S^T a lane takes consecutive features of one slot, for O^T the same
 // features of two slots, whose codes are first interleaved (byte = feature, halves =
@@ -42,7 +42,8 @@ namespace q4_detail {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = kQ4Warps * 32;
-constexpr int kStages = 4;         // ring depth per warp
+constexpr int kSlots = kQ4Slots, kTiles = kSlots / kQ4Step;
+constexpr int kStages = 2;         // ring depth per warp, in steps
 constexpr float kHead = 8.f;       // log2 of the weight of a new reference maximum
 constexpr float kRaise = 15.f;     // log2 of the weight that moves the reference
 constexpr unsigned FULL = 0xFFFFFFFFu;
@@ -52,8 +53,8 @@ struct Shape {
   static constexpr int KW = HD / 32;                 // words of 8 codes per lane and K row
   static constexpr int MT = HD / 16;                 // 16-feature blocks
   static constexpr int TILE = 16 * (HD + HD / 8);    // bytes of a whole tile
-  // a step of small pages: each tile is padded to 16 bytes
-  static constexpr int STEP = 16 * ((HD + HD / 8 + 15) / 16 * 16);
+  // small pages: each tile is padded to 16 bytes
+  static constexpr int SMALL = 16 * ((HD + HD / 8 + 15) / 16 * 16);
 };
 template <typename T>
 struct Parts {
@@ -129,6 +130,12 @@ __device__ __forceinline__ uint32_t lds8(uint32_t a) {
   uint32_t v;
   asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
   return v;
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 // First of the two neighbouring features of accumulator block m of lane row g.
@@ -224,14 +231,9 @@ struct Math {
     return a;
   }
 
-  // One step at shared address st; t0: its first slot; live: bit per slot that is there
-  // and below the unit's largest limit; whole: every column sees every slot.
-  __device__ __forceinline__ void step(uint32_t st, const At& at, int lane, int t0, uint32_t live, bool whole) {
-    const int g = lane >> 2, c = lane & 3;
-    // ---- S^T
-    float s[NB][4];
-#pragma unroll
-    for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+  // S^T of the 16 slots at shared address st.
+  __device__ __forceinline__ void scores(uint32_t st, const At& at, int lane, float (&s)[NB][4]) {
+    const int c = lane & 3;
     uint32_t kw[2][SH::KW], sc[2][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -242,20 +244,20 @@ struct Math {
                      : "r"(a)
                      : "memory");
         const uint32_t b = lds16(st + at.ks[i]);
-        sc[i][0] = __byte_perm(b, 0, 0x4040);  // byte 0 in both halves
-        sc[i][1] = __byte_perm(b, 0, 0x4141);
+        sc[i][0] = (b & 0xFFu) * 0x00800080u;  // an fp16 pair
+        sc[i][1] = (b >> 8) * 0x00800080u;
       } else if constexpr (HD == 64) {
         asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(kw[i][0]), "=r"(kw[i][1]) : "r"(a) : "memory");
-        sc[i][0] = sc[i][1] = lds8(st + at.ks[i]) * 0x00010001u;
+        sc[i][0] = sc[i][1] = lds8(st + at.ks[i]) * 0x00800080u;
       } else {
 #pragma unroll
         for (int w = 0; w < SH::KW; ++w) kw[i][w] = lds32(a + 4 * w);
-        sc[i][0] = lds8(st + at.ks[i]) * 0x00010001u;
-        sc[i][1] = lds8(st + at.ks[i] + 1) * 0x00010001u;
+        sc[i][0] = lds8(st + at.ks[i]) * 0x00800080u;
+        sc[i][1] = lds8(st + at.ks[i] + 1) * 0x00800080u;
       }
-      sc[i][0] <<= 7;
-      sc[i][1] <<= 7;
     }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
 #pragma unroll
     for (int w = 0; w < SH::KW; ++w) {
       uint32_t r0[4], r1[4];
@@ -293,72 +295,27 @@ struct Math {
           }
         }
     }
+  }
 
-    // ---- weights: slots t0 + g + 8 (i / 2), columns 2 c + i % 2 of block n
-    bool raise = false;
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int slot = g + 8 * (i >> 1);
-        s[n][i] *= mul[n][i & 1];
-        if (!whole && !(((live >> slot) & 1u) && t0 + slot < lim[n][i & 1])) s[n][i] = -INFINITY;
-        raise |= s[n][i] - ref[n][i & 1] > kRaise;
-      }
-    if (__any_sync(FULL, raise)) {
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float top = fmaxf(s[n][i], s[n][i + 2]);
-#pragma unroll
-          for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, d));
-          const float to = fmaxf(ref[n][i], top - kHead), corr = exp2f(ref[n][i] - to);
-          ref[n][i] = to;
-          l[n][i] *= corr;
-#pragma unroll
-          for (int m = 0; m < SH::MT; ++m) {
-            o[n][m][i] *= corr;
-            o[n][m][i + 2] *= corr;
-          }
-        }
-    }
-    uint32_t p[NB][NP][2];  // column g, slots 2 c + {0, 1} and 8 more
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float x = exp2f(s[n][2 * h] - ref[n][0]), y = exp2f(s[n][2 * h + 1] - ref[n][1]);
-        l[n][0] += x;
-        l[n][1] += y;
-        p[n][0][h] = half2_of(x, y);
-        if constexpr (NP == 2) {  // the rest, 2^11 larger so that it is no subnormal
-          const float2 f = floats_of(p[n][0][h]);
-          p[n][1][h] = transposed(half2_of((x - f.x) * 2048.f, (y - f.y) * 2048.f));
-        }
-        p[n][0][h] = transposed(p[n][0][h]);
-      }
-
-    // ---- O^T
+  // O^T += V^T P^T of the 16 slots at st; live: bit per slot that is there.
+  __device__ __forceinline__ void values(uint32_t st, const At& at, int lane, uint32_t live,
+                                         const uint32_t (&p)[NB][NP][2]) {
+    const int g = lane >> 2, c = lane & 3;
     uint32_t vs[2][2];  // scales of two slots, for the pairs 2 c + {0, 1} and 8 more
-    uint32_t b[4];
+    auto pair_scales = [&](int off, uint32_t (&to)[2]) {
+      uint32_t b[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = lds8(st + at.vs[i]);
-    if (live != 0xFFFFu)  // what lies in other slots must not reach the sums: 0 times any code
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (!((live >> (2 * c + (i & 1) + 8 * (i >> 1))) & 1u)) b[i] = 0u;
-    vs[0][0] = (b[0] | b[1] << 16) << 7;
-    vs[0][1] = (b[2] | b[3] << 16) << 7;
-    if constexpr (HD == 96) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) b[i] = lds8(st + at.vs[i] - (g >> 1) + 4 + (g >> 2));
-      if (live != 0xFFFFu)
+      for (int i = 0; i < 4; ++i) b[i] = lds8(st + at.vs[i] + off);
+      if (live != 0xFFFFu)  // what lies in other slots must not reach the sums: 0 times any code
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (!((live >> (2 * c + (i & 1) + 8 * (i >> 1))) & 1u)) b[i] = 0u;
-      vs[1][0] = (b[0] | b[1] << 16) << 7;
-      vs[1][1] = (b[2] | b[3] << 16) << 7;
+      to[0] = b[0] * 0x80u + b[1] * 0x800000u;
+      to[1] = b[2] * 0x80u + b[3] * 0x800000u;
+    };
+    pair_scales(0, vs[0]);
+    if constexpr (HD == 96) {
+      pair_scales(4 + (g >> 2) - (g >> 1), vs[1]);
     } else {
       vs[1][0] = vs[0][0];
       vs[1][1] = vs[0][1];
@@ -407,6 +364,86 @@ struct Math {
     }
   }
 
+  // One step of kTiles tiles, `stride` bytes apart, at shared address st; t0: its first
+  // slot; live: bit per slot that is there and below the unit's largest limit;
+  // whole: every column sees every slot.
+  __device__ __forceinline__ void step(uint32_t st, uint32_t stride, const At& at, int lane, int t0, uint32_t live,
+                                       bool whole) {
+    const int g = lane >> 2;
+    float s[kTiles][NB][4];
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) scores(st + x * stride, at, lane, s[x]);
+    if (!whole) {
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int slot = 16 * x + g + 8 * (i >> 1);
+            if (!(((live >> slot) & 1u) && t0 + slot < lim[n][i & 1])) s[x][n][i] = -INFINITY;
+          }
+    }
+    // score - reference: slots t0 + 16 x + g + 8 (i / 2), columns 2 c + i % 2 of block n.
+    // (Two roundings: the score is the reference's own kind of number, however large.)
+    float d[kTiles][NB][4], most = -INFINITY;
+    auto differences = [&]() {
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) d[x][n][i] = __fsub_rn(__fmul_rn(s[x][n][i], mul[n][i & 1]), ref[n][i & 1]);
+    };
+    differences();
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = fmaxf(most, d[x][n][i]);
+    if (__any_sync(FULL, most > kRaise)) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int x = 0; x < kTiles; ++x) top = fmaxf(top, fmaxf(s[x][n][i], s[x][n][i + 2]));
+#pragma unroll
+          for (int y = 4; y < 32; y *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, y));
+          const float to = fmaxf(ref[n][i], __fsub_rn(__fmul_rn(top, mul[n][i]), kHead)), corr = ex2(ref[n][i] - to);
+          ref[n][i] = to;
+          l[n][i] *= corr;
+#pragma unroll
+          for (int m = 0; m < SH::MT; ++m) {
+            o[n][m][i] *= corr;
+            o[n][m][i + 2] *= corr;
+          }
+        }
+      differences();
+    }
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) {
+      uint32_t p[NB][NP][2];  // column g, slots 2 c + {0, 1} and 8 more
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float u = ex2(d[x][n][2 * h]), v = ex2(d[x][n][2 * h + 1]);
+          l[n][0] += u;
+          l[n][1] += v;
+          p[n][0][h] = half2_of(u, v);
+          if constexpr (NP == 2) {  // the rest, 2^11 larger so that it is no subnormal
+            const float2 f = floats_of(p[n][0][h]);
+            p[n][1][h] = transposed(half2_of((u - f.x) * 2048.f, (v - f.y) * 2048.f));
+          }
+          p[n][0][h] = transposed(p[n][0][h]);
+        }
+      values(st + x * stride, at, lane, live >> (16 * x) & 0xFFFFu, p);
+    }
+  }
+
   // rec[col][HD], then (reference, sum) per column
   __device__ __forceinline__ void store(float* rec, int cols, int lane) {
     const int g = lane >> 2, c = lane & 3;
@@ -434,7 +471,7 @@ template <typename T, int HD, int NB, bool BIG>
 __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasPerSm : 2)
     q4_attn_kernel(const Q4AttnParams p) {
   using SH = Shape<HD>;
-  constexpr int STAGE = BIG ? SH::TILE : SH::STEP;
+  constexpr int STAGE = kTiles * (BIG ? SH::TILE : SH::SMALL);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ uint64_t full[kQ4Warps][kStages];
   __shared__ uint32_t live_s[kQ4Warps][kStages];
@@ -474,44 +511,46 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
     S = __reduce_max_sync(FULL, S);
     least = __reduce_min_sync(FULL, least);
   }
-  const int nsteps = (S + kQ4Step - 1) / kQ4Step;
+  const int nsteps = (S + kSlots - 1) / kSlots;
   const int nparts = C * kQ4Warps, mine = piece * kQ4Warps + warp;
   const int j0 = (int)((int64_t)mine * nsteps / nparts);
   const int nmine = (int)((int64_t)(mine + 1) * nsteps / nparts) - j0;
 
   // lane i < tiles of a step: tile i of step j (-1: not seen, or no such page)
   const int32_t* ptab = p.page_table + (int64_t)b * p.max_pages;
-  const int tiles = BIG ? 1 : kQ4Step >> p.log2tile, per_page = BIG ? p.P / kQ4Step : 1;
+  const int tiles = BIG ? kTiles : kSlots >> p.log2tile, per_page = BIG ? p.P / kQ4Step : 1;
   auto tile_at = [&](int j) -> int {
     int at = -1;
-    if (lane < tiles && j < j0 + nmine) {
-      const int t = j * kQ4Step + (BIG ? 0 : lane << p.log2tile);
-      if (t < S) {
-        const int pg = __ldg(ptab + (t >> p.log2P));
-        if (pg >= 0 && pg < p.num_pages) at = (pg * p.Hkv + h) * per_page + (BIG ? (t & (p.P - 1)) / kQ4Step : 0);
-        else report(p.status, WM_ERR_BOUNDS);
-      }
+    const int t = j * kSlots + (BIG ? lane * kQ4Step : lane << p.log2tile);
+    if (lane < tiles && j < j0 + nmine && t < S) {
+      const int pg = __ldg(ptab + (t >> p.log2P));
+      if (pg >= 0 && pg < p.num_pages) at = (pg * p.Hkv + h) * per_page + (BIG ? (t & (p.P - 1)) / kQ4Step : 0);
+      else report(p.status, WM_ERR_BOUNDS);
     }
     return at;
   };
   const uint64_t policy = l2_evict_first_policy();
   const uint32_t tile_bytes = BIG ? SH::TILE : p.tile_bytes;
+  const uint32_t stride = BIG ? SH::TILE : kQ4Step / p.tile * tile_bytes;
   auto issue = [&](int i, int at) {  // the warp's i-th step into ring slot i % kStages
     const uint32_t mask = __ballot_sync(FULL, at >= 0);
     uint64_t* bar = &full[warp][i % kStages];
     if (lane == 0) {
-      uint32_t live = mask ? 0xFFFFu : 0u;
-      if (!BIG) {
-        live = 0;
+      uint32_t live = 0;
+      if (BIG) {
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x)
+          if ((mask >> x) & 1u) live |= 0xFFFFu << (16 * x);
+      } else {
+        const uint32_t one = (1u << p.tile) - 1;
         for (int x = 0; x < tiles; ++x)
-          if ((mask >> x) & 1u) live |= ((1u << p.tile) - 1) << (x << p.log2tile);
+          if ((mask >> x) & 1u) live |= one << (x << p.log2tile);
       }
-      const int rest = S - (j0 + i) * kQ4Step;
-      if (rest < kQ4Step) live &= (1u << rest) - 1;
+      const int rest = S - (j0 + i) * kSlots;
+      if (rest < kSlots) live &= (1u << rest) - 1;
       live_s[warp][i % kStages] = live;
       mbar_arrive_expect_tx(bar, __popc(mask) * tile_bytes);
     }
-    __syncwarp();
     if (at >= 0)
       bulk_g2s(ring + (i % kStages) * STAGE + lane * tile_bytes, p.pool + (int64_t)at * tile_bytes, tile_bytes, bar, policy);
   };
@@ -547,8 +586,8 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
     ok = __all_sync(FULL, mbar_wait(&full[warp][i % kStages], (i / kStages) & 1));
     if (!ok) break;
     const uint32_t live = live_s[warp][i % kStages];
-    const int t0 = (j0 + i) * kQ4Step;
-    mm.step(smem_u32(ring + (i % kStages) * STAGE), at, lane, t0, live, live == 0xFFFFu && t0 + kQ4Step <= least);
+    const int t0 = (j0 + i) * kSlots;
+    mm.step(smem_u32(ring + (i % kStages) * STAGE), stride, at, lane, t0, live, live == FULL && t0 + kSlots <= least);
     __syncwarp();  // every lane is done with this ring slot
     const int to = next;
     next = tile_at(j0 + i + kStages + 1);
@@ -713,7 +752,8 @@ inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
   using SH = Shape<HD>;
   static size_t smem_set[kSmemOptDevices] = {};
   auto kern = q4_attn_kernel<T, HD, NB, BIG>;
-  constexpr size_t ring = (size_t)kStages * (BIG ? SH::TILE : SH::STEP), rec = q4_rec(8 * NB, HD) * sizeof(float);
+  constexpr size_t ring = (size_t)kStages * kTiles * (BIG ? SH::TILE : SH::SMALL), rec = q4_rec(8 * NB, HD) * sizeof(float);
+  static_assert(kTiles <= 2, "a bit per slot");
   static_assert(rec <= ring && ring % 16 == 0, "a warp's record goes into its ring");
   const size_t smem = kQ4Warps * ring + (p.part ? 0 : rec);
   if (cudaError_t e = opt_in_smem(kern, smem, smem_set); e != cudaSuccess) return e;
