@@ -9,8 +9,8 @@
 //
 // A unit is one (sequence, kv head) and 8 NB of its columns.  `pieces` CTAs of 4
 // warps share a unit; each warp takes a contiguous part of its steps of 32 slots
-// through a private ring of bulk copies (a tile of 16 slots is contiguous: one copy,
-// or one per page for pages below 16 slots).
+// through a private ring of cp.async copies, whose issue costs all lanes less than that of
+// bulk copies (addresses in uniform registers: lane by lane).
 //
 // Both products are mma.sync m16n8k16 with the 8 columns as the narrow operand:
 //   S^T [16 slots x 8 columns] += K [16 x d] Q^T,   O^T [d x 8] += V^T [d x 16] P^T,
@@ -74,6 +74,16 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool on) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(dst),
+               "l"(src), "r"((int)on)
+               : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 // The four bytes of w, two codes each, to fp16 pairs (low half first).
 __device__ __forceinline__ void codes4(uint32_t w, uint32_t (&r)[4]) {
@@ -147,7 +157,7 @@ __device__ __forceinline__ int feature(int g, int m) {
 }
 
 // One warp's columns.  Lane: g = lane / 4, c = lane % 4.
-template <typename T, int HD, int NB>
+template <typename T, int HD, int NB, bool BIG>
 struct Math {
   using SH = Shape<HD>;
   static constexpr int NQ = Parts<T>::Q, NP = Parts<T>::P;
@@ -201,33 +211,32 @@ struct Math {
     }
   }
 
-  // Offsets of this lane's slots in a step (small pages), or for whole tiles.
+  // Offsets of this lane's slots in a tile (or 16 slots of small pages): codes and
+  // scales of K rows g, g + 8 and of V rows 2 c, 2 c + 1, 2 c + 8, 2 c + 9.
   struct At {
-    uint32_t k[2], ks[2], v[4], vs[4];
+    uint32_t k_[BIG ? 1 : 2], ks_[BIG ? 1 : 2], v_[BIG ? 1 : 4], vs_[BIG ? 1 : 4];
+    __device__ __forceinline__ uint32_t k(int i) const { return BIG ? k_[0] + i * 8 * (HD / 2) : k_[i]; }
+    __device__ __forceinline__ uint32_t ks(int i) const { return BIG ? ks_[0] + i * 8 * (HD / kQ4Group) : ks_[i]; }
+    __device__ __forceinline__ uint32_t v(int i) const {
+      return BIG ? v_[0] + ((i & 1) + 8 * (i >> 1)) * (HD / 2) : v_[i];
+    }
+    __device__ __forceinline__ uint32_t vs(int i) const {
+      return BIG ? vs_[0] + ((i & 1) + 8 * (i >> 1)) * (HD / kQ4Group) : vs_[i];
+    }
   };
   __device__ __forceinline__ static At offsets(int tile, int log2tile, int tile_bytes, int lane) {
     const int g = lane >> 2, c = lane & 3;
     At a;
     auto put = [&](int slot, int X, uint32_t& codes, uint32_t& scales) {
-      const uint32_t base = (uint32_t)(slot >> log2tile) * tile_bytes;
-      const int r = slot & (tile - 1);
-      codes = base + (X * tile + r) * (HD / 2);
-      scales = base + tile * HD + (X * tile + r) * (HD / kQ4Group);
+      const uint32_t base = BIG ? 0u : (uint32_t)(slot >> log2tile) * tile_bytes;
+      const int n = BIG ? kQ4Step : tile, r = X * n + (slot & (n - 1));
+      codes = base + r * (HD / 2) + (X ? (HD == 128 ? 8 * g : 4 * g) : HD / 8 * c);
+      scales = base + n * HD + r * (HD / kQ4Group) + (X ? (HD == 128 ? g : g >> 1) : HD == 128 ? 2 * c : HD == 64 ? c : (3 * c) >> 1);
     };
 #pragma unroll
-    for (int i = 0; i < 2; ++i) put(g + 8 * i, 0, a.k[i], a.ks[i]);
+    for (int i = 0; i < (BIG ? 1 : 2); ++i) put(g + 8 * i, 0, a.k_[i], a.ks_[i]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) put(2 * c + (i & 1) + 8 * (i >> 1), 1, a.v[i], a.vs[i]);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      a.k[i] += HD / 8 * c;
-      a.ks[i] += HD == 128 ? 2 * c : HD == 64 ? c : (3 * c) >> 1;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      a.v[i] += HD == 128 ? 8 * g : 4 * g;
-      a.vs[i] += HD == 128 ? g : g >> 1;
-    }
+    for (int i = 0; i < (BIG ? 1 : 4); ++i) put(2 * c + (i & 1) + 8 * (i >> 1), 1, a.v_[i], a.vs_[i]);
     return a;
   }
 
@@ -237,23 +246,22 @@ struct Math {
     uint32_t kw[2][SH::KW], sc[2][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const uint32_t a = st + at.k[i];
+      const uint32_t a = st + at.k(i);
       if constexpr (HD == 128) {
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                      : "=r"(kw[i][0]), "=r"(kw[i][1]), "=r"(kw[i][2]), "=r"(kw[i][3])
                      : "r"(a)
                      : "memory");
-        const uint32_t b = lds16(st + at.ks[i]);
-        sc[i][0] = (b & 0xFFu) * 0x00800080u;  // an fp16 pair
-        sc[i][1] = (b >> 8) * 0x00800080u;
+        sc[i][0] = lds8(st + at.ks(i)) * 0x00800080u;  // an fp16 pair
+        sc[i][1] = lds8(st + at.ks(i) + 1) * 0x00800080u;
       } else if constexpr (HD == 64) {
         asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(kw[i][0]), "=r"(kw[i][1]) : "r"(a) : "memory");
-        sc[i][0] = sc[i][1] = lds8(st + at.ks[i]) * 0x00800080u;
+        sc[i][0] = sc[i][1] = lds8(st + at.ks(i)) * 0x00800080u;
       } else {
 #pragma unroll
         for (int w = 0; w < SH::KW; ++w) kw[i][w] = lds32(a + 4 * w);
-        sc[i][0] = lds8(st + at.ks[i]) * 0x00800080u;
-        sc[i][1] = lds8(st + at.ks[i] + 1) * 0x00800080u;
+        sc[i][0] = lds8(st + at.ks(i)) * 0x00800080u;
+        sc[i][1] = lds8(st + at.ks(i) + 1) * 0x00800080u;
       }
     }
 #pragma unroll
@@ -297,7 +305,8 @@ struct Math {
     }
   }
 
-  // O^T += V^T P^T of the 16 slots at st; live: bit per slot that is there.
+  // O^T += V^T P^T of the 16 slots at st; live: bit per slot that is there (WHOLE: all).
+  template <bool WHOLE>
   __device__ __forceinline__ void values(uint32_t st, const At& at, int lane, uint32_t live,
                                          const uint32_t (&p)[NB][NP][2]) {
     const int g = lane >> 2, c = lane & 3;
@@ -305,8 +314,8 @@ struct Math {
     auto pair_scales = [&](int off, uint32_t (&to)[2]) {
       uint32_t b[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) b[i] = lds8(st + at.vs[i] + off);
-      if (live != 0xFFFFu)  // what lies in other slots must not reach the sums: 0 times any code
+      for (int i = 0; i < 4; ++i) b[i] = lds8(st + at.vs(i) + off);
+      if (!WHOLE)  // what lies in other slots must not reach the sums: 0 times any code
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (!((live >> (2 * c + (i & 1) + 8 * (i >> 1))) & 1u)) b[i] = 0u;
@@ -323,7 +332,7 @@ struct Math {
     uint32_t vw[4][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t a = st + at.v[i];
+      const uint32_t a = st + at.v(i);
       if constexpr (HD == 128) {
         asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(vw[i][0]), "=r"(vw[i][1]) : "r"(a) : "memory");
       } else {
@@ -366,14 +375,14 @@ struct Math {
 
   // One step of kTiles tiles, `stride` bytes apart, at shared address st; t0: its first
   // slot; live: bit per slot that is there and below the unit's largest limit;
-  // whole: every column sees every slot.
-  __device__ __forceinline__ void step(uint32_t st, uint32_t stride, const At& at, int lane, int t0, uint32_t live,
-                                       bool whole) {
+  // WHOLE: every column sees every slot.
+  template <bool WHOLE>
+  __device__ __forceinline__ void step(uint32_t st, uint32_t stride, const At& at, int lane, int t0, uint32_t live) {
     const int g = lane >> 2;
     float s[kTiles][NB][4];
 #pragma unroll
     for (int x = 0; x < kTiles; ++x) scores(st + x * stride, at, lane, s[x]);
-    if (!whole) {
+    if (!WHOLE) {
 #pragma unroll
       for (int x = 0; x < kTiles; ++x)
 #pragma unroll
@@ -384,18 +393,14 @@ struct Math {
             if (!(((live >> slot) & 1u) && t0 + slot < lim[n][i & 1])) s[x][n][i] = -INFINITY;
           }
     }
-    // score - reference: slots t0 + 16 x + g + 8 (i / 2), columns 2 c + i % 2 of block n.
-    // (Two roundings: the score is the reference's own kind of number, however large.)
+    // score - reference: slots t0 + 16 x + g + 8 (i / 2), columns 2 c + i % 2 of block n
     float d[kTiles][NB][4], most = -INFINITY;
-    auto differences = [&]() {
 #pragma unroll
-      for (int x = 0; x < kTiles; ++x)
+    for (int x = 0; x < kTiles; ++x)
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+      for (int n = 0; n < NB; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) d[x][n][i] = __fsub_rn(__fmul_rn(s[x][n][i], mul[n][i & 1]), ref[n][i & 1]);
-    };
-    differences();
+        for (int i = 0; i < 4; ++i) d[x][n][i] = fmaf(s[x][n][i], mul[n][i & 1], -ref[n][i & 1]);
 #pragma unroll
     for (int x = 0; x < kTiles; ++x)
 #pragma unroll
@@ -421,7 +426,14 @@ struct Math {
             o[n][m][i + 2] *= corr;
           }
         }
-      differences();
+      // (Two roundings: the rounded score is what the reference is made of.  One would
+      // leave scores past 2^24 off it by more than the reference's lead.)
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) d[x][n][i] = __fsub_rn(__fmul_rn(s[x][n][i], mul[n][i & 1]), ref[n][i & 1]);
     }
 #pragma unroll
     for (int x = 0; x < kTiles; ++x) {
@@ -440,7 +452,7 @@ struct Math {
           }
           p[n][0][h] = transposed(p[n][0][h]);
         }
-      values(st + x * stride, at, lane, live >> (16 * x) & 0xFFFFu, p);
+      values<WHOLE>(st + x * stride, at, lane, live >> (16 * x), p);
     }
   }
 
@@ -473,8 +485,6 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
   using SH = Shape<HD>;
   constexpr int STAGE = kTiles * (BIG ? SH::TILE : SH::SMALL);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  __shared__ uint64_t full[kQ4Warps][kStages];
-  __shared__ uint32_t live_s[kQ4Warps][kStages];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int C = p.pieces;
   const int unit = (int)(blockIdx.x / (unsigned)C), piece = (int)(blockIdx.x - (unsigned)unit * C);
@@ -483,11 +493,6 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
   const int cols = min(8 * NB, p.Tq * p.G - x0), max_slots = p.max_pages * p.P;
   unsigned char* ring = smem_raw + warp * kStages * STAGE;
   float* crec = reinterpret_cast<float*>(smem_raw + kQ4Warps * kStages * STAGE);
-  if (lane == 0) {
-    for (int i = 0; i < kStages; ++i) mbar_init(&full[warp][i], 1);
-    fence_mbar_init();
-  }
-  __syncwarp();
 
   // Dependents start only after this grid's own wait, so that everything before
   // it is visible to them whatever they wait for.
@@ -516,54 +521,71 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
   const int j0 = (int)((int64_t)mine * nsteps / nparts);
   const int nmine = (int)((int64_t)(mine + 1) * nsteps / nparts) - j0;
 
-  // lane i < tiles of a step: tile i of step j (-1: not seen, or no such page)
+  // ---- the warp's copies: step i into ring slot i % kStages, in 16-byte chunks
   const int32_t* ptab = p.page_table + (int64_t)b * p.max_pages;
-  const int tiles = BIG ? kTiles : kSlots >> p.log2tile, per_page = BIG ? p.P / kQ4Step : 1;
-  auto tile_at = [&](int j) -> int {
-    int at = -1;
-    const int t = j * kSlots + (BIG ? lane * kQ4Step : lane << p.log2tile);
-    if (lane < tiles && j < j0 + nmine && t < S) {
-      const int pg = __ldg(ptab + (t >> p.log2P));
-      if (pg >= 0 && pg < p.num_pages) at = (pg * p.Hkv + h) * per_page + (BIG ? (t & (p.P - 1)) / kQ4Step : 0);
-      else report(p.status, WM_ERR_BOUNDS);
-    }
-    return at;
-  };
-  const uint64_t policy = l2_evict_first_policy();
+  const uint32_t ring_s = smem_u32(ring), to_s = ring_s + lane * 16;
+  const uint8_t* pool_lane = p.pool + lane * 16;
   const uint32_t tile_bytes = BIG ? SH::TILE : p.tile_bytes;
   const uint32_t stride = BIG ? SH::TILE : kQ4Step / p.tile * tile_bytes;
-  auto issue = [&](int i, int at) {  // the warp's i-th step into ring slot i % kStages
-    const uint32_t mask = __ballot_sync(FULL, at >= 0);
-    uint64_t* bar = &full[warp][i % kStages];
-    if (lane == 0) {
-      uint32_t live = 0;
-      if (BIG) {
-#pragma unroll
-        for (int x = 0; x < kTiles; ++x)
-          if ((mask >> x) & 1u) live |= 0xFFFFu << (16 * x);
-      } else {
-        const uint32_t one = (1u << p.tile) - 1;
-        for (int x = 0; x < tiles; ++x)
-          if ((mask >> x) & 1u) live |= one << (x << p.log2tile);
-      }
-      const int rest = S - (j0 + i) * kSlots;
-      if (rest < kSlots) live &= (1u << rest) - 1;
-      live_s[warp][i % kStages] = live;
-      mbar_arrive_expect_tx(bar, __popc(mask) * tile_bytes);
+  const int log2tile = BIG ? 4 : p.log2tile, tiles = kSlots >> log2tile, per_batch = 1 << log2tile;
+  // Tiles of `per_batch` steps from step i on, one per lane: its place in the pool
+  // (-1: not seen, or no such page).
+  auto look_up = [&](int i) -> int {
+    const int x = i + (lane >> (5 - log2tile)), t = (j0 + i) * kSlots + (lane << log2tile);
+    if (x >= nmine || t >= S) return -1;
+    const int pg = __ldg(ptab + (t >> p.log2P));
+    if ((unsigned)pg >= (unsigned)p.num_pages) {
+      report(p.status, WM_ERR_BOUNDS);
+      return -1;
     }
-    if (at >= 0)
-      bulk_g2s(ring + (i % kStages) * STAGE + lane * tile_bytes, p.pool + (int64_t)at * tile_bytes, tile_bytes, bar, policy);
+    return BIG ? (pg * p.Hkv + h) * (p.P / kQ4Step) + (t & (p.P - 1)) / kQ4Step : pg * p.Hkv + h;
   };
-  int next = tile_at(j0);
+  int batch = look_up(0), ahead = look_up(per_batch);
+  // Returns which of the step's tiles are there (a bit per tile).
+  auto issue = [&](int i) -> uint32_t {
+    const int first = (i & (per_batch - 1)) * tiles;  // lane that holds the step's first tile
+    const uint32_t to = to_s + (i % kStages) * STAGE;
+    uint32_t there;
+    if constexpr (BIG) {
+      constexpr int CH = SH::TILE / 16;
+      there = 0;
 #pragma unroll
-  for (int i = 0; i < kStages; ++i) {
-    const int at = next;
-    next = tile_at(j0 + i + 1);
-    if (i < nmine) issue(i, at);
-  }
+      for (int x = 0; x < kTiles; ++x) {
+        const int at = __shfl_sync(FULL, batch, first + x);
+        const uint8_t* from = pool_lane + (int64_t)at * SH::TILE;
+        if (at >= 0) {
+          there |= 1u << x;
+#pragma unroll
+          for (int y = 0; y < CH; y += 32)
+            cp_async16(to + x * SH::TILE + y * 16, from + y * 16, y + 32 <= CH || lane < CH - y);
+        }
+      }
+    } else {
+      const int chunks = (int)tile_bytes / 16, magic = 65536 / chunks + 1;
+      there = __ballot_sync(FULL, batch >= 0) >> first;
+      if (tiles < 32) there &= (1u << tiles) - 1;
+      for (int y = lane; y < (tiles * chunks + 31) / 32 * 32; y += 32) {
+        const int x = y * magic >> 16, at = __shfl_sync(FULL, batch, (first + x) & 31);
+        cp_async16(to + (y - lane) * 16, p.pool + (int64_t)at * tile_bytes + (y - x * chunks) * 16, x < tiles && at >= 0);
+      }
+    }
+    if ((i & (per_batch - 1)) == per_batch - 1) {
+      batch = ahead;
+      ahead = look_up(i + 1 + per_batch);
+    }
+    return there;
+  };
+  // one commit group per step, empty ones included, so that group i is step i
+  static_assert(kStages == 2 && kTiles == 2, "two steps in flight, two tiles each");
+  uint32_t there = 0, there_next = 0;
+  if (nmine > 0) there = issue(0);
+  cp_async_commit();
+  if (nmine > 1) there_next = issue(1);
+  cp_async_commit();
 
   // ---- queries
-  Math<T, HD, NB> mm;
+  using Mm = Math<T, HD, NB, BIG>;
+  Mm mm;
   mm.init();
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
@@ -577,32 +599,29 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
     }
     mm.load(n, row, lim, lane, p.qscale);
   }
-  const typename Math<T, HD, NB>::At at =
-      BIG ? Math<T, HD, NB>::offsets(kQ4Step, 4, SH::TILE, lane)
-          : Math<T, HD, NB>::offsets(p.tile, p.log2tile, p.tile_bytes, lane);
+  const typename Mm::At at = Mm::offsets(p.tile, p.log2tile, p.tile_bytes, lane);
 
-  bool ok = true;
-  for (int i = 0; i < nmine; ++i) {
-    ok = __all_sync(FULL, mbar_wait(&full[warp][i % kStages], (i / kStages) & 1));
-    if (!ok) break;
-    const uint32_t live = live_s[warp][i % kStages];
-    const int t0 = (j0 + i) * kSlots;
-    mm.step(smem_u32(ring + (i % kStages) * STAGE), stride, at, lane, t0, live, live == FULL && t0 + kSlots <= least);
-    __syncwarp();  // every lane is done with this ring slot
-    const int to = next;
-    next = tile_at(j0 + i + kStages + 1);
-    if (i + kStages < nmine) issue(i + kStages, to);
-  }
-  if (!ok) {
-    // a copy never arrived: report it, and give the others their time before the ring is
-    // used for records
-    if (lane == 0) report(p.status, WM_ERR_TIMEOUT);
-    for (int i = 0; i < kStages; ++i) {
-      if (lane == 0) mbar_wait(&full[warp][i], 0, kWaitLimitNs / 100);
-      if (lane == 0) mbar_wait(&full[warp][i], 1, kWaitLimitNs / 100);
-      __syncwarp();
+  const uint32_t every = BIG || tiles < 32 ? (1u << tiles) - 1 : FULL;
+  int t0 = j0 * kSlots;
+  for (int i = 0; i < nmine; ++i, t0 += kSlots) {
+    cp_async_wait<kStages - 1>();
+    __syncwarp();
+    const uint32_t st = ring_s + (i % kStages) * STAGE;
+    if (there == every && t0 + kSlots <= least) {
+      mm.template step<true>(st, stride, at, lane, t0, FULL);
+    } else {
+      uint32_t live = 0;
+      for (int x = 0; x < tiles; ++x)
+        if ((there >> x) & 1u) live |= ((1u << per_batch) - 1) << (x << log2tile);
+      if (S - t0 < kSlots) live &= (1u << (S - t0)) - 1;
+      mm.template step<false>(st, stride, at, lane, t0, live);
     }
+    __syncwarp();  // every lane is done with this ring slot
+    there = there_next;
+    if (i + kStages < nmine) there_next = issue(i + kStages);
+    cp_async_commit();
   }
+  cp_async_wait<0>();
 
   // ---- join the CTA's warps (each warp's state in its idle ring)
   __syncwarp();
