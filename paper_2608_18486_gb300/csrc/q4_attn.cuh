@@ -63,8 +63,7 @@ struct Parts {
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                     uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
       "{%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -72,13 +71,40 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
 // The 8 x 8 matrix of 16-bit elements, row lane / 4, columns 2 (lane % 4) + {0, 1}, transposed.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool on) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(dst),
-               "l"(src), "r"((int)on)
-               : "memory");
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(dst),
+      "l"(src), "r"((int)on)
+      : "memory");
+}
+// A whole tile, 16 bytes per lane and copy (dst and src at the lane's first); at < 0: none.
+// One statement, so that its predicates are made once.
+template <int HD>
+__device__ __forceinline__ void cp_async_tile(uint32_t dst, const void* src, int at, int lane) {
+  constexpr int REST = 16 * (HD + HD / 8) / 16 % 32;  // lanes of the last copy
+  static_assert(HD == 64 || HD == 96 || HD == 128, "72, 108 or 144 chunks");
+#define WM_Q4_CP(N) "@p cp.async.cg.shared.global [%0 + " #N "], [%1 + " #N "], 16;\n\t"
+#define WM_Q4_CP_LAST(N) "@q cp.async.cg.shared.global [%0 + " #N "], [%1 + " #N "], 16;\n\t}"
+#define WM_Q4_CP_PRED \
+  "{\n\t.reg .pred p, q;\n\tsetp.ge.s32 p, %2, 0;\n\tsetp.lt.and.s32 q, %3, %4, p;\n\t"
+  if constexpr (HD == 64)
+    asm volatile(WM_Q4_CP_PRED WM_Q4_CP(0) WM_Q4_CP(512) WM_Q4_CP_LAST(1024) ::"r"(dst), "l"(src), "r"(at), "r"(lane),
+                 "n"(REST)
+                 : "memory");
+  else if constexpr (HD == 96)
+    asm volatile(WM_Q4_CP_PRED WM_Q4_CP(0) WM_Q4_CP(512) WM_Q4_CP(1024) WM_Q4_CP_LAST(1536) ::"r"(dst), "l"(src),
+                 "r"(at), "r"(lane), "n"(REST)
+                 : "memory");
+  else
+    asm volatile(WM_Q4_CP_PRED WM_Q4_CP(0) WM_Q4_CP(512) WM_Q4_CP(1024) WM_Q4_CP(1536) WM_Q4_CP_LAST(2048) ::"r"(dst),
+                 "l"(src), "r"(at), "r"(lane), "n"(REST)
+                 : "memory");
+#undef WM_Q4_CP
+#undef WM_Q4_CP_LAST
+#undef WM_Q4_CP_PRED
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -126,22 +152,6 @@ __device__ __forceinline__ void split(float x, float y, uint32_t (&part)[N]) {
     }
   }
 }
-__device__ __forceinline__ uint32_t lds32(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-  return v;
-}
-__device__ __forceinline__ uint32_t lds16(uint32_t a) {
-  uint16_t v;
-  asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
-  return v;
-}
-__device__ __forceinline__ uint32_t lds8(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-  return v;
-}
-
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -241,27 +251,30 @@ struct Math {
   }
 
   // S^T of the 16 slots at shared address st.
-  __device__ __forceinline__ void scores(uint32_t st, const At& at, int lane, float (&s)[NB][4]) {
+  __device__ __forceinline__ void scores(const unsigned char* st, const At& at, int lane, float (&s)[NB][4]) {
     const int c = lane & 3;
     uint32_t kw[2][SH::KW], sc[2][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const uint32_t a = st + at.k(i);
+      const unsigned char* a = st + at.k(i);
       if constexpr (HD == 128) {
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(kw[i][0]), "=r"(kw[i][1]), "=r"(kw[i][2]), "=r"(kw[i][3])
-                     : "r"(a)
-                     : "memory");
-        sc[i][0] = lds8(st + at.ks(i)) * 0x00800080u;  // an fp16 pair
-        sc[i][1] = lds8(st + at.ks(i) + 1) * 0x00800080u;
+        const uint4 v = *reinterpret_cast<const uint4*>(a);
+        kw[i][0] = v.x;
+        kw[i][1] = v.y;
+        kw[i][2] = v.z;
+        kw[i][3] = v.w;
+        sc[i][0] = st[at.ks(i)] * 0x00800080u;  // an fp16 pair
+        sc[i][1] = st[at.ks(i) + 1] * 0x00800080u;
       } else if constexpr (HD == 64) {
-        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(kw[i][0]), "=r"(kw[i][1]) : "r"(a) : "memory");
-        sc[i][0] = sc[i][1] = lds8(st + at.ks(i)) * 0x00800080u;
+        const uint2 v = *reinterpret_cast<const uint2*>(a);
+        kw[i][0] = v.x;
+        kw[i][1] = v.y;
+        sc[i][0] = sc[i][1] = st[at.ks(i)] * 0x00800080u;
       } else {
 #pragma unroll
-        for (int w = 0; w < SH::KW; ++w) kw[i][w] = lds32(a + 4 * w);
-        sc[i][0] = lds8(st + at.ks(i)) * 0x00800080u;
-        sc[i][1] = lds8(st + at.ks(i) + 1) * 0x00800080u;
+        for (int w = 0; w < SH::KW; ++w) kw[i][w] = reinterpret_cast<const uint32_t*>(a)[w];
+        sc[i][0] = st[at.ks(i)] * 0x00800080u;
+        sc[i][1] = st[at.ks(i) + 1] * 0x00800080u;
       }
     }
 #pragma unroll
@@ -307,14 +320,14 @@ struct Math {
 
   // O^T += V^T P^T of the 16 slots at st; live: bit per slot that is there (WHOLE: all).
   template <bool WHOLE>
-  __device__ __forceinline__ void values(uint32_t st, const At& at, int lane, uint32_t live,
+  __device__ __forceinline__ void values(const unsigned char* st, const At& at, int lane, uint32_t live,
                                          const uint32_t (&p)[NB][NP][2]) {
     const int g = lane >> 2, c = lane & 3;
     uint32_t vs[2][2];  // scales of two slots, for the pairs 2 c + {0, 1} and 8 more
     auto pair_scales = [&](int off, uint32_t (&to)[2]) {
       uint32_t b[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) b[i] = lds8(st + at.vs(i) + off);
+      for (int i = 0; i < 4; ++i) b[i] = st[at.vs(i) + off];
       if (!WHOLE)  // what lies in other slots must not reach the sums: 0 times any code
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -332,12 +345,14 @@ struct Math {
     uint32_t vw[4][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t a = st + at.v(i);
+      const unsigned char* a = st + at.v(i);
       if constexpr (HD == 128) {
-        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(vw[i][0]), "=r"(vw[i][1]) : "r"(a) : "memory");
+        const uint2 v = *reinterpret_cast<const uint2*>(a);
+        vw[i][0] = v.x;
+        vw[i][1] = v.y;
       } else {
-        vw[i][0] = lds32(a);
-        vw[i][1] = HD == 96 ? lds16(a - 4 * g + 32 + 2 * g) : 0u;
+        vw[i][0] = *reinterpret_cast<const uint32_t*>(a);
+        vw[i][1] = HD == 96 ? *reinterpret_cast<const uint16_t*>(a - 4 * g + 32 + 2 * g) : 0u;
       }
     }
 #pragma unroll
@@ -377,7 +392,7 @@ struct Math {
   // slot; live: bit per slot that is there and below the unit's largest limit;
   // WHOLE: every column sees every slot.
   template <bool WHOLE>
-  __device__ __forceinline__ void step(uint32_t st, uint32_t stride, const At& at, int lane, int t0, uint32_t live) {
+  __device__ __forceinline__ void step(const unsigned char* st, uint32_t stride, const At& at, int lane, int t0, uint32_t live) {
     const int g = lane >> 2;
     float s[kTiles][NB][4];
 #pragma unroll
@@ -547,18 +562,12 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
     const uint32_t to = to_s + (i % kStages) * STAGE;
     uint32_t there;
     if constexpr (BIG) {
-      constexpr int CH = SH::TILE / 16;
       there = 0;
 #pragma unroll
       for (int x = 0; x < kTiles; ++x) {
         const int at = __shfl_sync(FULL, batch, first + x);
-        const uint8_t* from = pool_lane + (int64_t)at * SH::TILE;
-        if (at >= 0) {
-          there |= 1u << x;
-#pragma unroll
-          for (int y = 0; y < CH; y += 32)
-            cp_async16(to + x * SH::TILE + y * 16, from + y * 16, y + 32 <= CH || lane < CH - y);
-        }
+        if (at >= 0) there |= 1u << x;
+        cp_async_tile<HD>(to + x * SH::TILE, pool_lane + (int64_t)at * SH::TILE, at, lane);
       }
     } else {
       const int chunks = (int)tile_bytes / 16, magic = 65536 / chunks + 1;
@@ -606,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
   for (int i = 0; i < nmine; ++i, t0 += kSlots) {
     cp_async_wait<kStages - 1>();
     __syncwarp();
-    const uint32_t st = ring_s + (i % kStages) * STAGE;
+    const unsigned char* st = ring + (i % kStages) * STAGE;
     if (there == every && t0 + kSlots <= least) {
       mm.template step<true>(st, stride, at, lane, t0, FULL);
     } else {
