@@ -65,7 +65,7 @@ cudaError_t launch_q4_read(const Q4CopyParams& p, int dtype, int d, int sms, cud
 constexpr int kQ4Warps = 4;        // warps per CTA
 constexpr int kQ4Slots = 32;       // slots of a warp's step
 constexpr int kQ4MaxCluster = 8;
-constexpr int kQ4MaxPieces = 64;
+constexpr int kQ4MinSteps = 4;     // steps of a warp at least where all steps are spread
 constexpr int kQ4CtasPerSm = 4;
 
 struct Q4AttnParams {
@@ -75,13 +75,14 @@ struct Q4AttnParams {
   const int32_t* page_table;  // [B][max_pages]
   const int32_t* lens;        // [B][Tq]: the row sees slots t < lens + len_add
   int32_t* status;
-  float* part;                // [units][pieces][q4_rec] where a second kernel joins
+  float* part;                // not NULL: all steps are spread over `pieces` CTAs, records
+                              // [pieces][2][q4_rec] of shared units are joined by a second kernel
   int64_t page_bytes;         // of one kv head
   int32_t len_add;
   int32_t B, Tq, Hq, Hkv, G, P, log2P, tile, log2tile, tile_bytes, num_pages, max_pages;
   int32_t col_blocks;         // units per (sequence, kv head): groups of 8 NB (row, head) columns
   int32_t nb;                 // NB
-  int32_t pieces;             // CTAs per unit
+  int32_t pieces;             // CTAs per unit (one cluster), or of the spread
   float qscale;               // log2(e) / sqrt(d)
 };
 // floats of a partial record: cols x d unnormalised outputs, (reference, sum) per column

@@ -98,19 +98,17 @@ wm_status copy_ranges(bool write, const wm_config* c, const wm_cache* cache, con
                            : launch_q4_read(p, c->dtype, c->d, sm_count(), (cudaStream_t)stream));
 }
 
-// Split of an attention call: columns per unit, CTAs per unit, and whether these
-// join on chip (a cluster) or through records in the workspace.
+// Split of an attention call.  Short units are one cluster each, joined on chip; the
+// steps of long ones are spread evenly over the resident CTAs, whatever the lengths,
+// and a second kernel joins the units that were cut.
 struct Q4Plan {
-  int nb, col_blocks, pieces;
-  bool records;
+  int nb, col_blocks;
+  int pieces;    // CTAs per unit, or of the spread
+  bool spread;
   size_t total;  // workspace
 };
 
-int clamp_int(int64_t x, int64_t lo, int64_t hi) { return (int)(x < lo ? lo : x > hi ? hi : x); }
-
-constexpr int kLongSteps = 12;  // steps of a warp from which a unit is cut into records
-constexpr int kMinSteps = 4;    // steps that a cut leaves each warp at least
-constexpr int kWaves = 4;       // waves of resident CTAs that a cut aims at
+constexpr int kLongSteps = 12;  // steps of a cluster's warp from which they are spread
 
 Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   const int64_t cols = (int64_t)Tq * (c.Hq / c.Hkv);
@@ -119,19 +117,15 @@ Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   pl.col_blocks = (int)((cols + 8 * pl.nb - 1) / (8 * pl.nb));
   const int64_t units = (int64_t)B * c.Hkv * pl.col_blocks;
   const int64_t steps = ((int64_t)max_pages * c.page_size + kQ4Slots - 1) / kQ4Slots;
-  const int64_t resident = (int64_t)sm_count() * (pl.nb == 1 && c.dtype == WM_DT_BF16 ? kQ4CtasPerSm : 2);
+  const int resident = sm_count() * (pl.nb == 1 && c.dtype == WM_DT_BF16 ? kQ4CtasPerSm : 2);
   int C = 1;
   while (C < kQ4MaxCluster && units * C * 2 <= resident && (int64_t)C * kQ4Warps < steps) C *= 2;
   pl.pieces = C;
   pl.total = 256;
-  if (steps > (int64_t)C * kQ4Warps * kLongSteps) {
-    const int64_t by_work = steps / (kQ4Warps * kMinSteps), by_sms = (resident * kWaves + units - 1) / units;
-    const int n = clamp_int(by_work < by_sms ? by_work : by_sms, 1, kQ4MaxPieces);
-    if (n > C) {
-      pl.pieces = n;
-      pl.records = true;
-      pl.total = align256(sizeof(float) * (size_t)units * n * q4_rec(8 * pl.nb, c.d));
-    }
+  if (pl.col_blocks == 1 && steps > (int64_t)C * kQ4Warps * kLongSteps) {
+    pl.pieces = resident;
+    pl.spread = true;
+    pl.total = align256(sizeof(float) * 2 * (size_t)resident * q4_rec(8 * pl.nb, c.d));
   }
   return pl;
 }
@@ -150,7 +144,7 @@ wm_status attn(const wm_config& c, const wm_q4_cache& q4, int32_t layer, const v
   p.page_table = page_table;
   p.lens = lens;
   p.status = dev_status;
-  p.part = pl.records ? (float*)workspace : nullptr;
+  p.part = pl.spread ? (float*)workspace : nullptr;
   p.page_bytes = q4_page_bytes(c.page_size, c.d);
   p.len_add = len_add;
   p.B = B;

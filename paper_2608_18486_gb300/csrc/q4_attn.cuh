@@ -493,6 +493,73 @@ struct Math {
   }
 };
 
+// Slots that row x / G of sequence b sees (0: a bad length).
+__device__ __forceinline__ int row_limit(const Q4AttnParams& p, int b, int row, bool& bad) {
+  const int n = __ldg(p.lens + (int64_t)b * p.Tq + row);
+  bad = n < 0 || n > p.max_pages * p.P - p.len_add;
+  return bad ? 0 : n + p.len_add;
+}
+// Steps of a sequence's units.
+__device__ __forceinline__ int seq_steps(const Q4AttnParams& p, int b, bool reporter) {
+  int S = 0;
+  for (int r = 0; r < p.Tq; ++r) {
+    bool bad;
+    S = max(S, row_limit(p, b, r, bad));
+    if (bad && reporter) report(p.status, WM_ERR_BOUNDS);
+  }
+  return (S + kSlots - 1) / kSlots;
+}
+
+// Where the steps of all units are spread evenly over the CTAs (col_blocks 1): in the
+// order (sequence, kv head, step) CTA i of n takes steps T i / n .. T (i + 1) / n - 1.
+// Counts steps of all sequences, and of those before sequence b_end; all threads of
+// the block (NT) call it.
+template <int NT>
+struct Spread {
+  int64_t total, before, own;  // steps x Hkv; own: of this thread's sequences, from `mine` on
+  int64_t mine;
+  int n;                       // CTAs
+  __device__ __forceinline__ int first_seq(const Q4AttnParams& p) const {
+    return (int)threadIdx.x * ((p.B + NT - 1) / NT);
+  }
+  __device__ __forceinline__ void count(const Q4AttnParams& p, int b_end, int ctas, bool reporter) {
+    __shared__ int64_t sums[2][NT / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = (p.B + NT - 1) / NT;
+    own = 0;
+    int64_t low = 0;
+    for (int b = first_seq(p); b < min(first_seq(p) + per, p.B); ++b) {
+      const int64_t w = (int64_t)seq_steps(p, b, reporter) * p.Hkv;
+      own += w;
+      if (b < b_end) low += w;
+    }
+    int64_t incl = own;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int64_t x = __shfl_up_sync(FULL, incl, o);
+      if (lane >= o) incl += x;
+      low += __shfl_xor_sync(FULL, low, o);
+    }
+    if (lane == 31) {
+      sums[0][warp] = incl;
+      sums[1][warp] = low;
+    }
+    __syncthreads();
+    total = before = 0;
+    mine = incl - own;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) {
+      if (w < warp) mine += sums[0][w];
+      total += sums[0][w];
+      before += sums[1][w];
+    }
+    const int64_t most = total / (kQ4Warps * kQ4MinSteps);
+    n = (int)(most < 1 ? 1 : most < ctas ? most : ctas);
+  }
+  __device__ __forceinline__ int64_t start(int i) const { return total * i / n; }
+  // the CTA that takes step x: the last one that starts at or before it
+  __device__ __forceinline__ int cta_of(int64_t x) const { return (int)(((x + 1) * n + total - 1) / total) - 1; }
+};
+
 // BIG: pages of at least 16 slots
 template <typename T, int HD, int NB, bool BIG>
 __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasPerSm : 2)
@@ -500,12 +567,8 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
   using SH = Shape<HD>;
   constexpr int STAGE = kTiles * (BIG ? SH::TILE : SH::SMALL);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
+  __shared__ int64_t at_s[2];  // spread: first sequence, and the step within its units
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int C = p.pieces;
-  const int unit = (int)(blockIdx.x / (unsigned)C), piece = (int)(blockIdx.x - (unsigned)unit * C);
-  const int bh = unit / p.col_blocks, x0 = (unit - bh * p.col_blocks) * 8 * NB;
-  const int b = bh / p.Hkv, h = bh - b * p.Hkv;
-  const int cols = min(8 * NB, p.Tq * p.G - x0), max_slots = p.max_pages * p.P;
   unsigned char* ring = smem_raw + warp * kStages * STAGE;
   float* crec = reinterpret_cast<float*>(smem_raw + kQ4Warps * kStages * STAGE);
 
@@ -514,27 +577,66 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  // ---- limits: slots that column x sees (0: a bad length)
-  auto limit = [&](int x, bool& bad) -> int {
-    const int n = __ldg(p.lens + (int64_t)b * p.Tq + x / p.G);
-    bad = n < 0 || n > max_slots - p.len_add;
-    return bad ? 0 : n + p.len_add;
-  };
+  int b, h, x0 = 0, piece = 0, C = 1;
+  int64_t off = 0, left = 0;  // spread: step among the sequence's units, steps left to take
+  const bool spread = p.part != nullptr;
+  if (spread) {
+    Spread<kThreads> sp;
+    sp.count(p, 0, (int)gridDim.x, blockIdx.x == 0);
+    if ((int)blockIdx.x >= sp.n) return;
+    const int64_t pos = sp.start(blockIdx.x);
+    left = sp.start(blockIdx.x + 1) - pos;
+    if (left == 0) return;
+    if (pos >= sp.mine && pos < sp.mine + sp.own) {
+      int64_t x = pos - sp.mine, w;
+      int y = sp.first_seq(p);
+      while (x >= (w = (int64_t)seq_steps(p, y, false) * p.Hkv)) {
+        x -= w;
+        ++y;
+      }
+      at_s[0] = y;
+      at_s[1] = x;
+    }
+    __syncthreads();
+    b = (int)at_s[0];
+    off = at_s[1];
+    h = 0;
+  } else {
+    C = p.pieces;
+    const int unit = (int)(blockIdx.x / (unsigned)C);
+    piece = (int)(blockIdx.x - (unsigned)unit * C);
+    const int bh = unit / p.col_blocks;
+    x0 = (unit - bh * p.col_blocks) * 8 * NB;
+    b = bh / p.Hkv;
+    h = bh - b * p.Hkv;
+  }
+  const int cols = min(8 * NB, p.Tq * p.G - x0), E = cols * HD;
+
+  for (;;) {  // units (one, unless spread)
   int S = 0, least = INT32_MAX;  // largest and smallest limit of the unit's columns
   {
     bool bad = false;
     if (lane < cols) {
-      S = limit(x0 + lane, bad);
-      least = S;
-      if (bad && h == 0 && piece == 0 && warp == 0) report(p.status, WM_ERR_BOUNDS);
+      least = S = row_limit(p, b, (x0 + lane) / p.G, bad);
+      if (bad && !spread && h == 0 && piece == 0 && warp == 0) report(p.status, WM_ERR_BOUNDS);
     }
     S = __reduce_max_sync(FULL, S);
     least = __reduce_min_sync(FULL, least);
   }
   const int nsteps = (S + kSlots - 1) / kSlots;
-  const int nparts = C * kQ4Warps, mine = piece * kQ4Warps + warp;
-  const int j0 = (int)((int64_t)mine * nsteps / nparts);
-  const int nmine = (int)((int64_t)(mine + 1) * nsteps / nparts) - j0;
+  int from = (int)((int64_t)piece * nsteps / C), steps = (int)((int64_t)(piece + 1) * nsteps / C) - from;
+  if (spread) {
+    if (off >= (int64_t)nsteps * p.Hkv) {  // on to the next sequence
+      off = 0;
+      ++b;
+      continue;
+    }
+    h = (int)(off / nsteps);
+    from = (int)(off - (int64_t)h * nsteps);
+    steps = (int)min((int64_t)(nsteps - from), left);
+  }
+  const int j0 = from + (int)((int64_t)warp * steps / kQ4Warps);
+  const int nmine = from + (int)((int64_t)(warp + 1) * steps / kQ4Warps) - j0;
 
   // ---- the warp's copies: step i into ring slot i % kStages, in 16-byte chunks
   const int32_t* ptab = p.page_table + (int64_t)b * p.max_pages;
@@ -604,7 +706,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
     if (col < cols) {
       bool bad;
       row = reinterpret_cast<const T*>(p.q) + (((int64_t)b * p.Tq + x / p.G) * p.Hq + h * p.G + x % p.G) * HD;
-      lim = limit(x, bad);
+      lim = row_limit(p, b, x / p.G, bad);
     }
     mm.load(n, row, lim, lane, p.qscale);
   }
@@ -637,7 +739,6 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
   float* wrec = reinterpret_cast<float*>(ring);
   mm.store(wrec, cols, lane);
   __syncthreads();
-  const int E = cols * HD;
   auto warp_rec = [&](int w) -> const float* {
     return reinterpret_cast<const float*>(smem_raw + w * kStages * STAGE);
   };
@@ -645,8 +746,11 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
     const int x = x0 + col;
     return reinterpret_cast<T*>(p.out) + (((int64_t)b * p.Tq + x / p.G) * p.Hq + h * p.G + x % p.G) * HD;
   };
-  float* gpart = p.part ? p.part + (int64_t)blockIdx.x * q4_rec(8 * NB, HD) : nullptr;
-  const bool direct = C == 1 && !gpart;
+  // a unit that a CTA has to itself is done; its part of a shared one goes to the
+  // CTA's record 0 (the unit began before its steps) or 1
+  const bool direct = steps == nsteps;
+  float* rec = spread ? p.part + ((int64_t)blockIdx.x * 2 + (from == 0)) * q4_rec(8 * NB, HD) : crec;
+  const int ml = spread ? 8 * NB * HD : E;  // where (reference, sum) are in it
   for (int e = tid; e < E; e += kThreads) {
     const int r = e / HD;
     float M = -FLT_MAX, L = 0.f, O = 0.f;
@@ -658,18 +762,24 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
       L = fmaf(wt, warp_rec(w)[E + 2 * r + 1], L);
       O = fmaf(wt, warp_rec(w)[e], O);
     }
-    if (direct) {
+    if (direct && C == 1) {
       out_row(r)[e - r * HD] = Elem<T>::from_f(L == 0.f ? 0.f : O / L);
     } else {
-      float* rec = gpart ? gpart : crec;
       rec[e] = O;
       if (e == r * HD) {
-        rec[(gpart ? 8 * NB * HD : E) + 2 * r] = M;
-        rec[(gpart ? 8 * NB * HD : E) + 2 * r + 1] = L;
+        rec[ml + 2 * r] = M;
+        rec[ml + 2 * r + 1] = L;
       }
     }
   }
-  if (direct || gpart) return;
+  if (spread) {
+    left -= steps;
+    if (left == 0) return;
+    off += steps;
+    __syncthreads();  // the rings take copies again
+    continue;
+  }
+  if (C == 1) return;
 
   // ---- join the cluster's CTAs through distributed shared memory: CTA `piece`
   // finishes its share.  The last barrier keeps each CTA's shared memory until
@@ -698,68 +808,90 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasP
     out_row(r)[e - r * HD] = Elem<T>::from_f(L == 0.f ? 0.f : O / L);
   }
   cluster.sync();
+  return;
+  }
 }
 
-// Joins the records of a unit's pieces: out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i.
+// Joins the records of units whose steps several CTAs took: out = sum_i 2^(m_i - M) O_i /
+// sum_i 2^(m_i - M) l_i.  blockIdx.x is the unit, blockIdx.y 32 groups of four of its
+// outputs; 8 threads share a group's records.  Units without steps get their zeros.
 template <typename T, int HD>
-__global__ void __launch_bounds__(256) q4_join_kernel(const Q4AttnParams p) {
+__global__ void __launch_bounds__(256) q4_join_kernel(const Q4AttnParams p, int ctas) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  constexpr int MAXC = 16;
-  __shared__ float w_s[MAXC][kQ4MaxPieces], inv_s[MAXC];
-  const int unit = blockIdx.x, most = 8 * p.nb;
-  const int bh = unit / p.col_blocks, x0 = (unit - bh * p.col_blocks) * most;
-  const int b = bh / p.Hkv, h = bh - b * p.Hkv, cols = min(most, p.Tq * p.G - x0);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, recf = q4_rec(most, HD);
-  const float* part = p.part + (int64_t)unit * p.pieces * recf;
-  for (int r = warp; r < cols; r += 8) {
-    const float* ml = part + most * HD + 2 * r;
-    float M = -FLT_MAX, L = 0.f;
-    for (int i = lane; i < p.pieces; i += 32) M = fmaxf(M, __ldcg(ml + (int64_t)i * recf));
+  __shared__ float4 o_s[8][32];
+  __shared__ float l_s[8][32];
+  const int b = (int)blockIdx.x / p.Hkv, h = (int)blockIdx.x - b * p.Hkv, cols = p.Tq * p.G, most = 8 * p.nb;
+  const int tid = threadIdx.x, lane = tid & 31, grp = tid >> 5, recf = q4_rec(most, HD);
+  const int y = blockIdx.y * 32 + lane;  // four outputs
+  const bool on = y < cols * HD / 4;
+  const int r = on ? y / (HD / 4) : 0, e = on ? (y - r * (HD / 4)) * 4 : 0;
+  Spread<256> sp;
+  sp.count(p, b, ctas, false);
+  const int ns = seq_steps(p, b, false);
+  float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+  float L = 0.f;
+  if (ns > 0) {
+    const int64_t x = sp.before + (int64_t)h * ns;
+    const int first = sp.cta_of(x), n = sp.cta_of(x + ns - 1) - first + 1;
+    if (n == 1) return;  // written by its CTA
+    // record i: the first CTA's begins with the unit
+    auto rec = [&](int i) -> const float* { return p.part + ((int64_t)(first + i) * 2 + (i == 0)) * recf; };
+    float M = -FLT_MAX;
+    for (int i = grp; i < n; i += 8) M = fmaxf(M, __ldcg(rec(i) + most * HD + 2 * r));
+    l_s[grp][lane] = M;
+    __syncthreads();
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(FULL, M, o));
-    for (int i = lane; i < p.pieces; i += 32) {
-      const float w = exp2f(__ldcg(ml + (int64_t)i * recf) - M);
-      w_s[r][i] = w;
-      L = fmaf(w, __ldcg(ml + (int64_t)i * recf + 1), L);
-    }
-    L = warp_sum(L);
-    if (lane == 0) inv_s[r] = L == 0.f ? 0.f : 1.f / L;
-  }
-  __syncthreads();
-  for (int y = tid; y < cols * HD / 4; y += 256) {
-    const int r = y / (HD / 4), e = (y - r * (HD / 4)) * 4, x = x0 + r;
-    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int NBUF = 8;
-    for (int i0 = 0; i0 < p.pieces; i0 += NBUF) {
+    for (int i = 0; i < 8; ++i) M = fmaxf(M, l_s[i][lane]);
+    __syncthreads();
+    constexpr int NBUF = 4;
+    for (int i0 = grp; i0 < n; i0 += 8 * NBUF) {
       float4 v[NBUF];
+      float2 ml[NBUF];
 #pragma unroll
       for (int i = 0; i < NBUF; ++i)
-        if (i0 + i < p.pieces) v[i] = __ldcg(reinterpret_cast<const float4*>(part + (int64_t)(i0 + i) * recf) + y);
+        if (i0 + 8 * i < n) {
+          v[i] = __ldcg(reinterpret_cast<const float4*>(rec(i0 + 8 * i) + r * HD + e));
+          ml[i] = __ldcg(reinterpret_cast<const float2*>(rec(i0 + 8 * i) + most * HD + 2 * r));
+        }
 #pragma unroll
       for (int i = 0; i < NBUF; ++i) {
-        if (i0 + i >= p.pieces) continue;
-        const float w = w_s[r][i0 + i];
+        if (i0 + 8 * i >= n) continue;
+        const float w = exp2f(ml[i].x - M);
+        L = fmaf(w, ml[i].y, L);
         O.x = fmaf(w, v[i].x, O.x);
         O.y = fmaf(w, v[i].y, O.y);
         O.z = fmaf(w, v[i].z, O.z);
         O.w = fmaf(w, v[i].w, O.w);
       }
     }
-    const float inv = inv_s[r];
-    T* out = reinterpret_cast<T*>(p.out) + (((int64_t)b * p.Tq + x / p.G) * p.Hq + h * p.G + x % p.G) * HD + e;
-    out[0] = Elem<T>::from_f(O.x * inv);
-    out[1] = Elem<T>::from_f(O.y * inv);
-    out[2] = Elem<T>::from_f(O.z * inv);
-    out[3] = Elem<T>::from_f(O.w * inv);
   }
+  o_s[grp][lane] = O;
+  l_s[grp][lane] = L;
+  __syncthreads();
+  if (grp > 0 || !on) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    const float4 v = o_s[i][lane];
+    L += l_s[i][lane];
+    O.x += v.x;
+    O.y += v.y;
+    O.z += v.z;
+    O.w += v.w;
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  T* out = reinterpret_cast<T*>(p.out) + (((int64_t)b * p.Tq + r / p.G) * p.Hq + h * p.G + r % p.G) * HD + e;
+  out[0] = Elem<T>::from_f(O.x * inv);
+  out[1] = Elem<T>::from_f(O.y * inv);
+  out[2] = Elem<T>::from_f(O.z * inv);
+  out[3] = Elem<T>::from_f(O.w * inv);
 }
 
-template <typename Kern>
-inline cudaError_t launch_chained(Kern kern, const Q4AttnParams& p, unsigned grid, int threads, size_t smem, int cluster,
-                                  cudaStream_t s) {
+template <typename Kern, typename... Args>
+inline cudaError_t launch_chained(Kern kern, dim3 grid, int threads, size_t smem, int cluster, cudaStream_t s,
+                                  const Args&... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
@@ -772,7 +904,7 @@ inline cudaError_t launch_chained(Kern kern, const Q4AttnParams& p, unsigned gri
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 0 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, p);
+  return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
 template <typename T, int HD, int NB, bool BIG>
@@ -786,9 +918,11 @@ inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
   const size_t smem = kQ4Warps * ring + (p.part ? 0 : rec);
   if (cudaError_t e = opt_in_smem(kern, smem, smem_set); e != cudaSuccess) return e;
   const unsigned units = (unsigned)p.B * p.Hkv * p.col_blocks;
-  const cudaError_t e = launch_chained(kern, p, units * (unsigned)p.pieces, kThreads, smem, p.part ? 0 : p.pieces, s);
-  if (e != cudaSuccess || !p.part) return e;
-  return launch_chained(q4_join_kernel<T, HD>, p, units, 256, 0, 0, s);
+  if (!p.part) return launch_chained(kern, dim3(units * (unsigned)p.pieces), kThreads, smem, p.pieces, s, p);
+  const cudaError_t e = launch_chained(kern, dim3(p.pieces), kThreads, smem, 0, s, p);
+  if (e != cudaSuccess) return e;
+  const unsigned groups = (unsigned)(p.Tq * p.G * HD / 4 + 31) / 32;
+  return launch_chained(q4_join_kernel<T, HD>, dim3(units, groups), 256, 0, 0, s, p, (int)p.pieces);
 }
 
 template <typename T, int HD>
