@@ -61,6 +61,25 @@ struct Q4CopyParams {
 cudaError_t launch_q4_write(const Q4CopyParams& p, int dtype, int d, int sms, cudaStream_t s);
 cudaError_t launch_q4_read(const Q4CopyParams& p, int dtype, int d, int sms, cudaStream_t s);
 
+// Many rows (bf16): a group of sequences is read back into the workspace and runs on
+// the tensor-core kernel of range_attn.h.
+struct Q4RowsPrep {
+  const int32_t* pos;         // [B][Tq]
+  const int32_t* q4_table;    // [B][max_pages]
+  int32_t* last;              // [B]: slots that some row sees
+  int32_t* lens;              // [B][Tq]: slots that each row sees, -1 for a bad position
+  int32_t* table;             // [B][max_pages]: pages of the rows in the workspace (-1: none)
+  int32_t Tq, max_pages, P, q4_pages;
+};
+cudaError_t launch_q4_rows_prep(const Q4RowsPrep& p, int B, cudaStream_t s);
+
+struct Q4RowsJoin {
+  const float* part;          // [B][Hkv][Tq * G][records][tile_rec(d)]
+  void* out;                  // [B][Tq][Hq][d]
+  int32_t B, Tq, Hq, Hkv, G, records;
+};
+cudaError_t launch_q4_rows_join(const Q4RowsJoin& p, int d, cudaStream_t s);
+
 // ------------------------------------------------------------ attention
 constexpr int kQ4Warps = 4;        // warps per CTA
 constexpr int kQ4Slots = 32;       // slots of a warp's step

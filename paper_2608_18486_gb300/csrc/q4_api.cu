@@ -2,6 +2,7 @@
 // of a cache to 4 bits and back, the pool appended in 4 bits, and attention over
 // it.  Argument checks, work splits and kernel dispatch; all device memory
 // belongs to the caller.
+#include <cuda_bf16.h>
 #include <math.h>
 #include <string.h>
 
@@ -166,6 +167,151 @@ wm_status attn(const wm_config& c, const wm_q4_cache& q4, int32_t layer, const v
   return cuda_status(launch_q4_attn(p, c.dtype, c.d, (cudaStream_t)stream));
 }
 
+// Many rows: a group of sequences is read back into the workspace (bf16 rows of one
+// channel) and attended to by the tensor-core kernel.  Where the group's rows alone make
+// too few items for the SMs, its KV tiles are cut as well, by the form of that kernel
+// for a prefix that rows of unequal lengths share: the rows of a sequence are such.
+struct RowsPlan {
+  bool tiles;
+  int group;                       // sequences read back at once
+  bool cut;
+  int pair, blocks, splits, records;
+  size_t off_v, off_table, off_last, off_lens, off_part, total;
+};
+
+// us per MB of codes, and per call, by which the two forms are chosen: the streaming
+// kernel per 16 columns, the tensor cores per 256 rows, reading back, the launches.
+constexpr double kStreamUs = 0.28, kTileUs = 0.71, kReadUs = 1.23, kTileLaunchUs = 20.;
+constexpr size_t kGroupBytes = 256 << 20;  // rows read back at once, beyond one sequence
+
+RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
+  RowsPlan pl{};
+  const int G = c.Hq / c.Hkv;
+  const int64_t rows = (int64_t)Tq * G, slots = (int64_t)max_pages * c.page_size;
+  if (c.dtype != WM_DT_BF16 || c.page_size < 8 || !tma_available()) return pl;
+  if (slots * c.Hkv >= INT32_MAX || (int64_t)B * Tq >= INT32_MAX || rows >= INT32_MAX / 2) return pl;
+  const double mb = (double)B * slots * c.Hkv * (c.d + c.d / 8) * 1e-6;
+  const double stream = kStreamUs * mb * (double)((rows + 15) / 16);
+  const double tile = kTileLaunchUs + mb * (kReadUs + kTileUs * (double)((rows + 255) / 256));
+  if (stream <= tile) return pl;
+  pl.tiles = true;
+  const size_t one = (size_t)slots * c.Hkv * c.d * 2 * 2;
+  int64_t group = kGroupBytes / one;
+  if (group > (INT32_MAX - 1) / (slots * c.Hkv)) group = (INT32_MAX - 1) / (slots * c.Hkv);
+  pl.group = (int)(group < 1 ? 1 : group > B ? B : group);
+  // items without cuts: two heads of 128 rows, or one of 256
+  const int64_t items = (int64_t)pl.group * (G % 2 == 0 ? c.Hq / 2 * ((Tq + kTileRows - 1) / kTileRows)
+                                                        : c.Hq * ((Tq + 2 * kTileRows - 1) / (2 * kTileRows)));
+  const int sms = sm_count();
+  pl.cut = items < 2 * sms;
+  pl.pair = rows <= kTileRows ? 1 : 0;
+  pl.blocks = pl.pair ? 1 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
+  pl.splits = 1;
+  if (pl.cut) {  // the count with the shortest last CTA, a CTA's start as two KV tiles
+    const int64_t units = (int64_t)pl.blocks * c.Hkv, tiles = (slots + kTileSlots - 1) / kTileSlots;
+    double least = 1e30;
+    for (int n = 1; n <= 32 && n <= tiles; ++n) {
+      const double cost = (double)((units * n + sms - 1) / sms) * ((double)((tiles + n - 1) / n) + 2.) + 0.05 * n;
+      if (cost < least) {
+        least = cost;
+        pl.splits = n;
+      }
+    }
+  }
+  pl.records = pl.splits * (pl.pair ? 2 : 1);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += align256(bytes);
+    return at;
+  };
+  take(one / 2 * pl.group);
+  pl.off_v = take(one / 2 * pl.group);
+  pl.off_table = take(sizeof(int32_t) * (size_t)pl.group * max_pages);
+  pl.off_last = take(sizeof(int32_t) * (size_t)pl.group);
+  pl.off_lens = take(sizeof(int32_t) * (size_t)pl.group * Tq);
+  pl.off_part = take(pl.cut ? sizeof(float) * (size_t)pl.group * c.Hkv * rows * pl.records * tile_rec(c.d) : 0);
+  pl.total = off;
+  return pl;
+}
+
+wm_status rows_on_tiles(const RowsPlan& pl, const wm_config& c, const wm_q4_cache& q4, int32_t layer, const void* q,
+                        const int32_t* pos, const int32_t* page_table, int32_t B, int32_t Tq, int32_t max_pages,
+                        void* out, char* ws, int32_t* dev_status, cudaStream_t s) {
+  const int G = c.Hq / c.Hkv, chan = c.chan_of_layer[layer];
+  int32_t* const table = (int32_t*)(ws + pl.off_table);
+  int32_t* const last = (int32_t*)(ws + pl.off_last);
+  int32_t* const lens = (int32_t*)(ws + pl.off_lens);
+  float* const part = (float*)(ws + pl.off_part);
+  const size_t row_elems = (size_t)Tq * c.Hq * c.d;
+  for (int32_t b0 = 0; b0 < B; b0 += pl.group) {
+    const int32_t n = B - b0 < pl.group ? B - b0 : pl.group;
+    Q4RowsPrep prep{};
+    prep.pos = pos + (size_t)b0 * Tq;
+    prep.q4_table = page_table + (size_t)b0 * max_pages;
+    prep.last = last;
+    prep.lens = lens;
+    prep.table = table;
+    prep.Tq = Tq;
+    prep.max_pages = max_pages;
+    prep.P = c.page_size;
+    prep.q4_pages = q4.num_pages;
+    if (launch_q4_rows_prep(prep, n, s) != cudaSuccess) return WM_ERR_CUDA;
+    Q4CopyParams r = copy_params(c, q4, n, max_pages, max_pages * c.page_size, dev_status);
+    r.pool += chan * channel_bytes(c, q4.num_pages);
+    r.k = 1;
+    r.k_rows = ws;
+    r.v_rows = ws + pl.off_v;
+    r.q4_table = prep.q4_table;
+    r.last = last;
+    r.rows_at = kQ4Dense;
+    r.row_pages = INT32_MAX;
+    if (launch_q4_read(r, c.dtype, c.d, sm_count(), s) != cudaSuccess) return WM_ERR_CUDA;
+    TileParams t{};
+    t.status = dev_status;
+    t.page_table = table;
+    t.Hq = c.Hq;
+    t.G = G;
+    t.Hkv = c.Hkv;
+    t.num_pages = n * max_pages;
+    t.max_pages = max_pages;
+    t.P = c.page_size;
+    t.log2P = ilog2(c.page_size);
+    t.qscale = (float)(1.4426950408889634 / sqrt((double)c.d));
+    t.splits = pl.splits;
+    __nv_bfloat16* const o = (__nv_bfloat16*)out + b0 * row_elems;
+    const __nv_bfloat16* const x = (const __nv_bfloat16*)q + b0 * row_elems;
+    if (!pl.cut) {
+      t.pos = prep.pos;
+      t.out = o;
+      t.rows = Tq;
+      t.window = max_pages * c.page_size;
+      t.pair = G % 2 == 0 ? 1 : 0;
+      const int block = t.pair ? kTileRows : 2 * kTileRows;
+      t.blocks = (Tq + block - 1) / block;
+      t.items = n * (t.pair ? c.Hq / 2 : c.Hq) * t.blocks;
+      const TileInputs in{x, ws, ws + pl.off_v, n, 1, c.d};
+      if (launch_tile_attn(t, in, sm_count(), s) != cudaSuccess) return WM_ERR_CUDA;
+      continue;
+    }
+    for (int32_t i = 0; i < n; ++i) {
+      t.pos = lens + (size_t)i * Tq;
+      t.page_table = table + (size_t)i * max_pages;
+      t.part = part + (size_t)i * c.Hkv * Tq * G * pl.records * tile_rec(c.d);
+      t.rows = Tq * G;
+      t.prefix_slots = max_pages * c.page_size;
+      t.pair = pl.pair;
+      t.records = pl.records;
+      t.items = pl.blocks * c.Hkv * pl.splits;
+      const TileInputs in{x + i * row_elems, ws, ws + pl.off_v, Tq, 1, c.d};
+      if (launch_tile_attn(t, in, sm_count(), s) != cudaSuccess) return WM_ERR_CUDA;
+    }
+    const Q4RowsJoin j{part, o, n, Tq, c.Hq, c.Hkv, G, pl.records};
+    if (launch_q4_rows_join(j, c.d, s) != cudaSuccess) return WM_ERR_CUDA;
+  }
+  return WM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -204,7 +350,8 @@ wm_status wm_q4_read(const wm_config* c, const wm_q4_cache* q4, const int32_t* q
 }
 
 size_t wm_q4_decode_attn_workspace(const wm_config* c, int32_t B, int32_t max_pages) {
-  return wm_q4_rows_attn_workspace(c, B, 1, max_pages);
+  if (wm_config_check(c) != WM_OK || B < 0 || max_pages < 1) return 0;
+  return B == 0 ? 256 : attn_plan(*c, B, 1, max_pages).total;
 }
 
 wm_status wm_q4_decode_attn(const wm_config* c, const wm_q4_cache* q4, int32_t layer, const void* q,
@@ -221,7 +368,8 @@ wm_status wm_q4_decode_attn(const wm_config* c, const wm_q4_cache* q4, int32_t l
 size_t wm_q4_rows_attn_workspace(const wm_config* c, int32_t B, int32_t Tq, int32_t max_pages) {
   if (wm_config_check(c) != WM_OK || B < 0 || Tq < 0 || max_pages < 1) return 0;
   if (B == 0 || Tq == 0) return 256;
-  return attn_plan(*c, B, Tq, max_pages).total;
+  const RowsPlan pl = rows_plan(*c, B, Tq, max_pages);
+  return pl.tiles ? pl.total : attn_plan(*c, B, Tq, max_pages).total;
 }
 
 wm_status wm_q4_rows_attn(const wm_config* c, const wm_q4_cache* q4, int32_t layer, const void* q, const int32_t* pos,
@@ -232,6 +380,14 @@ wm_status wm_q4_rows_attn(const wm_config* c, const wm_q4_cache* q4, int32_t lay
   if (layer < 0 || layer >= c->L || Tq < 0) return WM_ERR_INVALID_ARG;
   if (B == 0 || Tq == 0) return WM_OK;
   if (B > kMaxBatch || (int64_t)B * Tq > INT32_MAX / 2 / c->Hq) return WM_ERR_UNSUPPORTED;
+  const RowsPlan pl = rows_plan(*c, B, Tq, max_pages);
+  if (pl.tiles) {
+    if (!q || !pos || !page_table || !out || !workspace) return WM_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256) || ws_bytes < pl.total)
+      return WM_ERR_INVALID_ARG;
+    return rows_on_tiles(pl, *c, *q4, layer, q, pos, page_table, B, Tq, max_pages, out, (char*)workspace, dev_status,
+                         (cudaStream_t)stream);
+  }
   return attn(*c, *q4, layer, q, page_table, pos, 1, B, Tq, max_pages, out, workspace, ws_bytes, dev_status, stream);
 }
 

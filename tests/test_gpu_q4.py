@@ -278,3 +278,75 @@ def test_scores_of_any_size(dtype):
     s.q4_decode_attn(0, y.cuda(), q4, table, n, out)
     got = to_f64(out)
     assert np.isnan(got[1]).all() and np.isnan(got[2]).all() and np.isfinite(got[[0, 3]]).all()
+
+
+def on_tiles(x, Tq):
+    """Whether rows of this shape run on the tensor-core kernel: its workspace holds rows read back."""
+    c = x.session_cfg()
+    return W.wm_q4_rows_attn_workspace(c, x.B, Tq, x.max_pages) >= x.max_pages * x.P * x.Hkv * x.d * 4
+
+
+def check_many(x, q, pos, got, layer=0):
+    """All rows at once, against 64 bits.  Weights enter the product as bf16 (2^-8), sums of its 128-slot
+    steps are cut as in tests/_q4.py, the result is rounded by 2^-8 of itself."""
+    T = int(pos.max()) + 1
+    for b in range(x.B):
+        n = int(pos[b].max()) + 1
+        for h in range(x.Hkv):
+            ts = np.arange(n)
+            K, V = (x.rows(p, layer, b, h, ts) for p in (x.kd, x.vd))
+            for g in range(x.G):
+                Q_ = to_f64(q[b, :, h * x.G + g])
+                s = Q_ @ K.T / np.sqrt(x.d)
+                s[np.arange(n)[None] > pos[b][:, None]] = -np.inf
+                p = np.exp(s - s.max(1, keepdims=True))
+                want = p / p.sum(1, keepdims=True) @ V
+                ds = (110 + x.d) * 2.0 ** -24 * (np.abs(Q_) @ np.abs(K).T).max() / np.sqrt(x.d)
+                tol = (2 * ds + 2.0 ** -8 + T / 16 * 17 * 2.0 ** -23) * np.abs(V).max() + 2.0 ** -8 * np.abs(want).max()
+                err = np.abs(got[b, :, h * x.G + g] - want).max()
+                assert err <= tol, (b, h, g, err, tol)
+
+
+@pytest.mark.parametrize("G,Tq,lens,Hkv,d,page,maxp,order", [
+    (4, 300, [4001], 2, 128, 16, 1024, "last"),         # KV tiles cut, 256 rows per item
+    (8, 16, [700, 90], 2, 128, 32, 8192, "last"),       # at most 128 rows: their even and odd KV tiles
+    (1, 257, [300, 1500, 257], 2, 64, 8, 16384, "any"),  # more than one group of sequences, any order
+    (2, 200, [611, 200], 3, 96, 64, 1024, "last"),
+    (8, 260, [300] * 8, 4, 64, 16, 400, "last"),        # items enough: no cuts
+    (1, 513, [513, 600], 32, 64, 128, 100, "last")])
+def test_many_rows(G, Tq, lens, Hkv, d, page, maxp, order):
+    x = Q.Q4(lens, Hkv=Hkv, G=G, d=d, page=page, k=1, max_pages=maxp, seed=G)
+    assert on_tiles(x, Tq)
+    s, q4 = x.session(), x.q4()
+    table, _ = x.q4_dev()
+    rng = np.random.default_rng(1)
+    pos = np.stack([rng.integers(0, n, Tq) if order == "any" else np.arange(n - Tq, n) for n in lens]).astype(np.int32)
+    q = x.queries(x.B, Tq)
+    out = torch.full((x.B, Tq, x.Hq, d), float("nan"), dtype=x.tdt, device="cuda")
+    s.q4_rows_attn(0, q.cuda(), torch.from_numpy(pos).cuda(), q4, table, out)
+    assert s.read_status() == 0
+    check_many(x, q, pos, to_f64(out))
+
+
+@pytest.mark.parametrize("G,Tq,B,maxp", [(8, 260, 8, 400), (4, 300, 2, 4096)])
+def test_many_rows_leave_out_what_is_bad(G, Tq, B, maxp):
+    x = Q.Q4([Tq] * B, Hkv=4, G=G, d=64, page=16, k=1, max_pages=maxp)
+    assert on_tiles(x, Tq)
+    s, q4 = x.session(), x.q4()
+    table, _ = x.q4_dev()
+    table[1, 3], table[0, 5] = -1, x.q4_pages
+    pos = np.tile(np.arange(Tq, dtype=np.int32), (B, 1))
+    q = x.queries(B, Tq)
+    dev = torch.from_numpy(pos).cuda()
+    dev[0, 7], dev[1, 9] = -1, x.T
+    out = torch.full((B, Tq, x.Hq, 64), float("nan"), dtype=x.tdt, device="cuda")
+    s.q4_rows_attn(0, q.cuda(), dev, q4, table, out)
+    assert s.read_status() == W.WM_ERR_BOUNDS
+    got = to_f64(out)
+    assert (got[0, 7] == 0).all() and (got[1, 9] == 0).all()
+    for b, page in ((0, 5), (1, 3)):
+        for r in (0, 15, 47, 48, 100, Tq - 1):
+            ts = [t for t in range(r + 1) if t // 16 != page]
+            for hq in (0, x.Hq - 1):
+                want, tol = x.bound(0, b, hq, to_f64(q[b, r, hq]), ts, Tq / 16)
+                assert np.abs(got[b, r, hq] - want).max() <= tol + 2.0 ** -8 * np.abs(x.vd[np.isfinite(x.vd)]).max(), (b, r)
