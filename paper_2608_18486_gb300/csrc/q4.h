@@ -57,6 +57,8 @@ struct Q4CopyParams {
   int32_t B, k, Hkv, P, log2P, tile, log2tile, tile_bytes, row_pages, q4_pages, max_pages;
   int32_t span;               // slots of a range at most
   int32_t steps;              // tiles of 16 slots that a range touches at most
+  int32_t wide, heads, items; // set by the launch: rows are 32-byte aligned, kv heads per
+                              // item, items
 };
 cudaError_t launch_q4_write(const Q4CopyParams& p, int dtype, int d, int sms, cudaStream_t s);
 cudaError_t launch_q4_read(const Q4CopyParams& p, int dtype, int d, int sms, cudaStream_t s);
@@ -85,7 +87,8 @@ constexpr int kQ4Warps = 4;        // warps per CTA
 constexpr int kQ4Slots = 32;       // slots of a warp's step
 constexpr int kQ4MaxCluster = 8;
 constexpr int kQ4MinSteps = 4;     // steps of a warp at least where all steps are spread
-constexpr int kQ4CtasPerSm = 4;
+// resident CTAs per SM, by registers
+constexpr int q4_ctas_per_sm(bool bf16, int nb) { return !bf16 ? 2 : nb == 1 ? 4 : 2; }
 
 struct Q4AttnParams {
   const uint8_t* pool;        // channel base

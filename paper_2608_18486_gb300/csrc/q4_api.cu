@@ -118,12 +118,14 @@ Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   pl.col_blocks = (int)((cols + 8 * pl.nb - 1) / (8 * pl.nb));
   const int64_t units = (int64_t)B * c.Hkv * pl.col_blocks;
   const int64_t steps = ((int64_t)max_pages * c.page_size + kQ4Slots - 1) / kQ4Slots;
-  const int resident = sm_count() * (pl.nb == 1 && c.dtype == WM_DT_BF16 ? kQ4CtasPerSm : 2);
-  int C = 1;
-  while (C < kQ4MaxCluster && units * C * 2 <= resident && (int64_t)C * kQ4Warps < steps) C *= 2;
-  pl.pieces = C;
+  const int resident = sm_count() * q4_ctas_per_sm(c.dtype == WM_DT_BF16, pl.nb);
+  // as many CTAs per unit as are resident, a step per warp at least
+  int64_t C = resident / units;
+  if (C > steps / kQ4Warps) C = steps / kQ4Warps;
+  C = C < 1 ? 1 : C > kQ4MaxCluster ? kQ4MaxCluster : C;
+  pl.pieces = (int)C;
   pl.total = 256;
-  if (pl.col_blocks == 1 && steps > (int64_t)C * kQ4Warps * kLongSteps) {
+  if (pl.col_blocks == 1 && steps > C * kQ4Warps * kLongSteps) {
     pl.pieces = resident;
     pl.spread = true;
     pl.total = align256(sizeof(float) * 2 * (size_t)resident * q4_rec(8 * pl.nb, c.d));

@@ -388,18 +388,18 @@ struct Math {
     }
   }
 
-  // One step of kTiles tiles, `stride` bytes apart, at shared address st; t0: its first
-  // slot; live: bit per slot that is there and below the unit's largest limit;
-  // WHOLE: every column sees every slot.
-  template <bool WHOLE>
-  __device__ __forceinline__ void step(const unsigned char* st, uint32_t stride, const At& at, int lane, int t0, uint32_t live) {
+  // NT tiles, `stride` bytes apart, from shared memory st on; t0: the first slot; live:
+  // bit per slot that is there and below the unit's largest limit; WHOLE: every column
+  // sees every slot.
+  template <bool WHOLE, int NT>
+  __device__ __forceinline__ void tiles(const unsigned char* st, uint32_t stride, const At& at, int lane, int t0, uint32_t live) {
     const int g = lane >> 2;
-    float s[kTiles][NB][4];
+    float s[NT][NB][4];
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x) scores(st + x * stride, at, lane, s[x]);
+    for (int x = 0; x < NT; ++x) scores(st + x * stride, at, lane, s[x]);
     if (!WHOLE) {
 #pragma unroll
-      for (int x = 0; x < kTiles; ++x)
+      for (int x = 0; x < NT; ++x)
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -409,15 +409,15 @@ struct Math {
           }
     }
     // score - reference: slots t0 + 16 x + g + 8 (i / 2), columns 2 c + i % 2 of block n
-    float d[kTiles][NB][4], most = -INFINITY;
+    float d[NT][NB][4], most = -INFINITY;
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x)
+    for (int x = 0; x < NT; ++x)
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) d[x][n][i] = fmaf(s[x][n][i], mul[n][i & 1], -ref[n][i & 1]);
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x)
+    for (int x = 0; x < NT; ++x)
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -429,7 +429,7 @@ struct Math {
         for (int i = 0; i < 2; ++i) {
           float top = -INFINITY;
 #pragma unroll
-          for (int x = 0; x < kTiles; ++x) top = fmaxf(top, fmaxf(s[x][n][i], s[x][n][i + 2]));
+          for (int x = 0; x < NT; ++x) top = fmaxf(top, fmaxf(s[x][n][i], s[x][n][i + 2]));
 #pragma unroll
           for (int y = 4; y < 32; y *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, y));
           const float to = fmaxf(ref[n][i], __fsub_rn(__fmul_rn(top, mul[n][i]), kHead)), corr = ex2(ref[n][i] - to);
@@ -444,14 +444,14 @@ struct Math {
       // (Two roundings: the rounded score is what the reference is made of.  One would
       // leave scores past 2^24 off it by more than the reference's lead.)
 #pragma unroll
-      for (int x = 0; x < kTiles; ++x)
+      for (int x = 0; x < NT; ++x)
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) d[x][n][i] = __fsub_rn(__fmul_rn(s[x][n][i], mul[n][i & 1]), ref[n][i & 1]);
     }
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x) {
+    for (int x = 0; x < NT; ++x) {
       uint32_t p[NB][NP][2];  // column g, slots 2 c + {0, 1} and 8 more
 #pragma unroll
       for (int n = 0; n < NB; ++n)
@@ -469,6 +469,18 @@ struct Math {
         }
       values<WHOLE>(st + x * stride, at, lane, live >> (16 * x), p);
     }
+  }
+
+  // One step of kTiles tiles, fp32's (more parts) one by one: registers.  16 columns of
+  // bf16 heads of 128 (4 drafted rows behind 8 x 32768 slots): both at once, 2 CTAs per
+  // SM, 81 us; one by one 82, with 3 CTAs 87.
+  static constexpr int kAtOnce = NQ == 1 ? kTiles : 1;
+  template <bool WHOLE>
+  __device__ __forceinline__ void step(const unsigned char* st, uint32_t stride, const At& at, int lane, int t0,
+                                       uint32_t live) {
+#pragma unroll
+    for (int x = 0; x < kTiles; x += kAtOnce)
+      tiles<WHOLE, kAtOnce>(st + x * stride, stride, at, lane, t0 + 16 * x, live >> (16 * x));
   }
 
   // rec[col][HD], then (reference, sum) per column
@@ -562,7 +574,7 @@ struct Spread {
 
 // BIG: pages of at least 16 slots
 template <typename T, int HD, int NB, bool BIG>
-__global__ void __launch_bounds__(kThreads, NB == 1 && sizeof(T) == 2 ? kQ4CtasPerSm : 2)
+__global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
     q4_attn_kernel(const Q4AttnParams p) {
   using SH = Shape<HD>;
   constexpr int STAGE = kTiles * (BIG ? SH::TILE : SH::SMALL);
