@@ -493,6 +493,23 @@ wm_status wm_q4_read(const wm_config* cfg, const wm_q4_cache* q4, const int32_t*
                      const int32_t* last, int32_t span, int32_t B, int32_t max_pages,
                      int32_t* dev_status, void* stream);
 
+/* Workspace bytes of wm_q4_kv_mix (0 for bad arguments). */
+size_t wm_q4_kv_mix_workspace(const wm_config* cfg, int32_t B);
+
+/*
+ * wm_kv_mix into a 4-bit cache: token b's keys and values, rounded to the config's type
+ * as wm_kv_mix rounds them, are written in 4 bits to slot[b] (page_table: the 4-bit
+ * cache's pages).  pos: the positions, or NULL for slot[b] - 1.  The other arguments,
+ * the errors and the promise about the weights are wm_kv_mix's;
+ *   workspace  device, >= wm_q4_kv_mix_workspace(cfg, B) bytes, 256-byte aligned, no
+ *              contents required; calls that share one must not overlap on the GPU
+ * One launch more than wm_kv_mix.
+ */
+wm_status wm_q4_kv_mix(const wm_config* cfg, const wm_q4_cache* q4, const wm_mix_weights* w,
+                       const void* h, const int32_t* page_table, const int32_t* slot,
+                       const int32_t* pos, int32_t B, int32_t max_pages, void* workspace,
+                       size_t ws_bytes, int32_t* dev_status, void* stream);
+
 /* Workspace bytes of wm_q4_decode_attn (0 for bad arguments). */
 size_t wm_q4_decode_attn_workspace(const wm_config* cfg, int32_t B, int32_t max_pages);
 

@@ -23,7 +23,7 @@ EXPORTED = ["wm_status_string", "wm_config_check", "wm_cache_bytes", "wm_cache_a
             "wm_prefix_attn_workspace", "wm_prefix_attn", "wm_decode_attn_mass_workspace",
             "wm_decode_attn_mass", "wm_cache_evict", "wm_q4_cache_bytes", "wm_q4_cache_alloc",
             "wm_q4_write", "wm_q4_read", "wm_q4_decode_attn_workspace", "wm_q4_decode_attn",
-            "wm_q4_rows_attn_workspace", "wm_q4_rows_attn"]
+            "wm_q4_rows_attn_workspace", "wm_q4_rows_attn", "wm_q4_kv_mix_workspace", "wm_q4_kv_mix"]
 WM_ATTN_INPUTS_READY = 1
 WM_ATTN_DYNAMIC_SPLIT = 2
 WM_ATTN_UNIT_SPLIT = 4
@@ -129,6 +129,11 @@ def lib():
         L.wm_q4_write.argtypes = [cp, ccp, vp, qcp, vp, vp, vp, i32, i32, i32, vp, vp]
         L.wm_q4_read.restype = ctypes.c_int
         L.wm_q4_read.argtypes = [cp, qcp, vp, ccp, vp, vp, vp, i32, i32, i32, vp, vp]
+        L.wm_q4_kv_mix_workspace.restype = sz
+        L.wm_q4_kv_mix_workspace.argtypes = [cp, i32]
+        L.wm_q4_kv_mix.restype = ctypes.c_int
+        L.wm_q4_kv_mix.argtypes = [cp, qcp, ctypes.POINTER(wm_mix_weights), vp, vp, vp, vp, i32, i32, vp,
+                                   sz, vp, vp]
         L.wm_q4_decode_attn_workspace.restype = sz
         L.wm_q4_decode_attn_workspace.argtypes = [cp, i32, i32]
         L.wm_q4_decode_attn.restype = ctypes.c_int
@@ -323,6 +328,17 @@ def wm_q4_read(cfg, q4, q4_table, cache, page_table, first, last, span, B, max_p
     return lib().wm_q4_read(ctypes.byref(cfg), ctypes.byref(q4), _p(q4_table), ctypes.byref(cache),
                             _p(page_table), _p(first), _p(last), span, B, max_pages, _p(dev_status),
                             stream)
+
+
+def wm_q4_kv_mix_workspace(cfg, B) -> int:
+    return int(lib().wm_q4_kv_mix_workspace(ctypes.byref(cfg), int(B)))
+
+
+def wm_q4_kv_mix(cfg, q4, weights, h, page_table, slot, pos, B, max_pages, workspace, ws_bytes,
+                 dev_status, stream) -> int:
+    return lib().wm_q4_kv_mix(ctypes.byref(cfg), ctypes.byref(q4), ctypes.byref(weights), _p(h),
+                              _p(page_table), _p(slot), _p(pos), B, max_pages, _p(workspace), ws_bytes,
+                              _p(dev_status), stream)
 
 
 def wm_q4_decode_attn_workspace(cfg, B, max_pages) -> int:

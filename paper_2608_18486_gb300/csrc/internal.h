@@ -124,7 +124,7 @@ struct MixParams {
   const void* ch_g[2];
   const void* Wkv[2];
   const void* qk_g;
-  const int32_t* page_table;
+  const int32_t* page_table;      // NULL: token b goes to page b (P = 1: to row b)
   const int32_t* slot;
   const int32_t* pos;             // [B] positions, or NULL: slot - 1
   // cache
@@ -149,6 +149,11 @@ struct MixWorkspace {
 
 MixWorkspace mix_workspace_layout(const wm_config& cfg, int32_t B, int sm_count);
 cudaError_t launch_kv_mix(MixParams& p, int dtype, cudaStream_t s);
+// The pool's rows of B tokens as [k][B][Hkv][d] (K, V) instead of in a cache; arguments
+// and errors otherwise as wm_kv_mix, slots below max_slots.
+wm_status kv_mix_to_rows(const wm_config* c, const wm_mix_weights* w, const void* h, const int32_t* slot,
+                         const int32_t* pos, int32_t B, int32_t max_slots, void* k_rows, void* v_rows, void* workspace,
+                         size_t ws_bytes, int32_t* dev_status, void* stream);
 int kv_mix_launches(const MixParams& p, int dtype);  // kernels launch_kv_mix enqueues
 
 // tcgen05 projection with the fused key/value epilogue, and the tcgen05

@@ -604,7 +604,7 @@ __global__ void __launch_bounds__(128) kv_epilogue_kernel(const MixParams p) {
     if (threadIdx.x == 0 && j == 0 && X == 0) report(p.status, WM_ERR_BOUNDS);
     return;
   }
-  const int pg = p.page_table[(int64_t)b * p.max_pages + (s >> p.log2P)];
+  const int pg = p.page_table ? p.page_table[(int64_t)b * p.max_pages + (s >> p.log2P)] : b;
   if (pg < 0 || pg >= p.num_pages) {
     if (threadIdx.x == 0 && j == 0 && X == 0) report(p.status, WM_ERR_BOUNDS);
     return;

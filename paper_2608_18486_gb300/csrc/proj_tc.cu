@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       const int s = p.slot[n0 + n];
       int pg = -1;
       if (s >= 1 && s < p.max_pages * p.P)
-        pg = p.page_table[(int64_t)(n0 + n) * p.max_pages + (s >> p.log2P)];
+        pg = p.page_table ? p.page_table[(int64_t)(n0 + n) * p.max_pages + (s >> p.log2P)] : n0 + n;
       s_slot[n] = s;
       s_page[n] = (pg >= 0 && pg < p.num_pages) ? pg : -1;
     }

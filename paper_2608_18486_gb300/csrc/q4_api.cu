@@ -54,6 +54,11 @@ size_t channel_bytes(const wm_config& c, int32_t num_pages) {
   return (size_t)num_pages * c.Hkv * q4_page_bytes(c.page_size, c.d);
 }
 
+// K (or V) rows of one token of each of B sequences, all channels
+size_t row_bytes(const wm_config& c, int32_t B) {
+  return align256((size_t)c.k * B * c.Hkv * c.d * elem_size(c.dtype));
+}
+
 Q4CopyParams copy_params(const wm_config& c, const wm_q4_cache& q4, int32_t B, int32_t max_pages, int32_t span,
                          int32_t* dev_status) {
   Q4CopyParams p{};
@@ -349,6 +354,36 @@ wm_status wm_q4_read(const wm_config* c, const wm_q4_cache* q4, const int32_t* q
                      const int32_t* page_table, const int32_t* first, const int32_t* last, int32_t span, int32_t B,
                      int32_t max_pages, int32_t* dev_status, void* stream) {
   return copy_ranges(false, c, cache, page_table, q4, q4_table, first, last, span, B, max_pages, dev_status, stream);
+}
+
+size_t wm_q4_kv_mix_workspace(const wm_config* c, int32_t B) {
+  const size_t mix = wm_kv_mix_workspace(c, B);
+  return mix == 0 ? 0 : mix + 2 * row_bytes(*c, B);
+}
+
+wm_status wm_q4_kv_mix(const wm_config* c, const wm_q4_cache* q4, const wm_mix_weights* w, const void* h,
+                       const int32_t* page_table, const int32_t* slot, const int32_t* pos, int32_t B,
+                       int32_t max_pages, void* workspace, size_t ws_bytes, int32_t* dev_status, void* stream) {
+  wm_status st = check_call(c, q4, B, max_pages);
+  if (st != WM_OK) return st;
+  if (!w) return WM_ERR_INVALID_ARG;
+  if (B == 0) return WM_OK;
+  if (!page_table || !workspace || ws_bytes < wm_q4_kv_mix_workspace(c, B)) return WM_ERR_INVALID_ARG;
+  if ((int64_t)c->k * B * c->Hkv > INT32_MAX / 2) return WM_ERR_UNSUPPORTED;
+  const size_t mix = wm_kv_mix_workspace(c, B), rows = row_bytes(*c, B);
+  char* const ws = (char*)workspace;
+  st = kv_mix_to_rows(c, w, h, slot, pos, B, max_pages * c->page_size, ws + mix, ws + mix + rows, workspace, mix,
+                      dev_status, stream);
+  if (st != WM_OK) return st;
+  Q4CopyParams p = copy_params(*c, *q4, B, max_pages, 1, dev_status);
+  p.k_rows = ws + mix;
+  p.v_rows = ws + mix + rows;
+  p.rows_at = kQ4Staged;
+  p.row_pages = B;
+  p.q4_table = page_table;
+  p.first = slot;
+  p.steps = 1;
+  return cuda_status(launch_q4_write(p, c->dtype, c->d, sm_count(), (cudaStream_t)stream));
 }
 
 size_t wm_q4_decode_attn_workspace(const wm_config* c, int32_t B, int32_t max_pages) {

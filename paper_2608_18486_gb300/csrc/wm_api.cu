@@ -264,20 +264,11 @@ wm_status decode_attn_impl(const wm_config* c, const wm_cache* cache, int32_t la
   return e == cudaSuccess ? WM_OK : WM_ERR_CUDA;
 }
 
-// Checks and launches one pool call; pos: the tokens' positions, or NULL for
-// slot - 1.
-wm_status kv_mix_impl(const wm_config* c, const wm_cache* cache, const wm_mix_weights* w,
-                      const void* h, const int32_t* page_table, const int32_t* slot,
-                      const int32_t* pos, int32_t B, int32_t max_pages, void* workspace,
-                      size_t ws_bytes, int32_t* dev_status, void* stream) {
-  wm_status st = wm_config_check(c);
-  if (st != WM_OK) return st;
-  if ((st = check_cache(*c, cache)) != WM_OK) return st;
-  if (B < 0 || max_pages < 1 || !w) return WM_ERR_INVALID_ARG;
-  if ((int64_t)max_pages * c->page_size > INT32_MAX / 2) return WM_ERR_INVALID_ARG;
-  if (B == 0) return WM_OK;
+// The arguments that every pool call has.
+wm_status check_mix(const wm_config* c, const wm_mix_weights* w, const void* h, const int32_t* slot, int32_t B,
+                    void* workspace, size_t ws_bytes) {
   if (B > 65535) return WM_ERR_UNSUPPORTED;
-  if (!h || !page_table || !slot || !workspace || !w->qk_g) return WM_ERR_INVALID_ARG;
+  if (!h || !slot || !workspace || !w->qk_g) return WM_ERR_INVALID_ARG;
   for (int X = 0; X < 2; ++X)
     if (!w->pre_g[X] || !w->Wr[X] || !w->br[X] || !w->ch_g[X] || !w->Wkv[X])
       return WM_ERR_INVALID_ARG;
@@ -287,13 +278,14 @@ wm_status kv_mix_impl(const wm_config* c, const wm_cache* cache, const wm_mix_we
       return WM_ERR_INVALID_ARG;
   if (!aligned(h, 16)) return WM_ERR_INVALID_ARG;
   if (!aligned(workspace, 256)) return WM_ERR_INVALID_ARG;
-  const wm::MixWorkspace ws = wm::mix_workspace_layout(*c, B, sm_count());
-  if (ws_bytes < ws.total) return WM_ERR_INVALID_ARG;
+  return ws_bytes < wm::mix_workspace_layout(*c, B, sm_count()).total ? WM_ERR_INVALID_ARG : WM_OK;
+}
 
-  wm::MixParams p{};
-  mix_shape(*c, B, p);
-  p.num_pages = cache->num_pages;
-  p.max_pages = max_pages;
+// Launches one pool call whose destination (page table, pages, pools) `p` holds.
+wm_status launch_mix(wm::MixParams& p, const wm_config* c, const wm_mix_weights* w, const void* h,
+                     const int32_t* slot, const int32_t* pos, int32_t B, void* workspace,
+                     int32_t* dev_status, void* stream) {
+  const wm::MixWorkspace ws = wm::mix_workspace_layout(*c, B, sm_count());
   p.h = h;
   for (int X = 0; X < 2; ++X) {
     p.pre_g[X] = w->pre_g[X];
@@ -303,11 +295,8 @@ wm_status kv_mix_impl(const wm_config* c, const wm_cache* cache, const wm_mix_we
     p.Wkv[X] = w->Wkv[X];
   }
   p.qk_g = w->qk_g;
-  p.page_table = page_table;
   p.slot = slot;
   p.pos = pos;
-  p.k_pool = cache->k_pool;
-  p.v_pool = cache->v_pool;
   char* base = (char*)workspace;
   p.inv_rms = (float*)(base + ws.inv_rms);
   p.xi = base + ws.xi;
@@ -323,7 +312,49 @@ wm_status kv_mix_impl(const wm_config* c, const wm_cache* cache, const wm_mix_we
   return e == cudaSuccess ? WM_OK : WM_ERR_CUDA;
 }
 
+// Checks and launches one pool call; pos: the tokens' positions, or NULL for
+// slot - 1.
+wm_status kv_mix_impl(const wm_config* c, const wm_cache* cache, const wm_mix_weights* w,
+                      const void* h, const int32_t* page_table, const int32_t* slot,
+                      const int32_t* pos, int32_t B, int32_t max_pages, void* workspace,
+                      size_t ws_bytes, int32_t* dev_status, void* stream) {
+  wm_status st = wm_config_check(c);
+  if (st != WM_OK) return st;
+  if ((st = check_cache(*c, cache)) != WM_OK) return st;
+  if (B < 0 || max_pages < 1 || !w) return WM_ERR_INVALID_ARG;
+  if ((int64_t)max_pages * c->page_size > INT32_MAX / 2) return WM_ERR_INVALID_ARG;
+  if (B == 0) return WM_OK;
+  if ((st = check_mix(c, w, h, slot, B, workspace, ws_bytes)) != WM_OK) return st;
+  if (!page_table) return WM_ERR_INVALID_ARG;
+
+  wm::MixParams p{};
+  mix_shape(*c, B, p);
+  p.num_pages = cache->num_pages;
+  p.max_pages = max_pages;
+  p.page_table = page_table;
+  p.k_pool = cache->k_pool;
+  p.v_pool = cache->v_pool;
+  return launch_mix(p, c, w, h, slot, pos, B, workspace, dev_status, stream);
+}
+
 }  // namespace
+
+// A cache of pages of one slot, token b's page being b, is rows one after the other.
+wm_status wm::kv_mix_to_rows(const wm_config* c, const wm_mix_weights* w, const void* h, const int32_t* slot,
+                             const int32_t* pos, int32_t B, int32_t max_slots, void* k_rows, void* v_rows,
+                             void* workspace, size_t ws_bytes, int32_t* dev_status, void* stream) {
+  const wm_status st = check_mix(c, w, h, slot, B, workspace, ws_bytes);
+  if (st != WM_OK) return st;
+  wm::MixParams p{};
+  mix_shape(*c, B, p);
+  p.P = 1;
+  p.log2P = 0;
+  p.num_pages = B;
+  p.max_pages = max_slots;
+  p.k_pool = k_rows;
+  p.v_pool = v_rows;
+  return launch_mix(p, c, w, h, slot, pos, B, workspace, dev_status, stream);
+}
 
 extern "C" {
 

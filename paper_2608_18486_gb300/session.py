@@ -391,6 +391,26 @@ class DecodeSession:
         self._q4_copy(self._lib.wm_q4_read, "wm_q4_read", q4, q4_table, page_table, first, last, span, B,
                       stream, False)
 
+    def q4_kv_mix(self, h, q4: Q4Cache, page_table, slot, *, pos=None, B: int | None = None,
+                  stream=None) -> None:
+        """kv_mix that appends the tokens to a 4-bit cache (its pages: page_table)."""
+        if self._weights is None:
+            raise RuntimeError("set_weights() first")
+        B = self.B if B is None else B
+        q4r = self._q4_ref(q4)
+        self._check((h, self.dtype, B * self.cfg.L * self.cfg.D), (slot, _I32, B))
+        if pos is not None:
+            self._check((pos, _I32, B))
+        self._check_table(page_table, B)
+        need = self._bytes(("q4 mix", B), W.wm_q4_kv_mix_workspace, B)
+        raw = self._raw_stream(stream)
+        rc = self._lib.wm_q4_kv_mix(self._refs[0], q4r, ctypes.byref(self._weights), h.data_ptr(),
+                                    page_table.data_ptr(), slot.data_ptr(),
+                                    None if pos is None else pos.data_ptr(), B, self.max_pages,
+                                    self._scratch_for(need, raw, stream), need, self._status_ptr, raw)
+        if rc != W.WM_OK:
+            raise W.WMError(rc, "wm_q4_kv_mix")
+
     def q4_decode_attn(self, layer: int, q, q4: Q4Cache, page_table, seq_lens, out, *,
                        B: int | None = None, stream=None) -> None:
         """Decode attention of layer ``layer`` over a 4-bit cache (its pages:

@@ -34,7 +34,13 @@ def rows(c, cache, q4, layer=0, q=FAKE, pos=FAKE, table=FAKE, B=2, Tq=3, maxp=4,
     return W.wm_q4_rows_attn(c, q4, layer, q, pos, table, B, Tq, maxp, out, ws, n, None, None)
 
 
-CALLS = {"write": write, "read": read, "decode": decode, "rows": rows}
+def mix(c, cache, q4, h=FAKE, table=FAKE, slot=FAKE, pos=None, B=2, maxp=4, ws=FAKE, n=None, w=FAKE, g=FAKE):
+    n = W.wm_q4_kv_mix_workspace(c, 2) if n is None else n
+    weights = W.mix_weights((g, g), (w, w), (FAKE, FAKE), (FAKE, FAKE), (FAKE, FAKE), FAKE)
+    return W.wm_q4_kv_mix(c, q4, weights, h, table, slot, pos, B, maxp, ws, n, None, None)
+
+
+CALLS = {"write": write, "read": read, "decode": decode, "rows": rows, "mix": mix}
 
 
 @host_refusals_only
@@ -45,6 +51,9 @@ CALLS = {"write": write, "read": read, "decode": decode, "rows": rows}
     ("decode", dict(out=None)), ("decode", dict(out=FAKE + 2)), ("decode", dict(table=None)), ("decode", dict(lens=None)),
     ("decode", dict(ws=None)), ("decode", dict(ws=FAKE + 16)), ("decode", dict(n=0)), ("decode", dict(B=-1)),
     ("decode", dict(maxp=0)), ("rows", dict(Tq=-1)), ("rows", dict(pos=None)), ("rows", dict(layer=32)),
+    ("mix", dict(h=None)), ("mix", dict(h=FAKE + 8)), ("mix", dict(table=None)), ("mix", dict(slot=None)),
+    ("mix", dict(ws=None)), ("mix", dict(ws=FAKE + 128)), ("mix", dict(n=256)), ("mix", dict(w=None)), ("mix", dict(g=FAKE + 4)),
+    ("mix", dict(B=-1)), ("mix", dict(maxp=0)),
     ("rows", dict(q=FAKE + 4)), ("rows", dict(out=None)), ("rows", dict(ws=None)), ("rows", dict(n=0))])
 def test_bad_arguments_are_refused(name, bad):
     assert CALLS[name](*parts(), **bad) == INV
@@ -73,6 +82,8 @@ def test_nothing_to_do_and_too_much():
     assert write(*p, span=0) == OK and read(*p, span=0) == OK and rows(*p, Tq=0) == OK
     assert decode(*p, B=4097) == UNS and rows(*p, B=4097) == UNS and rows(*p, B=4096, Tq=1 << 20) == UNS
     assert write(*p, B=4096, span=1 << 24, maxp=1 << 20) == UNS
+    assert mix(*p, B=65536, n=1 << 50) == UNS and W.wm_q4_kv_mix_workspace(p[0], -1) == 0
+    assert W.wm_q4_kv_mix_workspace(p[0], 2) > W.wm_kv_mix_workspace(p[0], 2)
 
 
 def test_sizes():
