@@ -572,6 +572,12 @@ struct Spread {
   __device__ __forceinline__ int cta_of(int64_t x) const { return (int)(((x + 1) * n + total - 1) / total) - 1; }
 };
 
+// Where a cluster's (reference, sum) pairs are in a CTA's record space, and its size.
+template <int HD, int NB>
+constexpr int kMlAt = 8 * NB * HD + kQ4MaxCluster;
+template <int HD, int NB>
+constexpr int kJoinFloats = kMlAt<HD, NB> + 2 * kQ4MaxCluster * 8 * NB;
+
 // BIG: pages of at least 16 slots
 template <typename T, int HD, int NB, bool BIG>
 __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
@@ -621,6 +627,7 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
     x0 = (unit - bh * p.col_blocks) * 8 * NB;
     b = bh / p.Hkv;
     h = bh - b * p.Hkv;
+    if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // (this CTA is there)
   }
   const int cols = min(8 * NB, p.Tq * p.G - x0), E = cols * HD;
 
@@ -758,30 +765,40 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
     const int x = x0 + col;
     return reinterpret_cast<T*>(p.out) + (((int64_t)b * p.Tq + x / p.G) * p.Hq + h * p.G + x % p.G) * HD;
   };
-  // a unit that a CTA has to itself is done; its part of a shared one goes to the
-  // CTA's record 0 (the unit began before its steps) or 1
-  const bool direct = steps == nsteps;
+  // a unit that a CTA has to itself is done.  Its part of one that the spread cut goes to
+  // the CTA's record 0 (the unit began before its steps) or 1; in a cluster CTA c finishes
+  // outputs c * share .. and gets the others' parts of them through distributed shared
+  // memory: [C][share], then [C][cols] (reference, sum).
+  const bool direct = C == 1 && steps == nsteps;
   float* rec = spread ? p.part + ((int64_t)blockIdx.x * 2 + (from == 0)) * q4_rec(8 * NB, HD) : crec;
-  const int ml = spread ? 8 * NB * HD : E;  // where (reference, sum) are in it
-  for (int e = tid; e < E; e += kThreads) {
-    const int r = e / HD;
-    float M = -FLT_MAX, L = 0.f, O = 0.f;
+  const int share = (E + C - 1) / C;
+  cg::cluster_group cluster = cg::this_cluster();
+  if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // every CTA is there
+  auto joined_ml = [&](int r, float& M, float& L) {
+    M = -FLT_MAX;
+    L = 0.f;
 #pragma unroll
     for (int w = 0; w < kQ4Warps; ++w) M = fmaxf(M, warp_rec(w)[E + 2 * r]);
 #pragma unroll
-    for (int w = 0; w < kQ4Warps; ++w) {
-      const float wt = exp2f(warp_rec(w)[E + 2 * r] - M);
-      L = fmaf(wt, warp_rec(w)[E + 2 * r + 1], L);
-      O = fmaf(wt, warp_rec(w)[e], O);
-    }
-    if (direct && C == 1) {
+    for (int w = 0; w < kQ4Warps; ++w) L = fmaf(exp2f(warp_rec(w)[E + 2 * r] - M), warp_rec(w)[E + 2 * r + 1], L);
+  };
+  for (int e = tid; e < E; e += kThreads) {
+    const int r = e / HD;
+    float M, L, O = 0.f;
+    joined_ml(r, M, L);
+#pragma unroll
+    for (int w = 0; w < kQ4Warps; ++w) O = fmaf(exp2f(warp_rec(w)[E + 2 * r] - M), warp_rec(w)[e], O);
+    if (direct) {
       out_row(r)[e - r * HD] = Elem<T>::from_f(L == 0.f ? 0.f : O / L);
-    } else {
+    } else if (spread) {
       rec[e] = O;
       if (e == r * HD) {
-        rec[ml + 2 * r] = M;
-        rec[ml + 2 * r + 1] = L;
+        rec[8 * NB * HD + 2 * r] = M;
+        rec[8 * NB * HD + 2 * r + 1] = L;
       }
+    } else {
+      const int c = e / share;
+      cluster.map_shared_rank(crec, c)[piece * share + e - c * share] = O;
     }
   }
   if (spread) {
@@ -792,34 +809,26 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
     continue;
   }
   if (C == 1) return;
-
-  // ---- join the cluster's CTAs through distributed shared memory: CTA `piece`
-  // finishes its share.  The last barrier keeps each CTA's shared memory until
-  // every reader is done.
-  cg::cluster_group cluster = cg::this_cluster();
+  for (int x = tid; x < cols * C; x += kThreads) {
+    const int r = x / C, c = x - r * C;
+    float M, L;
+    joined_ml(r, M, L);
+    *reinterpret_cast<float2*>(cluster.map_shared_rank(crec, c) + kMlAt<HD, NB> + 2 * (piece * cols + r)) = make_float2(M, L);
+  }
+  // (nothing is written to a CTA's shared memory behind this, so it may end before the others)
   cluster.sync();
-  for (int e = piece * E / C + tid; e < (piece + 1) * E / C; e += kThreads) {
+  for (int e = piece * share + tid; e < min((piece + 1) * share, E); e += kThreads) {
     const int r = e / HD;
-    float mq[kQ4MaxCluster], lq[kQ4MaxCluster], oq[kQ4MaxCluster];
-#pragma unroll
-    for (int c = 0; c < kQ4MaxCluster; ++c) {
-      const float* cr = cluster.map_shared_rank(crec, c < C ? c : 0);
-      mq[c] = c < C ? cr[E + 2 * r] : -FLT_MAX;
-      lq[c] = c < C ? cr[E + 2 * r + 1] : 0.f;
-      oq[c] = c < C ? cr[e] : 0.f;
-    }
     float M = -FLT_MAX, L = 0.f, O = 0.f;
-#pragma unroll
-    for (int c = 0; c < kQ4MaxCluster; ++c) M = fmaxf(M, mq[c]);
-#pragma unroll
-    for (int c = 0; c < kQ4MaxCluster; ++c) {
-      const float wt = exp2f(mq[c] - M);
-      L = fmaf(wt, lq[c], L);
-      O = fmaf(wt, oq[c], O);
+    for (int c = 0; c < C; ++c) M = fmaxf(M, crec[kMlAt<HD, NB> + 2 * (c * cols + r)]);
+    for (int c = 0; c < C; ++c) {
+      const float2 ml = *reinterpret_cast<const float2*>(crec + kMlAt<HD, NB> + 2 * (c * cols + r));
+      const float wt = exp2f(ml.x - M);
+      L = fmaf(wt, ml.y, L);
+      O = fmaf(wt, crec[c * share + e - piece * share], O);
     }
     out_row(r)[e - r * HD] = Elem<T>::from_f(L == 0.f ? 0.f : O / L);
   }
-  cluster.sync();
   return;
   }
 }
@@ -925,9 +934,10 @@ inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
   static size_t smem_set[kSmemOptDevices] = {};
   auto kern = q4_attn_kernel<T, HD, NB, BIG>;
   constexpr size_t ring = (size_t)kStages * kTiles * (BIG ? SH::TILE : SH::SMALL), rec = q4_rec(8 * NB, HD) * sizeof(float);
+  constexpr size_t join = kJoinFloats<HD, NB> * sizeof(float);
   static_assert(kTiles <= 2, "a bit per slot");
   static_assert(rec <= ring && ring % 16 == 0, "a warp's record goes into its ring");
-  const size_t smem = kQ4Warps * ring + (p.part ? 0 : rec);
+  const size_t smem = kQ4Warps * ring + (p.part || p.pieces == 1 ? 0 : join);
   if (cudaError_t e = opt_in_smem(kern, smem, smem_set); e != cudaSuccess) return e;
   const unsigned units = (unsigned)p.B * p.Hkv * p.col_blocks;
   if (!p.part) return launch_chained(kern, dim3(units * (unsigned)p.pieces), kThreads, smem, p.pieces, s, p);
