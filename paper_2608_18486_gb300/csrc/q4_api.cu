@@ -186,45 +186,55 @@ struct RowsPlan {
   size_t off_v, off_table, off_last, off_lens, off_part, total;
 };
 
-// us per MB of codes, and per call, by which the two forms are chosen: the streaming
-// kernel per 16 columns, the tensor cores per 256 rows, reading back, the launches.
-constexpr double kStreamUs = 0.28, kTileUs = 0.71, kReadUs = 1.23, kTileLaunchUs = 20.;
+// Estimates in us that choose between the two forms, and whether the KV tiles are cut.
+// Streaming: 16 columns take as long as the codes' stream, and every CTA has a start
+// and an end.  Tensor cores: reading back (codes in, rows out, rows in again), one step
+// of 2 x 128 rows over a KV tile, the launches.  Measured (streaming / tensor cores; heads
+// of 128, 32 query and 8 kv heads): 1 sequence of 8192 slots, 32 rows 28 / 39, 64 rows 47 /
+// 39, 256 rows 157 / 52; 8 of 32768, 16 rows 296 / 632, 32 rows 587 / 653, 64 rows 1069 /
+// 623; 32 of 1024, 16 rows 70 / 118, 32 rows 124 / 96.
+constexpr double kCallUs = 6., kCtaUs = 0.022, kReadUs = 1., kGroupUs = 10., kLeastTileUs = 6.;
+constexpr double stream_us(int d) { return d == 64 ? 0.33 : d == 96 ? 0.27 : 0.23; }  // per MB of codes and 16 columns
+constexpr double tile_step_us(int d) { return d == 64 ? 1.6 : 2.3; }
 constexpr size_t kGroupBytes = 256 << 20;  // rows read back at once, beyond one sequence
 
 RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   RowsPlan pl{};
-  const int G = c.Hq / c.Hkv;
+  const int G = c.Hq / c.Hkv, sms = sm_count();
   const int64_t rows = (int64_t)Tq * G, slots = (int64_t)max_pages * c.page_size;
   if (c.dtype != WM_DT_BF16 || c.page_size < 8 || !tma_available()) return pl;
   if (slots * c.Hkv >= INT32_MAX || (int64_t)B * Tq >= INT32_MAX || rows >= INT32_MAX / 2) return pl;
-  const double mb = (double)B * slots * c.Hkv * (c.d + c.d / 8) * 1e-6;
-  const double stream = kStreamUs * mb * (double)((rows + 15) / 16);
-  const double tile = kTileLaunchUs + mb * (kReadUs + kTileUs * (double)((rows + 255) / 256));
-  if (stream <= tile) return pl;
-  pl.tiles = true;
   const size_t one = (size_t)slots * c.Hkv * c.d * 2 * 2;
   int64_t group = kGroupBytes / one;
   if (group > (INT32_MAX - 1) / (slots * c.Hkv)) group = (INT32_MAX - 1) / (slots * c.Hkv);
   pl.group = (int)(group < 1 ? 1 : group > B ? B : group);
-  // items without cuts: two heads of 128 rows, or one of 256
+  const int64_t tiles = (slots + kTileSlots - 1) / kTileSlots;
+  const double step = tile_step_us(c.d);
+  // whole items: two heads of 128 rows, or one of 256
   const int64_t items = (int64_t)pl.group * (G % 2 == 0 ? c.Hq / 2 * ((Tq + kTileRows - 1) / kTileRows)
                                                         : c.Hq * ((Tq + 2 * kTileRows - 1) / (2 * kTileRows)));
-  const int sms = sm_count();
-  pl.cut = items < 2 * sms;
+  const double whole = (double)((items + sms - 1) / sms) * tiles * step;
+  // cut ones: the count of parts with the shortest last CTA, a CTA's start as one KV tile
   pl.pair = rows <= kTileRows ? 1 : 0;
   pl.blocks = pl.pair ? 1 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
-  pl.splits = 1;
-  if (pl.cut) {  // the count with the shortest last CTA, a CTA's start as two KV tiles
-    const int64_t units = (int64_t)pl.blocks * c.Hkv, tiles = (slots + kTileSlots - 1) / kTileSlots;
-    double least = 1e30;
-    for (int n = 1; n <= 32 && n <= tiles; ++n) {
-      const double cost = (double)((units * n + sms - 1) / sms) * ((double)((tiles + n - 1) / n) + 2.) + 0.05 * n;
-      if (cost < least) {
-        least = cost;
-        pl.splits = n;
-      }
+  const int64_t units = (int64_t)pl.blocks * c.Hkv;
+  double least = 1e30;
+  int splits = 1;
+  for (int n = 1; n <= 32 && n <= tiles; ++n) {
+    const double cost = (double)((units * n + sms - 1) / sms) * ((double)((tiles + n - 1) / n) + 1.) + 0.05 * n;
+    if (cost < least) {
+      least = cost;
+      splits = n;
     }
   }
+  const double part = least * step, cut = kLeastTileUs + pl.group * (part > kLeastTileUs ? part : kLeastTileUs);
+  pl.cut = cut < whole;
+  pl.splits = pl.cut ? splits : 1;
+  const double mb = (double)B * slots * c.Hkv * (c.d + c.d / 8) * 1e-6, blocks = (double)((rows + 15) / 16);
+  const double tensor = kReadUs * mb + (double)((B + pl.group - 1) / pl.group) * (kGroupUs + (pl.cut ? cut : whole));
+  const double stream = kCallUs + blocks * (mb * stream_us(c.d) + kCtaUs * B * c.Hkv);
+  if (stream <= tensor) return pl;
+  pl.tiles = true;
   pl.records = pl.splits * (pl.pair ? 2 : 1);
   size_t off = 0;
   auto take = [&](size_t bytes) {

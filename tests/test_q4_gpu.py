@@ -309,7 +309,7 @@ def check_many(x, q, pos, got, layer=0):
 
 @pytest.mark.parametrize("G,Tq,lens,Hkv,d,page,maxp,order", [
     (4, 300, [4001], 2, 128, 16, 1024, "last"),         # KV tiles cut, 256 rows per item
-    (8, 16, [700, 90], 2, 128, 32, 8192, "last"),       # at most 128 rows: their even and odd KV tiles
+    (8, 16, [700, 90], 8, 64, 32, 4096, "last"),        # at most 128 rows: their even and odd KV tiles
     (1, 257, [300, 1500, 257], 2, 64, 8, 16384, "any"),  # more than one group of sequences, any order
     (2, 200, [611, 200], 3, 96, 64, 1024, "last"),
     (8, 260, [300] * 8, 4, 64, 16, 400, "last"),        # items enough: no cuts
