@@ -114,12 +114,18 @@ struct Q4Plan {
   size_t total;  // workspace
 };
 
+constexpr double kWideMb = 55.;  // MB of codes times groups of 8 columns
 constexpr int kLongSteps = 12;  // steps of a cluster's warp from which they are spread
 
 Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   const int64_t cols = (int64_t)Tq * (c.Hq / c.Hkv);
   Q4Plan pl{};
-  pl.nb = cols > 8 && c.dtype == WM_DT_BF16 ? 2 : 1;
+  // 16 columns per unit read the codes once for both eights, but run half the warps: for
+  // enough work only.  us with 16 / 8 columns per unit (32 query, 8 kv heads of 128): 1 sequence
+  // of 512 slots, 4 rows 10.6 / 7.6; of 8192, 8 rows 18.6 / 14.9, 32 rows 28.4 / 35.0; 8 of
+  // 32768, 4 rows 84 / 114; 16 of 2048, 12 heads of 64, 16 rows 31.7 / 20.6.
+  const double mb = (double)B * max_pages * c.page_size * c.Hkv * (c.d + c.d / 8) * 1e-6;
+  pl.nb = cols > 8 && c.dtype == WM_DT_BF16 && mb * (double)((cols + 7) / 8) > kWideMb ? 2 : 1;
   pl.col_blocks = (int)((cols + 8 * pl.nb - 1) / (8 * pl.nb));
   const int64_t units = (int64_t)B * c.Hkv * pl.col_blocks;
   const int64_t steps = ((int64_t)max_pages * c.page_size + kQ4Slots - 1) / kQ4Slots;
