@@ -199,6 +199,75 @@ def test_decode_attention_of_long_contexts(dtype, G, lens, page):
     assert torch.equal(out, again)
 
 
+def spread(x, Tq=1):
+    """Whether the steps of this call are spread over the CTAs: it needs records then."""
+    ws = W.wm_q4_rows_attn_workspace(x.session_cfg(), x.B, Tq, x.max_pages)
+    return 256 < ws < 1 << 24
+
+
+@pytest.mark.parametrize("dtype,Hkv,G,d,page,lens", [
+    ("bf16", 3, 1, 64, 16, [0, 1, 31, 32, 33, 700, 0, 2500]),
+    ("bf16", 1, 8, 128, 32, [5003, 0, 17]),
+    ("bf16", 2, 4, 96, 4, [999]),
+    ("bf16", 1, 2, 64, 16, [(7 * i) % 90 for i in range(300)]),  # more sequences than threads
+    ("bf16", 2, 1, 64, 16, [0] * 5),
+    ("bf16", 1, 1, 64, 64, [100001]),                            # one unit, all records its own
+    ("f32", 2, 1, 64, 16, [0, 1, 31, 32, 33, 700, 0, 2500]),
+    ("f32", 1, 4, 128, 2, [600, 3, 5])])
+def test_decode_attention_spread_over_the_ctas(dtype, Hkv, G, d, page, lens):
+    x = Q.Q4(lens, Hkv=Hkv, G=G, d=d, page=page, dtype=dtype, k=1, seed=d, max_pages=-(-max(150000, 12 * max(lens)) // page))
+    assert spread(x)
+    s, q4 = x.session(), x.q4()
+    table, n = x.q4_dev()
+    q = x.queries(x.B)
+    out = torch.full((x.B, x.Hq, d), float("nan"), dtype=x.tdt, device="cuda")
+    s.q4_decode_attn(0, q.cuda(), q4, table, n, out)
+    assert s.read_status() == 0
+    attend_all(x, s, q4, q, lens, to_f64(out), 0, max(lens) / 16)
+    again = torch.empty_like(out)
+    s.q4_decode_attn(0, q.cuda(), q4, table, n, again)
+    assert torch.equal(out, again)
+    # bad lengths beside good ones
+    n[0], n[-1] = -3, x.T + 1
+    s.q4_decode_attn(0, q.cuda(), q4, table, n, again)
+    assert s.read_status() == W.WM_ERR_BOUNDS
+    assert bool((again[0] == 0).all()) and bool((again[-1] == 0).all())
+    got = to_f64(again)
+    for b in range(1, x.B - 1):
+        want, tol = x.bound(0, b, 0, to_f64(q[b, 0]), list(range(lens[b])), max(lens) / 16)
+        assert np.abs(got[b, 0] - want).max() <= tol
+
+
+@pytest.mark.parametrize("G,Tq,d,page,lens,slots", [
+    (4, 4, 128, 16, [900, 40, 33], 400000), (1, 13, 64, 8, [600, 13], 900000), (8, 2, 96, 64, [70, 2, 500], 400000),
+    (1, 40, 64, 16, [300, 41], 120000), (4, 9, 128, 32, [200, 90], 100000), (2, 10, 96, 4, [100, 33], 150000)])
+def test_rows_of_16_columns(G, Tq, d, page, lens, slots):
+    """Few columns are spread over the CTAs, more make several units per kv head."""
+    x = Q.Q4(lens, Hkv=2, G=G, d=d, page=page, k=1, max_pages=slots // page)
+    assert spread(x, Tq) == (Tq * G <= 16) and not (on_tiles(x, Tq) and Tq * G > 16)
+    s, q4 = x.session(), x.q4()
+    table, _ = x.q4_dev()
+    pos = np.stack([np.arange(n - Tq, n)[::-1] for n in lens]).astype(np.int32)
+    pos[0, 1] = 0
+    q = x.queries(x.B, Tq)
+    dev = torch.from_numpy(pos).cuda()
+    out = torch.full((x.B, Tq, x.Hq, d), float("nan"), dtype=x.tdt, device="cuda")
+    s.q4_rows_attn(0, q.cuda(), dev, q4, table, out)
+    assert s.read_status() == 0
+    first = to_f64(out)
+    dev[-1, 0] = -1  # (the cuts go by the lengths, so the others may change in their last bits)
+    s.q4_rows_attn(0, q.cuda(), dev, q4, table, out)
+    assert s.read_status() == W.WM_ERR_BOUNDS and bool((out[-1, 0] == 0).all())
+    second = to_f64(out)
+    for b in range(x.B):
+        for r in range(Tq):
+            for hq in range(x.Hq):
+                want, tol = x.bound(0, b, hq, to_f64(q[b, r, hq]), list(range(int(pos[b, r]) + 1)), max(lens) / 16)
+                assert np.abs(first[b, r, hq] - want).max() <= tol, (b, r, hq)
+                if b < x.B - 1 or r > 0:
+                    assert np.abs(second[b, r, hq] - want).max() <= tol, (b, r, hq)
+
+
 @pytest.mark.parametrize("dtype,d", KINDS)
 @pytest.mark.parametrize("G,Tq,page", [(1, 3, 16), (4, 5, 16), (8, 1, 8), (2, 19, 32), (1, 33, 2)])
 def test_rows_attention(dtype, d, G, Tq, page):
