@@ -167,7 +167,12 @@ __device__ __forceinline__ int feature(int g, int m) {
 }
 
 // One warp's columns.  Lane: g = lane / 4, c = lane % 4.
-template <typename T, int HD, int NB, bool BIG>
+// ONE: there is one column.  Its query fills all eight of S^T's product, column n
+// with zeros but for the features of scale group n, so that the product leaves one sum
+// per group: the scales of K then cost two products per slot and lane instead of
+// one per pair of codes (32 x 8192 slots, 32 heads of 128: ONE_US us against 153).  In O^T's all
+// columns are the same.
+template <typename T, int HD, int NB, bool BIG, bool ONE>
 struct Math {
   using SH = Shape<HD>;
   static constexpr int NQ = Parts<T>::Q, NP = Parts<T>::P;
@@ -210,6 +215,7 @@ struct Math {
       for (int i = 0; i < 2; ++i) {
         uint32_t part[NQ];
         split(x[4 * j + 2 * i] * up, x[4 * j + 2 * i + 1] * up, part);
+        if (ONE && ((HD / 4 * c + 4 * j) >> 4) != lane >> 2) part[0] = 0u;
 #pragma unroll
         for (int y = 0; y < NQ; ++y) q[n][y][j][i] = part[y];
       }
@@ -241,7 +247,8 @@ struct Math {
       const uint32_t base = BIG ? 0u : (uint32_t)(slot >> log2tile) * tile_bytes;
       const int n = BIG ? kQ4Step : tile, r = X * n + (slot & (n - 1));
       codes = base + r * (HD / 2) + (X ? (HD == 128 ? 8 * g : 4 * g) : HD / 8 * c);
-      scales = base + n * HD + r * (HD / kQ4Group) + (X ? (HD == 128 ? g : g >> 1) : HD == 128 ? 2 * c : HD == 64 ? c : (3 * c) >> 1);
+      scales = base + n * HD + r * (HD / kQ4Group) + 
+               (X ? (HD == 128 ? g : g >> 1) : ONE ? min(2 * c, HD / kQ4Group - 2) : HD == 128 ? 2 * c : HD == 64 ? c : (3 * c) >> 1);
     };
 #pragma unroll
     for (int i = 0; i < (BIG ? 1 : 2); ++i) put(g + 8 * i, 0, a.k_[i], a.ks_[i]);
@@ -250,32 +257,57 @@ struct Math {
     return a;
   }
 
+  // The lane's codes of K row g + 8 i.
+  __device__ __forceinline__ static void load_codes(const unsigned char* a, uint32_t (&w)[SH::KW]) {
+    if constexpr (HD == 128) {
+      const uint4 v = *reinterpret_cast<const uint4*>(a);
+      w[0] = v.x;
+      w[1] = v.y;
+      w[2] = v.z;
+      w[3] = v.w;
+    } else if constexpr (HD == 64) {
+      const uint2 v = *reinterpret_cast<const uint2*>(a);
+      w[0] = v.x;
+      w[1] = v.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < SH::KW; ++i) w[i] = reinterpret_cast<const uint32_t*>(a)[i];
+    }
+  }
+
+  // ONE: scores of slots g and g + 8 of the 16 at st, in all four lanes of a slot.
+  __device__ __forceinline__ void scores_one(const unsigned char* st, const At& at, float (&s)[2]) {
+    uint32_t kw[2][SH::KW];
+    float z[4] = {0.f, 0.f, 0.f, 0.f};  // slots g, g + 8; groups 2 c, 2 c + 1
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load_codes(st + at.k(i), kw[i]);
+#pragma unroll
+    for (int w = 0; w < SH::KW; ++w) {
+      uint32_t r0[4], r1[4];
+      codes4(kw[0][w], r0);
+      codes4(kw[1][w], r1);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        mma(z, r0[2 * u], r1[2 * u], r0[2 * u + 1], r1[2 * u + 1], q[0][0][2 * w + u][0], q[0][0][2 * w + u][1]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 f = floats_of((st[at.ks(i)] | (uint32_t)st[at.ks(i) + 1] << 16) << 7);
+      s[i] = fmaf(z[2 * i + 1], f.y, z[2 * i] * f.x);
+      s[i] += __shfl_xor_sync(FULL, s[i], 1);
+      s[i] += __shfl_xor_sync(FULL, s[i], 2);
+    }
+  }
+
   // S^T of the 16 slots at shared address st.
   __device__ __forceinline__ void scores(const unsigned char* st, const At& at, int lane, float (&s)[NB][4]) {
     const int c = lane & 3;
     uint32_t kw[2][SH::KW], sc[2][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const unsigned char* a = st + at.k(i);
-      if constexpr (HD == 128) {
-        const uint4 v = *reinterpret_cast<const uint4*>(a);
-        kw[i][0] = v.x;
-        kw[i][1] = v.y;
-        kw[i][2] = v.z;
-        kw[i][3] = v.w;
-        sc[i][0] = st[at.ks(i)] * 0x00800080u;  // an fp16 pair
-        sc[i][1] = st[at.ks(i) + 1] * 0x00800080u;
-      } else if constexpr (HD == 64) {
-        const uint2 v = *reinterpret_cast<const uint2*>(a);
-        kw[i][0] = v.x;
-        kw[i][1] = v.y;
-        sc[i][0] = sc[i][1] = st[at.ks(i)] * 0x00800080u;
-      } else {
-#pragma unroll
-        for (int w = 0; w < SH::KW; ++w) kw[i][w] = reinterpret_cast<const uint32_t*>(a)[w];
-        sc[i][0] = st[at.ks(i)] * 0x00800080u;
-        sc[i][1] = st[at.ks(i) + 1] * 0x00800080u;
-      }
+      load_codes(st + at.k(i), kw[i]);
+      sc[i][0] = st[at.ks(i)] * 0x00800080u;  // an fp16 pair
+      sc[i][1] = HD == 64 ? sc[i][0] : st[at.ks(i) + 1] * 0x00800080u;
     }
 #pragma unroll
     for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
@@ -388,11 +420,63 @@ struct Math {
     }
   }
 
+  // tiles() for one column.
+  template <bool WHOLE, int NT>
+  __device__ __forceinline__ void tiles_one(const unsigned char* st, uint32_t stride, const At& at, int lane, int t0,
+                                            uint32_t live) {
+    const int g = lane >> 2;
+    float s[NT][2], d[NT][2], most = -INFINITY;  // slots t0 + 16 x + g + 8 i
+#pragma unroll
+    for (int x = 0; x < NT; ++x) scores_one(st + x * stride, at, s[x]);
+#pragma unroll
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int slot = 16 * x + g + 8 * i;
+        if (!WHOLE && !(((live >> slot) & 1u) && t0 + slot < lim[0][0])) s[x][i] = -INFINITY;
+        d[x][i] = fmaf(s[x][i], mul[0][0], -ref[0][0]);
+        most = fmaxf(most, d[x][i]);
+      }
+    if (__any_sync(FULL, most > kRaise)) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < NT; ++x) top = fmaxf(top, fmaxf(s[x][0], s[x][1]));
+#pragma unroll
+      for (int y = 4; y < 32; y *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, y));
+      const float to = fmaxf(ref[0][0], __fsub_rn(__fmul_rn(top, mul[0][0]), kHead)), corr = ex2(ref[0][0] - to);
+      ref[0][0] = to;
+      l[0][0] *= corr;
+#pragma unroll
+      for (int m = 0; m < SH::MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[0][m][i] *= corr;
+#pragma unroll
+      for (int x = 0; x < NT; ++x)  // (two roundings: see tiles())
+#pragma unroll
+        for (int i = 0; i < 2; ++i) d[x][i] = __fsub_rn(__fmul_rn(s[x][i], mul[0][0]), ref[0][0]);
+    }
+#pragma unroll
+    for (int x = 0; x < NT; ++x) {
+      uint32_t p[1][1][2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float u = ex2(d[x][i]);
+        l[0][0] += u;
+        p[0][0][i] = transposed(half2_of(u, u));
+      }
+      values<WHOLE>(st + x * stride, at, lane, live >> (16 * x), p);
+    }
+  }
+
   // NT tiles, `stride` bytes apart, from shared memory st on; t0: the first slot; live:
   // bit per slot that is there and below the unit's largest limit; WHOLE: every column
   // sees every slot.
   template <bool WHOLE, int NT>
   __device__ __forceinline__ void tiles(const unsigned char* st, uint32_t stride, const At& at, int lane, int t0, uint32_t live) {
+    if constexpr (ONE) {
+      tiles_one<WHOLE, NT>(st, stride, at, lane, t0, live);
+      return;
+    }
     const int g = lane >> 2;
     float s[NT][NB][4];
 #pragma unroll
@@ -578,8 +662,8 @@ constexpr int kMlAt = 8 * NB * HD + kQ4MaxCluster;
 template <int HD, int NB>
 constexpr int kJoinFloats = kMlAt<HD, NB> + 2 * kQ4MaxCluster * 8 * NB;
 
-// BIG: pages of at least 16 slots
-template <typename T, int HD, int NB, bool BIG>
+// BIG: pages of at least 16 slots; ONE: one column
+template <typename T, int HD, int NB, bool BIG, bool ONE>
 __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
     q4_attn_kernel(const Q4AttnParams p) {
   using SH = Shape<HD>;
@@ -714,12 +798,12 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
   cp_async_commit();
 
   // ---- queries
-  using Mm = Math<T, HD, NB, BIG>;
+  using Mm = Math<T, HD, NB, BIG, ONE>;
   Mm mm;
   mm.init();
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    const int col = 8 * n + (lane >> 2), x = x0 + col;
+    const int col = ONE ? 0 : 8 * n + (lane >> 2), x = x0 + col;
     const T* row = nullptr;
     int lim = 0;
     if (col < cols) {
@@ -928,11 +1012,11 @@ inline cudaError_t launch_chained(Kern kern, dim3 grid, int threads, size_t smem
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
-template <typename T, int HD, int NB, bool BIG>
+template <typename T, int HD, int NB, bool BIG, bool ONE = false>
 inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
   using SH = Shape<HD>;
   static size_t smem_set[kSmemOptDevices] = {};
-  auto kern = q4_attn_kernel<T, HD, NB, BIG>;
+  auto kern = q4_attn_kernel<T, HD, NB, BIG, ONE>;
   constexpr size_t ring = (size_t)kStages * kTiles * (BIG ? SH::TILE : SH::SMALL), rec = q4_rec(8 * NB, HD) * sizeof(float);
   constexpr size_t join = kJoinFloats<HD, NB> * sizeof(float);
   static_assert(kTiles <= 2, "a bit per slot");
@@ -949,8 +1033,10 @@ inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
 
 template <typename T, int HD>
 inline cudaError_t launch_d(const Q4AttnParams& p, cudaStream_t s) {
-  if constexpr (sizeof(T) == 2)
+  if constexpr (sizeof(T) == 2) {
+    if (p.Tq * p.G == 1) return p.P >= kQ4Step ? launch_t<T, HD, 1, true, true>(p, s) : launch_t<T, HD, 1, false, true>(p, s);
     if (p.nb == 2) return p.P >= kQ4Step ? launch_t<T, HD, 2, true>(p, s) : launch_t<T, HD, 2, false>(p, s);
+  }
   return p.P >= kQ4Step ? launch_t<T, HD, 1, true>(p, s) : launch_t<T, HD, 1, false>(p, s);
 }
 
