@@ -170,7 +170,7 @@ __device__ __forceinline__ int feature(int g, int m) {
 // ONE: there is one column.  Its query fills all eight of S^T's product, column n
 // with zeros but for the features of scale group n, so that the product leaves one sum
 // per group: the scales of K then cost two products per slot and lane instead of
-// one per pair of codes (32 x 8192 slots, 32 heads of 128: ONE_US us against 153).  In O^T's all
+// one per pair of codes (32 x 8192 slots, 32 heads of 128: 151 us against 153).  In O^T's all
 // columns are the same.
 template <typename T, int HD, int NB, bool BIG, bool ONE>
 struct Math {
@@ -741,7 +741,7 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
   const int j0 = from + (int)((int64_t)warp * steps / kQ4Warps);
   const int nmine = from + (int)((int64_t)(warp + 1) * steps / kQ4Warps) - j0;
 
-  // ---- the warp's copies: step i into ring slot i % kStages, in 16-byte chunks
+  // ---- the warp's copies: step i into ring slot i modulo kStages, in 16-byte chunks
   const int32_t* ptab = p.page_table + (int64_t)b * p.max_pages;
   const uint32_t ring_s = smem_u32(ring), to_s = ring_s + lane * 16;
   const uint8_t* pool_lane = p.pool + lane * 16;
@@ -762,9 +762,9 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
   };
   int batch = look_up(0), ahead = look_up(per_batch);
   // Returns which of the step's tiles are there (a bit per tile).
-  auto issue = [&](int i) -> uint32_t {
+  auto issue = [&](int i, int stage) -> uint32_t {
     const int first = (i & (per_batch - 1)) * tiles;  // lane that holds the step's first tile
-    const uint32_t to = to_s + (i % kStages) * STAGE;
+    const uint32_t to = to_s + stage * STAGE;
     uint32_t there;
     if constexpr (BIG) {
       there = 0;
@@ -790,12 +790,12 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
     return there;
   };
   // one commit group per step, empty ones included, so that group i is step i
-  static_assert(kStages == 2 && kTiles == 2, "two steps in flight, two tiles each");
-  uint32_t there = 0, there_next = 0;
-  if (nmine > 0) there = issue(0);
-  cp_async_commit();
-  if (nmine > 1) there_next = issue(1);
-  cp_async_commit();
+  uint32_t there[kStages];  // of the steps in flight, the next one first
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) {
+    there[i] = i < nmine ? issue(i, i) : 0u;
+    cp_async_commit();
+  }
 
   // ---- queries
   using Mm = Math<T, HD, NB, BIG, ONE>;
@@ -816,24 +816,26 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
   const typename Mm::At at = Mm::offsets(p.tile, p.log2tile, p.tile_bytes, lane);
 
   const uint32_t every = BIG || tiles < 32 ? (1u << tiles) - 1 : FULL;
-  int t0 = j0 * kSlots;
+  int t0 = j0 * kSlots, stage = 0;
   for (int i = 0; i < nmine; ++i, t0 += kSlots) {
     cp_async_wait<kStages - 1>();
     __syncwarp();
-    const unsigned char* st = ring + (i % kStages) * STAGE;
-    if (there == every && t0 + kSlots <= least) {
+    const unsigned char* st = ring + stage * STAGE;
+    if (there[0] == every && t0 + kSlots <= least) {
       mm.template step<true>(st, stride, at, lane, t0, FULL);
     } else {
       uint32_t live = 0;
       for (int x = 0; x < tiles; ++x)
-        if ((there >> x) & 1u) live |= ((1u << per_batch) - 1) << (x << log2tile);
+        if ((there[0] >> x) & 1u) live |= ((1u << per_batch) - 1) << (x << log2tile);
       if (S - t0 < kSlots) live &= (1u << (S - t0)) - 1;
       mm.template step<false>(st, stride, at, lane, t0, live);
     }
     __syncwarp();  // every lane is done with this ring slot
-    there = there_next;
-    if (i + kStages < nmine) there_next = issue(i + kStages);
+#pragma unroll
+    for (int x = 0; x + 1 < kStages; ++x) there[x] = there[x + 1];
+    if (i + kStages < nmine) there[kStages - 1] = issue(i + kStages, stage);
     cp_async_commit();
+    stage = stage + 1 < kStages ? stage + 1 : 0;
   }
   cp_async_wait<0>();
 
