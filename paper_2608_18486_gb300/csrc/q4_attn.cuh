@@ -158,6 +158,13 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// The reference below a largest score x.  Past 2^27 the difference may be rounded to 16,
+// and 2^16 is no fp16: the score itself then.
+__device__ __forceinline__ float below(float x) {
+  const float y = __fsub_rn(x, kHead);
+  return __fsub_rn(x, y) > kRaise ? x : y;
+}
+
 // First of the two neighbouring features of accumulator block m of lane row g.
 template <int HD>
 __device__ __forceinline__ int feature(int g, int m) {
@@ -443,7 +450,7 @@ struct Math {
       for (int x = 0; x < NT; ++x) top = fmaxf(top, fmaxf(s[x][0], s[x][1]));
 #pragma unroll
       for (int y = 4; y < 32; y *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, y));
-      const float to = fmaxf(ref[0][0], __fsub_rn(__fmul_rn(top, mul[0][0]), kHead)), corr = ex2(ref[0][0] - to);
+      const float to = fmaxf(ref[0][0], below(__fmul_rn(top, mul[0][0]))), corr = ex2(ref[0][0] - to);
       ref[0][0] = to;
       l[0][0] *= corr;
 #pragma unroll
@@ -516,7 +523,7 @@ struct Math {
           for (int x = 0; x < NT; ++x) top = fmaxf(top, fmaxf(s[x][n][i], s[x][n][i + 2]));
 #pragma unroll
           for (int y = 4; y < 32; y *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, y));
-          const float to = fmaxf(ref[n][i], __fsub_rn(__fmul_rn(top, mul[n][i]), kHead)), corr = ex2(ref[n][i] - to);
+          const float to = fmaxf(ref[n][i], below(__fmul_rn(top, mul[n][i]))), corr = ex2(ref[n][i] - to);
           ref[n][i] = to;
           l[n][i] *= corr;
 #pragma unroll

@@ -419,3 +419,26 @@ def test_many_rows_leave_out_what_is_bad(G, Tq, B, maxp):
             for hq in (0, x.Hq - 1):
                 want, tol = x.bound(0, b, hq, to_f64(q[b, r, hq]), ts, Tq / 16)
                 assert np.abs(got[b, r, hq] - want).max() <= tol + 2.0 ** -8 * np.abs(x.vd[np.isfinite(x.vd)]).max(), (b, r)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G", [1, 2])
+def test_scores_past_24_bits(dtype, G):
+    """Scores so large that the reference is rounded: the largest one takes all, at every size."""
+    x = Q.Q4([100] * 3, Hkv=2, G=G, d=64, page=16, dtype=dtype, k=1)
+    s, q4 = x.session(), x.q4()
+    table, n = x.q4_dev()
+    q = x.queries(x.B)
+    best = np.empty((x.B, x.Hq, 64))
+    for b in range(x.B):
+        for hq in range(x.Hq):
+            K, V = (x.rows(p, 0, b, hq // G, np.arange(100)) for p in (x.kd, x.vd))
+            z = np.sort(K @ to_f64(q[b, hq]))
+            assert z[-1] - z[-2] > 1e-3  # (2^17 of it are 128 and more: nothing is left of the others)
+            best[b, hq] = V[np.argmax(K @ to_f64(q[b, hq]))]
+    for e in range(20, 40):
+        y = q * 2.0 ** e
+        out = torch.empty((x.B, x.Hq, 64), dtype=x.tdt, device="cuda")
+        s.q4_decode_attn(0, y.cuda(), q4, table, n, out)
+        assert np.array_equal(to_f64(out), best), e
+    assert s.read_status() == 0
