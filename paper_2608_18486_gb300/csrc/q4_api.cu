@@ -136,7 +136,10 @@ Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   C = C < 1 ? 1 : C > kQ4MaxCluster ? kQ4MaxCluster : C;
   pl.pieces = (int)C;
   pl.total = 256;
-  if (pl.col_blocks == 1 && steps > C * kQ4Warps * kLongSteps) {
+  // (A share of the spread drains its rings at each unit's end: not where a CTA would take
+  // several.  us, spread / a CTA per unit, 32 heads of 128, lengths within a factor of 2:
+  // 16 sequences 152 / 185, 32 153 / 164, 48 158 / 154, 128 198 / 149.)
+  if (pl.col_blocks == 1 && units <= 2 * resident && steps > C * kQ4Warps * kLongSteps) {
     pl.pieces = resident;
     pl.spread = true;
     pl.total = align256(sizeof(float) * 2 * (size_t)resident * q4_rec(8 * pl.nb, c.d));

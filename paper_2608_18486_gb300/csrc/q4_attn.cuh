@@ -615,48 +615,66 @@ __device__ __forceinline__ int seq_steps(const Q4AttnParams& p, int b, bool repo
 
 // Where the steps of all units are spread evenly over the CTAs (col_blocks 1): in the
 // order (sequence, kv head, step) CTA i of n takes steps T i / n .. T (i + 1) / n - 1.
-// Counts steps of all sequences, and of those before sequence b_end; all threads of
-// the block (NT) call it.
+// All threads of the block (NT) call count and find.
 template <int NT>
 struct Spread {
-  int64_t total, before, own;  // steps x Hkv; own: of this thread's sequences, from `mine` on
-  int64_t mine;
-  int n;                       // CTAs
+  int64_t total;      // steps x Hkv of all sequences
+  int64_t mine, own;  // of this thread's sequences: where they begin, how many they are
+  int n;              // CTAs
   __device__ __forceinline__ int first_seq(const Q4AttnParams& p) const {
     return (int)threadIdx.x * ((p.B + NT - 1) / NT);
   }
-  __device__ __forceinline__ void count(const Q4AttnParams& p, int b_end, int ctas, bool reporter) {
-    __shared__ int64_t sums[2][NT / 32];
+  __device__ __forceinline__ void count(const Q4AttnParams& p, int ctas, bool reporter) {
+    __shared__ int64_t sums[NT / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = (p.B + NT - 1) / NT;
     own = 0;
-    int64_t low = 0;
-    for (int b = first_seq(p); b < min(first_seq(p) + per, p.B); ++b) {
-      const int64_t w = (int64_t)seq_steps(p, b, reporter) * p.Hkv;
-      own += w;
-      if (b < b_end) low += w;
-    }
+    for (int b = first_seq(p); b < min(first_seq(p) + per, p.B); ++b) own += (int64_t)seq_steps(p, b, reporter) * p.Hkv;
     int64_t incl = own;
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
       const int64_t x = __shfl_up_sync(FULL, incl, o);
       if (lane >= o) incl += x;
-      low += __shfl_xor_sync(FULL, low, o);
     }
-    if (lane == 31) {
-      sums[0][warp] = incl;
-      sums[1][warp] = low;
-    }
+    if (lane == 31) sums[warp] = incl;
     __syncthreads();
-    total = before = 0;
+    total = 0;
     mine = incl - own;
 #pragma unroll
     for (int w = 0; w < NT / 32; ++w) {
-      if (w < warp) mine += sums[0][w];
-      total += sums[0][w];
-      before += sums[1][w];
+      if (w < warp) mine += sums[w];
+      total += sums[w];
     }
     const int64_t most = total / (kQ4Warps * kQ4MinSteps);
     n = (int)(most < 1 ? 1 : most < ctas ? most : ctas);
+  }
+  // Sequence b of step pos < total, and the step's place among the sequence's.
+  __device__ __forceinline__ void find(const Q4AttnParams& p, int64_t pos, int& b, int64_t& off) const {
+    __shared__ int64_t at_s[2];
+    if (pos >= mine && pos < mine + own) {
+      int64_t x = pos - mine, w;
+      int y = first_seq(p);
+      while (x >= (w = (int64_t)seq_steps(p, y, false) * p.Hkv)) {
+        x -= w;
+        ++y;
+      }
+      at_s[0] = y;
+      at_s[1] = x;
+    }
+    __syncthreads();
+    b = (int)at_s[0];
+    off = at_s[1];
+  }
+  // Steps before sequence b's.
+  __device__ __forceinline__ int64_t before(const Q4AttnParams& p, int b) const {
+    __shared__ int64_t before_s;
+    const int per = (p.B + NT - 1) / NT;
+    if (b / per == (int)threadIdx.x) {
+      int64_t x = mine;
+      for (int y = first_seq(p); y < b; ++y) x += (int64_t)seq_steps(p, y, false) * p.Hkv;
+      before_s = x;
+    }
+    __syncthreads();
+    return before_s;
   }
   __device__ __forceinline__ int64_t start(int i) const { return total * i / n; }
   // the CTA that takes step x: the last one that starts at or before it
@@ -676,7 +694,6 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
   using SH = Shape<HD>;
   constexpr int STAGE = kTiles * (BIG ? SH::TILE : SH::SMALL);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  __shared__ int64_t at_s[2];  // spread: first sequence, and the step within its units
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   unsigned char* ring = smem_raw + warp * kStages * STAGE;
   float* crec = reinterpret_cast<float*>(smem_raw + kQ4Warps * kStages * STAGE);
@@ -691,24 +708,18 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
   const bool spread = p.part != nullptr;
   if (spread) {
     Spread<kThreads> sp;
-    sp.count(p, 0, (int)gridDim.x, blockIdx.x == 0);
+    sp.count(p, (int)gridDim.x, blockIdx.x == 0);
+    // sequences without steps get their zeros
+    for (int y = blockIdx.x; y < p.B; y += (int)gridDim.x)
+      if (seq_steps(p, y, false) == 0) {
+        T* out = reinterpret_cast<T*>(p.out) + (int64_t)y * p.Tq * p.Hq * HD;
+        for (int e = tid; e < p.Tq * p.Hq * HD; e += kThreads) out[e] = Elem<T>::from_f(0.f);
+      }
     if ((int)blockIdx.x >= sp.n) return;
     const int64_t pos = sp.start(blockIdx.x);
     left = sp.start(blockIdx.x + 1) - pos;
     if (left == 0) return;
-    if (pos >= sp.mine && pos < sp.mine + sp.own) {
-      int64_t x = pos - sp.mine, w;
-      int y = sp.first_seq(p);
-      while (x >= (w = (int64_t)seq_steps(p, y, false) * p.Hkv)) {
-        x -= w;
-        ++y;
-      }
-      at_s[0] = y;
-      at_s[1] = x;
-    }
-    __syncthreads();
-    b = (int)at_s[0];
-    off = at_s[1];
+    sp.find(p, pos, b, off);
     h = 0;
   } else {
     C = p.pieces;
@@ -927,57 +938,74 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
 }
 
 // Joins the records of units whose steps several CTAs took: out = sum_i 2^(m_i - M) O_i /
-// sum_i 2^(m_i - M) l_i.  blockIdx.x is the unit, blockIdx.y 32 groups of four of its
-// outputs; 8 threads share a group's records.  Units without steps get their zeros.
+// sum_i 2^(m_i - M) l_i.  blockIdx.x is the unit, or (fewer CTAs than units) the CTA that
+// took such a unit's first steps, blockIdx.y 32 groups of four of its outputs; 8 threads
+// share a group's records.
 template <typename T, int HD>
-__global__ void __launch_bounds__(256) q4_join_kernel(const Q4AttnParams p, int ctas) {
+__global__ void __launch_bounds__(256) q4_join_kernel(const Q4AttnParams p, int by_unit) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __shared__ float4 o_s[8][32];
   __shared__ float l_s[8][32];
-  const int b = (int)blockIdx.x / p.Hkv, h = (int)blockIdx.x - b * p.Hkv, cols = p.Tq * p.G, most = 8 * p.nb;
+  Spread<256> sp;
+  sp.count(p, p.pieces, false);
+  int b, h, first;
+  int64_t unit;  // the unit's first step
+  if (by_unit) {
+    b = (int)blockIdx.x / p.Hkv;
+    h = (int)blockIdx.x - b * p.Hkv;
+    const int ns = seq_steps(p, b, false);
+    if (ns == 0) return;
+    unit = sp.before(p, b) + (int64_t)h * ns;
+    first = sp.cta_of(unit);
+  } else {
+    first = blockIdx.x;
+    if (first + 1 >= sp.n) return;
+    const int64_t end = sp.start(first + 1);
+    int64_t off;
+    sp.find(p, end - 1, b, off);  // the unit that the CTA's last step belongs to
+    const int ns = seq_steps(p, b, false);
+    h = (int)(off / ns);
+    unit = end - 1 - (off - (int64_t)h * ns);
+    if (unit < sp.start(first)) return;  // begun by another CTA
+  }
+  const int n = sp.cta_of(unit + seq_steps(p, b, false) - 1) - first + 1;
+  if (n == 1) return;  // written by its CTA
+  const int cols = p.Tq * p.G, most = 8 * p.nb;
   const int tid = threadIdx.x, lane = tid & 31, grp = tid >> 5, recf = q4_rec(most, HD);
   const int y = blockIdx.y * 32 + lane;  // four outputs
   const bool on = y < cols * HD / 4;
   const int r = on ? y / (HD / 4) : 0, e = on ? (y - r * (HD / 4)) * 4 : 0;
-  Spread<256> sp;
-  sp.count(p, b, ctas, false);
-  const int ns = seq_steps(p, b, false);
   float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
   float L = 0.f;
-  if (ns > 0) {
-    const int64_t x = sp.before + (int64_t)h * ns;
-    const int first = sp.cta_of(x), n = sp.cta_of(x + ns - 1) - first + 1;
-    if (n == 1) return;  // written by its CTA
-    // record i: the first CTA's begins with the unit
-    auto rec = [&](int i) -> const float* { return p.part + ((int64_t)(first + i) * 2 + (i == 0)) * recf; };
-    float M = -FLT_MAX;
-    for (int i = grp; i < n; i += 8) M = fmaxf(M, __ldcg(rec(i) + most * HD + 2 * r));
-    l_s[grp][lane] = M;
-    __syncthreads();
+  // record i: the first CTA's begins with the unit
+  auto rec = [&](int i) -> const float* { return p.part + ((int64_t)(first + i) * 2 + (i == 0)) * recf; };
+  float M = -FLT_MAX;
+  for (int i = grp; i < n; i += 8) M = fmaxf(M, __ldcg(rec(i) + most * HD + 2 * r));
+  l_s[grp][lane] = M;
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) M = fmaxf(M, l_s[i][lane]);
-    __syncthreads();
-    constexpr int NBUF = 4;
-    for (int i0 = grp; i0 < n; i0 += 8 * NBUF) {
-      float4 v[NBUF];
-      float2 ml[NBUF];
+  for (int i = 0; i < 8; ++i) M = fmaxf(M, l_s[i][lane]);
+  __syncthreads();
+  constexpr int NBUF = 4;
+  for (int i0 = grp; i0 < n; i0 += 8 * NBUF) {
+    float4 v[NBUF];
+    float2 ml[NBUF];
 #pragma unroll
-      for (int i = 0; i < NBUF; ++i)
-        if (i0 + 8 * i < n) {
-          v[i] = __ldcg(reinterpret_cast<const float4*>(rec(i0 + 8 * i) + r * HD + e));
-          ml[i] = __ldcg(reinterpret_cast<const float2*>(rec(i0 + 8 * i) + most * HD + 2 * r));
-        }
-#pragma unroll
-      for (int i = 0; i < NBUF; ++i) {
-        if (i0 + 8 * i >= n) continue;
-        const float w = exp2f(ml[i].x - M);
-        L = fmaf(w, ml[i].y, L);
-        O.x = fmaf(w, v[i].x, O.x);
-        O.y = fmaf(w, v[i].y, O.y);
-        O.z = fmaf(w, v[i].z, O.z);
-        O.w = fmaf(w, v[i].w, O.w);
+    for (int i = 0; i < NBUF; ++i)
+      if (i0 + 8 * i < n) {
+        v[i] = __ldcg(reinterpret_cast<const float4*>(rec(i0 + 8 * i) + r * HD + e));
+        ml[i] = __ldcg(reinterpret_cast<const float2*>(rec(i0 + 8 * i) + most * HD + 2 * r));
       }
+#pragma unroll
+    for (int i = 0; i < NBUF; ++i) {
+      if (i0 + 8 * i >= n) continue;
+      const float w = exp2f(ml[i].x - M);
+      L = fmaf(w, ml[i].y, L);
+      O.x = fmaf(w, v[i].x, O.x);
+      O.y = fmaf(w, v[i].y, O.y);
+      O.z = fmaf(w, v[i].z, O.z);
+      O.w = fmaf(w, v[i].w, O.w);
     }
   }
   o_s[grp][lane] = O;
@@ -1037,7 +1065,8 @@ inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
   const cudaError_t e = launch_chained(kern, dim3(p.pieces), kThreads, smem, 0, s, p);
   if (e != cudaSuccess) return e;
   const unsigned groups = (unsigned)(p.Tq * p.G * HD / 4 + 31) / 32;
-  return launch_chained(q4_join_kernel<T, HD>, dim3(units, groups), 256, 0, 0, s, p, (int)p.pieces);
+  const bool by_unit = units <= (unsigned)p.pieces;
+  return launch_chained(q4_join_kernel<T, HD>, dim3(by_unit ? units : (unsigned)p.pieces, groups), 256, 0, 0, s, p, (int)by_unit);
 }
 
 template <typename T, int HD>

@@ -210,6 +210,7 @@ def spread(x, Tq=1):
     ("bf16", 1, 8, 128, 32, [5003, 0, 17]),
     ("bf16", 2, 4, 96, 4, [999]),
     ("bf16", 1, 2, 64, 16, [(7 * i) % 90 for i in range(300)]),  # more sequences than threads
+    ("bf16", 2, 1, 64, 16, [(11 * i) % 200 for i in range(350)]),  # more units than CTAs
     ("bf16", 2, 1, 64, 16, [0] * 5),
     ("bf16", 1, 1, 64, 64, [100001]),                            # one unit, all records its own
     ("f32", 2, 1, 64, 16, [0, 1, 31, 32, 33, 700, 0, 2500]),
