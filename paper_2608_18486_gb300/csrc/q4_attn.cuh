@@ -52,9 +52,11 @@ template <int HD>
 struct Shape {
   static constexpr int KW = HD / 32;                 // words of 8 codes per lane and K row
   static constexpr int MT = HD / 16;                 // 16-feature blocks
-  static constexpr int TILE = 16 * (HD + HD / 8);    // bytes of a whole tile
-  // small pages: each tile is padded to 16 bytes
-  static constexpr int SMALL = 16 * ((HD + HD / 8 + 15) / 16 * 16);
+  static constexpr int BYTES16 = 16 * (HD + HD / 8);  // of 16 slots
+  // pages of 1 or 2 slots: each tile is padded to 16 bytes
+  static constexpr int PADDED16 = 16 * ((HD + HD / 8 + 15) / 16 * 16);
+  template <int LT>
+  static constexpr int tile() { return BYTES16 >> (4 - LT); }
 };
 template <typename T>
 struct Parts {
@@ -179,7 +181,8 @@ __device__ __forceinline__ int feature(int g, int m) {
 // per group: the scales of K then cost two products per slot and lane instead of
 // one per pair of codes (32 x 8192 slots, 32 heads of 128: 151 us against 153).  In O^T's all
 // columns are the same.
-template <typename T, int HD, int NB, bool BIG, bool ONE>
+// LT: log2 of a tile's slots, 2 to 4, or 0 for tiles of 1 or 2 slots.
+template <typename T, int HD, int NB, int LT, bool ONE>
 struct Math {
   using SH = Shape<HD>;
   static constexpr int NQ = Parts<T>::Q, NP = Parts<T>::P;
@@ -237,30 +240,33 @@ struct Math {
   // Offsets of this lane's slots in a tile (or 16 slots of small pages): codes and
   // scales of K rows g, g + 8 and of V rows 2 c, 2 c + 1, 2 c + 8, 2 c + 9.
   struct At {
-    uint32_t k_[BIG ? 1 : 2], ks_[BIG ? 1 : 2], v_[BIG ? 1 : 4], vs_[BIG ? 1 : 4];
-    __device__ __forceinline__ uint32_t k(int i) const { return BIG ? k_[0] + i * 8 * (HD / 2) : k_[i]; }
-    __device__ __forceinline__ uint32_t ks(int i) const { return BIG ? ks_[0] + i * 8 * (HD / kQ4Group) : ks_[i]; }
+    static constexpr int N = LT > 0 ? 1 : 4;
+    uint32_t k_[N], ks_[N], v_[N], vs_[N];
+    // from a slot to the one 8 further on, codes (PER = HD / 2) or scales (HD / 16)
+    static constexpr uint32_t eight(int per) { return LT == 4 ? 8 * per : (8 >> LT) * SH::template tile<LT>(); }
+    __device__ __forceinline__ uint32_t k(int i) const { return LT > 0 ? k_[0] + i * eight(HD / 2) : k_[i]; }
+    __device__ __forceinline__ uint32_t ks(int i) const { return LT > 0 ? ks_[0] + i * eight(HD / kQ4Group) : ks_[i]; }
     __device__ __forceinline__ uint32_t v(int i) const {
-      return BIG ? v_[0] + ((i & 1) + 8 * (i >> 1)) * (HD / 2) : v_[i];
+      return LT > 0 ? v_[0] + (i & 1) * (HD / 2) + (i >> 1) * eight(HD / 2) : v_[i];
     }
     __device__ __forceinline__ uint32_t vs(int i) const {
-      return BIG ? vs_[0] + ((i & 1) + 8 * (i >> 1)) * (HD / kQ4Group) : vs_[i];
+      return LT > 0 ? vs_[0] + (i & 1) * (HD / kQ4Group) + (i >> 1) * eight(HD / kQ4Group) : vs_[i];
     }
   };
-  __device__ __forceinline__ static At offsets(int tile, int log2tile, int tile_bytes, int lane) {
+  __device__ __forceinline__ static At offsets(int log2tile, int tile_bytes, int lane) {
     const int g = lane >> 2, c = lane & 3;
     At a;
     auto put = [&](int slot, int X, uint32_t& codes, uint32_t& scales) {
-      const uint32_t base = BIG ? 0u : (uint32_t)(slot >> log2tile) * tile_bytes;
-      const int n = BIG ? kQ4Step : tile, r = X * n + (slot & (n - 1));
+      const int l2 = LT > 0 ? LT : log2tile, n = 1 << l2, r = X * n + (slot & (n - 1));
+      const uint32_t base = (uint32_t)(slot >> l2) * (LT > 0 ? SH::template tile<LT>() : tile_bytes);
       codes = base + r * (HD / 2) + (X ? (HD == 128 ? 8 * g : 4 * g) : HD / 8 * c);
-      scales = base + n * HD + r * (HD / kQ4Group) + 
+      scales = base + n * HD + r * (HD / kQ4Group) +
                (X ? (HD == 128 ? g : g >> 1) : ONE ? min(2 * c, HD / kQ4Group - 2) : HD == 128 ? 2 * c : HD == 64 ? c : (3 * c) >> 1);
     };
 #pragma unroll
-    for (int i = 0; i < (BIG ? 1 : 2); ++i) put(g + 8 * i, 0, a.k_[i], a.ks_[i]);
+    for (int i = 0; i < (LT > 0 ? 1 : 2); ++i) put(g + 8 * i, 0, a.k_[i], a.ks_[i]);
 #pragma unroll
-    for (int i = 0; i < (BIG ? 1 : 4); ++i) put(2 * c + (i & 1) + 8 * (i >> 1), 1, a.v_[i], a.vs_[i]);
+    for (int i = 0; i < (LT > 0 ? 1 : 4); ++i) put(2 * c + (i & 1) + 8 * (i >> 1), 1, a.v_[i], a.vs_[i]);
     return a;
   }
 
@@ -687,12 +693,11 @@ constexpr int kMlAt = 8 * NB * HD + kQ4MaxCluster;
 template <int HD, int NB>
 constexpr int kJoinFloats = kMlAt<HD, NB> + 2 * kQ4MaxCluster * 8 * NB;
 
-// BIG: pages of at least 16 slots; ONE: one column
-template <typename T, int HD, int NB, bool BIG, bool ONE>
+template <typename T, int HD, int NB, int LT, bool ONE>
 __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
     q4_attn_kernel(const Q4AttnParams p) {
   using SH = Shape<HD>;
-  constexpr int STAGE = kTiles * (BIG ? SH::TILE : SH::SMALL);
+  constexpr int STAGE = kTiles * (LT > 0 ? SH::BYTES16 : SH::PADDED16);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   unsigned char* ring = smem_raw + warp * kStages * STAGE;
@@ -763,20 +768,23 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
   const int32_t* ptab = p.page_table + (int64_t)b * p.max_pages;
   const uint32_t ring_s = smem_u32(ring), to_s = ring_s + lane * 16;
   const uint8_t* pool_lane = p.pool + lane * 16;
-  const uint32_t tile_bytes = BIG ? SH::TILE : p.tile_bytes;
-  const uint32_t stride = BIG ? SH::TILE : kQ4Step / p.tile * tile_bytes;
-  const int log2tile = BIG ? 4 : p.log2tile, tiles = kSlots >> log2tile, per_batch = 1 << log2tile;
-  // Tiles of `per_batch` steps from step i on, one per lane: its place in the pool
-  // (-1: not seen, or no such page).
+  const int log2tile = LT > 0 ? LT : p.log2tile, tiles = kSlots >> log2tile, per_batch = 1 << log2tile;
+  const uint32_t tile_bytes = LT > 0 ? SH::template tile<LT>() : p.tile_bytes;
+  const uint32_t stride = LT > 0 ? SH::BYTES16 : kQ4Step / p.tile * tile_bytes;
+  // Tiles of `per_batch` steps from step i on, one per lane: its place in the pool (kGone:
+  // not seen, or no such page), for tiles below 16 slots less its place in the step, so that
+  // a step's chunk y lies y * 16 bytes behind it whichever tile it is of.
+  constexpr int kGone = INT32_MIN;
   auto look_up = [&](int i) -> int {
     const int x = i + (lane >> (5 - log2tile)), t = (j0 + i) * kSlots + (lane << log2tile);
-    if (x >= nmine || t >= S) return -1;
+    if (x >= nmine || t >= S) return kGone;
     const int pg = __ldg(ptab + (t >> p.log2P));
     if ((unsigned)pg >= (unsigned)p.num_pages) {
       report(p.status, WM_ERR_BOUNDS);
-      return -1;
+      return kGone;
     }
-    return BIG ? (pg * p.Hkv + h) * (p.P / kQ4Step) + (t & (p.P - 1)) / kQ4Step : pg * p.Hkv + h;
+    const int at = LT == 4 ? (pg * p.Hkv + h) * (p.P / kQ4Step) + (t & (p.P - 1)) / kQ4Step : pg * p.Hkv + h;
+    return LT == 4 ? at : at - (lane & (tiles - 1));
   };
   int batch = look_up(0), ahead = look_up(per_batch);
   // Returns which of the step's tiles are there (a bit per tile).
@@ -784,21 +792,31 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
     const int first = (i & (per_batch - 1)) * tiles;  // lane that holds the step's first tile
     const uint32_t to = to_s + stage * STAGE;
     uint32_t there;
-    if constexpr (BIG) {
+    if constexpr (LT == 4) {
       there = 0;
 #pragma unroll
       for (int x = 0; x < kTiles; ++x) {
         const int at = __shfl_sync(FULL, batch, first + x);
         if (at >= 0) there |= 1u << x;
-        cp_async_tile<HD>(to + x * SH::TILE, pool_lane + (int64_t)at * SH::TILE, at, lane);
+        cp_async_tile<HD>(to + x * SH::BYTES16, pool_lane + (int64_t)at * SH::BYTES16, at, lane);
       }
     } else {
-      const int chunks = (int)tile_bytes / 16, magic = 65536 / chunks + 1;
-      there = __ballot_sync(FULL, batch >= 0) >> first;
+      there = __ballot_sync(FULL, batch != kGone) >> first;
       if (tiles < 32) there &= (1u << tiles) - 1;
-      for (int y = lane; y < (tiles * chunks + 31) / 32 * 32; y += 32) {
-        const int x = y * magic >> 16, at = __shfl_sync(FULL, batch, (first + x) & 31);
-        cp_async16(to + (y - lane) * 16, p.pool + (int64_t)at * tile_bytes + (y - x * chunks) * 16, x < tiles && at >= 0);
+      if constexpr (LT > 0) {
+        constexpr int CH = SH::template tile<LT>() / 16, ALL = kTiles * SH::BYTES16 / 16;
+#pragma unroll
+        for (int y = 0; y < ALL; y += 32) {
+          const int x = min((y + lane) / CH, (kSlots >> LT) - 1), at = __shfl_sync(FULL, batch, first + x);
+          cp_async16(to + y * 16, pool_lane + (int64_t)at * SH::template tile<LT>() + y * 16,
+                     at != kGone && (y + 32 <= ALL || y + lane < ALL));
+        }
+      } else {
+        const int chunks = (int)tile_bytes / 16, magic = 65536 / chunks + 1;
+        for (int y = 0; y < tiles * chunks; y += 32) {
+          const int x = (y + lane) * magic >> 16, at = __shfl_sync(FULL, batch, (first + x) & 31);
+          cp_async16(to + y * 16, pool_lane + (int64_t)at * tile_bytes + y * 16, x < tiles && at != kGone);
+        }
       }
     }
     if ((i & (per_batch - 1)) == per_batch - 1) {
@@ -816,7 +834,7 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
   }
 
   // ---- queries
-  using Mm = Math<T, HD, NB, BIG, ONE>;
+  using Mm = Math<T, HD, NB, LT, ONE>;
   Mm mm;
   mm.init();
 #pragma unroll
@@ -831,9 +849,9 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
     }
     mm.load(n, row, lim, lane, p.qscale);
   }
-  const typename Mm::At at = Mm::offsets(p.tile, p.log2tile, p.tile_bytes, lane);
+  const typename Mm::At at = Mm::offsets(p.log2tile, p.tile_bytes, lane);
 
-  const uint32_t every = BIG || tiles < 32 ? (1u << tiles) - 1 : FULL;
+  const uint32_t every = tiles < 32 ? (1u << tiles) - 1 : FULL;
   int t0 = j0 * kSlots, stage = 0;
   for (int i = 0; i < nmine; ++i, t0 += kSlots) {
     cp_async_wait<kStages - 1>();
@@ -1049,12 +1067,12 @@ inline cudaError_t launch_chained(Kern kern, dim3 grid, int threads, size_t smem
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
-template <typename T, int HD, int NB, bool BIG, bool ONE = false>
+template <typename T, int HD, int NB, int LT, bool ONE>
 inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
   using SH = Shape<HD>;
   static size_t smem_set[kSmemOptDevices] = {};
-  auto kern = q4_attn_kernel<T, HD, NB, BIG, ONE>;
-  constexpr size_t ring = (size_t)kStages * kTiles * (BIG ? SH::TILE : SH::SMALL), rec = q4_rec(8 * NB, HD) * sizeof(float);
+  auto kern = q4_attn_kernel<T, HD, NB, LT, ONE>;
+  constexpr size_t ring = (size_t)kStages * kTiles * (LT > 0 ? SH::BYTES16 : SH::PADDED16), rec = q4_rec(8 * NB, HD) * sizeof(float);
   constexpr size_t join = kJoinFloats<HD, NB> * sizeof(float);
   static_assert(kTiles <= 2, "a bit per slot");
   static_assert(rec <= ring && ring % 16 == 0, "a warp's record goes into its ring");
@@ -1069,13 +1087,23 @@ inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
   return launch_chained(q4_join_kernel<T, HD>, dim3(by_unit ? units : (unsigned)p.pieces, groups), 256, 0, 0, s, p, (int)by_unit);
 }
 
+template <typename T, int HD, int NB, bool ONE>
+inline cudaError_t launch_lt(const Q4AttnParams& p, cudaStream_t s) {
+  switch (p.log2tile) {
+    case 4: return launch_t<T, HD, NB, 4, ONE>(p, s);
+    case 3: return launch_t<T, HD, NB, 3, ONE>(p, s);
+    case 2: return launch_t<T, HD, NB, 2, ONE>(p, s);
+    default: return launch_t<T, HD, NB, 0, ONE>(p, s);
+  }
+}
+
 template <typename T, int HD>
 inline cudaError_t launch_d(const Q4AttnParams& p, cudaStream_t s) {
   if constexpr (sizeof(T) == 2) {
-    if (p.Tq * p.G == 1) return p.P >= kQ4Step ? launch_t<T, HD, 1, true, true>(p, s) : launch_t<T, HD, 1, false, true>(p, s);
-    if (p.nb == 2) return p.P >= kQ4Step ? launch_t<T, HD, 2, true>(p, s) : launch_t<T, HD, 2, false>(p, s);
+    if (p.Tq * p.G == 1) return launch_lt<T, HD, 1, true>(p, s);
+    if (p.nb == 2) return launch_lt<T, HD, 2, false>(p, s);
   }
-  return p.P >= kQ4Step ? launch_t<T, HD, 1, true>(p, s) : launch_t<T, HD, 1, false>(p, s);
+  return launch_lt<T, HD, 1, false>(p, s);
 }
 
 }  // namespace q4_detail
