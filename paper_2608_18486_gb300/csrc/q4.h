@@ -86,7 +86,7 @@ cudaError_t launch_q4_rows_join(const Q4RowsJoin& p, int d, cudaStream_t s);
 constexpr int kQ4Warps = 4;        // warps per CTA
 constexpr int kQ4Slots = 32;       // slots of a warp's step
 constexpr int kQ4MaxCluster = 8;
-constexpr int kQ4MinSteps = 4;     // steps of a warp at least where all steps are spread
+constexpr int kQ4MinSteps = 1;     // steps of a warp at least where all steps are spread
 // resident CTAs per SM, by registers
 constexpr int q4_ctas_per_sm(bool bf16, int nb) { return !bf16 ? 2 : nb == 1 ? 4 : 2; }
 

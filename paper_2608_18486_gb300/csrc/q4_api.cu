@@ -115,7 +115,8 @@ struct Q4Plan {
 };
 
 constexpr double kWideMb = 55.;  // MB of codes times groups of 8 columns
-constexpr int kLongSteps = 12;  // steps of a cluster's warp from which they are spread
+constexpr int kLongSteps = 16;    // steps of a warp from which they are spread, with few CTAs,
+constexpr int kFilledSteps = 32;  // and so many more where the CTAs fill the SMs
 
 Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   const int64_t cols = (int64_t)Tq * (c.Hq / c.Hkv);
@@ -136,10 +137,15 @@ Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   C = C < 1 ? 1 : C > kQ4MaxCluster ? kQ4MaxCluster : C;
   pl.pieces = (int)C;
   pl.total = 256;
-  // (A share of the spread drains its rings at each unit's end: not where a CTA would take
-  // several.  us, spread / a CTA per unit, 32 heads of 128, lengths within a factor of 2:
-  // 16 sequences 152 / 185, 32 153 / 164, 48 158 / 154, 128 198 / 149.)
-  if (pl.col_blocks == 1 && units <= 2 * resident && steps > C * kQ4Warps * kLongSteps) {
+  // The spread has a start (a scan of the lengths), a second kernel, and a share of it drains its
+  // rings at each unit's end: for long units, the sooner the fewer CTAs these would make
+  // otherwise, and not where a CTA would take several units.  us, spread / not: 32 heads of
+  // 128, lengths within a factor of 2: 16 x 16384 slots 152 / 185, 32 x 8192 153 / 164, 48 x
+  // 5461 158 / 154, 128 x 2048 198 / 149; 32/8 heads: 16 x 8192 46 / 36, 64 x 4096 72 / 60,
+  // 1 x 32768 20 / 28.
+  const double fill = (double)(units * C) / resident;
+  const double longest = kLongSteps + kFilledSteps * (fill < 1. ? fill : 1.);
+  if (pl.col_blocks == 1 && units <= 2 * resident && (double)steps > (double)(C * kQ4Warps) * longest) {
     pl.pieces = resident;
     pl.spread = true;
     pl.total = align256(sizeof(float) * 2 * (size_t)resident * q4_rec(8 * pl.nb, c.d));

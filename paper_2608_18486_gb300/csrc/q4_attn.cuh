@@ -26,8 +26,13 @@
 //  * fp32: queries in three fp16 parts and P in two; each feature block's products
 //    start at zero and are added with rounding, since a matrix instruction
 //    truncates its sums.
-// One byte of cache costs 3.6 values to unpack: at HBM's rate the conversions take half of
-// the SM's rate (41 of 82 values a cycle), the matrix instructions a third.
+// Bound by HBM and, just below it, by instruction issue: 16 slots of a head of 128 are 2304
+// bytes and 250 (one column) to 268 instructions, 66 of them conversions; four warps
+// per scheduler issue 60 to 64% of the time.  Measured: 32 sequences of 4096 to 8192 slots, 32
+// heads of 128: 150 us, 6.0 TB/s of codes (the copies alone, without the products, 136); 8
+// of 70001 to 131072, 32/8 heads: 153 us.  Two tiles of 16 slots per step: one, with more
+// CTAs, 202 against 169 us.  4 CTAs per SM at 128 registers: 5 at 96, 171 against 162;
+// CTAs of 8 warps 165 against 161; three steps in a ring 172 against 169.
 #include <cooperative_groups.h>
 #include <float.h>
 #include <math.h>
