@@ -87,8 +87,10 @@ constexpr int kQ4Warps = 4;        // warps per CTA
 constexpr int kQ4Slots = 32;       // slots of a warp's step
 constexpr int kQ4MaxCluster = 8;
 constexpr int kQ4MinSteps = 1;     // steps of a warp at least where all steps are spread
-// resident CTAs per SM, by registers
-constexpr int q4_ctas_per_sm(bool bf16, int nb) { return !bf16 ? 2 : nb == 1 ? 4 : 2; }
+// Resident CTAs per SM, by registers.  (fp32 parts among the columns, 16 x 8192 slots of 32
+// heads of 128: 3 CTAs 97 us, 2 108, 4 with the tiles of a step one by one 109.)
+constexpr int q4_ctas_per_sm(bool bf16, int nb, bool fold) { return fold ? 3 : bf16 && nb == 1 ? 4 : 2; }
+constexpr int kQ4Fold = 2;         // fp32: columns of a unit up to which their parts are columns
 
 struct Q4AttnParams {
   const uint8_t* pool;        // channel base

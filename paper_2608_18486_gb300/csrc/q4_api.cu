@@ -130,7 +130,7 @@ Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   pl.col_blocks = (int)((cols + 8 * pl.nb - 1) / (8 * pl.nb));
   const int64_t units = (int64_t)B * c.Hkv * pl.col_blocks;
   const int64_t steps = ((int64_t)max_pages * c.page_size + kQ4Slots - 1) / kQ4Slots;
-  const int resident = sm_count() * q4_ctas_per_sm(c.dtype == WM_DT_BF16, pl.nb);
+  const int resident = sm_count() * q4_ctas_per_sm(c.dtype == WM_DT_BF16, pl.nb, c.dtype == WM_DT_F32 && cols <= kQ4Fold);
   // as many CTAs per unit as are resident, a step per warp at least
   int64_t C = resident / units;
   if (C > steps / kQ4Warps) C = steps / kQ4Warps;

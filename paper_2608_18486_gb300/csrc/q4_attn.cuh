@@ -23,9 +23,9 @@
 //    8 bits in fp16; P is rounded to fp16 (11 bits) against a reference 2^8 below
 //    the running maximum, so that weights down to 2^-22 of the largest keep
 //    them, and the reference moves only when a score passes it by 2^15.
-//  * fp32: queries in three fp16 parts and P in two; each feature block's products
-//    start at zero and are added with rounding, since a matrix instruction
-//    truncates its sums.
+//  * fp32: queries in three fp16 parts and P in two, beside each other among the
+//    columns where there is room (see Fill); each feature block's products start at zero
+//    and are added with rounding, since a matrix instruction truncates its sums.
 // Bound by HBM and, just below it, by instruction issue: 16 slots of a head of 128 are 2304
 // bytes and 250 (one column) to 268 instructions, 66 of them conversions; four warps
 // per scheduler issue 60 to 64% of the time.  Measured: 32 sequences of 4096 to 8192 slots, 32
@@ -180,17 +180,25 @@ __device__ __forceinline__ int feature(int g, int m) {
   return 64 + 4 * g + 2 * (m - 4);
 }
 
-// One warp's columns.  Lane: g = lane / 4, c = lane % 4.
-// ONE: there is one column.  Its query fills all eight of S^T's product, column n
-// with zeros but for the features of scale group n, so that the product leaves one sum
-// per group: the scales of K then cost two products per slot and lane instead of
-// one per pair of codes (32 x 8192 slots, 32 heads of 128: 151 us against 153).  In O^T's all
-// columns are the same.
+// What the eight columns of the products hold:
+//  * kColumns: the unit's columns.
+//  * kOne (bf16, one column): its query fills all eight of S^T's, column n with zeros but
+//    for the features of scale group n, so that the product leaves one sum per group:
+//    the scales of K then cost two products per slot and lane instead of one per pair
+//    of codes (32 x 8192 slots, 32 heads of 128: 151 us against 153).  In O^T's all
+//    columns are the same.
+//  * kFold (fp32, up to two columns): column 4 i + n the n-th part of column i's query, and of
+//    its weights, so that a product is one instruction and not three or two (16 x 8192
+//    slots, 32 heads of 128: 97 us against 137).
+enum Fill { kColumns, kOne, kFold };
 // LT: log2 of a tile's slots, 2 to 4, or 0 for tiles of 1 or 2 slots.
-template <typename T, int HD, int NB, int LT, bool ONE>
+// One warp's columns.  Lane: g = lane / 4, c = lane % 4.
+template <typename T, int HD, int NB, int LT, Fill FILL>
 struct Math {
   using SH = Shape<HD>;
-  static constexpr int NQ = Parts<T>::Q, NP = Parts<T>::P;
+  static constexpr bool ONE = FILL == kOne, FOLD = FILL == kFold;
+  static constexpr bool EXACT = sizeof(T) == 4;  // products start at zero and are added with rounding
+  static constexpr int NQ = FOLD ? 1 : Parts<T>::Q, NP = FOLD ? 1 : Parts<T>::P;
   uint32_t q[NB][NQ][SH::MT][2];  // column g: features (HD / 4) c + 8 w + 4 u + {0, 1}, {2, 3} at [2 w + u]
   float o[NB][SH::MT][4];         // features feature(g, m) (+ 1), columns 2 c, 2 c + 1
   float ref[NB][2], l[NB][2];     // columns 2 c, 2 c + 1; l: this lane's slots only
@@ -228,8 +236,12 @@ struct Math {
     for (int j = 0; j < SH::MT; ++j)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        uint32_t part[NQ];
+        uint32_t part[Parts<T>::Q];
         split(x[4 * j + 2 * i] * up, x[4 * j + 2 * i + 1] * up, part);
+        if constexpr (FOLD) {
+          const int y = (lane >> 2) & 3;
+          part[0] = y == 0 ? part[0] : y == 1 ? part[1] : y == 2 ? part[2] : 0u;
+        }
         if (ONE && ((HD / 4 * c + 4 * j) >> 4) != lane >> 2) part[0] = 0u;
 #pragma unroll
         for (int y = 0; y < NQ; ++y) q[n][y][j][i] = part[y];
@@ -237,8 +249,9 @@ struct Math {
     const float down = qscale * __uint_as_float((uint32_t)(254 - field) << 23);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      mul[n][i] = __shfl_sync(FULL, down, 4 * (2 * c + i));
-      lim[n][i] = __shfl_sync(FULL, limit, 4 * (2 * c + i));
+      const int from = FOLD ? 16 * (c >> 1) : 4 * (2 * c + i);  // a lane of that column
+      mul[n][i] = __shfl_sync(FULL, down, from);
+      lim[n][i] = __shfl_sync(FULL, limit, from);
     }
   }
 
@@ -354,7 +367,7 @@ struct Math {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           const int j = 2 * w + u;
-          if constexpr (NQ == 1) {
+          if constexpr (!EXACT) {
             mma(s[n], r0[2 * u], r1[2 * u], r0[2 * u + 1], r1[2 * u + 1], q[n][0][j][0], q[n][0][j][1]);
           } else {
             float z[4] = {0.f, 0.f, 0.f, 0.f};  // (smallest parts first)
@@ -425,8 +438,13 @@ struct Math {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           float(&to)[4] = o[n][4 * w + i];
-          if constexpr (NP == 1) {
+          if constexpr (!EXACT) {
             mma(to, e[0][i], f[0][i], e[1][i], f[1][i], p[n][0][0], p[n][0][1]);
+          } else if constexpr (FOLD) {
+            float z[4] = {0.f, 0.f, 0.f, 0.f};
+            mma(z, e[0][i], f[0][i], e[1][i], f[1][i], p[n][0][0], p[n][0][1]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) to[x] += z[x];
           } else {
             float y[4] = {0.f, 0.f, 0.f, 0.f}, z[4] = {0.f, 0.f, 0.f, 0.f};
             mma(y, e[0][i], f[0][i], e[1][i], f[1][i], p[n][NP - 1][0], p[n][NP - 1][1]);
@@ -438,14 +456,28 @@ struct Math {
     }
   }
 
-  // tiles() for one column.
+  // FOLD: scores of slots g and g + 8, of column c / 2.
+  __device__ __forceinline__ void scores_fold(const unsigned char* st, const At& at, int lane, float (&s)[2]) {
+    float z[NB][4];
+    scores(st, at, lane, z);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      s[i] = z[0][2 * i] + z[0][2 * i + 1];
+      s[i] += __shfl_xor_sync(FULL, s[i], 1);
+    }
+  }
+
+  // tiles() where a lane has scores of one column.
   template <bool WHOLE, int NT>
   __device__ __forceinline__ void tiles_one(const unsigned char* st, uint32_t stride, const At& at, int lane, int t0,
                                             uint32_t live) {
     const int g = lane >> 2;
     float s[NT][2], d[NT][2], most = -INFINITY;  // slots t0 + 16 x + g + 8 i
 #pragma unroll
-    for (int x = 0; x < NT; ++x) scores_one(st + x * stride, at, s[x]);
+    for (int x = 0; x < NT; ++x) {
+      if constexpr (ONE) scores_one(st + x * stride, at, s[x]);
+      else scores_fold(st + x * stride, at, lane, s[x]);
+    }
 #pragma unroll
     for (int x = 0; x < NT; ++x)
 #pragma unroll
@@ -475,12 +507,17 @@ struct Math {
     }
 #pragma unroll
     for (int x = 0; x < NT; ++x) {
-      uint32_t p[1][1][2];
+      uint32_t p[NB][NP][2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const float u = ex2(d[x][i]);
         l[0][0] += u;
-        p[0][0][i] = transposed(half2_of(u, u));
+        uint32_t w = half2_of(u, u);
+        if constexpr (FOLD) {  // the rest, 2^11 larger, beside it; the odd lanes' columns are empty
+          w = half2_of(u, (u - floats_of(w).x) * 2048.f);
+          if (lane & 1) w = 0u;
+        }
+        p[0][0][i] = transposed(w);
       }
       values<WHOLE>(st + x * stride, at, lane, live >> (16 * x), p);
     }
@@ -491,7 +528,7 @@ struct Math {
   // sees every slot.
   template <bool WHOLE, int NT>
   __device__ __forceinline__ void tiles(const unsigned char* st, uint32_t stride, const At& at, int lane, int t0, uint32_t live) {
-    if constexpr (ONE) {
+    if constexpr (ONE || FOLD) {
       tiles_one<WHOLE, NT>(st, stride, at, lane, t0, live);
       return;
     }
@@ -573,7 +610,7 @@ struct Math {
     }
   }
 
-  // One step of kTiles tiles, fp32's (more parts) one by one: registers.  16 columns of
+  // One step of kTiles tiles, at once but for fp32 in several parts: registers.  16 columns of
   // bf16 heads of 128 (4 drafted rows behind 8 x 32768 slots): both at once, 2 CTAs per
   // SM, 81 us; one by one 82, with 3 CTAs 87.
   static constexpr int kAtOnce = NQ == 1 ? kTiles : 1;
@@ -594,11 +631,14 @@ struct Math {
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
         for (int d = 4; d < 32; d *= 2) l[n][i] += __shfl_xor_sync(FULL, l[n][i], d);
-        const int col = 8 * n + 2 * c + i;
-        if (col >= cols) continue;
+        const int col = FOLD ? (c >> 1) : 8 * n + 2 * c + i;
+        if (col >= cols || (FOLD && ((c & 1) || i))) continue;
 #pragma unroll
-        for (int m = 0; m < SH::MT; ++m)
-          *reinterpret_cast<float2*>(rec + col * HD + feature<HD>(g, m)) = make_float2(o[n][m][i], o[n][m][i + 2]);
+        for (int m = 0; m < SH::MT; ++m) {
+          float2 v = make_float2(o[n][m][i], o[n][m][i + 2]);
+          if (FOLD) v = make_float2(fmaf(o[n][m][1], 1.f / 2048.f, v.x), fmaf(o[n][m][3], 1.f / 2048.f, v.y));
+          *reinterpret_cast<float2*>(rec + col * HD + feature<HD>(g, m)) = v;
+        }
         if (g == 0) {
           rec[cols * HD + 2 * col] = ref[n][i];
           rec[cols * HD + 2 * col + 1] = l[n][i];
@@ -698,8 +738,8 @@ constexpr int kMlAt = 8 * NB * HD + kQ4MaxCluster;
 template <int HD, int NB>
 constexpr int kJoinFloats = kMlAt<HD, NB> + 2 * kQ4MaxCluster * 8 * NB;
 
-template <typename T, int HD, int NB, int LT, bool ONE>
-__global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
+template <typename T, int HD, int NB, int LT, Fill FILL>
+__global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB, FILL == kFold))
     q4_attn_kernel(const Q4AttnParams p) {
   using SH = Shape<HD>;
   constexpr int STAGE = kTiles * (LT > 0 ? SH::BYTES16 : SH::PADDED16);
@@ -839,12 +879,12 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB))
   }
 
   // ---- queries
-  using Mm = Math<T, HD, NB, LT, ONE>;
+  using Mm = Math<T, HD, NB, LT, FILL>;
   Mm mm;
   mm.init();
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    const int col = ONE ? 0 : 8 * n + (lane >> 2), x = x0 + col;
+    const int col = FILL == kOne ? 0 : FILL == kFold ? lane >> 4 : 8 * n + (lane >> 2), x = x0 + col;
     const T* row = nullptr;
     int lim = 0;
     if (col < cols) {
@@ -1072,11 +1112,11 @@ inline cudaError_t launch_chained(Kern kern, dim3 grid, int threads, size_t smem
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
-template <typename T, int HD, int NB, int LT, bool ONE>
+template <typename T, int HD, int NB, int LT, Fill FILL>
 inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
   using SH = Shape<HD>;
   static size_t smem_set[kSmemOptDevices] = {};
-  auto kern = q4_attn_kernel<T, HD, NB, LT, ONE>;
+  auto kern = q4_attn_kernel<T, HD, NB, LT, FILL>;
   constexpr size_t ring = (size_t)kStages * kTiles * (LT > 0 ? SH::BYTES16 : SH::PADDED16), rec = q4_rec(8 * NB, HD) * sizeof(float);
   constexpr size_t join = kJoinFloats<HD, NB> * sizeof(float);
   static_assert(kTiles <= 2, "a bit per slot");
@@ -1092,23 +1132,25 @@ inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
   return launch_chained(q4_join_kernel<T, HD>, dim3(by_unit ? units : (unsigned)p.pieces, groups), 256, 0, 0, s, p, (int)by_unit);
 }
 
-template <typename T, int HD, int NB, bool ONE>
+template <typename T, int HD, int NB, Fill FILL>
 inline cudaError_t launch_lt(const Q4AttnParams& p, cudaStream_t s) {
   switch (p.log2tile) {
-    case 4: return launch_t<T, HD, NB, 4, ONE>(p, s);
-    case 3: return launch_t<T, HD, NB, 3, ONE>(p, s);
-    case 2: return launch_t<T, HD, NB, 2, ONE>(p, s);
-    default: return launch_t<T, HD, NB, 0, ONE>(p, s);
+    case 4: return launch_t<T, HD, NB, 4, FILL>(p, s);
+    case 3: return launch_t<T, HD, NB, 3, FILL>(p, s);
+    case 2: return launch_t<T, HD, NB, 2, FILL>(p, s);
+    default: return launch_t<T, HD, NB, 0, FILL>(p, s);
   }
 }
 
 template <typename T, int HD>
 inline cudaError_t launch_d(const Q4AttnParams& p, cudaStream_t s) {
   if constexpr (sizeof(T) == 2) {
-    if (p.Tq * p.G == 1) return launch_lt<T, HD, 1, true>(p, s);
-    if (p.nb == 2) return launch_lt<T, HD, 2, false>(p, s);
+    if (p.Tq * p.G == 1) return launch_lt<T, HD, 1, kOne>(p, s);
+    if (p.nb == 2) return launch_lt<T, HD, 2, kColumns>(p, s);
+  } else {
+    if (p.Tq * p.G <= kQ4Fold) return launch_lt<T, HD, 1, kFold>(p, s);
   }
-  return launch_lt<T, HD, 1, false>(p, s);
+  return launch_lt<T, HD, 1, kColumns>(p, s);
 }
 
 }  // namespace q4_detail
