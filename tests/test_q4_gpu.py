@@ -239,6 +239,23 @@ def test_decode_attention_spread_over_the_ctas(dtype, Hkv, G, d, page, lens):
         assert np.abs(got[b, 0] - want).max() <= tol
 
 
+@pytest.mark.parametrize("dtype,G,B", [("bf16", 4, 76), ("bf16", 1, 100), ("bf16", 2, 200), ("f32", 1, 56), ("f32", 4, 40)])
+def test_decode_attention_where_larger_clusters_do_not_all_fit(dtype, G, B):
+    lens = [(37 * i) % 300 for i in range(B)]
+    x = Q.Q4(lens, Hkv=1, G=G, d=64, page=16, dtype=dtype, k=1, seed=B, max_pages=128)
+    assert not spread(x)
+    s, q4 = x.session(), x.q4()
+    table, n = x.q4_dev()
+    q = x.queries(x.B)
+    out = torch.full((x.B, x.Hq, 64), float("nan"), dtype=x.tdt, device="cuda")
+    s.q4_decode_attn(0, q.cuda(), q4, table, n, out)
+    assert s.read_status() == 0
+    attend_all(x, s, q4, q, lens, to_f64(out), 0, 8)
+    again = torch.empty_like(out)
+    s.q4_decode_attn(0, q.cuda(), q4, table, n, again)
+    assert torch.equal(out, again)
+
+
 @pytest.mark.parametrize("G,Tq,d,page,lens,slots", [
     (4, 4, 128, 16, [900, 40, 33], 400000), (1, 13, 64, 8, [600, 13], 900000), (8, 2, 96, 64, [70, 2, 500], 400000),
     (1, 40, 64, 16, [300, 41], 120000), (4, 9, 128, 32, [200, 90], 100000), (2, 10, 96, 4, [100, 33], 150000)])
