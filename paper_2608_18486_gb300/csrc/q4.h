@@ -90,6 +90,7 @@ constexpr int kQ4MinSteps = 1;     // steps of a warp at least where all steps a
 // Resident CTAs per SM, by registers.  (fp32 parts among the columns, 16 x 8192 slots of 32
 // heads of 128: 3 CTAs 97 us, 2 108, 4 with the tiles of a step one by one 109.)
 constexpr int q4_ctas_per_sm(bool bf16, int nb, bool fold) { return fold ? 3 : bf16 && nb == 1 ? 4 : 2; }
+constexpr int kQ4MaxCtas = 4;      // the most of q4_ctas_per_sm
 constexpr int kQ4Fold = 2;         // fp32: columns of a unit up to which their parts are columns
 
 struct Q4AttnParams {

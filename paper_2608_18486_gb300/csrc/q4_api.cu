@@ -104,12 +104,69 @@ wm_status copy_ranges(bool write, const wm_config* c, const wm_cache* cache, con
                            : launch_q4_read(p, c->dtype, c->d, sm_count(), (cudaStream_t)stream));
 }
 
+// Clusters of C CTAs that are resident at once where an SM takes k CTAs (a GPC's SMs
+// are not always taken whole).  0: unknown.
+__global__ void __launch_bounds__(kQ4Warps * 32) q4_places_kernel() {}  // (asked about, never launched)
+
+int cluster_places(int C, int k) {
+  static int known[kSmemOptDevices][kQ4MaxCtas][kQ4MaxCluster] = {};
+  static size_t smem_set[kSmemOptDevices] = {};
+  int dev = 0, per_sm = 0, reserved = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kSmemOptDevices) return 0;
+  int& slot = known[dev][k - 1][C - 1];
+  if ((n = __atomic_load_n(&slot, __ATOMIC_RELAXED)) != 0) return n;
+  if (cudaDeviceGetAttribute(&per_sm, cudaDevAttrMaxSharedMemoryPerMultiprocessor, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&reserved, cudaDevAttrReservedSharedMemoryPerBlock, dev) != cudaSuccess)
+    return 0;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)C);
+  cfg.blockDim = dim3(kQ4Warps * 32);
+  cfg.dynamicSmemBytes = (size_t)((per_sm / k - reserved) / 128 * 128);  // k of them, not k + 1
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)C;
+  attr.val.clusterDim.y = 1;
+  attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (opt_in_smem(q4_places_kernel, cfg.dynamicSmemBytes, smem_set) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, q4_places_kernel, &cfg) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return 0;
+  }
+  __atomic_store_n(&slot, n, __ATOMIC_RELAXED);
+  return n;
+}
+
+// CTAs per unit, at most `most`, where an SM takes per_sm of them.  The units of an SM that
+// has k CTAs take k / C of a CTA's time each, with k small a little more: fewer
+// loads in flight.  One cluster more than are resident at once takes a second wave.  us by C
+// (bf16, 4 query heads of 128, 4096 slots): 60 units 1: 20.7, 2: 17.0, 4: 13.5, 7: 14.5, 8: 13.7;
+// 84 units 2: 21.2, 4: 16.8, 5: 15.3, 6: 16.2, 7 (two waves): 22.1; 120 units 1: 31.3, 2: 22.6,
+// 4: 22.1, 5 (two waves): 27.8; 152 units 1: 28.4, 2: 23.0, 3: 27.0.
+int cluster_size(int64_t units, int most, int per_sm) {
+  constexpr double load[kQ4MaxCtas] = {1.5, 2.2, 3.1, 4.};
+  double least = 1e30;
+  int best = 1;
+  for (int C = 1; C <= most; ++C)
+    for (int k = 1; k <= per_sm; ++k)
+      if (units <= cluster_places(C, k)) {
+        if (load[k - 1] / C < least) {
+          least = load[k - 1] / C;
+          best = C;
+        }
+        break;
+      }
+  return best;
+}
+
 // Split of an attention call.  Short units are one cluster each, joined on chip; the
 // steps of long ones are spread evenly over the resident CTAs, whatever the lengths,
 // and a second kernel joins the units that were cut.
 struct Q4Plan {
   int nb, col_blocks;
-  int pieces;    // CTAs per unit, or of the spread
+  int pieces;    // CTAs per unit at most, or of the spread
+  int per_sm;    // CTAs
   bool spread;
   size_t total;  // workspace
 };
@@ -130,8 +187,9 @@ Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   pl.col_blocks = (int)((cols + 8 * pl.nb - 1) / (8 * pl.nb));
   const int64_t units = (int64_t)B * c.Hkv * pl.col_blocks;
   const int64_t steps = ((int64_t)max_pages * c.page_size + kQ4Slots - 1) / kQ4Slots;
-  const int resident = sm_count() * q4_ctas_per_sm(c.dtype == WM_DT_BF16, pl.nb, c.dtype == WM_DT_F32 && cols <= kQ4Fold);
-  // as many CTAs per unit as are resident, a step per warp at least
+  pl.per_sm = q4_ctas_per_sm(c.dtype == WM_DT_BF16, pl.nb, c.dtype == WM_DT_F32 && cols <= kQ4Fold);
+  const int resident = sm_count() * pl.per_sm;
+  // at most as many CTAs per unit as are resident, a step per warp at least
   int64_t C = resident / units;
   if (C > steps / kQ4Warps) C = steps / kQ4Warps;
   C = C < 1 ? 1 : C > kQ4MaxCluster ? kQ4MaxCluster : C;
@@ -184,7 +242,7 @@ wm_status attn(const wm_config& c, const wm_q4_cache& q4, int32_t layer, const v
   p.max_pages = max_pages;
   p.col_blocks = pl.col_blocks;
   p.nb = pl.nb;
-  p.pieces = pl.pieces;
+  p.pieces = pl.spread ? pl.pieces : cluster_size((int64_t)B * c.Hkv * pl.col_blocks, pl.pieces, pl.per_sm);
   p.qscale = (float)(1.4426950408889634 / sqrt((double)c.d));
   return cuda_status(launch_q4_attn(p, c.dtype, c.d, (cudaStream_t)stream));
 }

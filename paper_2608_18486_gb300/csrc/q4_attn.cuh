@@ -749,9 +749,11 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB, F
   float* crec = reinterpret_cast<float*>(smem_raw + kQ4Warps * kStages * STAGE);
 
   // Dependents start only after this grid's own wait, so that everything before
-  // it is visible to them whatever they wait for.
+  // it is visible to them whatever they wait for; and early only where this grid fills
+  // the SMs.  Elsewhere CTAs that start beside these would crowd on the SMs that have
+  // most room: 400 units of 2048 slots, back to back, 27.3 us instead of 33.4.
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (p.part) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   int b, h, x0 = 0, piece = 0, C = 1;
   int64_t off = 0, left = 0;  // spread: step among the sequence's units, steps left to take
@@ -1112,47 +1114,10 @@ inline cudaError_t launch_chained(Kern kern, dim3 grid, int threads, size_t smem
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
-// Clusters that a GPC's SMs do not take whole leave some of their places empty, so fewer
-// are resident than the registers allow, and one too many waits for a second wave: the
-// largest size up to C at which `units` clusters run at once, with some to spare for
-// the larger ones, which are placed less well than they could be.  us with C / C - 1 CTAs, 2048
-// slots per unit, four query heads: 72 units, C 8 12.4 / 11.0; 81, 7 12.8 / 11.1; 97, 6 15.2 / 12.6;
-// 117, 5 18.4 / 13.6; 194, 3 23.3 / 21.9; but 69, 8 10.3 / 11.1; 192, 3 18.9 / 21.9.
-template <typename Kern>
-inline int fitting_pieces(Kern kern, size_t smem, int64_t units, int C, int (&known)[kSmemOptDevices][kQ4MaxCluster + 1]) {
-  int dev = 0;
-  if (C == 1 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kSmemOptDevices) return C;
-  for (; C > 1; --C) {
-    int n = __atomic_load_n(&known[dev][C], __ATOMIC_RELAXED);
-    if (n == 0) {
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3(C);
-      cfg.blockDim = dim3(kThreads);
-      cfg.dynamicSmemBytes = smem;
-      cudaLaunchAttribute attr;
-      attr.id = cudaLaunchAttributeClusterDimension;
-      attr.val.clusterDim.x = (unsigned)C;
-      attr.val.clusterDim.y = 1;
-      attr.val.clusterDim.z = 1;
-      cfg.attrs = &attr;
-      cfg.numAttrs = 1;
-      if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return 1;
-      }
-      __atomic_store_n(&known[dev][C], n, __ATOMIC_RELAXED);
-    }
-    if (C <= 4 ? units < n : 16 * units <= 15 * (int64_t)n) break;
-  }
-  return C;
-}
-
 template <typename T, int HD, int NB, int LT, Fill FILL>
-inline cudaError_t launch_t(const Q4AttnParams& given, cudaStream_t s) {
+inline cudaError_t launch_t(const Q4AttnParams& p, cudaStream_t s) {
   using SH = Shape<HD>;
   static size_t smem_set[kSmemOptDevices] = {};
-  static int clusters[kSmemOptDevices][kQ4MaxCluster + 1] = {};
-  Q4AttnParams p = given;
   auto kern = q4_attn_kernel<T, HD, NB, LT, FILL>;
   constexpr size_t ring = (size_t)kStages * kTiles * (LT > 0 ? SH::BYTES16 : SH::PADDED16), rec = q4_rec(8 * NB, HD) * sizeof(float);
   constexpr size_t join = kJoinFloats<HD, NB> * sizeof(float);
@@ -1161,7 +1126,6 @@ inline cudaError_t launch_t(const Q4AttnParams& given, cudaStream_t s) {
   const size_t smem = kQ4Warps * ring + (p.part || p.pieces == 1 ? 0 : join);
   if (cudaError_t e = opt_in_smem(kern, smem, smem_set); e != cudaSuccess) return e;
   const unsigned units = (unsigned)p.B * p.Hkv * p.col_blocks;
-  if (!p.part) p.pieces = fitting_pieces(kern, smem, units, p.pieces, clusters);
   if (!p.part) return launch_chained(kern, dim3(units * (unsigned)p.pieces), kThreads, smem, p.pieces, s, p);
   const cudaError_t e = launch_chained(kern, dim3(p.pieces), kThreads, smem, 0, s, p);
   if (e != cudaSuccess) return e;
