@@ -172,7 +172,7 @@ struct Q4Plan {
 };
 
 constexpr double kWideMb = 55.;  // MB of codes times groups of 8 columns
-constexpr int kLongSteps = 16;    // steps of a warp from which they are spread, with few CTAs,
+constexpr int kLongSteps = 14;    // steps of a warp from which they are spread, with few CTAs,
 constexpr int kFilledSteps = 32;  // and so many more where the CTAs fill the SMs
 
 Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
@@ -180,8 +180,8 @@ Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   Q4Plan pl{};
   // 16 columns per unit read the codes once for both eights, but run half the warps: for
   // enough work only.  us with 16 / 8 columns per unit (32 query, 8 kv heads of 128): 1 sequence
-  // of 512 slots, 4 rows 10.6 / 7.6; of 8192, 8 rows 18.6 / 14.9, 32 rows 28.4 / 35.0; 8 of
-  // 32768, 4 rows 84 / 114; 16 of 2048, 12 heads of 64, 16 rows 31.7 / 20.6.
+  // of 512 slots, 4 rows 10.6 / 7.5; of 8192, 8 rows 18.4 / 14.7, 32 rows 28.6 / 35.2; 8 of
+  // 32768, 4 rows 84 / 114; 16 of 2048, 4 rows 21.2 / 23.3, 12 heads of 64, 16 rows 17.8 / 17.1.
   const double mb = (double)B * max_pages * c.page_size * c.Hkv * (c.d + c.d / 8) * 1e-6;
   pl.nb = cols > 8 && c.dtype == WM_DT_BF16 && mb * (double)((cols + 7) / 8) > kWideMb ? 2 : 1;
   pl.col_blocks = (int)((cols + 8 * pl.nb - 1) / (8 * pl.nb));
@@ -198,9 +198,9 @@ Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   // The spread has a start (a scan of the lengths), a second kernel, and a share of it drains its
   // rings at each unit's end: for long units, the sooner the fewer CTAs these would make
   // otherwise, and not where a CTA would take several units.  us, spread / not: 32 heads of
-  // 128, lengths within a factor of 2: 16 x 16384 slots 152 / 185, 32 x 8192 153 / 164, 48 x
-  // 5461 158 / 154, 128 x 2048 198 / 149; 32/8 heads: 16 x 8192 46 / 36, 64 x 4096 72 / 60,
-  // 1 x 32768 20 / 28.
+  // 128, lengths within a factor of 2: 16 x 16384 slots 146 / 175, 32 x 8192 148 / 161, 48 x
+  // 5461 152 / 152, 128 x 2048 179 / 149; 32/8 heads: 16 x 8192 40 / 32, 64 x 4096 63 / 54,
+  // 1 x 32768 20 / 28; 8/2 heads: 1 x 16384 14.6 / 16.6, 8 x 16384 18.6 / 20.8, 8 x 8192 15.5 / 13.1.
   const double fill = (double)(units * C) / resident;
   const double longest = kLongSteps + kFilledSteps * (fill < 1. ? fill : 1.);
   if (pl.col_blocks == 1 && units <= 2 * resident && (double)steps > (double)(C * kQ4Warps) * longest) {
