@@ -612,7 +612,7 @@ struct Math {
 
   // One step of kTiles tiles, at once but for fp32 in several parts: registers.  16 columns of
   // bf16 heads of 128 (4 drafted rows behind 8 x 32768 slots): both at once, 2 CTAs per
-  // SM, 81 us; one by one 82, with 3 CTAs 87.
+  // SM, 84 us; one by one 85, with 3 CTAs and the queries in shared memory 85.
   static constexpr int kAtOnce = NQ == 1 ? kTiles : 1;
   template <bool WHOLE>
   __device__ __forceinline__ void step(const unsigned char* st, uint32_t stride, const At& at, int lane, int t0,
