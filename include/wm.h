@@ -478,8 +478,11 @@ wm_status wm_q4_cache_alloc(const wm_config* cfg, void* dev_buf, size_t bytes, i
  *   span         no range is longer; the launch is sized by it (1: one token per
  *                sequence).  A longer range is cut to it and sets WM_ERR_BOUNDS
  * Other slots of the 4-bit cache keep what they hold.  A bad range is left out, a
- * bad page id (in either table) leaves its slots out; both set WM_ERR_BOUNDS.
- * B = 0 or span = 0 is a no-op.
+ * bad page id (in either table) leaves its slots out; both set WM_ERR_BOUNDS.  Two
+ * sequences of a call must not write the same slot: which one it holds then, part
+ * by part, is open (pages that they share are written for one of them).
+ * B = 0 or span = 0 is a no-op; k * B * Hkv * (min(span, max_pages*page_size) + 30) / 16
+ * above 2^30 returns WM_ERR_UNSUPPORTED.
  */
 wm_status wm_q4_write(const wm_config* cfg, const wm_cache* cache, const int32_t* page_table,
                       const wm_q4_cache* q4, const int32_t* q4_table, const int32_t* first,
@@ -503,7 +506,7 @@ size_t wm_q4_kv_mix_workspace(const wm_config* cfg, int32_t B);
  * the errors and the promise about the weights are wm_kv_mix's;
  *   workspace  device, >= wm_q4_kv_mix_workspace(cfg, B) bytes, 256-byte aligned, no
  *              contents required; calls that share one must not overlap on the GPU
- * One launch more than wm_kv_mix.
+ * One launch more than wm_kv_mix.  k * B * Hkv above 2^30 returns WM_ERR_UNSUPPORTED.
  */
 wm_status wm_q4_kv_mix(const wm_config* cfg, const wm_q4_cache* q4, const wm_mix_weights* w,
                        const void* h, const int32_t* page_table, const int32_t* slot,
