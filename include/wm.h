@@ -545,7 +545,7 @@ size_t wm_q4_rows_attn_workspace(const wm_config* cfg, int32_t B, int32_t Tq, in
  * wm_prefill_attn: the query at position i = pos[b][r] sees slots 0 .. i.  For drafted
  * tokens that are checked at once, and for a prompt's next tokens.  Few rows run as
  * wm_q4_decode_attn; many (bf16, pages of at least 8 slots; by estimated times) on the
- * tensor cores over rows read back into the workspace, which then takes up to 256 MB, or
+ * tensor cores over rows read back into the workspace, which then takes up to 512 MB, or
  * one sequence's bf16 rows of a channel if those are more, and the softmax weights are rounded to
  * bf16 (relative error of the results 0.0023 instead of 0.0017).
  *   q, out     device [B][Tq][Hq][d], 16-byte aligned

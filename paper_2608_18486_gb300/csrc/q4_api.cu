@@ -269,7 +269,10 @@ struct RowsPlan {
 constexpr double kCallUs = 6., kCtaUs = 0.022, kReadUs = 1., kGroupUs = 10., kLeastTileUs = 6.;
 constexpr double stream_us(int d) { return d == 64 ? 0.33 : d == 96 ? 0.27 : 0.23; }  // per MB of codes and 16 columns
 constexpr double tile_step_us(int d) { return d == 64 ? 1.6 : 2.3; }
-constexpr size_t kGroupBytes = 256 << 20;  // rows read back at once, beyond one sequence
+// Rows read back at once, beyond one sequence.  Fewer and larger groups leave less of their
+// last waves empty: 64 sequences of 2048 slots, 64 rows, up to 64 MB 467 us, 128 407, 256 386,
+// 512 321 (39 and 25), all in one 313; 16 of 4096, 256 rows 439, 363, 350, 287.
+constexpr size_t kGroupBytes = 512 << 20;
 
 RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   RowsPlan pl{};
@@ -280,13 +283,19 @@ RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages)
   const size_t one = (size_t)slots * c.Hkv * c.d * 2 * 2;
   int64_t group = kGroupBytes / one;
   if (group > (INT32_MAX - 1) / (slots * c.Hkv)) group = (INT32_MAX - 1) / (slots * c.Hkv);
-  pl.group = (int)(group < 1 ? 1 : group > B ? B : group);
+  group = group < 1 ? 1 : group > B ? B : group;
   const int64_t tiles = (slots + kTileSlots - 1) / kTileSlots;
   const double step = tile_step_us(c.d);
   // whole items: two heads of 128 rows, or one of 256
-  const int64_t items = (int64_t)pl.group * (G % 2 == 0 ? c.Hq / 2 * ((Tq + kTileRows - 1) / kTileRows)
-                                                        : c.Hq * ((Tq + 2 * kTileRows - 1) / (2 * kTileRows)));
-  const double whole = (double)((items + sms - 1) / sms) * tiles * step;
+  const int64_t items = G % 2 == 0 ? (int64_t)c.Hq / 2 * ((Tq + kTileRows - 1) / kTileRows)
+                                   : (int64_t)c.Hq * ((Tq + 2 * kTileRows - 1) / (2 * kTileRows));
+  auto whole = [&](int64_t n) { return (double)((n * items + sms - 1) / sms) * tiles * step; };
+  auto all = [&](int64_t n) {
+    return (double)(B / n) * (kGroupUs + whole(n)) + (B % n ? kGroupUs + whole(B % n) : 0.);
+  };
+  pl.group = (int)group;
+  for (int64_t n = group - 1; group < B && n > group / 2; --n)  // (whichever fills the waves best)
+    if (all(n) < all(pl.group)) pl.group = (int)n;
   // cut ones: the count of parts with the shortest last CTA, a CTA's start as one KV tile
   pl.pair = rows <= kTileRows ? 1 : 0;
   pl.blocks = pl.pair ? 1 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
@@ -301,10 +310,10 @@ RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages)
     }
   }
   const double part = least * step, cut = kLeastTileUs + pl.group * (part > kLeastTileUs ? part : kLeastTileUs);
-  pl.cut = cut < whole;
+  pl.cut = cut < whole(pl.group);
   pl.splits = pl.cut ? splits : 1;
   const double mb = (double)B * slots * c.Hkv * (c.d + c.d / 8) * 1e-6, blocks = (double)((rows + 15) / 16);
-  const double tensor = kReadUs * mb + (double)((B + pl.group - 1) / pl.group) * (kGroupUs + (pl.cut ? cut : whole));
+  const double tensor = kReadUs * mb + (pl.cut ? (double)((B + pl.group - 1) / pl.group) * (kGroupUs + cut) : all(pl.group));
   const double stream = kCallUs + blocks * (mb * stream_us(c.d) + kCtaUs * B * c.Hkv);
   if (stream <= tensor) return pl;
   pl.tiles = true;

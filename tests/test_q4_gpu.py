@@ -415,6 +415,23 @@ def test_many_rows(G, Tq, lens, Hkv, d, page, maxp, order):
     check_many(x, q, pos, to_f64(out))
 
 
+@pytest.mark.parametrize("G,Tq,lens,Hkv,maxp", [
+    (4, 300, [400, 300, 350, 333, 500], 8, 512),  # up to four sequences at once
+    (8, 70, [71, 300, 70], 8, 2048)])             # one after the other
+def test_many_rows_in_groups(G, Tq, lens, Hkv, maxp):
+    x = Q.Q4(lens, Hkv=Hkv, G=G, d=128, page=64, k=1, max_pages=maxp, seed=G)
+    one, ws = maxp * 64 * Hkv * 128 * 4, W.wm_q4_rows_attn_workspace(x.session_cfg(), x.B, Tq, maxp)
+    assert on_tiles(x, Tq) and ws < one * x.B
+    s, q4 = x.session(), x.q4()
+    table, _ = x.q4_dev()
+    pos = np.stack([np.arange(n - Tq, n) for n in lens]).astype(np.int32)
+    q = x.queries(x.B, Tq)
+    out = torch.full((x.B, Tq, x.Hq, 128), float("nan"), dtype=x.tdt, device="cuda")
+    s.q4_rows_attn(0, q.cuda(), torch.from_numpy(pos).cuda(), q4, table, out)
+    assert s.read_status() == 0
+    check_many(x, q, pos, to_f64(out))
+
+
 @pytest.mark.parametrize("G,Tq,B,maxp", [(8, 260, 8, 400), (4, 300, 2, 4096)])
 def test_many_rows_leave_out_what_is_bad(G, Tq, B, maxp):
     x = Q.Q4([Tq] * B, Hkv=4, G=G, d=64, page=16, k=1, max_pages=maxp)
