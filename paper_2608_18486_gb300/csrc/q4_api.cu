@@ -271,7 +271,7 @@ constexpr double stream_us(int d) { return d == 64 ? 0.33 : d == 96 ? 0.27 : 0.2
 constexpr double tile_step_us(int d) { return d == 64 ? 1.6 : 2.3; }
 // Rows read back at once, beyond one sequence.  Fewer and larger groups leave less of their
 // last waves empty: 64 sequences of 2048 slots, 64 rows, up to 64 MB 467 us, 128 407, 256 386,
-// 512 321 (39 and 25), all in one 313; 16 of 4096, 256 rows 439, 363, 350, 287.
+// 512 321 (57 and 7), all in one 313; 16 of 4096, 256 rows 439, 363, 350, 287.
 constexpr size_t kGroupBytes = 512 << 20;
 
 RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
