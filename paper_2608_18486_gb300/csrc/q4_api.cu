@@ -256,6 +256,7 @@ struct RowsPlan {
   int group;                       // sequences read back at once
   bool cut;
   int pair, blocks, splits, records;
+  int joined;                      // cut: sequences whose partial records are held, and joined, at once
   size_t off_v, off_table, off_last, off_lens, off_part, total;
 };
 
@@ -273,6 +274,9 @@ constexpr double tile_step_us(int d) { return d == 64 ? 1.6 : 2.3; }
 // last waves empty: 64 sequences of 2048 slots, 64 rows, up to 64 MB 467 us, 128 407, 256 386,
 // 512 321 (57 and 7), all in one 313; 16 of 4096, 256 rows 439, 363, 350, 287.
 constexpr size_t kGroupBytes = 512 << 20;
+// Partial records held at once: as many sequences' as fit are joined together, and a
+// sequence is cut into no more parts than fit.
+constexpr size_t kRecordBytes = 128 << 20;
 
 RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   RowsPlan pl{};
@@ -300,18 +304,21 @@ RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages)
   pl.pair = rows <= kTileRows ? 1 : 0;
   pl.blocks = pl.pair ? 1 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
   const int64_t units = (int64_t)pl.blocks * c.Hkv;
+  const size_t part = sizeof(float) * (size_t)c.Hkv * rows * (pl.pair ? 2 : 1) * tile_rec(c.d);  // a part's records
   double least = 1e30;
   int splits = 1;
-  for (int n = 1; n <= 32 && n <= tiles; ++n) {
+  for (int n = 1; n <= 32 && n <= tiles && part * n <= kRecordBytes; ++n) {
     const double cost = (double)((units * n + sms - 1) / sms) * ((double)((tiles + n - 1) / n) + 1.) + 0.05 * n;
     if (cost < least) {
       least = cost;
       splits = n;
     }
   }
-  const double part = least * step, cut = kLeastTileUs + pl.group * (part > kLeastTileUs ? part : kLeastTileUs);
+  const double one_cut = least * step, cut = kLeastTileUs + pl.group * (one_cut > kLeastTileUs ? one_cut : kLeastTileUs);
   pl.cut = cut < whole(pl.group);
   pl.splits = pl.cut ? splits : 1;
+  const size_t most = kRecordBytes / (part * pl.splits);
+  pl.joined = !pl.cut ? 0 : most < (size_t)pl.group ? (int)most : pl.group;
   const double mb = (double)B * slots * c.Hkv * (c.d + c.d / 8) * 1e-6, blocks = (double)((rows + 15) / 16);
   const double tensor = kReadUs * mb + (pl.cut ? (double)((B + pl.group - 1) / pl.group) * (kGroupUs + cut) : all(pl.group));
   const double stream = kCallUs + blocks * (mb * stream_us(c.d) + kCtaUs * B * c.Hkv);
@@ -329,7 +336,7 @@ RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages)
   pl.off_table = take(sizeof(int32_t) * (size_t)pl.group * max_pages);
   pl.off_last = take(sizeof(int32_t) * (size_t)pl.group);
   pl.off_lens = take(sizeof(int32_t) * (size_t)pl.group * Tq);
-  pl.off_part = take(pl.cut ? sizeof(float) * (size_t)pl.group * c.Hkv * rows * pl.records * tile_rec(c.d) : 0);
+  pl.off_part = take(part * pl.splits * pl.joined);
   pl.total = off;
   return pl;
 }
@@ -393,10 +400,10 @@ wm_status rows_on_tiles(const RowsPlan& pl, const wm_config& c, const wm_q4_cach
       if (launch_tile_attn(t, in, sm_count(), s) != cudaSuccess) return WM_ERR_CUDA;
       continue;
     }
-    for (int32_t i = 0; i < n; ++i) {
+    for (int32_t i = 0, first = 0; i < n; ++i) {  // first: of the sequences that are joined next
       t.pos = lens + (size_t)i * Tq;
       t.page_table = table + (size_t)i * max_pages;
-      t.part = part + (size_t)i * c.Hkv * Tq * G * pl.records * tile_rec(c.d);
+      t.part = part + (size_t)(i - first) * c.Hkv * Tq * G * pl.records * tile_rec(c.d);
       t.rows = Tq * G;
       t.prefix_slots = max_pages * c.page_size;
       t.pair = pl.pair;
@@ -404,9 +411,11 @@ wm_status rows_on_tiles(const RowsPlan& pl, const wm_config& c, const wm_q4_cach
       t.items = pl.blocks * c.Hkv * pl.splits;
       const TileInputs in{x + i * row_elems, ws, ws + pl.off_v, Tq, 1, c.d};
       if (launch_tile_attn(t, in, sm_count(), s) != cudaSuccess) return WM_ERR_CUDA;
+      if (i + 1 < n && i + 1 - first < pl.joined) continue;
+      const Q4RowsJoin j{part, o + first * row_elems, i + 1 - first, Tq, c.Hq, c.Hkv, G, pl.records};
+      if (launch_q4_rows_join(j, c.d, s) != cudaSuccess) return WM_ERR_CUDA;
+      first = i + 1;
     }
-    const Q4RowsJoin j{part, o, n, Tq, c.Hq, c.Hkv, G, pl.records};
-    if (launch_q4_rows_join(j, c.d, s) != cudaSuccess) return WM_ERR_CUDA;
   }
   return WM_OK;
 }
