@@ -14,6 +14,7 @@ import torch
 from . import _lib as W
 
 _I32, _F32 = torch.int32, torch.float32
+_LARGE = 1 << 25  # bytes of scratch beyond which no more is held than calls ask for
 
 
 def torch_dtype(dtype: str):
@@ -90,6 +91,8 @@ class DecodeSession:
         self._weights = None
         self._weight_refs = None
         self._scratch = {}   # per stream
+        self._large_scratch = {}  # per stream, for calls that need more than _LARGE bytes
+        self._in_graphs = set()   # streams whose large scratch a graph was captured with
         self._outgrown = []  # scratch replaced by larger: graphs captured before may use it
         self._need = {}      # workspace bytes by call and shape
         self._lib = W.lib()
@@ -233,6 +236,8 @@ class DecodeSession:
         # less than twice the largest size asked for.  The first call of a size
         # may allocate: make it before a graph capture.  Graphs captured on one
         # stream share its buffer: their replays must not overlap.
+        if nbytes > _LARGE:
+            return self._large_scratch_for(nbytes, raw, stream)
         buf = self._scratch.get(raw)
         if buf is None or buf.numel() < nbytes:
             if buf is not None:
@@ -242,6 +247,25 @@ class DecodeSession:
             with torch.cuda.stream(s):
                 buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
             self._scratch[raw] = buf
+        return buf.data_ptr()
+
+    def _large_scratch_for(self, nbytes: int, raw: int, stream):
+        # as above, but of the size asked for, and an outgrown buffer is kept (and the
+        # next one made twice its size) only where a graph was captured with it
+        s = torch.cuda.current_stream(self.device) if stream is None else stream
+        with torch.cuda.stream(s):
+            buf = self._large_scratch.get(raw)
+            if buf is None or buf.numel() < nbytes:
+                if raw in self._in_graphs:
+                    self._in_graphs.remove(raw)
+                    self._outgrown.append(buf)
+                    nbytes = max(nbytes, 2 * buf.numel())
+                buf = None
+                self._large_scratch.pop(raw, None)  # (freed on its stream, before the next is allocated)
+                buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+                self._large_scratch[raw] = buf
+            if torch.cuda.is_current_stream_capturing():
+                self._in_graphs.add(raw)
         return buf.data_ptr()
 
     def _bytes(self, key, query, *args) -> int:
