@@ -545,11 +545,11 @@ size_t wm_q4_rows_attn_workspace(const wm_config* cfg, int32_t B, int32_t Tq, in
  * wm_prefill_attn: the query at position i = pos[b][r] sees slots 0 .. i.  For drafted
  * tokens that are checked at once, and for a prompt's next tokens.  Few rows run as
  * wm_q4_decode_attn; many (bf16, pages of at least 8 slots; by estimated times) on the
- * tensor cores over rows read back into the workspace, and the softmax weights are rounded to
- * bf16 (relative error of the results 0.0023 instead of 0.0017).  The workspace then takes
- * up to 512 MB (2^29 bytes) of rows, or one sequence's bf16 rows of a channel (4 * Hkv * d bytes
- * per slot of its page table) if those are more; up to 128 MB of partial results; and 4
- * bytes per page-table entry and position.
+ * tensor cores over rows read back into the workspace, with the same rounding of the
+ * softmax weights.  The workspace then takes up to 512 MB (2^29 bytes) of rows, or one
+ * sequence's bf16 rows of a channel (4 * Hkv * d bytes per slot of its page table) if
+ * those are more; up to 128 MB of partial results; and 4 bytes per page-table entry and
+ * position.
  *   q, out     device [B][Tq][Hq][d], 16-byte aligned
  *   pos        device int32 [B][Tq], 0 <= pos < max_pages*page_size, any order
  *   workspace  device, >= wm_q4_rows_attn_workspace(cfg, B, Tq, max_pages) bytes,

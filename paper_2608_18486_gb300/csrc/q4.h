@@ -40,7 +40,7 @@ inline int64_t q4_page_bytes(int page_size, int d) {  // of one kv head
 enum Q4Rows : int32_t {
   kQ4Paged = 0,   // a cache, through row_table
   kQ4Staged = 1,  // [k][B][Hkv][d]: one row per sequence, of its slot `first`
-  kQ4Dense = 2    // one channel, pages b * max_pages + t / page_size
+  kQ4Dense = 2    // one channel, pages b * max_pages + t / page_size (bf16: V as fp16)
 };
 
 struct Q4CopyParams {
@@ -64,7 +64,8 @@ cudaError_t launch_q4_write(const Q4CopyParams& p, int dtype, int d, int sms, cu
 cudaError_t launch_q4_read(const Q4CopyParams& p, int dtype, int d, int sms, cudaStream_t s);
 
 // Many rows (bf16): a group of sequences is read back into the workspace and runs on
-// the tensor-core kernel of range_attn.h.
+// the tensor-core kernel of range_attn.h.  V as fp16, in which it is exact as well: the
+// weights then enter its product with 11 bits, as in the streaming kernel, and not 8.
 struct Q4RowsPrep {
   const int32_t* pos;         // [B][Tq]
   const int32_t* q4_table;    // [B][max_pages]

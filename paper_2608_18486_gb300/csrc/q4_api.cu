@@ -385,6 +385,7 @@ wm_status rows_on_tiles(const RowsPlan& pl, const wm_config& c, const wm_q4_cach
     t.log2P = ilog2(c.page_size);
     t.qscale = (float)(1.4426950408889634 / sqrt((double)c.d));
     t.splits = pl.splits;
+    t.v_half = 1;
     __nv_bfloat16* const o = (__nv_bfloat16*)out + b0 * row_elems;
     const __nv_bfloat16* const x = (const __nv_bfloat16*)q + b0 * row_elems;
     if (!pl.cut) {

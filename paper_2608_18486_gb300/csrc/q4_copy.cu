@@ -172,6 +172,18 @@ struct Row16 {
     for (int i = 0; i < NV; i += 2) load32(reinterpret_cast<const uint4*>(p) + i, wide, v[i], v[i + 1]);
   }
 };
+// Values as fp16 pairs, in which they are exact as well.
+__device__ __forceinline__ uint32_t half_pair(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+__device__ __forceinline__ void put16_half(void* p, bool wide, const float (&f)[16]) {
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = half_pair(f[2 * i], f[2 * i + 1]);
+  store32(p, wide, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
+}
 __device__ __forceinline__ uint4 bits4(const float* f) {
   return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
 }
@@ -352,7 +364,8 @@ __global__ void __launch_bounds__(kThreads, write_ctas(sizeof(T), HD)) q4_write_
   }
 }
 
-template <typename T, int HD, bool BIG>
+// VHALF: V rows as fp16 instead of bf16.
+template <typename T, int HD, bool BIG, bool VHALF>
 __global__ void __launch_bounds__(kThreads) q4_read_kernel(const Q4CopyParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   using G = Groups<HD, BIG>;
@@ -379,7 +392,9 @@ __global__ void __launch_bounds__(kThreads) q4_read_kernel(const Q4CopyParams p)
         const uint32_t s2 = s[X][i] * 0x00800080u;
         values8(w[X][i].x, s2, f);
         values8(w[X][i].y, s2, f + 8);
-        put16(reinterpret_cast<T*>(X ? p.v_rows : p.k_rows) + at.row(i, lane), p.wide, f);
+        T* const to = reinterpret_cast<T*>(X ? p.v_rows : p.k_rows) + at.row(i, lane);
+        if (VHALF && X == 1) put16_half(to, p.wide, f);
+        else put16(to, p.wide, f);
       }
   };
   for (int it = (int)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); at.next(p, it, p.items, nwarps, lane); it += nwarps) {
@@ -413,34 +428,41 @@ cudaError_t launch(Kern kern, Q4CopyParams p, int sms, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
+// 16 slots of a head lie together (rows staged one per sequence do not).
+bool whole_tiles(const Q4CopyParams& p) { return p.P >= kQ4Step && p.rows_at != kQ4Staged; }
+
+template <typename T, int HD>
+cudaError_t launch_write(const Q4CopyParams& p, int sms, cudaStream_t s) {
+  return whole_tiles(p) ? launch(q4_write_kernel<T, HD, true>, p, sms, s) : launch(q4_write_kernel<T, HD, false>, p, sms, s);
+}
+
+template <typename T, int HD>
+cudaError_t launch_read(const Q4CopyParams& p, int sms, cudaStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (p.rows_at == kQ4Dense)
+      return whole_tiles(p) ? launch(q4_read_kernel<T, HD, true, true>, p, sms, s)
+                            : launch(q4_read_kernel<T, HD, false, true>, p, sms, s);
+  }
+  return whole_tiles(p) ? launch(q4_read_kernel<T, HD, true, false>, p, sms, s)
+                        : launch(q4_read_kernel<T, HD, false, false>, p, sms, s);
+}
+
 }  // namespace
 
-// (rows staged one per sequence do not lie together)
-#define WM_Q4_COPY(KERNEL, T, HD)                                                        \
-  return p.P >= kQ4Step && p.rows_at != kQ4Staged ? launch(KERNEL<T, HD, true>, p, sms, s) \
-                                                  : launch(KERNEL<T, HD, false>, p, sms, s)
-
 cudaError_t launch_q4_write(const Q4CopyParams& p, int dtype, int d, int sms, cudaStream_t s) {
-  if (dtype == WM_DT_F32) {
-    if (d == 64) WM_Q4_COPY(q4_write_kernel, float, 64);
-    if (d == 96) WM_Q4_COPY(q4_write_kernel, float, 96);
-    WM_Q4_COPY(q4_write_kernel, float, 128);
-  }
-  if (d == 64) WM_Q4_COPY(q4_write_kernel, __nv_bfloat16, 64);
-  if (d == 96) WM_Q4_COPY(q4_write_kernel, __nv_bfloat16, 96);
-  WM_Q4_COPY(q4_write_kernel, __nv_bfloat16, 128);
+  if (dtype == WM_DT_F32)
+    return d == 64 ? launch_write<float, 64>(p, sms, s) : d == 96 ? launch_write<float, 96>(p, sms, s)
+                                                                  : launch_write<float, 128>(p, sms, s);
+  return d == 64 ? launch_write<__nv_bfloat16, 64>(p, sms, s) : d == 96 ? launch_write<__nv_bfloat16, 96>(p, sms, s)
+                                                                        : launch_write<__nv_bfloat16, 128>(p, sms, s);
 }
 
 cudaError_t launch_q4_read(const Q4CopyParams& p, int dtype, int d, int sms, cudaStream_t s) {
-  if (dtype == WM_DT_F32) {
-    if (d == 64) WM_Q4_COPY(q4_read_kernel, float, 64);
-    if (d == 96) WM_Q4_COPY(q4_read_kernel, float, 96);
-    WM_Q4_COPY(q4_read_kernel, float, 128);
-  }
-  if (d == 64) WM_Q4_COPY(q4_read_kernel, __nv_bfloat16, 64);
-  if (d == 96) WM_Q4_COPY(q4_read_kernel, __nv_bfloat16, 96);
-  WM_Q4_COPY(q4_read_kernel, __nv_bfloat16, 128);
+  if (dtype == WM_DT_F32)
+    return d == 64 ? launch_read<float, 64>(p, sms, s) : d == 96 ? launch_read<float, 96>(p, sms, s)
+                                                                 : launch_read<float, 128>(p, sms, s);
+  return d == 64 ? launch_read<__nv_bfloat16, 64>(p, sms, s) : d == 96 ? launch_read<__nv_bfloat16, 96>(p, sms, s)
+                                                                       : launch_read<__nv_bfloat16, 128>(p, sms, s);
 }
-#undef WM_Q4_COPY
 
 }  // namespace wm

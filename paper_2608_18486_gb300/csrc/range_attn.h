@@ -99,6 +99,7 @@ struct TileParams {
   int32_t blocks;             // window: row blocks per head
   int32_t items;
   int32_t wide_out;           // out is 32-byte aligned
+  int32_t v_half;             // the V pool holds fp16, and the weights enter P V as fp16
   float qscale;               // log2(e) / sqrt(d)
 };
 struct TileInputs {

@@ -162,14 +162,16 @@ __device__ __forceinline__ uint64_t sdesc_mnmajor_sw128(uint32_t smem_addr, uint
 // Instruction-descriptor bit: the B operand is MN-major (N contiguous).
 constexpr uint32_t kIdescBMajorMN = 1u << 16;
 
-// Instruction descriptor of kind::f16: fp32 accumulator, bf16 A and B, both
+// Instruction descriptor of kind::f16: fp32 accumulator, fp16 A and B, both
 // K-major, M x N tile.
-__host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N) {
-  return (1u << 4)                       // D format: fp32
-         | (1u << 7)                     // A format: bf16
-         | (1u << 10)                    // B format: bf16
+__host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N) {
+  return (1u << 4)                       // D format: fp32 (A and B format: 0, fp16)
          | ((uint32_t)(N >> 3) << 17)    // N / 8
          | ((uint32_t)(M >> 4) << 24);   // M / 16
+}
+// The same with bf16 A and B.
+__host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N) {
+  return idesc_f16_f32(M, N) | (1u << 7) | (1u << 10);
 }
 
 }  // namespace tc

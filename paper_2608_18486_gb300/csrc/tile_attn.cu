@@ -70,6 +70,13 @@ constexpr int kTThreads = (kSoftWarps + 4) * 32;
 constexpr uint32_t kBlock = 128u * 128u;  // bytes of a 64-column block of a 128-row tile
 constexpr uint32_t kTmemCols = 512;       // S_i at 128 i (P_i at its columns 0-31 and 64-95), O_i at 256 + 128 i
 constexpr float kStaleMax = 8.f;          // log2 headroom before O is rescaled
+// V and weights in fp16 (11 bits, of weights down to 2^-22 of the largest; bf16 has 8): the
+// reference lies 2^8 below the maximum and moves when a score passes it by 2^15.  256 rows behind
+// 16 x 4096 slots, 32/8 heads of 128: 293 us, with bf16 286; the distance rounded twice
+// wherever it is needed, behind a vote, 299.
+constexpr float kHalfHead = 8.f, kHalfRoom = 7.f;
+constexpr float kHalfExact = 4194304.f;  // 2^22: a score's distance to a reference is off by 2^-2 at most
+constexpr float kHalfHuge = 268435456.f;  // 2^28: by 2^3 up to here
 
 template <int HD>
 struct TShape {
@@ -85,6 +92,25 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+
+// A row's reference, where its weights are fp16: they have to stay below 2^16, although y = s *
+// scale - ref is rounded once and its maximum was rounded before.
+struct HalfRef {
+  float scale;  // of the row's scores
+  float ref, head;
+  // max: the largest score, not scaled; qscale: its scale
+  __device__ __forceinline__ void set(float max, float qscale) {
+    const float x = max * qscale;
+    scale = qscale;
+    head = fabsf(x) > kHalfExact ? 0.f : kHalfHead;
+    if (fabsf(x) >= kHalfHuge) {
+      // Unequal scores lie 16 and more apart here, so that a larger scale changes no weight by more
+      // than 2^-16; under a power of two (the next one) the distances are exact.
+      scale = __uint_as_float((__float_as_uint(qscale) + 0x7FFFFFu) & 0x7F800000u);
+    }
+    ref = max * scale - head;
+  }
+};
 
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
 __device__ __forceinline__ bool elect_one() {
@@ -332,7 +358,7 @@ __device__ __forceinline__ bool unseen(const TileParams& p, const Item& I, const
   return true;
 }
 
-template <int HD, bool WIN>
+template <int HD, bool WIN, bool HALF>
 __global__ void __launch_bounds__(kTThreads, 1)
     tile_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                      const __grid_constant__ CUtensorMap tmV, const TileParams p) {
@@ -559,7 +585,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
     if (!ok && lane == 0) report(p.status, WM_ERR_TIMEOUT);
   } else if (warp == kMmaWarp) {
     // ================================================================ MMA
-    const uint32_t idesc_o = tc::idesc_bf16_f32(kTM, HD) | tc::kIdescBMajorMN;
+    const uint32_t idesc_o = (HALF ? tc::idesc_f16_f32(kTM, HD) : tc::idesc_bf16_f32(kTM, HD)) | tc::kIdescBMajorMN;
     const int la = !WIN && p.pair ? 2 : 1;  // steps that S runs ahead of P V
     const uint32_t lead = elect_one();
     // descriptors of the first tiles (a tile further on: plus its bytes / 16)
@@ -711,6 +737,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
       const int steps = I.steps;
       float m = -INFINITY, l = 0.f;  // max used for P (log2 units) and running sum
       int x = 0;                     // steps of this tile in the item
+      HalfRef hr{p.qscale, 0.f, kHalfHead};
       for (int j = 0; j < steps && ok; ++j) {
         const int kt = tile_at<WIN>(I, j), s0 = kt * kTN;
         if (!WIN && p.pair ? (j & 1) != i : !mine.has(kt)) continue;
@@ -773,12 +800,15 @@ __global__ void __launch_bounds__(kTThreads, 1)
         float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), mo = 0.f;
         ok = exchange(mt, mo);
         if (!ok) break;
-        mt = fmaxf(mt, mo) * p.qscale;  // qscale > 0: the max commutes with the scale
+        const float top = fmaxf(mt, mo);
+        mt = top * (HALF ? hr.scale : p.qscale);  // qscale > 0: the max commutes with the scale
         float scale = 1.f;
-        const bool raise = (m == -INFINITY) ? (mt != -INFINITY) : (mt > m + kStaleMax);
+        const bool raise = (m == -INFINITY) ? (mt != -INFINITY) : (mt > m + (HALF ? hr.head + kHalfRoom : kStaleMax));
         if (raise) {
-          scale = (m == -INFINITY) ? 0.f : ex2(m - mt);
-          m = mt;
+          if (HALF) hr.set(top, p.qscale);
+          const float to = HALF ? hr.ref : mt;
+          scale = (m == -INFINITY) ? 0.f : ex2(m - to);
+          m = to;
         }
         if (__any_sync(FULL, raise && x > 0)) {
           // a row's max grew past the headroom: rescale O (every lane of the
@@ -805,10 +835,11 @@ __global__ void __launch_bounds__(kTThreads, 1)
         __syncwarp();
         if (half == 1 && lane == 0) mbar_arrive(&pfull[i]);
         // p = 2^(s * qscale - m) in pairs; masked slots give 0, and so do rows
-        // that have seen nothing yet.  P enters the product as bf16 (the tensor
-        // cores' operand); the row sum is kept in fp32 from the unrounded values.
+        // that have seen nothing yet.  P enters the product in V's type (bf16, or fp16
+        // with 3 bits more); the row sum is kept in fp32 from the unrounded values.
         const float nm = m == -INFINITY ? 0.f : -m;
-        const float2 qs2 = make_float2(p.qscale, p.qscale), nm2 = make_float2(nm, nm);
+        const float qs = HALF ? hr.scale : p.qscale;
+        const float2 qs2 = make_float2(qs, qs), nm2 = make_float2(nm, nm);
         float2 sum2 = make_float2(0.f, 0.f);
         float2 sum2b = make_float2(0.f, 0.f);
         if (mine_too) {
@@ -831,8 +862,12 @@ __global__ void __launch_bounds__(kTThreads, 1)
               const float2 pr = make_float2(ex2(y.x), ex2(y.y));
               if (e & 2) sum2b = __fadd2_rn(sum2b, pr);
               else sum2 = __fadd2_rn(sum2, pr);
-              const __nv_bfloat162 h = __floats2bfloat162_rn(pr.x, pr.y);
-              pk[e / 2] = *reinterpret_cast<const uint32_t*>(&h);
+              if constexpr (HALF) {
+                asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(pk[e / 2]) : "f"(pr.y), "f"(pr.x));
+              } else {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(pr.x, pr.y);
+                pk[e / 2] = *reinterpret_cast<const uint32_t*>(&h);
+              }
             }
             // P over this thread's own S columns that have been read
             tc::tmem_st16(lane_base + scol + 16 * c, pk);
@@ -915,11 +950,11 @@ __global__ void __launch_bounds__(kTThreads, 1)
   }
 }
 
-template <int HD, bool WIN>
+template <int HD, bool WIN, bool HALF>
 cudaError_t launch_t(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const TileParams& p, int sms,
                      cudaStream_t s) {
   static size_t smem_set[kSmemOptDevices] = {};
-  auto kern = tile_attn_kernel<HD, WIN>;
+  auto kern = tile_attn_kernel<HD, WIN, HALF>;
   constexpr size_t smem = TShape<HD>::TILES + sizeof(Shared<TShape<HD>::NSK, TShape<HD>::NSV>);
   if (cudaError_t e = opt_in_smem(kern, smem, smem_set); e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -933,6 +968,14 @@ cudaError_t launch_t(const CUtensorMap& q, const CUtensorMap& k, const CUtensorM
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, q, k, v, p);
+}
+
+template <int HD>
+cudaError_t launch_d(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const TileParams& p, int sms,
+                     cudaStream_t s) {
+  if (p.part == nullptr)
+    return p.v_half ? launch_t<HD, true, true>(q, k, v, p, sms, s) : launch_t<HD, true, false>(q, k, v, p, sms, s);
+  return p.v_half ? launch_t<HD, false, true>(q, k, v, p, sms, s) : launch_t<HD, false, false>(q, k, v, p, sms, s);
 }
 
 }  // namespace
@@ -951,9 +994,9 @@ cudaError_t launch_tile_attn(TileParams p, const TileInputs& in, int sms, cudaSt
       !tma_map_bf16_2d(&tv, in.v_pool, pool_rows, in.d, in.d, box_rows))
     return cudaErrorInvalidValue;
   switch (in.d) {
-    case 64: return win ? launch_t<64, true>(tq, tk, tv, p, sms, s) : launch_t<64, false>(tq, tk, tv, p, sms, s);
-    case 96: return win ? launch_t<96, true>(tq, tk, tv, p, sms, s) : launch_t<96, false>(tq, tk, tv, p, sms, s);
-    case 128: return win ? launch_t<128, true>(tq, tk, tv, p, sms, s) : launch_t<128, false>(tq, tk, tv, p, sms, s);
+    case 64: return launch_d<64>(tq, tk, tv, p, sms, s);
+    case 96: return launch_d<96>(tq, tk, tv, p, sms, s);
+    case 128: return launch_d<128>(tq, tk, tv, p, sms, s);
     default: return cudaErrorInvalidValue;
   }
 }

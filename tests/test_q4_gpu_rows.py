@@ -7,7 +7,6 @@ import torch
 from paper_2608_18486_gb300 import _lib as W
 from tests import _q4 as Q
 from tests._longctx import to_f64
-from tests.test_q4_gpu import check_many
 
 pytestmark = pytest.mark.gpu
 
@@ -87,4 +86,137 @@ def test_cut_rows_of_more_sequences_than_their_records_fit():
     assert g == x.B and 0 < records <= RECORDS and round(records / part) % x.B != 0
     pos = np.stack([np.arange(n - 300, n) for n in x.lens]).astype(np.int32)
     q, got = run(x, pos)
-    check_many(x, q, pos, got)
+    check_rows(x, q, pos, got)
+
+
+# (group size, positions, lengths, kv heads, head size, page, pages of a row of the table, whether cut)
+FORMS = [(2, 128, [256] * 38, 8, 64, 16, 16, False), (1, 128, [256] * 38, 8, 64, 16, 16, False),
+         (1, 257, [600] * 10, 8, 64, 8, 75, False), (4, 130, [200, 190, 130, 140] * 3, 6, 96, 32, 7, False),
+         (8, 40, [60] * 40, 2, 128, 64, 3, False),
+         (4, 300, [400], 2, 128, 16, 1024, True), (8, 16, [70, 90], 8, 64, 32, 4096, True), (2, 200, [211, 200], 3, 96, 64, 1024, True)]
+
+
+def case(G, Tq, lens, Hkv, d, page, maxp, cut, seed=3):
+    x = Q.Q4(lens, Hkv=Hkv, G=G, d=d, page=page, k=1, max_pages=maxp, seed=seed)
+    at = form(x.session_cfg(), x.B, Tq, maxp)
+    assert at is not None and (at[1] > 0) == cut
+    return x
+
+
+def check_rows(x, q, pos, got, visible=None):
+    """Every element within what the arithmetic may move it: scores as in tests/_q4.py, weights rounded to 11
+    bits (2^-11; below 2^-22 of the largest to a multiple of 2^-32 of it), sums of steps cut by 17 *
+    2^-23, the result rounded by 2^-8 of itself."""
+    T = int(pos.max()) + 1
+    for b in range(x.B):
+        n = max(int(pos[b].max()) + 1, 1)
+        ts = np.arange(n)
+        see = ts[None] <= pos[b][:, None]
+        if visible is not None:
+            see &= visible[b][:n]
+        for h in range(x.Hkv):
+            K, V = (np.where(see.any(0)[:, None], x.rows(p, 0, b, h, ts), 0) for p in (x.kd, x.vd))
+            for g in range(x.G):
+                y = to_f64(q[b, :, h * x.G + g])
+                s = np.where(see, y @ K.T / np.sqrt(x.d), -np.inf)
+                p = np.where(see, np.exp(s - np.maximum(s.max(1, keepdims=True), -1e300)), 0)
+                p /= np.maximum(p.sum(1, keepdims=True), 1e-300)
+                want = p @ V
+                ds = (110 + x.d) * 2.0 ** -24 * (np.abs(y) @ np.abs(K).T).max(1, keepdims=True) / np.sqrt(x.d)
+                rel = 2 * ds + 2.0 ** -11 + T / 16 * 17 * 2.0 ** -23 + 64 * 2.0 ** -24
+                tol = rel * (p @ np.abs(V)) + n * 2.0 ** -32 * np.abs(V).max() + 2.0 ** -8 * np.abs(want)
+                over = (np.abs(got[b, :, h * x.G + g] - want) - tol).max()
+                assert over <= 0, (b, h, g, over)
+
+
+@pytest.mark.parametrize("order", ["last", "any", "few"])
+@pytest.mark.parametrize("f", FORMS)
+def test_both_forms_element_by_element(f, order):
+    """few: rows that see so few slots that a weight's own rounding shows."""
+    x, Tq = case(*f), f[1]
+    rng = np.random.default_rng(2)
+    pos = np.stack([np.arange(n - Tq, n) if order == "last" else rng.integers(0, n if order == "any" else 6, Tq)
+                    for n in x.lens]).astype(np.int32)
+    q, got = run(x, pos)
+    check_rows(x, q, pos, got)
+
+
+@pytest.mark.parametrize("f", FORMS)
+def test_both_forms_leave_out_what_is_bad(f):
+    """Pages and positions out of range, positions in no order, sequences of which no row sees a slot."""
+    x, Tq = case(*f), f[1]
+    rng = np.random.default_rng(4)
+    s, q4 = x.session(), x.q4()
+    table, _ = x.q4_dev()
+    pos = np.stack([rng.integers(0, n, Tq) for n in x.lens]).astype(np.int32)
+    visible = np.ones((x.B, x.T), dtype=bool)
+    for b in range(0, x.B, 2):
+        page = int(rng.integers(0, -(-int(x.lens[b]) // x.P)))
+        table[b, page] = (-1, x.q4_pages, -2 ** 31, 2 ** 31 - 1)[b // 2 % 4]
+        visible[b, page * x.P:(page + 1) * x.P] = False
+    for b in range(x.B):
+        pos[b, rng.integers(0, Tq, 3)] = (-1, x.T, -2 ** 31)
+    if x.B > 2:
+        pos[2] = -5
+    q = x.queries(x.B, Tq)
+    out = torch.full((x.B, Tq, x.Hq, x.d), float("nan"), dtype=x.tdt, device="cuda")
+    s.q4_rows_attn(0, q.cuda(), torch.from_numpy(pos).cuda(), q4, table, out)
+    assert s.read_status() == W.WM_ERR_BOUNDS
+    got = to_f64(out)
+    bad = (pos < 0) | (pos >= x.T)
+    assert (got[bad] == 0).all()
+    check_rows(x, q, np.where(bad, -1, pos), got, visible)
+
+
+def test_whole_ranges_in_several_groups():
+    rng = np.random.default_rng(6)
+    x = Q.Q4(rng.integers(128, 200, 70).tolist(), Hkv=8, G=2, d=64, page=16, k=1, max_pages=256, seed=5)
+    g, records = form(x.session_cfg(), x.B, 128, x.max_pages)
+    assert g < x.B and records == 0
+    pos = np.stack([np.arange(n - 128, n) for n in x.lens]).astype(np.int32)
+    q, got = run(x, pos)
+    check_rows(x, q, pos, got)
+
+
+@pytest.mark.parametrize("f", [FORMS[0], FORMS[5], FORMS[6]])
+def test_scores_of_any_size_in_both_forms(f):
+    """Scores so large that a reference is rounded: the largest one takes all, whichever step it comes in."""
+    x, Tq = case(*f), f[1]
+    s, q4 = x.session(), x.q4()
+    table, _ = x.q4_dev()
+    pos = np.stack([np.arange(n - Tq, n) for n in x.lens]).astype(np.int32)
+    q = x.queries(x.B, Tq)
+    best = np.full((x.B, Tq, x.Hq, x.d), np.nan)
+    for b in range(x.B):
+        for hq in range(x.Hq):
+            K, V = (x.rows(p, 0, b, hq // x.G, np.arange(x.lens[b])) for p in (x.kd, x.vd))
+            z = to_f64(q[b, :, hq]) @ K.T
+            z[np.arange(len(K))[None] > pos[b][:, None]] = -np.inf
+            top = np.sort(z, 1)
+            clear = top[:, -1] - top[:, -2] > 0.05  # (2^18 of it are 1000 and more: nothing is left of the others)
+            best[b, clear, hq] = V[z.argmax(1)][clear]
+    clear = ~np.isnan(best)
+    assert clear.mean() > 0.5
+    for e in range(18, 42):
+        out = torch.full(q.shape, float("nan"), dtype=x.tdt, device="cuda")
+        s.q4_rows_attn(0, (q * 2.0 ** e).cuda(), torch.from_numpy(pos).cuda(), q4, table, out)
+        got = to_f64(out)
+        # (its weight in fp16 against the sum of the unrounded one, and the result in bf16)
+        assert (np.abs(got - best)[clear] <= (2.0 ** -11 + 2.0 ** -8 + 2.0 ** -16) * np.abs(best)[clear]).all(), e
+        assert np.isfinite(got).all(), e
+    assert s.read_status() == 0
+
+
+@pytest.mark.parametrize("f", [FORMS[0], FORMS[5], FORMS[6]])
+def test_rows_of_nan_queries_are_nan_in_both_forms(f):
+    x, Tq = case(*f), f[1]
+    pos = np.stack([np.arange(n - Tq, n) for n in x.lens]).astype(np.int32)
+    s, q4 = x.session(), x.q4()
+    table, _ = x.q4_dev()
+    q = x.queries(x.B, Tq)
+    q[0, 3, 1, 5], q[-1, Tq - 1, 0, 7] = float("nan"), float("inf")
+    out = torch.zeros(q.shape, dtype=x.tdt, device="cuda")
+    s.q4_rows_attn(0, q.cuda(), torch.from_numpy(pos).cuda(), q4, table, out)
+    assert s.read_status() == 0
+    nan = np.isnan(to_f64(out))
+    assert nan[0, 3, 1].all() and nan[-1, Tq - 1, 0].all() and nan.sum() == 2 * x.d
