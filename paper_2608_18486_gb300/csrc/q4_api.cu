@@ -263,13 +263,18 @@ struct RowsPlan {
 // Estimates in us that choose between the two forms, and whether the KV tiles are cut.
 // Streaming: 16 columns take as long as the codes' stream, and every CTA has a start
 // and an end.  Tensor cores: reading back (codes in, rows out, rows in again), one step
-// of 2 x 128 rows over a KV tile, the launches.  Measured (streaming / tensor cores; heads
-// of 128, 32 query and 8 kv heads): 1 sequence of 8192 slots, 32 rows 28 / 39, 64 rows 47 /
-// 39, 256 rows 157 / 52; 8 of 32768, 16 rows 296 / 632, 32 rows 587 / 653, 64 rows 1069 /
-// 623; 32 of 1024, 16 rows 70 / 118, 32 rows 124 / 96.
-constexpr double kCallUs = 6., kCtaUs = 0.022, kReadUs = 1., kGroupUs = 10., kLeastTileUs = 6.;
+// of 2 x 128 rows over a KV tile, the launches, the partial records' way to their join.
+// Measured (streaming / tensor cores; heads of 128, 32 query and 8 kv heads): 1 sequence of 8192
+// slots, 32 rows 28 / 33, 64 rows 47 / 35, 256 rows 157 / 50; 8 of 32768, 16 rows 296 / 532, 32
+// rows 587 / 553, 64 rows 1059 / 557; 32 of 1024, 16 rows 63 / 123, 32 rows 116 / 97.  Whole
+// KV ranges / cut ones: 16 of 4096, 256 rows 293 / 520; 32 of 8192, 300 rows, 32/4 heads 1480 /
+// 1720; 1 of 131072, 64 rows 1790 / 225.  The
+// constants fit 100 sizes; of 60 others, drawn, 5 take a form that is more than 5% behind
+// the best one (6 of 543 slots, 35 rows, 64/16 heads of 64: 35 and 26).
+constexpr double kCallUs = 6., kCtaUs = 0.022, kReadUs = 0.9, kGroupUs = 10., kCutUs = 6., kLeastTileUs = 15.;
+constexpr double kRecordUs = 0.1;  // per MB
 constexpr double stream_us(int d) { return d == 64 ? 0.33 : d == 96 ? 0.27 : 0.23; }  // per MB of codes and 16 columns
-constexpr double tile_step_us(int d) { return d == 64 ? 1.6 : 2.3; }
+constexpr double tile_step_us(int d) { return d == 64 ? 1.4 : 1.9; }
 // Rows read back at once, beyond one sequence.  Fewer and larger groups leave less of their
 // last waves empty: 64 sequences of 2048 slots, 64 rows, up to 64 MB 467 us, 128 407, 256 386,
 // 512 321 (57 and 7), all in one 313; 16 of 4096, 256 rows 439, 363, 350, 287.
@@ -290,17 +295,17 @@ RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages)
   group = group < 1 ? 1 : group > B ? B : group;
   const int64_t tiles = (slots + kTileSlots - 1) / kTileSlots;
   const double step = tile_step_us(c.d);
-  // whole items: two heads of 128 rows, or one of 256
+  // whole items: two heads of 128 rows, or one of 256; an item's start as one KV tile
   const int64_t items = G % 2 == 0 ? (int64_t)c.Hq / 2 * ((Tq + kTileRows - 1) / kTileRows)
                                    : (int64_t)c.Hq * ((Tq + 2 * kTileRows - 1) / (2 * kTileRows));
-  auto whole = [&](int64_t n) { return (double)((n * items + sms - 1) / sms) * tiles * step; };
+  auto whole = [&](int64_t n) { return (double)((n * items + sms - 1) / sms) * (double)(tiles + 1) * step; };
   auto all = [&](int64_t n) {
     return (double)(B / n) * (kGroupUs + whole(n)) + (B % n ? kGroupUs + whole(B % n) : 0.);
   };
   pl.group = (int)group;
   for (int64_t n = group - 1; group < B && n > group / 2; --n)  // (whichever fills the waves best)
     if (all(n) < all(pl.group)) pl.group = (int)n;
-  // cut ones: the count of parts with the shortest last CTA, a CTA's start as one KV tile
+  // cut ones: the count of parts with the shortest last CTA, its start again as one KV tile
   pl.pair = rows <= kTileRows ? 1 : 0;
   pl.blocks = pl.pair ? 1 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
   const int64_t units = (int64_t)pl.blocks * c.Hkv;
@@ -308,13 +313,14 @@ RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages)
   double least = 1e30;
   int splits = 1;
   for (int n = 1; n <= 32 && n <= tiles && part * n <= kRecordBytes; ++n) {
-    const double cost = (double)((units * n + sms - 1) / sms) * ((double)((tiles + n - 1) / n) + 1.) + 0.05 * n;
+    const double us = step * ((double)((units * n + sms - 1) / sms) * ((double)((tiles + n - 1) / n) + 1.) + 0.05 * n);
+    const double cost = (us > kLeastTileUs ? us : kLeastTileUs) + kRecordUs * 1e-6 * (double)(part * n);
     if (cost < least) {
       least = cost;
       splits = n;
     }
   }
-  const double one_cut = least * step, cut = kLeastTileUs + pl.group * (one_cut > kLeastTileUs ? one_cut : kLeastTileUs);
+  const double cut = kCutUs + pl.group * least;
   pl.cut = cut < whole(pl.group);
   pl.splits = pl.cut ? splits : 1;
   const size_t most = kRecordBytes / (part * pl.splits);

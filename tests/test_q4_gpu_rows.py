@@ -220,3 +220,15 @@ def test_rows_of_nan_queries_are_nan_in_both_forms(f):
     assert s.read_status() == 0
     nan = np.isnan(to_f64(out))
     assert nan[0, 3, 1].all() and nan[-1, Tq - 1, 0].all() and nan.sum() == 2 * x.d
+
+
+@pytest.mark.parametrize("B,Tq,slots,Hq,Hkv,d,want", [
+    (1, 32, 8192, 32, 8, 128, "stream"), (1, 64, 8192, 32, 8, 128, "cut"), (1, 256, 8192, 32, 8, 128, "cut"),
+    (8, 16, 32768, 32, 8, 128, "stream"), (8, 64, 32768, 32, 8, 128, "cut"), (32, 16, 1024, 32, 8, 128, "stream"),
+    (32, 32, 1024, 32, 8, 128, "whole"), (16, 256, 4096, 32, 8, 128, "whole"), (32, 300, 8192, 32, 4, 128, "whole"),
+    (1, 64, 131072, 32, 8, 128, "cut"), (4, 200, 8192, 6, 3, 96, "stream")])
+def test_calls_take_the_form_that_measured_fastest(B, Tq, slots, Hq, Hkv, d, want):
+    """By 10% and more (us: streamed, whole, cut): 28 118 33; 47 119 35; 157 122 50; 296 1407 531; 1059 1064 557;
+    63 118 320; 116 97 381; 1141 293 515; 4841 1478 1717; 582 1779 225; 68 159 85."""
+    at = form(config(Hq, Hkv, d, 16), B, Tq, slots // 16)
+    assert ("stream" if at is None else "cut" if at[1] else "whole") == want
