@@ -34,7 +34,8 @@ class Q4Cache:
         self.device = torch.device(device)
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
-        nbytes = W.wm_q4_cache_bytes(cfg, num_pages)
+        # (the binding would keep the low 32 bits)
+        nbytes = W.wm_q4_cache_bytes(cfg, num_pages) if 0 < self.num_pages < 1 << 31 else 0
         if nbytes == 0:
             raise W.WMError(W.WM_ERR_INVALID_ARG, "wm_q4_cache_bytes")
         if cache_buf is None:
@@ -440,6 +441,8 @@ class DecodeSession:
         """Decode attention of layer ``layer`` over a 4-bit cache (its pages:
         page_table)."""
         B = self.B if B is None else B
+        if layer >> 31:
+            layer = -1  # (the binding would keep the low 32 bits)
         q4r = self._q4_ref(q4)
         self._check_rows(q, seq_lens, page_table, out, B, B)
         need = self._bytes(("q4", B, self.max_pages), W.wm_q4_decode_attn_workspace, B, self.max_pages)
@@ -454,6 +457,8 @@ class DecodeSession:
         """Causal attention of query rows q [B][Tq][Hq][d] at positions pos
         [B][Tq] over a 4-bit cache: position i sees slots 0 .. i."""
         B, Tq = q.shape[:2]
+        if layer >> 31:
+            layer = -1
         q4r = self._q4_ref(q4)
         self._check_rows(q, pos, page_table, out, B, B * Tq)
         need = self._bytes(("q4 rows", B, Tq, self.max_pages), W.wm_q4_rows_attn_workspace, B, Tq, self.max_pages)
