@@ -103,7 +103,6 @@ struct Q4AttnParams {
   int32_t* status;
   float* part;                // not NULL: all steps are spread over `pieces` CTAs, records
                               // [pieces][2][q4_rec] of shared units are joined by a second kernel
-  int64_t page_bytes;         // of one kv head
   int32_t len_add;
   int32_t B, Tq, Hq, Hkv, G, P, log2P, tile, log2tile, tile_bytes, num_pages, max_pages;
   int32_t col_blocks;         // units per (sequence, kv head): groups of 8 NB (row, head) columns

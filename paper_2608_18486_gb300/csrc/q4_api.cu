@@ -226,7 +226,6 @@ wm_status attn(const wm_config& c, const wm_q4_cache& q4, int32_t layer, const v
   p.lens = lens;
   p.status = dev_status;
   p.part = pl.spread ? (float*)workspace : nullptr;
-  p.page_bytes = q4_page_bytes(c.page_size, c.d);
   p.len_add = len_add;
   p.B = B;
   p.Tq = Tq;
