@@ -815,7 +815,8 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB, F
   const int32_t* ptab = p.page_table + (int64_t)b * p.max_pages;
   const uint32_t ring_s = smem_u32(ring), to_s = ring_s + lane * 16;
   const uint8_t* pool_lane = p.pool + lane * 16;
-  const int log2tile = LT > 0 ? LT : p.log2tile, tiles = kSlots >> log2tile, per_batch = 1 << log2tile;
+  const int log2tile = LT > 0 ? LT : p.log2tile, tiles = kSlots >> log2tile;
+  const int per_batch = 1 << log2tile;  // steps whose tiles the lanes hold, one each
   const uint32_t tile_bytes = LT > 0 ? SH::template tile<LT>() : p.tile_bytes;
   const uint32_t stride = LT > 0 ? SH::BYTES16 : kQ4Step / p.tile * tile_bytes;
   // Tiles of `per_batch` steps from step i on, one per lane: its place in the pool (kGone:
@@ -909,7 +910,7 @@ __global__ void __launch_bounds__(kThreads, q4_ctas_per_sm(sizeof(T) == 2, NB, F
     } else {
       uint32_t live = 0;
       for (int x = 0; x < tiles; ++x)
-        if ((there[0] >> x) & 1u) live |= ((1u << per_batch) - 1) << (x << log2tile);
+        if ((there[0] >> x) & 1u) live |= ((1u << (1 << log2tile)) - 1) << (x << log2tile);  // a tile's slots
       if (S - t0 < kSlots) live &= (1u << (S - t0)) - 1;
       mm.template step<false>(st, stride, at, lane, t0, live);
     }
