@@ -320,11 +320,15 @@ struct Groups {
   }
 };
 
-// CTAs per SM by registers: a lane holds a head's rows, K and V (fp32: one of them).
-constexpr int write_ctas(int elem, int hd) { return hd == 64 ? 6 : elem == 4 ? 4 : hd == 96 ? 4 : 3; }
+// CTAs per SM by registers: a lane holds a head's rows, K and V (fp32: one of them).  us of 8
+// prompts of 511 to 2047 slots, pages of 16 / 8: fp32, 4 channels of 16 heads of 128, 3 CTAs
+// 170 / 188, 4 with 106 / 298 bytes of spills 172 / 202; bf16, 12 channels of 12 heads of 64, 6 CTAs
+// with 16 / 98 bytes of spills 78 / 90, 5 without them 81 / 87; 4 channels of 32 heads of 128,
+// 3 CTAs 154 / 171 (68 bytes in pages of 8), 2 154 / 211.
+constexpr int write_ctas(int hd) { return hd == 64 ? 6 : hd == 96 ? 4 : 3; }
 
 template <typename T, int HD, bool BIG>
-__global__ void __launch_bounds__(kThreads, write_ctas(sizeof(T), HD)) q4_write_kernel(const Q4CopyParams p) {
+__global__ void __launch_bounds__(kThreads, write_ctas(HD)) q4_write_kernel(const Q4CopyParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   // (Dependents start when this grid ends: attention that starts beside it would crowd on
   // the SMs that have most room, 304 units of 2048 slots behind a write 40 us instead of 29.)
