@@ -269,9 +269,12 @@ struct RowsPlan {
 // KV ranges / cut ones: 16 of 4096, 256 rows 293 / 520; 32 of 8192, 300 rows, 32/4 heads 1480 /
 // 1720; 1 of 131072, 64 rows 1790 / 225.  The
 // constants fit 100 sizes; of 60 others, drawn, 5 take a form that is more than 5% behind
-// the best one (6 of 543 slots, 35 rows, 64/16 heads of 64: 35 and 26).
+// the best one (6 of 543 slots, 35 rows, 64/16 heads of 64: 35 and 26).  Several groups have to be
+// faster by kSeveral: their rounds take as long for sequences that fill little of their page
+// table, which streaming does not (32 of 1024 in tables of 131072, 32 rows: 1028 / 116).
 constexpr double kCallUs = 6., kCtaUs = 0.022, kReadUs = 0.9, kGroupUs = 10., kCutUs = 6., kLeastTileUs = 15.;
 constexpr double kRecordUs = 0.1;  // per MB
+constexpr double kSeveral = 0.85;
 constexpr double stream_us(int d) { return d == 64 ? 0.33 : d == 96 ? 0.27 : 0.23; }  // per MB of codes and 16 columns
 constexpr double tile_step_us(int d) { return d == 64 ? 1.4 : 1.9; }
 // Rows read back at once, beyond one sequence.  Fewer and larger groups leave less of their
@@ -327,7 +330,7 @@ RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages)
   const double mb = (double)B * slots * c.Hkv * (c.d + c.d / 8) * 1e-6, blocks = (double)((rows + 15) / 16);
   const double tensor = kReadUs * mb + (pl.cut ? (double)((B + pl.group - 1) / pl.group) * (kGroupUs + cut) : all(pl.group));
   const double stream = kCallUs + blocks * (mb * stream_us(c.d) + kCtaUs * B * c.Hkv);
-  if (stream <= tensor) return pl;
+  if (stream * (B > pl.group ? kSeveral : 1.) <= tensor) return pl;
   pl.tiles = true;
   pl.records = pl.splits * (pl.pair ? 2 : 1);
   size_t off = 0;
