@@ -267,11 +267,11 @@ struct RowsPlan {
 // slots, 32 rows 28 / 33, 64 rows 47 / 35, 256 rows 157 / 50; 8 of 32768, 16 rows 296 / 532, 32
 // rows 587 / 553, 64 rows 1059 / 557; 32 of 1024, 16 rows 63 / 123, 32 rows 116 / 97.  Whole
 // KV ranges / cut ones: 16 of 4096, 256 rows 293 / 520; 32 of 8192, 300 rows, 32/4 heads 1480 /
-// 1720; 1 of 131072, 64 rows 1790 / 225.  The
-// constants fit 100 sizes; of 60 others, drawn, 5 take a form that is more than 5% behind
-// the best one (6 of 543 slots, 35 rows, 64/16 heads of 64: 35 and 26).  Several groups have to be
-// faster by kSeveral: their rounds take as long for sequences that fill little of their page
-// table, which streaming does not (32 of 1024 in tables of 131072, 32 rows: 1028 / 116).
+// 1720; 1 of 131072, 64 rows 1790 / 225.  The constants fit 100 sizes; of 60 others, drawn, 3 take
+// a form that is more than 5% behind the best one (1 of 3053 slots, 97 rows, 256/32 heads
+// of 64: 72 and 62).  Several groups have to be faster by kSeveral: their rounds take as long
+// for sequences that fill little of their page table, which streaming does not (32 of 1024
+// in tables of 131072, 32 rows: 1028 / 116).
 constexpr double kCallUs = 6., kCtaUs = 0.022, kReadUs = 0.9, kGroupUs = 10., kCutUs = 6., kLeastTileUs = 15.;
 constexpr double kRecordUs = 0.1;  // per MB
 constexpr double kSeveral = 0.85;
@@ -282,8 +282,9 @@ constexpr double tile_step_us(int d) { return d == 64 ? 1.4 : 1.9; }
 // 512 321 (57 and 7), all in one 313; 16 of 4096, 256 rows 439, 363, 350, 287.
 constexpr size_t kGroupBytes = 512 << 20;
 // Partial records held at once: as many sequences' as fit are joined together, and a
-// sequence is cut into no more parts than fit.
-constexpr size_t kRecordBytes = 128 << 20;
+// sequence is cut into no more parts than fit (1 of 32048 slots, 2048 rows, 32/8 heads of 128,
+// 7 parts 249 MB: 849 us, 890 whole).
+constexpr size_t kRecordBytes = 256 << 20;
 
 RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   RowsPlan pl{};
@@ -312,17 +313,18 @@ RowsPlan rows_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages)
   pl.blocks = pl.pair ? 1 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
   const int64_t units = (int64_t)pl.blocks * c.Hkv;
   const size_t part = sizeof(float) * (size_t)c.Hkv * rows * (pl.pair ? 2 : 1) * tile_rec(c.d);  // a part's records
-  double least = 1e30;
+  double least = 1e30, one_cut = 1e30;
   int splits = 1;
   for (int n = 1; n <= 32 && n <= tiles && part * n <= kRecordBytes; ++n) {
     const double us = step * ((double)((units * n + sms - 1) / sms) * ((double)((tiles + n - 1) / n) + 1.) + 0.05 * n);
-    const double cost = (us > kLeastTileUs ? us : kLeastTileUs) + kRecordUs * 1e-6 * (double)(part * n);
-    if (cost < least) {
-      least = cost;
+    const double run = us > kLeastTileUs ? us : kLeastTileUs, join = kRecordUs * 1e-6 * (double)(part * n);
+    if (run + 0.5 * join < least) {  // (half: of 62 MB of records a third gets to HBM)
+      least = run + 0.5 * join;
+      one_cut = run + join;
       splits = n;
     }
   }
-  const double cut = kCutUs + pl.group * least;
+  const double cut = kCutUs + pl.group * one_cut;
   pl.cut = cut < whole(pl.group);
   pl.splits = pl.cut ? splits : 1;
   const size_t most = kRecordBytes / (part * pl.splits);

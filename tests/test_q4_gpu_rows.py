@@ -10,7 +10,7 @@ from tests._longctx import to_f64
 
 pytestmark = pytest.mark.gpu
 
-ROWS, RECORDS = 2 ** 29, 2 ** 27  # bytes of rows read back at once (or one sequence's), of partial records
+ROWS, RECORDS = 2 ** 29, 2 ** 28  # bytes of rows read back at once (or one sequence's), of partial records
 
 
 def config(Hq, Hkv, d, page):
@@ -80,7 +80,7 @@ def run(x, pos):
 
 
 def test_cut_rows_of_more_sequences_than_their_records_fit():
-    x = Q.Q4([300, 411, 300, 333, 300, 517, 300, 340], Hkv=4, G=8, d=64, page=16, k=1, max_pages=1600)
+    x = Q.Q4([300, 411, 300, 333, 300, 517, 300, 340] * 2, Hkv=4, G=8, d=64, page=16, k=1, max_pages=1600)
     g, records = form(x.session_cfg(), x.B, 300, x.max_pages)
     part = 4 * x.Hkv * 300 * x.G * (x.d + 8)
     assert g == x.B and 0 < records <= RECORDS and round(records / part) % x.B != 0
@@ -226,9 +226,10 @@ def test_rows_of_nan_queries_are_nan_in_both_forms(f):
     (1, 32, 8192, 32, 8, 128, "stream"), (1, 64, 8192, 32, 8, 128, "cut"), (1, 256, 8192, 32, 8, 128, "cut"),
     (8, 16, 32768, 32, 8, 128, "stream"), (8, 64, 32768, 32, 8, 128, "cut"), (32, 16, 1024, 32, 8, 128, "stream"),
     (32, 32, 1024, 32, 8, 128, "whole"), (16, 256, 4096, 32, 8, 128, "whole"), (32, 300, 8192, 32, 4, 128, "whole"),
-    (1, 64, 131072, 32, 8, 128, "cut"), (4, 200, 8192, 6, 3, 96, "stream")])
+    (1, 64, 131072, 32, 8, 128, "cut"), (4, 200, 8192, 6, 3, 96, "stream"), (32, 32, 131072, 32, 8, 128, "stream")])
 def test_calls_take_the_form_that_measured_fastest(B, Tq, slots, Hq, Hkv, d, want):
     """By 10% and more (us: streamed, whole, cut): 28 118 33; 47 119 35; 157 122 50; 296 1407 531; 1059 1064 557;
-    63 118 320; 116 97 381; 1141 293 515; 4841 1478 1717; 582 1779 225; 68 159 85."""
+    63 118 320; 116 97 381; 1141 293 515; 4841 1478 1717; 582 1779 225; 68 159 85; the last one's estimates are
+    close, and 1024 slots in such a table take 116 and 1028."""
     at = form(config(Hq, Hkv, d, 16), B, Tq, slots // 16)
     assert ("stream" if at is None else "cut" if at[1] else "whole") == want
