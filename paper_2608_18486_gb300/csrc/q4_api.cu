@@ -180,8 +180,11 @@ Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   Q4Plan pl{};
   // 16 columns per unit read the codes once for both eights, but run half the warps: for
   // enough work only.  us with 16 / 8 columns per unit (32 query, 8 kv heads of 128): 1 sequence
-  // of 512 slots, 4 rows 10.6 / 7.5; of 8192, 8 rows 18.4 / 14.7, 32 rows 28.6 / 35.2; 8 of
-  // 32768, 4 rows 84 / 114; 16 of 2048, 4 rows 21.2 / 23.3, 12 heads of 64, 16 rows 17.8 / 17.1.
+  // of 512 slots, 4 rows 10.1 / 9.0; of 8192, 8 rows 17.6 / 14.2, 32 rows 28.1 / 34.7; 8 of
+  // 32768, 4 rows 86 / 114; 16 of 2048, 4 rows 20.7 / 22.9; 8 of 4096, 12 heads of 64, 16 rows
+  // 15.5 / 17.2.  What the rule does not see is a second wave of the fewer CTAs that 16 columns
+  // leave on an SM; it takes the slower form of 1 of 16384, 8 rows 25.9 / 21.6, 16 of 2048, 12 heads
+  // of 64, 16 rows 17.4 / 16.7 and 20 rows 31.6 / 20.5.
   const double mb = (double)B * max_pages * c.page_size * c.Hkv * (c.d + c.d / 8) * 1e-6;
   pl.nb = cols > 8 && c.dtype == WM_DT_BF16 && mb * (double)((cols + 7) / 8) > kWideMb ? 2 : 1;
   pl.col_blocks = (int)((cols + 8 * pl.nb - 1) / (8 * pl.nb));
@@ -197,10 +200,12 @@ Q4Plan attn_plan(const wm_config& c, int32_t B, int32_t Tq, int32_t max_pages) {
   pl.total = 256;
   // The spread has a start (a scan of the lengths), a second kernel, and a share of it drains its
   // rings at each unit's end: for long units, the sooner the fewer CTAs these would make
-  // otherwise, and not where a CTA would take several units.  us, spread / not: 32 heads of
-  // 128, lengths within a factor of 2: 16 x 16384 slots 146 / 175, 32 x 8192 148 / 161, 48 x
-  // 5461 152 / 152, 128 x 2048 179 / 149; 32/8 heads: 16 x 8192 40 / 32, 64 x 4096 63 / 54,
-  // 1 x 32768 20 / 28; 8/2 heads: 1 x 16384 14.6 / 16.6, 8 x 16384 18.6 / 20.8, 8 x 8192 15.5 / 13.1.
+  // otherwise, and not where a CTA would take several units.  us, spread / not, heads of 128,
+  // lengths from half of the largest to it: 32 heads: 16 x 16384 slots 147 / 151, 32 x 8192 148 / 152, 48 x
+  // 5461 151 / 141, 128 x 2048 169 / 145; 32/8 heads: 16 x 8192 39 / 28, 64 x 4096 63 / 46,
+  // 1 x 32768 19 / 28; 8/2 heads: 1 x 16384 14.4 / 16.3, 8 x 32768 24 / 35, 8 x 16384 20.4 / 20.3.
+  // Of 168 sizes (half of them with equal lengths) 8 take the slower form, by 13% at most: 8 x 16384,
+  // 8/2 heads, equal lengths 18.1 / 20.5 (not spread); 48 x 5461, 32/8 heads 58 / 51 (spread).
   const double fill = (double)(units * C) / resident;
   const double longest = kLongSteps + kFilledSteps * (fill < 1. ? fill : 1.);
   if (pl.col_blocks == 1 && units <= 2 * resident && (double)steps > (double)(C * kQ4Warps) * longest) {

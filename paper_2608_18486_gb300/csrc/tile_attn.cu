@@ -10,8 +10,9 @@
 //
 // Both are dense contractions around a softmax and run on the tcgen05 tensor
 // cores like the causal prefill attention (prefill_attn.cu): 128-row query
-// tiles, 128-slot KV tiles, S and O in TMEM, P written over S as bf16 for the
-// second product, the running max raised only when it grows by more than 2^8.
+// tiles, 128-slot KV tiles, S and O in TMEM, P written over S as bf16 (fp16 where
+// V is) for the second product, the running max raised only when it grows by more
+// than 2^8.
 // What differs is the shape of the work.  A window makes every item short
 // (about window / 128 + 2 KV tiles), so the CTA is persistent (one per SM) and
 // its warps run ahead of each other across items: the TMA warp loads the next
