@@ -551,7 +551,8 @@ size_t wm_q4_rows_attn_workspace(const wm_config* cfg, int32_t B, int32_t Tq, in
  * those are more; up to 256 MB of partial results; and 4 bytes per page-table entry and
  * position.  The form, the split of the work and the workspace go by the width of the page
  * table, here and in wm_q4_decode_attn: tables much wider than the lengths cost time (16
- * sequences of 2048 slots, 256 rows: 158 us, in tables of 131072 slots 855 and a workspace of 622 MB).
+ * sequences of 2048 slots, 256 rows: 158 us, in tables of 131072 slots 855 and a
+ * workspace of 622 MB).
  *   q, out     device [B][Tq][Hq][d], 16-byte aligned
  *   pos        device int32 [B][Tq], 0 <= pos < max_pages*page_size, any order
  *   workspace  device, >= wm_q4_rows_attn_workspace(cfg, B, Tq, max_pages) bytes,

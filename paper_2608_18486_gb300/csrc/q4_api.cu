@@ -284,7 +284,7 @@ constexpr double stream_us(int d) { return d == 64 ? 0.33 : d == 96 ? 0.27 : 0.2
 constexpr double tile_step_us(int d) { return d == 64 ? 1.4 : 1.9; }
 // Rows read back at once, beyond one sequence.  Fewer and larger groups leave less of their
 // last waves empty: 64 sequences of 2048 slots, 64 rows, up to 64 MB 467 us, 128 407, 256 386,
-// 512 321 (57 and 7), all in one 313; 16 of 4096, 256 rows 439, 363, 350, 287.
+// 512 321 (57 and 7), all in one 313; 16 of 4096, 256 rows 439, 363, 350, 287 (weights in bf16).
 constexpr size_t kGroupBytes = 512 << 20;
 // Partial records held at once: as many sequences' as fit are joined together, and a
 // sequence is cut into no more parts than fit (1 of 32048 slots, 2048 rows, 32/8 heads of 128,
