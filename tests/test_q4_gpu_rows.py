@@ -233,3 +233,29 @@ def test_calls_take_the_form_that_measured_fastest(B, Tq, slots, Hq, Hkv, d, wan
     close, and 1024 slots in such a table take 116 and 1028."""
     at = form(config(Hq, Hkv, d, 16), B, Tq, slots // 16)
     assert ("stream" if at is None else "cut" if at[1] else "whole") == want
+
+
+@pytest.mark.parametrize("f", [FORMS[1], FORMS[5], FORMS[6]])
+def test_large_scores_of_few_slots_of_either_sign(f):
+    """Rows that see one to three slots, so that the largest score is as often negative; ties at every size."""
+    x, Tq = case(*f), f[1]
+    s, q4 = x.session(), x.q4()
+    table, _ = x.q4_dev()
+    pos = np.random.default_rng(8).integers(0, 3, (x.B, Tq)).astype(np.int32)
+    q = x.queries(x.B, Tq)
+    best, clear = np.empty((x.B, Tq, x.Hq, x.d)), np.empty((x.B, Tq, x.Hq), dtype=bool)
+    for b in range(x.B):
+        for hq in range(x.Hq):
+            K, V = (x.rows(p, 0, b, hq // x.G, np.arange(3)) for p in (x.kd, x.vd))
+            z = np.where(np.arange(3)[None] <= pos[b][:, None], to_f64(q[b, :, hq]) @ K.T, -np.inf)
+            top = np.sort(z, 1)
+            clear[b, :, hq] = top[:, -1] - top[:, -2] > 0.05
+            best[b, :, hq] = V[z.argmax(1)]
+    assert clear.mean() > 0.5 and (pos == 0).any()
+    for e in range(18, 100, 3):
+        out = torch.full(q.shape, float("nan"), dtype=x.tdt, device="cuda")
+        s.q4_rows_attn(0, (q * 2.0 ** e).cuda(), torch.from_numpy(pos).cuda(), q4, table, out)
+        got = to_f64(out)
+        assert (np.abs(got - best) <= (2.0 ** -11 + 2.0 ** -8 + 2.0 ** -16) * np.abs(best))[clear].all(), e
+        assert np.isfinite(got).all(), e
+    assert s.read_status() == 0
